@@ -318,6 +318,137 @@ sbd_status sbd_select(int32_t rule, int32_t batch, int32_t block_k, const float*
                       uint8_t* masked, int32_t* block_tokens, int32_t* n_unmasked,
                       void* stream);
 
+/* ------------------------------------------------------------------------
+ * A paged KV cache in 8 bits, for serving batches of uneven requests.
+ *
+ *   k_cache, v_cache [n_pages, Hkv, P, D]  e4m3 codes (4 exponent bits of bias 7,
+ *                                          3 mantissa bits, largest 448, no infinity)
+ *   k_scale, v_scale [n_pages, Hkv]        fp32; a value is its page's scale * code
+ *   block_table      [B, max_pages] int32  page of a request's tokens p P .. p P + P - 1
+ *                                          in column p; -1 where it holds none
+ * A token's slot is page * P + its place in the page.  P in {16, 32, 64, 128},
+ * D in {64, 128}, n_pages * P < 2^31.
+ *
+ * One turn of a serving loop: sbd_block_tables gives the requests the pages of
+ * the lengths they are to have, sbd_cache_append_q8 fills the new slots, and
+ * sbd_block_attention_q8 reads the cache.
+ * ---------------------------------------------------------------------- */
+
+/* ------------------------------------------------------------------------
+ * Block tables and slot maps from request lengths.  A request grows from
+ * cache_len[b] to target_len[b] tokens, or shrinks (0: it ends), holding
+ * ceil(length / P) pages before and after.
+ *
+ *   cache_len, target_len [B] int32       0 .. max_pages * P
+ *   block_table [B, max_pages] int32      as it is; not changed
+ *   free_pages [n_pages] int32, n_free [1] int32
+ *                                         the free pages: a stack of n_free entries;
+ *                                         released pages are written above them
+ *   block_table_out [B, max_pages] int32  as it is after; -1 past a request's pages
+ *   len_out [B] int32                     target_len[b], or cache_len[b] where refused
+ *   new_start [B + 1] int32               tokens gained before request b (last: in all)
+ *   slot_map [max_new] int32              slots of the new tokens, in request order from
+ *                                         new_start[b]; -1 for a refused request's and
+ *                                         past the last one
+ *   n_free_out [1] int32                  free pages after
+ *
+ * Released pages (request by request, in a request's order) go on the stack
+ * first, the first one topmost; then pages are granted from the top.  Shrinking
+ * what a call granted therefore restores the stack.  A request is refused as a
+ * whole when the pages of all requests up to and with it exceed the free ones,
+ * or its tokens end past max_new; it keeps what it has.  Nothing of block_table
+ * is overwritten, so a step in flight may still read it; block_table_out must
+ * be other memory.  A length out of range is clamped, its request left as it is,
+ * and SBD_DEVERR_CACHE_LEN set; a page id or an n_free out of range sets
+ * SBD_DEVERR_PAGE.  No workspace.
+ * Supported: 1 <= B <= 4096, B * max_pages < 2^31, max_new >= 0.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch;      /* B */
+  int32_t page_size;  /* P */
+  int32_t max_pages;  /* columns of a block table */
+  int32_t n_pages;    /* pages of the cache, entries of free_pages */
+  int32_t max_new;    /* entries of slot_map */
+} sbd_tables_desc;
+
+sbd_status sbd_block_tables(const sbd_tables_desc* desc, const int32_t* cache_len,
+                            const int32_t* target_len, const int32_t* block_table,
+                            int32_t* free_pages, const int32_t* n_free,
+                            int32_t* block_table_out, int32_t* len_out, int32_t* new_start,
+                            int32_t* slot_map, int32_t* n_free_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * New keys and values into their slots, in 8 bits.
+ *
+ *   k_new, v_new [T, Hkv, D]   desc->dtype; token t lies (t / group) * group_stride +
+ *                              (t % group) * token_stride elements behind the first
+ *                              (heads contiguous), so that they may be slices of a
+ *                              fused projection or the leading rows of a block
+ *   slot_map [T] int32         slot of every token; negative: not stored
+ *   k_cache, v_cache, k_scale, v_scale   written (see above)
+ *
+ * A run of tokens with consecutive slots of one page is a segment.  For every
+ * segment and head, with a = max |x| over its finite elements, s_new is the
+ * smallest power of two with a <= 448 s_new (2^-126 at least).  A segment that
+ * begins its page (place 0) sets the page's scale to s_new, whatever it was;
+ * another one to max(old, s_new), and where that is larger than the old one
+ * the codes in the places before it become e4m3(code * old / new).  New codes
+ * are e4m3(x / scale), to nearest even; infinities become +-448, NaN stays.
+ * A page may receive one segment a call, and its earlier places must hold
+ * tokens.  A slot past the cache is not stored and sets SBD_DEVERR_PAGE.
+ * Supported: strides that are multiples of 16 bytes; group >= 1.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t tokens;     /* T */
+  int32_t group;      /* tokens of a group; T where there is one stride only */
+  int32_t n_kv_heads; /* Hkv */
+  int32_t head_dim;   /* D */
+  int32_t page_size;  /* P */
+  int32_t n_pages;
+  int32_t dtype;      /* sbd_dtype of k_new and v_new */
+  int64_t k_group_stride, k_token_stride; /* elements */
+  int64_t v_group_stride, v_token_stride;
+} sbd_append_q8_desc;
+
+sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new,
+                               const void* v_new, const int32_t* slot_map, void* k_cache,
+                               void* v_cache, float* k_scale, float* v_scale, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Block attention over the paged 8-bit cache: sbd_block_attention with
+ * k_cache and v_cache as above.  Every block row sees the cached keys
+ * 0 .. cache_len[b]-1; row i >= n_causal sees all k block keys, row
+ * i < n_causal (the first iteration of a block, with the previous block's
+ * tokens as its leading rows) the block keys j <= i.  The cache is only read:
+ * a previous block enters it with sbd_cache_append_q8.
+ *
+ *   q [B, k, Hq, D], k_blk, v_blk [B, k, Hkv, D], out [B, k, Hq, D]  desc->dtype
+ *   cache_len [B] int32, 0 .. max_pages * P; what the cache holds past it (and
+ *   pages it does not reach) is never used and may be NaN
+ *
+ * Products of codes and activations accumulate in fp32, scales apply in fp32.
+ * A length out of range is clamped and sets SBD_DEVERR_CACHE_LEN; a page id out
+ * of range sets SBD_DEVERR_PAGE and its keys and values count as zeros.
+ * Supported: 1 <= k <= 32, D in {64, 128}, Hq % Hkv == 0, max_pages * P + k <
+ * 2^31; scale 0 is 1/sqrt(D); num_splits 0 picks the key ranges.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch, block_k, n_q_heads, n_kv_heads, head_dim;
+  int32_t page_size, max_pages, n_pages;
+  int32_t dtype;      /* sbd_dtype of q, k_blk, v_blk and out */
+  int32_t n_causal;   /* leading causal block rows, 0 .. k */
+  float scale;
+  int32_t num_splits;
+} sbd_attn_q8_desc;
+
+size_t sbd_block_attention_q8_workspace_size(const sbd_attn_q8_desc* desc);
+sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
+                                  const void* k_cache, const void* v_cache,
+                                  const float* k_scale, const float* v_scale,
+                                  const int32_t* block_table, const int32_t* cache_len,
+                                  const void* k_blk, const void* v_blk, void* out,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
 /* Status name ("SBD_OK", ...). Never NULL. */
 const char* sbd_status_string(sbd_status status);
 
@@ -332,6 +463,7 @@ sbd_status sbd_device_error(int32_t* code);
 #define SBD_DEVERR_CACHE_LEN 1   /* a cache_len entry was outside [0, Lmax] */
 #define SBD_DEVERR_TIMEOUT 2     /* a bounded wait inside a kernel gave up  */
 #define SBD_DEVERR_ROWS 4        /* more masked rows than the head supports */
+#define SBD_DEVERR_PAGE 8        /* a page id, slot or free-page count was out of range */
 
 /* Library version, major * 10000 + minor * 100 + patch. */
 int32_t sbd_version(void);

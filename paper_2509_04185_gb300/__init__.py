@@ -13,6 +13,13 @@ Eq. 3 / Algorithm 3) keep the names of the C ABI:
     sbd_block_attention(q, k_cache, v_cache, cache_len, k_blk, v_blk)
     sbd_head_entropy_sample(hidden, w, masked, gumbel, tau)
     sbd_eb_select(entropy, token, gamma, masked, block_tokens)
+
+A serving batch may keep its KV cache in 8-bit pages instead:
+
+    sbd_block_tables(cache_len, target_len, block_table, free_pages, n_free, page_size)
+    sbd_cache_append_q8(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale)
+    sbd_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table,
+                           cache_len, k_blk, v_blk)
 """
 from __future__ import annotations
 
@@ -32,6 +39,7 @@ SBD_DTYPE_BF16 = 1
 SBD_DEVERR_CACHE_LEN = 1
 SBD_DEVERR_TIMEOUT = 2
 SBD_DEVERR_ROWS = 4
+SBD_DEVERR_PAGE = 8
 SBD_HEAD_NOALLOC_MAX_SCRATCH = 8 << 20
 SBD_SELECT_EB_ENTROPY = 0
 SBD_SELECT_EB_CONFIDENCE = 1
@@ -53,6 +61,10 @@ EXPORTS = (
     "sbd_linear",
     "sbd_eb_select",
     "sbd_select",
+    "sbd_block_tables",
+    "sbd_cache_append_q8",
+    "sbd_block_attention_q8_workspace_size",
+    "sbd_block_attention_q8",
     "sbd_status_string",
     "sbd_last_error",
     "sbd_device_error",
@@ -77,6 +89,30 @@ class HeadDesc(ctypes.Structure):
 class LinearDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("in_features", ctypes.c_int32),
                 ("out_features", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class TablesDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_new", ctypes.c_int32)]
+
+
+class AppendQ8Desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32),
+                ("k_group_stride", ctypes.c_int64), ("k_token_stride", ctypes.c_int64),
+                ("v_group_stride", ctypes.c_int64), ("v_token_stride", ctypes.c_int64)]
+
+
+class AttnQ8Desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("block_k", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("n_causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("num_splits", ctypes.c_int32)]
 
 
 class SbdError(RuntimeError):
@@ -123,6 +159,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sbd_eb_select.restype = ctypes.c_int
     lib.sbd_select.argtypes = [i32, i32, i32, vp, vp, vp, f32, vp, vp, vp, vp]
     lib.sbd_select.restype = ctypes.c_int
+    lib.sbd_block_tables.argtypes = [ctypes.POINTER(TablesDesc)] + [vp] * 11
+    lib.sbd_block_tables.restype = ctypes.c_int
+    lib.sbd_cache_append_q8.argtypes = [ctypes.POINTER(AppendQ8Desc)] + [vp] * 8
+    lib.sbd_cache_append_q8.restype = ctypes.c_int
+    lib.sbd_block_attention_q8_workspace_size.argtypes = [ctypes.POINTER(AttnQ8Desc)]
+    lib.sbd_block_attention_q8_workspace_size.restype = sz
+    lib.sbd_block_attention_q8.argtypes = [ctypes.POINTER(AttnQ8Desc)] + [vp] * 11 + [sz, vp]
+    lib.sbd_block_attention_q8.restype = ctypes.c_int
     lib.sbd_status_string.argtypes = [ctypes.c_int]
     lib.sbd_status_string.restype = ctypes.c_char_p
     lib.sbd_last_error.argtypes = []
@@ -431,6 +475,164 @@ def sbd_select(rule: int, entropy, confidence, token, threshold: float, masked, 
     return n_unmasked
 
 
+# ------------------------------------------------------------------ paged 8-bit cache
+
+def _need_type(dtype, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _need_shape(shape, **tensors):
+    for name, t in tensors.items():
+        if t is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def block_tables_outputs(cache_len, block_table, max_new: int):
+    """Outputs for sbd_block_tables: (block_table [B, max_pages], length [B],
+    new_start [B + 1], slot_map [max_new], n_free [1]), all int32."""
+    torch = _torch()
+    B = cache_len.shape[0]
+    mk = lambda *shape: torch.empty(shape, dtype=torch.int32, device=cache_len.device)  # noqa: E731
+    return torch.empty_like(block_table), mk(B), mk(B + 1), mk(int(max_new)), mk(1)
+
+
+def _tables_args(cache_len, target_len, block_table, free_pages, n_free, page_size, outs, stream):
+    torch = _torch()
+    table_out, len_out, new_start, slot_map, n_free_out = outs
+    tensors = dict(cache_len=cache_len, target_len=target_len, block_table=block_table,
+                   free_pages=free_pages, n_free=n_free, block_table_out=table_out,
+                   len_out=len_out, new_start=new_start, slot_map=slot_map, n_free_out=n_free_out)
+    _need_cuda(**tensors)
+    _need_type(torch.int32, **tensors)
+    if cache_len.dim() != 1 or block_table.dim() != 2 or free_pages.dim() != 1 or slot_map.dim() != 1:
+        raise ValueError("cache_len, free_pages and slot_map have one dimension, block_table two")
+    B = cache_len.shape[0]
+    _need_shape((B,), target_len=target_len, len_out=len_out)
+    _need_shape((B, block_table.shape[1]), block_table=block_table, block_table_out=table_out)
+    _need_shape((B + 1,), new_start=new_start)
+    _need_shape((1,), n_free=n_free, n_free_out=n_free_out)
+    d = TablesDesc(B, int(page_size), block_table.shape[1], free_pages.shape[0], slot_map.shape[0])
+    return (ctypes.byref(d), *(_ptr(t) for t in tensors.values()), _stream(stream)), (d, tensors)
+
+
+def sbd_block_tables(cache_len, target_len, block_table, free_pages, n_free, page_size: int,
+                     max_new: int = 0, outputs=None, *, stream=None):
+    """Grows and releases the pages of a batch's requests and maps their new
+    tokens to slots: cache_len, target_len [B], block_table [B, max_pages],
+    free_pages [n_pages] (a stack, n_free [1] of it in use; released pages are
+    written above), all int32 on the device.  max_new is the length of the slot
+    map; `outputs` may hold the tensors of block_tables_outputs.  Returns
+    (block_table, length, new_start, slot_map, n_free) after the call; a request
+    that did not fit keeps its length and its new tokens get slot -1."""
+    outs = outputs if outputs is not None else block_tables_outputs(cache_len, block_table, max_new)
+    args, _ = _tables_args(cache_len, target_len, block_table, free_pages, n_free, page_size, outs,
+                           stream)
+    _check(lib.sbd_block_tables(*args))
+    return outs
+
+
+def _cache_desc(k_cache, v_cache, k_scale, v_scale):
+    """(n_pages, Hkv, P, D) of a paged 8-bit cache, checked."""
+    torch = _torch()
+    _need_cuda(k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale)
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [n_pages, Hkv, P, D]")
+    _need_type(torch.float8_e4m3fn, k_cache=k_cache, v_cache=v_cache)
+    _need_type(torch.float32, k_scale=k_scale, v_scale=v_scale)
+    _need_shape(k_cache.shape, v_cache=v_cache)
+    _need_shape(k_cache.shape[:2], k_scale=k_scale, v_scale=v_scale)
+    return tuple(k_cache.shape)
+
+
+def _token_strides(name, t):
+    """(tokens, group, group stride, token stride) of [T, Hkv, D] or [B, n, Hkv, D]."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor (libsbd has no CPU path)")
+    if t.dim() not in (3, 4):
+        raise ValueError(f"{name} must be [T, Hkv, D] or [B, n, Hkv, D]")
+    H, D = t.shape[-2:]
+    if t.stride(-1) != 1 or (H > 1 and t.stride(-2) != D):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    if t.dim() == 3:
+        n = max(1, t.shape[0])
+        return t.shape[0], n, 0, t.stride(0) if n > 1 else 0
+    B, n = t.shape[:2]
+    return B * n, max(1, n), t.stride(0) if B > 1 else 0, t.stride(1) if n > 1 else 0
+
+
+def _append_args(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale, stream):
+    torch = _torch()
+    n_pages, H, P, D = _cache_desc(k_cache, v_cache, k_scale, v_scale)
+    T, group, kg, kt = _token_strides("k_new", k_new)
+    _, _, vg, vt = _token_strides("v_new", v_new)
+    _need_shape(k_new.shape, v_new=v_new)
+    _need_type(k_new.dtype, v_new=v_new)
+    if tuple(k_new.shape[-2:]) != (H, D):
+        raise ValueError(f"k_new has heads {tuple(k_new.shape[-2:])}, the cache {(H, D)}")
+    _need_cuda(slot_map=slot_map)
+    _need_type(torch.int32, slot_map=slot_map)
+    if slot_map.dim() != 1 or slot_map.shape[0] < T:
+        raise ValueError(f"slot_map needs {T} entries")
+    d = AppendQ8Desc(T, group, H, D, P, n_pages, _dtype_code(k_new), kg, kt, vg, vt)
+    args = (ctypes.byref(d), _ptr(k_new), _ptr(v_new), _ptr(slot_map), _ptr(k_cache), _ptr(v_cache),
+            _ptr(k_scale), _ptr(v_scale), _stream(stream))
+    return args, (d, k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale)
+
+
+def sbd_cache_append_q8(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale, *, stream=None):
+    """Quantises new keys and values into their slots of a paged cache.  k_new,
+    v_new [T, Hkv, D] or [B, n, Hkv, D], bf16 or fp32, the heads of a token
+    contiguous and tokens any multiple of 16 bytes apart; slot_map [>= T] int32
+    (negative: not stored); k_cache, v_cache [n_pages, Hkv, P, D] float8_e4m3fn
+    and k_scale, v_scale [n_pages, Hkv] fp32 are updated in place."""
+    args, _ = _append_args(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale, stream)
+    _check(lib.sbd_cache_append_q8(*args))
+
+
+def _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk, v_blk, out,
+                  n_causal, scale, num_splits, workspace, stream):
+    torch = _torch()
+    n_pages, H, P, D = _cache_desc(k_cache, v_cache, k_scale, v_scale)
+    _need_cuda(q=q, block_table=block_table, cache_len=cache_len, k_blk=k_blk, v_blk=v_blk, out=out,
+               workspace=workspace)
+    _need_type(torch.int32, block_table=block_table, cache_len=cache_len)
+    if q.dim() != 4 or q.shape[3] != D:
+        raise ValueError(f"q must be [B, k, Hq, {D}]")
+    B, k, Hq, _ = q.shape
+    _need_type(q.dtype, k_blk=k_blk, v_blk=v_blk, out=out)
+    _need_shape((B, k, H, D), k_blk=k_blk, v_blk=v_blk)
+    _need_shape(q.shape, out=out)
+    _need_shape((B,), cache_len=cache_len)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    d = AttnQ8Desc(B, k, Hq, H, D, P, block_table.shape[1], n_pages, _dtype_code(q), int(n_causal),
+                   float(scale), int(num_splits))
+    ws = _workspace(lib.sbd_block_attention_q8_workspace_size(ctypes.byref(d)), q.device, workspace)
+    args = (ctypes.byref(d), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+            _ptr(block_table), _ptr(cache_len), _ptr(k_blk), _ptr(v_blk), _ptr(out), _ptr(ws),
+            _nbytes(ws), _stream(stream))
+    return args, (d, q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk, v_blk,
+                  out, ws)
+
+
+def sbd_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                           v_blk, out=None, *, n_causal: int = 0, scale: float = 0.0,
+                           num_splits: int = 0, workspace=None, stream=None):
+    """sbd_block_attention over a paged 8-bit cache.  Shapes: q [B,k,Hq,D],
+    k_cache/v_cache [n_pages,Hkv,P,D] float8_e4m3fn, k_scale/v_scale [n_pages,Hkv]
+    fp32, block_table [B,max_pages] int32, cache_len [B] int32, k_blk/v_blk
+    [B,k,Hkv,D]; block rows i < n_causal see the block keys j <= i only.
+    Returns out [B,k,Hq,D] (dtype of q)."""
+    if out is None:
+        out = _torch().empty_like(q)
+    args, _ = _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                            v_blk, out, n_causal, scale, num_splits, workspace, stream)
+    _check(lib.sbd_block_attention_q8(*args))
+    return out
+
+
 class Prepared:
     """A library call with every argument already marshalled: calling it
     re-issues the same C call (same tensors, stream and workspace) with no
@@ -507,6 +709,31 @@ def prepare_eb_select(entropy, token, gamma: float, masked, block_tokens, n_unma
     args = (B, k, _ptr(entropy), _ptr(token), float(gamma), _ptr(masked), _ptr(block_tokens),
             _ptr(n_unmasked), _stream(stream))
     return Prepared(lib.sbd_eb_select, args, (entropy, token, masked, block_tokens, n_unmasked))
+
+
+def prepare_block_tables(cache_len, target_len, block_table, free_pages, n_free, page_size: int,
+                         block_table_out, len_out, new_start, slot_map, n_free_out, *,
+                         stream=None) -> Prepared:
+    """sbd_block_tables bound to fixed tensors (see Prepared)."""
+    args, keep = _tables_args(cache_len, target_len, block_table, free_pages, n_free, page_size,
+                              (block_table_out, len_out, new_start, slot_map, n_free_out), stream)
+    return Prepared(lib.sbd_block_tables, args, keep)
+
+
+def prepare_cache_append_q8(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale, *,
+                            stream=None) -> Prepared:
+    """sbd_cache_append_q8 bound to fixed tensors (see Prepared)."""
+    args, keep = _append_args(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale, stream)
+    return Prepared(lib.sbd_cache_append_q8, args, keep)
+
+
+def prepare_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                               v_blk, out, workspace=None, *, n_causal: int = 0, scale: float = 0.0,
+                               num_splits: int = 0, stream=None) -> Prepared:
+    """sbd_block_attention_q8 bound to fixed tensors (see Prepared)."""
+    args, keep = _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                               v_blk, out, n_causal, scale, num_splits, workspace, stream)
+    return Prepared(lib.sbd_block_attention_q8, args, keep)
 
 
 def sbd_device_error() -> int:

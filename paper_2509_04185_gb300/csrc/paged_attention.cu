@@ -1,0 +1,458 @@
+// Block attention over the paged 8-bit cache: the plan, the launch, and the
+// kernel on fp32 FMAs.
+//
+//   O_r = sum_j p_rj v_j,   p_r = softmax_j(scale q_r . k_j)
+//
+// over the cached keys j < len_b, k_j = ks[page, head] * code, v_j alike, and the
+// k block keys, which are not cached and come in the activations' type.  Packed
+// rows r = i*G + g (block position i, query head g of the KV head's group).
+#include <math.h>
+
+#include "paged.cuh"
+
+namespace {
+
+using namespace sbd_dev;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ------------------------------------------------------- FMA kernel
+// One CTA per (key range, KV head and chunk of W RW packed rows, sequence), the
+// key ranges of a chunk one thread-block cluster that merges through distributed
+// shared memory.  Keys pass in tiles of 64: a thread fetches its 16-byte pieces of
+// the next tile's codes into registers while the present one is worked on, and
+// leaves their values in shared memory as fp32 (every e4m3 value is exact there).
+// Key scales multiply the scores, value scales the values.  A warp owns RW rows in
+// both products: S with lane = key (lane, lane + 32), O with lane = D / 32
+// dimensions, P through shared memory within the warp.
+// It serves fp32 activations, whose tolerance the tensor cores' types do not meet.
+constexpr int kKeys = 64;                    // keys per tile
+constexpr int kGranule = 16;                 // key ranges are multiples of this
+
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
+               "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A float at this CTA's shared location `p`, read in CTA `rank` of the cluster.
+__device__ __forceinline__ float ld_rank(const float* p, int rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// 4 consecutive elements as floats
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
+                     __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store2(float* p, float x, float y) {
+  *reinterpret_cast<float2*>(p) = make_float2(x, y);
+}
+__device__ __forceinline__ void store2(__nv_bfloat16* p, float x, float y) {
+  *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y);
+}
+
+template <typename T>
+struct Args {
+  const T* q;
+  const uint8_t *kc, *vc;
+  const float *ks, *vs;
+  const int32_t *table, *lens;
+  const T *kb, *vb;
+  T* out;
+  int* err;
+  int k, Hq, Hkv, G, M, P, max_pages, n_pages, n_causal, splits, chunks;
+  float scale_log2;
+};
+
+template <int D>
+__host__ __device__ constexpr int k_stride() { return D + 4; }   // lanes' rows in distinct banks
+
+template <int D, int RW, int W>
+constexpr size_t fma_smem_bytes() {
+  return sizeof(float) * ((size_t)W * RW * D                        // Q
+                          + (size_t)kKeys * (k_stride<D>() + D)     // K, V tile
+                          + (size_t)W * RW * kKeys                  // P
+                          + 2 * W * RW                              // m, l of the merge
+                          + kKeys);                                 // key scales
+}
+
+template <typename T, int D, int RW, int W>
+__global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args<T> a) {
+  constexpr int kThreads = 32 * W;
+  constexpr int kRowsCta = W * RW;
+  constexpr int kKS = k_stride<D>();
+  constexpr int kPer = D / 32;                 // output dimensions per lane
+  constexpr int kC4 = D / 4;
+  constexpr int kC16 = D / 16;                 // 16-byte pieces of a row of codes
+  constexpr int kFetch = kKeys * kC16 / kThreads;
+  static_assert(kFetch * kThreads == kKeys * kC16, "a tile is a whole number of turns");
+  extern __shared__ __align__(16) float sm[];
+  float* q_s = sm;                             // [kRowsCta][D]
+  float* k_s = q_s + kRowsCta * D;             // [kKeys][kKS]
+  float* v_s = k_s + kKeys * kKS;              // [kKeys][D]
+  float* p_s = v_s + kKeys * D;                // [kRowsCta][kKeys]
+  float* st_s = p_s + kRowsCta * kKeys;        // m, then l: [kRowsCta] each
+  float* sc_s = st_s + 2 * kRowsCta;           // [kKeys] key scales of the tile
+  float* o_s = k_s;                            // merge: [kRowsCta][D], over the dead K tile
+  static_assert(kRowsCta * D <= kKeys * kKS, "the partial rows fit the K tile");
+
+  grid_dependency_wait();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
+  const int b = blockIdx.z;
+  const int cap = a.max_pages * a.P;
+  int len = a.lens[b];
+  if (len < 0 || len > cap) {
+    if (tid == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
+    len = len < 0 ? 0 : cap;
+  }
+  const int total = len + a.k;
+  const int range = ((total + a.splits - 1) / a.splits + kGranule - 1) / kGranule * kGranule;
+  const int u_begin = min(total, split * range), u_end = min(total, u_begin + range);
+  const int32_t* table = a.table + (size_t)b * a.max_pages;
+
+  uint4 kf[kFetch], vf[kFetch];
+  float ksf[kFetch], vsf[kFetch];
+  auto fetch = [&](int t0) {
+#pragma unroll
+    for (int e = 0; e < kFetch; ++e) {
+      const int u = t0 + (tid + e * kThreads) / kC16, c = (tid + e * kThreads) % kC16;
+      kf[e] = vf[e] = make_uint4(0, 0, 0, 0);
+      ksf[e] = vsf[e] = 0.f;
+      if (u < u_end && u < len) {
+        const int page = table[u / a.P];
+        if (page < 0 || page >= a.n_pages) {
+          record_error(a.err, SBD_DEVERR_PAGE);
+          continue;
+        }
+        const size_t ph = (size_t)page * a.Hkv + hkv;
+        const size_t at = (ph * a.P + u % a.P) * D + 16 * c;
+        kf[e] = *reinterpret_cast<const uint4*>(a.kc + at);
+        vf[e] = *reinterpret_cast<const uint4*>(a.vc + at);
+        ksf[e] = a.ks[ph];
+        vsf[e] = a.vs[ph];
+      }
+    }
+  };
+  // rows past u_end are zeros (PV takes 4 keys at a time)
+  auto commit = [&](int t0) {
+#pragma unroll
+    for (int e = 0; e < kFetch; ++e) {
+      const int j = (tid + e * kThreads) / kC16, c = (tid + e * kThreads) % kC16, u = t0 + j;
+      float* kd = k_s + j * kKS + 16 * c;
+      float* vd = v_s + j * D + 16 * c;
+      if (u >= len && u < u_end) {
+        const size_t at = (((size_t)b * a.k + (u - len)) * a.Hkv + hkv) * D + 16 * c;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          *reinterpret_cast<float4*>(kd + i) = load4(a.kb + at + i);
+          *reinterpret_cast<float4*>(vd + i) = load4(a.vb + at + i);
+        }
+        if (c == 0) sc_s[j] = 1.f;
+        continue;
+      }
+      const uint32_t kw[4] = {kf[e].x, kf[e].y, kf[e].z, kf[e].w};
+      const uint32_t vw[4] = {vf[e].x, vf[e].y, vf[e].z, vf[e].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[4], y[4];
+        e4m3x4_values(kw[i], x);
+        e4m3x4_values(vw[i], y);
+        *reinterpret_cast<float4*>(kd + 4 * i) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(vd + 4 * i) =
+            make_float4(y[0] * vsf[e], y[1] * vsf[e], y[2] * vsf[e], y[3] * vsf[e]);
+      }
+      if (c == 0) sc_s[j] = ksf[e];
+    }
+  };
+  if (u_begin < u_end) fetch(u_begin);
+
+  // Q rows of the chunk (zeros past M)
+  for (int e = tid; e < kRowsCta * kC4; e += kThreads) {
+    const int rl = e / kC4, c = e % kC4, r = chunk * kRowsCta + rl;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < a.M)
+      v = load4(a.q + (((size_t)b * a.k + r / a.G) * a.Hq + hkv * a.G + r % a.G) * D + 4 * c);
+    *reinterpret_cast<float4*>(q_s + rl * D + 4 * c) = v;
+  }
+
+  // this warp's rows: local rows RW*warp .. + RW - 1; keys u < vis[r] are seen
+  int vis[RW], vis_min = u_end;
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    const int i = (chunk * kRowsCta + RW * warp + r) / a.G;
+    vis[r] = min(u_end, len + (i < a.n_causal ? i + 1 : a.k));
+    vis_min = min(vis_min, vis[r]);
+  }
+  float m[RW], l[RW];                          // l: this lane's share of the row sum
+  float o[RW][kPer];
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) o[r][c] = 0.f;
+  }
+  const float* qw = q_s + RW * warp * D;
+  float* pw = p_s + RW * warp * kKeys;
+
+  for (int t0 = u_begin; t0 < u_end; t0 += kKeys) {
+    const int n = min(kKeys, u_end - t0);
+    commit(t0);
+    __syncthreads();
+    if (t0 + kKeys < u_end) fetch(t0 + kKeys);
+    // ---- S: keys lane and lane + 32 of the tile
+    const bool two = n > 32;
+    float s[RW][2];
+    {
+      float acc[RW][2];
+#pragma unroll
+      for (int r = 0; r < RW; ++r) acc[r][0] = acc[r][1] = 0.f;
+      const float* k0 = k_s + lane * kKS;
+      const float* k1 = k0 + 32 * kKS;
+      if (two) {
+#pragma unroll 4
+        for (int c = 0; c < kC4; ++c) {
+          const float4 x0 = *reinterpret_cast<const float4*>(k0 + 4 * c);
+          const float4 x1 = *reinterpret_cast<const float4*>(k1 + 4 * c);
+#pragma unroll
+          for (int r = 0; r < RW; ++r) {
+            const float4 qv = *reinterpret_cast<const float4*>(qw + r * D + 4 * c);
+            acc[r][0] = dot4(qv, x0, acc[r][0]);
+            acc[r][1] = dot4(qv, x1, acc[r][1]);
+          }
+        }
+      } else {
+#pragma unroll 4
+        for (int c = 0; c < kC4; ++c) {
+          const float4 x0 = *reinterpret_cast<const float4*>(k0 + 4 * c);
+#pragma unroll
+          for (int r = 0; r < RW; ++r)
+            acc[r][0] = dot4(*reinterpret_cast<const float4*>(qw + r * D + 4 * c), x0, acc[r][0]);
+        }
+      }
+      const float f0 = sc_s[lane] * a.scale_log2, f1 = sc_s[lane + 32] * a.scale_log2;
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        s[r][0] = t0 + lane < vis[r] ? acc[r][0] * f0 : -INFINITY;
+        s[r][1] = two && t0 + lane + 32 < vis[r] ? acc[r][1] * f1 : -INFINITY;
+      }
+    }
+    // ---- softmax of the tile
+#pragma unroll
+    for (int r = 0; r < RW; ++r) {
+      const float mn = fmaxf(m[r], warp_max(fmaxf(s[r][0], s[r][1])));
+      const float alpha = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mn);
+      const float p0 = s[r][0] == -INFINITY ? 0.f : exp2f(s[r][0] - mn);
+      const float p1 = s[r][1] == -INFINITY ? 0.f : exp2f(s[r][1] - mn);
+      m[r] = mn;
+      l[r] = fmaf(l[r], alpha, p0 + p1);
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) o[r][c] *= alpha;
+      pw[r * kKeys + lane] = p0;
+      pw[r * kKeys + lane + 32] = p1;
+    }
+    __syncwarp();
+    // ---- O += P V, 4 keys at a time, as far as every row of the warp sees them
+    const int n_all = t0 + n <= vis_min ? n : max(0, vis_min - t0) & ~3;
+#pragma unroll 2
+    for (int j = 0; j < n_all; j += 4) {
+      float v[4][kPer];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (kPer == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(v_s + (j + e) * D + 4 * lane);
+          v[e][0] = x.x, v[e][1] = x.y, v[e][2] = x.z, v[e][3] = x.w;
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(v_s + (j + e) * D + 2 * lane);
+          v[e][0] = x.x, v[e][1] = x.y;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        const float4 p = *reinterpret_cast<const float4*>(pw + r * kKeys + j);
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) {
+          o[r][c] = fmaf(p.x, v[0][c], o[r][c]);
+          o[r][c] = fmaf(p.y, v[1][c], o[r][c]);
+          o[r][c] = fmaf(p.z, v[2][c], o[r][c]);
+          o[r][c] = fmaf(p.w, v[3][c], o[r][c]);
+        }
+      }
+    }
+    // The rest, block keys that some causal row must not see: their values are
+    // left out there, not multiplied by 0 (they may be infinite or NaN).
+#pragma unroll 1
+    for (int j = n_all; j < n; ++j) {
+      float v[kPer];
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) v[c] = v_s[j * D + kPer * lane + c];
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        if (t0 + j >= vis[r]) continue;
+        const float p = pw[r * kKeys + j];
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) o[r][c] = fmaf(p, v[c], o[r][c]);
+      }
+    }
+    __syncthreads();                           // the tile is consumed
+  }
+  grid_dependents_launch();
+
+  auto store_row = [&](int rl, const float (&x)[kPer], float sum) {
+    const int r = chunk * kRowsCta + rl;
+    if (r >= a.M) return;
+    T* dst = a.out + (((size_t)b * a.k + r / a.G) * a.Hq + hkv * a.G + r % a.G) * D + kPer * lane;
+#pragma unroll
+    for (int c = 0; c < kPer; c += 2) store2(dst + c, x[c] / sum, x[c + 1] / sum);
+  };
+  if (a.splits == 1) {
+#pragma unroll
+    for (int r = 0; r < RW; ++r) store_row(RW * warp + r, o[r], warp_sum(l[r]));
+    return;
+  }
+  // ---- merge over the cluster: every CTA leaves its rows' maximum, sum and
+  // unnormalised O in shared memory; CTA `split` merges rows split,
+  // split + splits, ...  The second barrier keeps shared memory alive until
+  // every CTA has read it.
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    const int rl = RW * warp + r;
+    const float lr = warp_sum(l[r]);
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) o_s[rl * D + kPer * lane + c] = o[r][c];
+    if (lane == 0) {
+      st_s[rl] = m[r];
+      st_s[kRowsCta + rl] = lr;
+    }
+  }
+  cluster_sync_all();
+  for (int rl = split + a.splits * warp; rl < kRowsCta && chunk * kRowsCta + rl < a.M;
+       rl += a.splits * W) {
+    const float ms = lane < a.splits ? ld_rank(st_s + rl, lane) : -INFINITY;
+    const float ls = lane < a.splits ? ld_rank(st_s + kRowsCta + rl, lane) : 0.f;
+    const float mx = warp_max(ms);
+    const float w = ms == -INFINITY ? 0.f : exp2f(ms - mx);
+    const float lsum = warp_sum(w * ls);
+    float acc[kPer];
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) acc[c] = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < a.splits; ++e) {
+      const float we = __shfl_sync(0xffffffffu, w, e);
+#pragma unroll
+      for (int c = 0; c < kPer; ++c)
+        acc[c] = fmaf(we, ld_rank(o_s + rl * D + kPer * lane + c, e), acc[c]);
+    }
+    store_row(rl, acc, lsum);
+  }
+  cluster_sync_all();
+}
+
+// The instance for M packed rows: few rows per warp at small M (a small block
+// keeps every warp busy), else chunks of 32 rows on 8 warps.
+struct Kernel {
+  const void* fn;
+  size_t smem;
+  int rows;          // packed rows per CTA
+  int threads;
+};
+template <typename T, int D>
+Kernel fma_kernel_of(int M) {
+  if (M <= 8) return {(const void*)paged_fma_kernel<T, D, 2, 4>, fma_smem_bytes<D, 2, 4>(), 8, 128};
+  if (M <= 16) return {(const void*)paged_fma_kernel<T, D, 4, 4>, fma_smem_bytes<D, 4, 4>(), 16, 128};
+  return {(const void*)paged_fma_kernel<T, D, 4, 8>, fma_smem_bytes<D, 4, 8>(), 32, 256};
+}
+Kernel fma_kernel_for(bool bf16, int D, int M) {
+  if (bf16) return D == 128 ? fma_kernel_of<__nv_bfloat16, 128>(M) : fma_kernel_of<__nv_bfloat16, 64>(M);
+  return D == 128 ? fma_kernel_of<float, 128>(M) : fma_kernel_of<float, 64>(M);
+}
+
+// Key ranges per (sequence, KV head, row chunk): as many as two CTAs per SM
+// allow, one range per kGranule keys at most, in a cluster size whose clusters
+// the device holds all at once.
+int fma_splits(const sbd::AttnQ8Plan& p, const Kernel& kern, int asked) {
+  const long long jobs = (long long)p.B * p.Hkv * p.chunks;
+  const long long by_keys = ((long long)p.max_pages * p.P + p.k + kGranule - 1) / kGranule;
+  if (jobs <= 0) return 1;
+  for (int s : {16, 12, 10, 8, 6, 5, 4, 3, 2}) {
+    if (asked > 0 ? s > asked : s > by_keys || s * jobs > 2ll * sbd::num_sms()) continue;
+    if (sbd::cluster_slots(kern.fn, kern.threads, kern.smem, s) >= (asked > 0 ? 1 : jobs)) return s;
+  }
+  return 1;
+}
+
+template <typename T>
+sbd_status fma_launch(const sbd::AttnQ8Plan& p, const sbd::AttnQ8Tensors& t, cudaStream_t st) {
+  const Kernel kern = fma_kernel_for(p.bf16, p.D, p.M);
+  Args<T> a;
+  a.q = (const T*)t.q;
+  a.kc = (const uint8_t*)t.k_cache;
+  a.vc = (const uint8_t*)t.v_cache;
+  a.ks = t.k_scale;
+  a.vs = t.v_scale;
+  a.table = t.table;
+  a.lens = t.lens;
+  a.kb = (const T*)t.kb;
+  a.vb = (const T*)t.vb;
+  a.out = (T*)t.out;
+  a.err = sbd::device_error_word();
+  a.k = p.k;
+  a.Hq = p.Hq;
+  a.Hkv = p.Hkv;
+  a.G = p.G;
+  a.M = p.M;
+  a.P = p.P;
+  a.max_pages = p.max_pages;
+  a.n_pages = p.n_pages;
+  a.n_causal = p.n_causal;
+  a.splits = p.splits;
+  a.chunks = p.chunks;
+  a.scale_log2 = p.scale_log2;
+  const sbd_status s = sbd::allow_smem(kern.fn, kern.smem, "cudaFuncSetAttribute(paged_fma_kernel)");
+  if (s != SBD_OK) return s;
+  void* args[] = {(void*)&a};
+  return sbd::launch_pdl(kern.fn, dim3(p.splits, p.Hkv * p.chunks, p.B), dim3(kern.threads),
+                         kern.smem, st, args, "paged_fma_kernel launch", p.splits);
+}
+
+}  // namespace
+
+namespace sbd {
+
+AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d) {
+  AttnQ8Plan p;
+  p.B = d.batch;
+  p.k = d.block_k;
+  p.Hq = d.n_q_heads;
+  p.Hkv = d.n_kv_heads;
+  p.G = d.n_q_heads / d.n_kv_heads;
+  p.D = d.head_dim;
+  p.P = d.page_size;
+  p.max_pages = d.max_pages;
+  p.n_pages = d.n_pages;
+  p.M = p.G * p.k;
+  p.n_causal = d.n_causal;
+  p.bf16 = d.dtype == SBD_DTYPE_BF16;
+  const float scale = d.scale != 0.f ? d.scale : 1.0f / sqrtf((float)d.head_dim);
+  p.scale_log2 = scale * kLog2e;
+  const Kernel kern = fma_kernel_for(p.bf16, p.D, p.M);
+  p.rows = kern.rows;
+  p.chunks = (p.M + kern.rows - 1) / kern.rows;
+  p.splits = fma_splits(p, kern, d.num_splits);
+  p.cluster = p.splits > 1;
+  return p;
+}
+
+size_t attn_q8_workspace_bytes(const AttnQ8Plan&) { return 0; }
+
+sbd_status attn_q8_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, void*, cudaStream_t st) {
+  return p.bf16 ? fma_launch<__nv_bfloat16>(p, t, st) : fma_launch<float>(p, t, st);
+}
+
+}  // namespace sbd
