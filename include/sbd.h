@@ -327,7 +327,7 @@ sbd_status sbd_select(int32_t rule, int32_t batch, int32_t block_k, const float*
  *   block_table      [B, max_pages] int32  page of a request's tokens p P .. p P + P - 1
  *                                          in column p; -1 where it holds none
  * A token's slot is page * P + its place in the page.  P in {16, 32, 64, 128},
- * D in {64, 128}, n_pages * P < 2^31.
+ * D in {64, 128}, n_pages * P < 2^31, n_pages * Hkv < 2^31.
  *
  * One turn of a serving loop: sbd_block_tables gives the requests the pages of
  * the lengths they are to have, sbd_cache_append_q8 fills the new slots, and

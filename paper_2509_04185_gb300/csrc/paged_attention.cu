@@ -1,5 +1,5 @@
 // Block attention over the paged 8-bit cache: the plan, the launch, and the
-// kernel on fp32 FMAs.
+// kernel on fp32 FMAs (fp32 activations; bf16 ones go to paged_attention_tc.cu).
 //
 //   O_r = sum_j p_rj v_j,   p_r = softmax_j(scale q_r . k_j)
 //
@@ -42,28 +42,13 @@ __device__ __forceinline__ float ld_rank(const float* p, int rank) {
   return v;
 }
 
-// 4 consecutive elements as floats
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
-                     __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-}
-__device__ __forceinline__ void store2(float* p, float x, float y) {
-  *reinterpret_cast<float2*>(p) = make_float2(x, y);
-}
-__device__ __forceinline__ void store2(__nv_bfloat16* p, float x, float y) {
-  *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y);
-}
-
-template <typename T>
 struct Args {
-  const T* q;
+  const float* q;
   const uint8_t *kc, *vc;
   const float *ks, *vs;
   const int32_t *table, *lens;
-  const T *kb, *vb;
-  T* out;
+  const float *kb, *vb;
+  float* out;
   int* err;
   int k, Hq, Hkv, G, M, P, max_pages, n_pages, n_causal, splits, chunks;
   float scale_log2;
@@ -81,8 +66,8 @@ constexpr size_t fma_smem_bytes() {
                           + kKeys);                                 // key scales
 }
 
-template <typename T, int D, int RW, int W>
-__global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args<T> a) {
+template <int D, int RW, int W>
+__global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args a) {
   constexpr int kThreads = 32 * W;
   constexpr int kRowsCta = W * RW;
   constexpr int kKS = k_stride<D>();
@@ -150,8 +135,8 @@ __global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args<T> a) {
         const size_t at = (((size_t)b * a.k + (u - len)) * a.Hkv + hkv) * D + 16 * c;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          *reinterpret_cast<float4*>(kd + i) = load4(a.kb + at + i);
-          *reinterpret_cast<float4*>(vd + i) = load4(a.vb + at + i);
+          *reinterpret_cast<float4*>(kd + i) = *reinterpret_cast<const float4*>(a.kb + at + i);
+          *reinterpret_cast<float4*>(vd + i) = *reinterpret_cast<const float4*>(a.vb + at + i);
         }
         if (c == 0) sc_s[j] = 1.f;
         continue;
@@ -177,7 +162,8 @@ __global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args<T> a) {
     const int rl = e / kC4, c = e % kC4, r = chunk * kRowsCta + rl;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < a.M)
-      v = load4(a.q + (((size_t)b * a.k + r / a.G) * a.Hq + hkv * a.G + r % a.G) * D + 4 * c);
+      v = *reinterpret_cast<const float4*>(
+          a.q + (((size_t)b * a.k + r / a.G) * a.Hq + hkv * a.G + r % a.G) * D + 4 * c);
     *reinterpret_cast<float4*>(q_s + rl * D + 4 * c) = v;
   }
 
@@ -307,9 +293,10 @@ __global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args<T> a) {
   auto store_row = [&](int rl, const float (&x)[kPer], float sum) {
     const int r = chunk * kRowsCta + rl;
     if (r >= a.M) return;
-    T* dst = a.out + (((size_t)b * a.k + r / a.G) * a.Hq + hkv * a.G + r % a.G) * D + kPer * lane;
+    float* dst = a.out + (((size_t)b * a.k + r / a.G) * a.Hq + hkv * a.G + r % a.G) * D + kPer * lane;
 #pragma unroll
-    for (int c = 0; c < kPer; c += 2) store2(dst + c, x[c] / sum, x[c + 1] / sum);
+    for (int c = 0; c < kPer; c += 2)
+      *reinterpret_cast<float2*>(dst + c) = make_float2(x[c] / sum, x[c + 1] / sum);
   };
   if (a.splits == 1) {
 #pragma unroll
@@ -362,16 +349,13 @@ struct Kernel {
   int rows;          // packed rows per CTA
   int threads;
 };
-template <typename T, int D>
+template <int D>
 Kernel fma_kernel_of(int M) {
-  if (M <= 8) return {(const void*)paged_fma_kernel<T, D, 2, 4>, fma_smem_bytes<D, 2, 4>(), 8, 128};
-  if (M <= 16) return {(const void*)paged_fma_kernel<T, D, 4, 4>, fma_smem_bytes<D, 4, 4>(), 16, 128};
-  return {(const void*)paged_fma_kernel<T, D, 4, 8>, fma_smem_bytes<D, 4, 8>(), 32, 256};
+  if (M <= 8) return {(const void*)paged_fma_kernel<D, 2, 4>, fma_smem_bytes<D, 2, 4>(), 8, 128};
+  if (M <= 16) return {(const void*)paged_fma_kernel<D, 4, 4>, fma_smem_bytes<D, 4, 4>(), 16, 128};
+  return {(const void*)paged_fma_kernel<D, 4, 8>, fma_smem_bytes<D, 4, 8>(), 32, 256};
 }
-Kernel fma_kernel_for(bool bf16, int D, int M) {
-  if (bf16) return D == 128 ? fma_kernel_of<__nv_bfloat16, 128>(M) : fma_kernel_of<__nv_bfloat16, 64>(M);
-  return D == 128 ? fma_kernel_of<float, 128>(M) : fma_kernel_of<float, 64>(M);
-}
+Kernel fma_kernel_for(int D, int M) { return D == 128 ? fma_kernel_of<128>(M) : fma_kernel_of<64>(M); }
 
 // Key ranges per (sequence, KV head, row chunk): as many as two CTAs per SM
 // allow, one range per kGranule keys at most, in a cluster size whose clusters
@@ -387,20 +371,19 @@ int fma_splits(const sbd::AttnQ8Plan& p, const Kernel& kern, int asked) {
   return 1;
 }
 
-template <typename T>
 sbd_status fma_launch(const sbd::AttnQ8Plan& p, const sbd::AttnQ8Tensors& t, cudaStream_t st) {
-  const Kernel kern = fma_kernel_for(p.bf16, p.D, p.M);
-  Args<T> a;
-  a.q = (const T*)t.q;
+  const Kernel kern = fma_kernel_for(p.D, p.M);
+  Args a;
+  a.q = (const float*)t.q;
   a.kc = (const uint8_t*)t.k_cache;
   a.vc = (const uint8_t*)t.v_cache;
   a.ks = t.k_scale;
   a.vs = t.v_scale;
   a.table = t.table;
   a.lens = t.lens;
-  a.kb = (const T*)t.kb;
-  a.vb = (const T*)t.vb;
-  a.out = (T*)t.out;
+  a.kb = (const float*)t.kb;
+  a.vb = (const float*)t.vb;
+  a.out = (float*)t.out;
   a.err = sbd::device_error_word();
   a.k = p.k;
   a.Hq = p.Hq;
@@ -441,7 +424,11 @@ AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d) {
   p.bf16 = d.dtype == SBD_DTYPE_BF16;
   const float scale = d.scale != 0.f ? d.scale : 1.0f / sqrtf((float)d.head_dim);
   p.scale_log2 = scale * kLog2e;
-  const Kernel kern = fma_kernel_for(p.bf16, p.D, p.M);
+  if (p.bf16) {
+    paged_tc_plan(&p, d.num_splits);
+    return p;
+  }
+  const Kernel kern = fma_kernel_for(p.D, p.M);
   p.rows = kern.rows;
   p.chunks = (p.M + kern.rows - 1) / kern.rows;
   p.splits = fma_splits(p, kern, d.num_splits);
@@ -452,7 +439,7 @@ AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d) {
 size_t attn_q8_workspace_bytes(const AttnQ8Plan&) { return 0; }
 
 sbd_status attn_q8_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, void*, cudaStream_t st) {
-  return p.bf16 ? fma_launch<__nv_bfloat16>(p, t, st) : fma_launch<float>(p, t, st);
+  return p.bf16 ? paged_tc_launch(p, t, st) : fma_launch(p, t, st);
 }
 
 }  // namespace sbd

@@ -1,0 +1,990 @@
+// Block attention over the paged 8-bit cache on the tcgen05 tensor cores, for
+// bf16 activations.
+//
+// The codes are what the tensor cores read (kind::f8f6f4): no conversion of the
+// cache anywhere.  Activations carry 8 significant bits and a code 4, so every
+// activation enters as a pair of codes, x / s = hi + lo: the rounding of x / s to
+// e4m3 and the rounding of what that leaves, s a power of two that brings the
+// row's largest element to 224 .. 448.  Keys are the M side of both products:
+//
+//   S[key, (hi|lo) row]  = K Q^T      A = K tile (128 keys, K-major),
+//                                     B = the rows' hi codes, then their lo codes
+//   O[dim, (hi|lo) row] += V^T P^T    A = V tile (MN-major), B = P (MN-major)
+//
+// so that N = 2 R is what the call needs (R = 16, 32 or 64 packed rows of the KV
+// head's group a CTA, r = i*G + g) and a thread of the softmax owns one key: its
+// page's scales are scalars of the thread, masks a comparison, the row's maximum
+// one redux a warp.
+//
+// P.  Probabilities span more octaves than two codes: next to a key that takes all
+// the weight, a thousand weak ones would vanish.  So P is relative to the maximum
+// of its own tile of 128 keys (times the value scale over the tile's largest, and
+// 2^8), every tile's product starts at zero, and four warps add it to fp32
+// accumulators in registers, weighted 2^(m_tile - m).  lo codes of P are scaled
+// by 2^5 and weighted back there.  No accumulator in tensor memory is ever
+// rescaled, and the softmax never waits for one.
+//
+// Block keys (not cached, bf16) form the last tile: the keys split into code pairs
+// like the rows, two products for S; the values as they are against P in bf16
+// (kind::f16), since a row may see a single small value of a key.
+//
+// Warp roles: 0 pages and TMA, 1 tensor memory and MMA issue, 2-9 softmax, 10-13
+// block keys first, then the accumulators.  With R = 64 softmax warps 2-5 take
+// rows 0-31 of every tile and 6-9 rows 32-63; else they take alternate tiles.
+#include <math.h>
+
+#include "paged.cuh"
+
+namespace {
+
+using namespace sbd_dev;
+
+constexpr int kTile = 128;                   // keys
+constexpr int kSoftWarps = 8;
+constexpr int kAccWarps = 4;
+constexpr int kThreads = 32 * (2 + kSoftWarps + kAccWarps);
+constexpr int kMaxStages = 8;
+constexpr int kBlkKeys = 32;                 // block keys, padded
+constexpr int kMaxSplits = 16;
+constexpr float kPScale = 256.f;             // P = 2^8 p
+constexpr float kLoScale = 32.f;             // lo codes of P hold 2^5 of the rest
+
+// ------------------------------------------------------------ tcgen05 PTX
+__device__ __forceinline__ void tc_alloc(uint32_t* dst_smem, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                   smem_u32(dst_smem)),
+               "r"(ncols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_dealloc(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols)
+               : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() {
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tc_fence_after() {
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                          uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                            uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+          smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tc_wait_ld() {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar,
+                                            int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+// The maximum over a warp (NaN only where every lane has it).
+__device__ __forceinline__ float redux_max(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// Shared-memory operands of rows of `W` = 32, 64 or 128 bytes, swizzled over W:
+// 16-byte pieces of a row permuted by the row's place, the pattern repeating every
+// 8 rows (one 8 W-byte atom).
+template <int W>
+__device__ __forceinline__ uint32_t swz(uint32_t base, int row, int piece) {
+  constexpr int kMask = W / 16 - 1;
+  constexpr int kShift = W == 128 ? 0 : W == 64 ? 1 : 2;
+  return base + row * W + ((piece ^ ((row >> kShift) & kMask)) << 4);
+}
+// Descriptor of such an operand: 8-row groups 8 W apart; `next` bytes from one
+// atom to the next along a row (MN-major operands wider than an atom).
+template <int W>
+__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t next = 16) {
+  constexpr uint64_t kMode = W == 128 ? 2 : W == 64 ? 4 : 6;
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(next >> 4) << 16 |
+         (uint64_t)(8 * W >> 4) << 32 | (uint64_t)1 << 46 | kMode << 61;
+}
+// e4m3 A and B, fp32 D.
+__device__ __forceinline__ uint32_t idesc_f8(int M, int N, bool mn_major) {
+  return 1u << 4 | (mn_major ? 1u : 0u) << 15 | (mn_major ? 1u : 0u) << 16 |
+         (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24;
+}
+// bf16 A and B, both MN-major, fp32 D.
+__device__ __forceinline__ uint32_t idesc_bf16_mn(int M, int N) {
+  return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(N >> 3) << 17 |
+         (uint32_t)(M >> 4) << 24;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z),
+               "r"(v.w)
+               : "memory");
+}
+__device__ __forceinline__ void st_shared_b32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void st_shared_b16(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"((uint16_t)v) : "memory");
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// ------------------------------------------------------------ clusters
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
+               "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t mapa_shared(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_cluster_v2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+
+struct Args {
+  const __nv_bfloat16 *q, *kb, *vb;
+  const float *ks, *vs;
+  const int32_t *table, *lens;
+  __nv_bfloat16* out;
+  int* err;
+  int B, k, Hq, Hkv, G, M, max_pages, n_pages, n_causal, splits, chunks;
+  int page_log2;
+  int order;                 // blockIdx.z -> sequence by descending length
+  float scale_log2;
+};
+
+template <int D, int R>
+struct Shape {
+  static constexpr int kRT = R < 32 ? R : 32;          // rows of a softmax thread
+  static constexpr int kRowGroups = R / kRT;
+  static constexpr int kTileGroups = 2 / kRowGroups;
+  static constexpr int kKV = kTile * D;                // a K or V tile
+  static constexpr int kQ = 2 * R * D;
+  static constexpr int kP = kTile * 2 * R;
+  // The block's keys (hi rows, then lo rows), or its values (bf16, 64 dimensions
+  // a sub-tile).
+  static constexpr int kBlk = 2 * kBlkKeys * D;
+  static constexpr int kBlkSub = kBlkKeys * 128;
+  static constexpr int kFixed = 1024 + kQ + 2 * kP + 2 * kBlk;
+  static constexpr int kLeft = 227 * 1024 - 6 * 1024 - kFixed;     // 6 KB: barriers and tables
+  static constexpr int kStages = kLeft / (2 * kKV) < kMaxStages ? kLeft / (2 * kKV) : kMaxStages;
+  static constexpr int kSmem = kFixed + kStages * 2 * kKV;
+  static constexpr int kPStride = D + 4;               // floats of a partial row
+  static_assert(R * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
+  static_assert(kBlk + kTile * D <= 2 * kBlk + kStages * 2 * kKV, "reads past the block's keys stay inside");
+};
+
+// x = s (hi + lo): the codes of n values of a row, s a power of two (inv = 1 / s).
+// What is not finite becomes NaN.
+__device__ __forceinline__ float finite_or_nan(float x) {
+  return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __int_as_float(0x7fffffff) : x;
+}
+__device__ __forceinline__ float finite_size(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+  return u < 0x7f800000u ? __uint_as_float(u) : 0.f;
+}
+template <int N>
+__device__ __forceinline__ void split_codes(const float (&x)[N], float inv, uint32_t* hi, uint32_t* lo) {
+  float y[4] = {0.f, 0.f, 0.f, 0.f}, h[4];
+#pragma unroll
+  for (int e = 0; e < N; ++e) y[e] = finite_or_nan(x[e]) * inv;
+  *hi = e4m3x4(y[0], y[1], y[2], y[3]);
+  e4m3x4_values(*hi, h);
+  *lo = e4m3x4(y[0] - h[0], y[1] - h[1], y[2] - h[2], y[3] - h[3]);
+}
+// One row of D values over a warp, D / 32 a lane.
+template <int D>
+struct WarpRow {
+  static constexpr int kN = D / 32;
+  uint32_t w[kN / 2];
+  __device__ __forceinline__ void load(const __nv_bfloat16* row, int lane) {
+    if constexpr (kN == 4) {
+      const uint2 v = *reinterpret_cast<const uint2*>(row + 4 * lane);
+      w[0] = v.x, w[1] = v.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(row + 2 * lane);
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int e = 0; e < kN / 2; ++e) w[e] = 0;
+  }
+  __device__ __forceinline__ void get(float (&x)[kN]) const {
+#pragma unroll
+    for (int e = 0; e < kN / 2; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+  // Writes the codes into rows `hi_row` and `lo_row` of the operand at `base`;
+  // returns the scale.
+  __device__ __forceinline__ float store(uint32_t base, int hi_row, int lo_row, int lane) const {
+    float x[kN];
+    get(x);
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) amax = fmaxf(amax, finite_size(x[e]));
+    amax = redux_max(amax);
+    const float s = scale_for(amax);
+    uint32_t hi, lo;
+    split_codes<kN>(x, 1.f / s, &hi, &lo);
+    const int byte = kN * lane;
+    const uint32_t ha = swz<D>(base, hi_row, byte / 16) + byte % 16;
+    const uint32_t la = swz<D>(base, lo_row, byte / 16) + byte % 16;
+    if constexpr (kN == 4) {
+      st_shared_b32(ha, hi);
+      st_shared_b32(la, lo);
+    } else {
+      st_shared_b16(ha, hi);
+      st_shared_b16(la, lo);
+    }
+    return s;
+  }
+};
+
+// v[i] of lane l becomes, in v[0], the sum over lanes of v[l % N].
+template <int N>
+__device__ __forceinline__ void sum_across(float (&v)[N], int lane) {
+  if constexpr (N == 16) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 16);
+  }
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) {
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const bool up = lane & o;
+      const float send = up ? v[i] : v[i + o];
+      v[i] = (up ? v[i + o] : v[i]) + __shfl_xor_sync(0xffffffffu, send, o);
+    }
+  }
+}
+
+template <int D, int R>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
+                const __grid_constant__ CUtensorMap tmap_v, const Args a) {
+  using C = Shape<D, R>;
+  constexpr int RT = C::kRT, kStages = C::kStages;
+  constexpr uint32_t kTmemCols = 8 * R;                // S: 2 x 2 R, O: 2 x 2 R
+  constexpr uint32_t kOCol = 4 * R;
+  constexpr int kHandIn = 4 * C::kRowGroups;           // softmax warps of a tile
+  static_assert(R == 16 || R == 32 || R == 64, "N = 2 R is one swizzle atom");
+
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
+  __shared__ __align__(8) uint64_t s_full[2], s_free[2], p_full[2], o_full[2], o_free[2];
+  __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ int b_pick, blk_bad;
+  __shared__ float ks_sh[kMaxStages][8], vs_sh[kMaxStages][8], vref_sh[kMaxStages];
+  __shared__ float bks_sh[kBlkKeys];
+  __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
+  __shared__ int vis_sh[R];                            // block keys that it sees
+  __shared__ __align__(16) float red_sh[2][4][RT];     // a warp's maxima; at the end its sums
+  __shared__ __align__(16) float mq_sh[2][RT], g_sh[2][RT], al_sh[2][RT];
+  __shared__ int moved_sh[2];
+  __shared__ float mt_sh[4][R], vr_sh[4];              // a tile's maxima and value reference
+  __shared__ __align__(16) float f_sh[2][R], fa_sh[2][R];
+  __shared__ int fmoved_sh[2];
+  __shared__ float mref_sh[2][RT];
+
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_s = sbase, p_s = q_s + C::kQ;
+  const uint32_t bk_s = p_s + 2 * C::kP, bv_s = bk_s + C::kBlk;
+  const uint32_t ring = bv_s + C::kBlk;
+  auto k_tile = [&](int j) { return ring + (uint32_t)(j % kStages) * 2 * C::kKV; };
+  auto v_tile = [&](int j) { return k_tile(j) + C::kKV; };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&kv_full[s], 1);
+      mbar_init(&kv_empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_full[i], 2);              // the product, and its issuer's view of the stage
+      mbar_init(&s_free[i], kHandIn);
+      mbar_init(&p_full[i], kHandIn);
+      mbar_init(&o_full[i], 2);
+      mbar_init(&o_free[i], kAccWarps);
+    }
+    mbar_init(&q_ready, kSoftWarps);
+    mbar_init(&blk_ready, kAccWarps);
+    mbar_init(&tail_bar, 1);
+    blk_bad = 0;
+    fence_mbar_init();
+  }
+  // Tensor memory is taken only after the previous grid is done, so that no CTA
+  // of it can be left waiting for it.
+  grid_dependency_wait();
+  const int cap = a.max_pages << a.page_log2;
+  if (a.order) {
+    longest_first_pick(a.lens, a.B, cap, blockIdx.z, &b_pick);
+    __syncthreads();
+  }
+  const int b = a.order ? b_pick : (int)blockIdx.z;
+  if (warp == 1) tc_alloc(&tmem_base_sh, kTmemCols);
+  int len = a.lens[b];
+  if (len < 0 || len > cap) {
+    if (threadIdx.x == 0 && split == 0 && blockIdx.y == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
+    len = len < 0 ? 0 : cap;
+  }
+  const int n_cache = (int)(((long long)len + kTile - 1) / kTile);
+  const int n_tiles = n_cache + 1;
+  const int t_begin = (int)((long long)split * n_tiles / a.splits);
+  const int t_end = (int)((long long)(split + 1) * n_tiles / a.splits);
+  const int n = t_end - t_begin;             // tiles of this CTA
+  const bool has_block = t_end == n_tiles && n > 0;
+  // keys of local tile j (the block's tile comes last)
+  auto keys_of = [&](int j) {
+    const int t = t_begin + j;
+    return t < n_cache ? min(kTile, len - t * kTile) : a.k;
+  };
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_sh;
+
+  if (warp == 0) {
+    // ------------------------------------------------ pages and TMA
+    if (lane == 0) {
+      tma_prefetch_desc(&tmap_k);
+      tma_prefetch_desc(&tmap_v);
+    }
+    const int P = 1 << a.page_log2, per_tile = kTile >> a.page_log2;
+    const int n_mine = n - (has_block ? 1 : 0);
+    const int p_first = t_begin * per_tile;
+    const int p_end = (int)(((long long)min((t_begin + n_mine) * (long long)kTile, (long long)len) + P - 1) >> a.page_log2);
+    const int32_t* table = a.table + (size_t)b * a.max_pages;
+    // Pages come in windows of 32, one a lane: ids a window ahead, their scales a
+    // tile into the window before.  A page out of range lies past the tensor's
+    // end for the copy, which reads zeros there.
+    auto id_at = [&](int p) {
+      if (p >= p_end) return -1;
+      const int id = table[p];
+      if (id >= 0 && id < a.n_pages) return id;
+      record_error(a.err, SBD_DEVERR_PAGE);
+      return a.n_pages;
+    };
+    auto scale_at = [&](const float* s, int id) {
+      return id >= 0 && id < a.n_pages ? s[(size_t)id * a.Hkv + hkv] : 0.f;
+    };
+    int id = id_at(p_first + lane), id_next = id_at(p_first + 32 + lane);
+    float ks = scale_at(a.ks, id), vs = scale_at(a.vs, id), ks_next = 0.f, vs_next = 0.f;
+    const int per_window = 32 / per_tile;
+    int issued = 0;
+    for (int j = 0; j < n_mine; ++j) {
+      const int w = j % per_window;
+      if (w == 0 && j > 0) {
+        id = id_next, ks = ks_next, vs = vs_next;
+        id_next = id_at(p_first + (j / per_window + 1) * 32 + lane);
+      }
+      if (w == 1) ks_next = scale_at(a.ks, id_next), vs_next = scale_at(a.vs, id_next);
+      const int stage = j % kStages;
+      const bool freed = mbar_wait(&kv_empty[stage], ((j / kStages) & 1) ^ 1, a.err);
+      if (!__all_sync(0xffffffffu, freed)) break;
+      const int valid = keys_of(j), n_pg = (valid + P - 1) >> a.page_log2;
+      const int src = w * per_tile + lane;   // lane i < n_pg: the tile's page i
+      const int pg = __shfl_sync(0xffffffffu, id, src & 31);
+      const float k_sc = __shfl_sync(0xffffffffu, ks, src & 31);
+      const float v_sc = __shfl_sync(0xffffffffu, vs, src & 31);
+      const float v_max = redux_max(lane < n_pg ? v_sc : 0.f);
+      if (lane < per_tile) {
+        ks_sh[stage][lane] = lane < n_pg ? k_sc : 0.f;
+        vs_sh[stage][lane] = lane < n_pg ? v_sc : 0.f;
+      }
+      if (lane == 0) vref_sh[stage] = v_max;
+      __syncwarp();
+      const bool tail = (valid & 31) != 0;
+      uint64_t* bar = tail ? &tail_bar : &kv_full[stage];
+      if (lane == 0) mbar_arrive_expect_tx(bar, 2 * n_pg * P * D);
+      __syncwarp();
+      if (lane < n_pg) {
+        const int row = pg < a.n_pages ? pg * a.Hkv + hkv : a.n_pages * a.Hkv;
+        tma_load_3d(k_tile(j) + lane * P * D, &tmap_k, bar, 0, 0, row);
+        tma_load_3d(v_tile(j) + lane * P * D, &tmap_v, bar, 0, 0, row);
+      }
+      issued = j + 1;
+      if (tail) {
+        // Values past the length may be anything (NaN); the products go on to the
+        // next multiple of 32 keys, so those become zeros.
+        mbar_wait(&tail_bar, 0, a.err);
+        const int end = (valid + 31) & ~31;
+        for (int c = lane; c < (end - valid) * (D / 16); c += 32)
+          st_shared_v4(v_tile(j) + valid * D + 16 * c, make_uint4(0, 0, 0, 0));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&kv_full[stage]);
+      }
+    }
+    // no copy is in flight when the CTA ends, whatever became of its consumers
+    for (int j = max(0, issued - kStages); j < issued; ++j)
+      mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
+  } else if (warp == 1) {
+    // ------------------------------------------------ MMA issuer
+    if (lane == 0 && n > 0) {
+      bool ok = mbar_wait(&q_ready, 0, a.err);
+      tc_fence_after();
+      const uint32_t id_s = idesc_f8(kTile, 2 * R, false), id_pv = idesc_f8(D, 2 * R, true);
+      auto is_block = [&](int j) { return has_block && j == n - 1; };
+      auto issue_s = [&](int j) {
+        const uint32_t d = tmem + (uint32_t)((j & 1) * 2 * R);
+        const int passes = is_block(j) ? 2 : 1;
+        for (int e = 0; e < passes; ++e) {
+          const uint32_t kt = is_block(j) ? bk_s + e * kBlkKeys * D : k_tile(j);
+#pragma unroll
+          for (int kk = 0; kk < D / 32; ++kk)
+            tc_mma_f8(d, desc<D>(kt + 32 * kk), desc<D>(q_s + 32 * kk), id_s, e > 0 || kk > 0);
+        }
+        tc_commit(&s_full[j & 1]);
+        mbar_arrive(&s_full[j & 1]);
+      };
+      auto issue_pv = [&](int j) {
+        const uint32_t o = tmem + kOCol + (uint32_t)((j & 1) * 2 * R);
+        const uint32_t pt = p_s + (j & 1) * C::kP;
+        if (is_block(j)) {
+#pragma unroll
+          for (int kk = 0; kk < kBlkKeys / 16; ++kk)
+            tc_mma_bf16(o, desc<128>(bv_s + kk * 16 * 128, C::kBlkSub), desc<2 * R>(pt + kk * 16 * 2 * R),
+                        idesc_bf16_mn(D, R), kk > 0);
+        } else {
+          const int steps = (keys_of(j) + 31) / 32;
+          for (int kk = 0; kk < steps; ++kk)
+            tc_mma_f8(o, desc<D>(v_tile(j) + kk * 32 * D), desc<2 * R>(pt + kk * 32 * 2 * R), id_pv,
+                      kk > 0);
+          tc_commit(&kv_empty[j % kStages]);
+        }
+        tc_commit(&o_full[j & 1]);
+        mbar_arrive(&o_full[j & 1]);
+      };
+      // Scores run up to two tiles ahead; whichever is ready first is issued.
+      int next_s = 0, next_pv = 0;
+      uint64_t t0 = 0;
+      for (uint32_t idle = 0; ok && next_pv < n;) {
+        bool moved = false;
+        if (next_s < n && next_s < next_pv + 2 &&
+            (is_block(next_s) ? mbar_poll_parity(&blk_ready, 0)
+                              : mbar_poll_parity(&kv_full[next_s % kStages], (next_s / kStages) & 1)) &&
+            mbar_poll_parity(&s_free[next_s & 1], ((next_s >> 1) & 1) ^ 1)) {
+          tc_fence_after();
+          issue_s(next_s++);
+          moved = true;
+        }
+        if (next_pv < next_s && mbar_poll_parity(&p_full[next_pv & 1], (next_pv >> 1) & 1) &&
+            mbar_poll_parity(&o_free[next_pv & 1], ((next_pv >> 1) & 1) ^ 1)) {
+          tc_fence_after();
+          issue_pv(next_pv++);
+          moved = true;
+        }
+        if (moved) {
+          idle = 0;
+        } else if ((++idle & 63u) == 0) {            // bounded, as mbar_wait
+          const uint64_t now = globaltimer();
+          if (idle == 64) t0 = now;
+          if (now - t0 > kWaitLimitNs) {
+            record_error(a.err, SBD_DEVERR_TIMEOUT);
+            ok = false;
+          }
+        }
+      }
+    }
+  } else if (warp < 2 + kSoftWarps) {
+    // ------------------------------------------------ softmax warps
+    const int sw = warp - 2, quad = warp & 3, grp = sw >> 2;
+    const int r0 = C::kRowGroups > 1 ? grp * RT : 0;   // first row of this thread
+    const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    {
+      constexpr int kRows = R / kSoftWarps;
+      WarpRow<D> x[kRows];
+#pragma unroll
+      for (int e = 0; e < kRows; ++e) {
+        const int row = chunk * R + sw * kRows + e;
+        if (row < a.M)
+          x[e].load(a.q + (((size_t)b * a.k + row / a.G) * a.Hq + hkv * a.G + row % a.G) * D, lane);
+        else
+          x[e].zero();
+      }
+#pragma unroll
+      for (int e = 0; e < kRows; ++e) {
+        const int r = sw * kRows + e, i = (chunk * R + r) / a.G;
+        const float s = x[e].store(q_s, r, R + r, lane);
+        if (lane == 0) {
+          c_sh[r] = s * a.scale_log2;
+          vis_sh[r] = i < a.n_causal ? i + 1 : a.k;
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_ready);
+      bar_sync(4, 32 * kSoftWarps);                    // c and vis of all rows
+    }
+    float l[RT];                                       // this key lane's sums, against m_ref
+#pragma unroll
+    for (int r = 0; r < RT; ++r) l[r] = 0.f;
+    float m_ref = -INFINITY;                           // of row r0 + lane, in the warp of quad 0
+    bool ok = true;
+    const int j_first = C::kTileGroups > 1 ? grp : 0;
+    for (int j = j_first; j < n; j += C::kTileGroups) {
+      const bool blk = has_block && j == n - 1;
+      const int stage = j % kStages, valid = keys_of(j);
+      const int key = quad * 32 + lane;
+      const bool warp_has = quad * 32 < valid;
+      if (ok && !mbar_wait(&s_full[j & 1], (j >> 1) & 1, a.err)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      float z[RT];
+      float vfac = 0.f, vref = 0.f;
+      if (ok) {
+        tc_fence_after();
+        float kf, vf;
+        if (blk) {
+          kf = bks_sh[key & 31];
+          vf = vref = 1.f;
+        } else {
+          kf = ks_sh[stage][key >> a.page_log2], vf = vs_sh[stage][key >> a.page_log2];
+          vref = vref_sh[stage];
+        }
+        vfac = vref > 0.f ? kPScale * (vf / vref) : vf * 0.f;
+        if (warp_has) {
+          const uint32_t sa = tmem + lane_addr + (uint32_t)((j & 1) * 2 * R + r0);
+#pragma unroll
+          for (int c = 0; c < RT / 16; ++c) {
+            uint32_t h[16], lo[16];
+            tc_ld16(sa + 16 * c, h);
+            tc_ld16(sa + R + 16 * c, lo);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              z[16 * c + e] = (__uint_as_float(h[e]) + __uint_as_float(lo[e])) * kf;
+          }
+          if (blk) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              if (key >= vis_sh[r0 + r]) z[r] = -INFINITY;
+          } else if (valid < quad * 32 + 32) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              if (key >= valid) z[r] = -INFINITY;
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_free[j & 1]);
+        if (warp_has) {
+#pragma unroll
+          for (int r = 0; r < RT; r += 4) {
+            const float4 m = make_float4(redux_max(z[r]), redux_max(z[r + 1]), redux_max(z[r + 2]),
+                                         redux_max(z[r + 3]));
+            if (lane == 0) *reinterpret_cast<float4*>(&red_sh[grp][quad][r]) = m;
+          }
+        } else if (lane < RT) {
+          red_sh[grp][quad][lane] = -INFINITY;
+        }
+      }
+      bar_sync(1 + grp, 128);
+      if (quad == 0) {
+        if (ok && lane < RT) {
+          const float mx = fmaxf(fmaxf(red_sh[grp][0][lane], red_sh[grp][1][lane]),
+                                 fmaxf(red_sh[grp][2][lane], red_sh[grp][3][lane]));
+          const float my = mx * c_sh[r0 + lane];       // the scale is positive
+          const float m_new = fmaxf(m_ref, my);
+          mq_sh[grp][lane] = my == -INFINITY ? 0.f : my;
+          g_sh[grp][lane] = my == -INFINITY ? 0.f : exp2f(my - m_new);
+          al_sh[grp][lane] = m_ref == -INFINITY ? 1.f : exp2f(m_ref - m_new);
+          mt_sh[j & 3][r0 + lane] = my;
+          if (lane == 0 && r0 == 0) vr_sh[j & 3] = vref;
+          const bool moved = m_new != m_ref && m_ref != -INFINITY;
+          m_ref = m_new;
+          const uint32_t any = __ballot_sync(RT == 32 ? 0xffffffffu : 0xffffu, moved);
+          if (lane == 0) moved_sh[grp] = any != 0;
+        }
+      }
+      bar_sync(1 + grp, 128);
+      // the P buffer is free once the product before last is done
+      if (ok && !mbar_wait(&o_full[j & 1], ((j >> 1) & 1) ^ 1, a.err)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) continue;
+      if (moved_sh[grp]) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) l[r] *= al_sh[grp][r];
+      }
+      if (warp_has) {
+        const uint32_t pb = p_s + (j & 1) * C::kP;
+#pragma unroll
+        for (int c = 0; c < RT / 16; ++c) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 16 * c + 4 * e;
+            const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r0 + r]);
+            const float4 mq = *reinterpret_cast<const float4*>(&mq_sh[grp][r]);
+            const float4 gg = *reinterpret_cast<const float4*>(&g_sh[grp][r]);
+            float p[4], h[4];
+            p[0] = ex2_ftz(fmaf(z[r], cc.x, -mq.x));
+            p[1] = ex2_ftz(fmaf(z[r + 1], cc.y, -mq.y));
+            p[2] = ex2_ftz(fmaf(z[r + 2], cc.z, -mq.z));
+            p[3] = ex2_ftz(fmaf(z[r + 3], cc.w, -mq.w));
+            l[r] = fmaf(p[0], gg.x, l[r]);
+            l[r + 1] = fmaf(p[1], gg.y, l[r + 1]);
+            l[r + 2] = fmaf(p[2], gg.z, l[r + 2]);
+            l[r + 3] = fmaf(p[3], gg.w, l[r + 3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] *= vfac;
+            if (blk) {                                 // bf16, two rows a word
+              hi[e] = pack_bf16(p[0], p[1]);
+              lo[e] = pack_bf16(p[2], p[3]);
+              continue;
+            }
+            hi[e] = e4m3x4(p[0], p[1], p[2], p[3]);
+            e4m3x4_values(hi[e], h);
+            lo[e] = e4m3x4((p[0] - h[0]) * kLoScale, (p[1] - h[1]) * kLoScale,
+                           (p[2] - h[2]) * kLoScale, (p[3] - h[3]) * kLoScale);
+          }
+          if (blk) {
+            const int piece = (r0 + 16 * c) / 8;
+            st_shared_v4(swz<2 * R>(pb, key, piece), make_uint4(hi[0], lo[0], hi[1], lo[1]));
+            st_shared_v4(swz<2 * R>(pb, key, piece + 1), make_uint4(hi[2], lo[2], hi[3], lo[3]));
+            continue;
+          }
+          st_shared_v4(swz<2 * R>(pb, key, r0 / 16 + c), make_uint4(hi[0], hi[1], hi[2], hi[3]));
+          st_shared_v4(swz<2 * R>(pb, key, R / 16 + r0 / 16 + c), make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        }
+        fence_proxy_async_smem();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[j & 1]);
+    }
+    grid_dependents_launch();
+    sum_across<RT>(l, lane);
+    bar_sync(1 + grp, 128);                            // the last maxima have been read
+    if (lane < RT) {
+      red_sh[grp][quad][lane] = l[0];
+      if (quad == 0) mref_sh[grp][lane] = m_ref;
+    }
+    bar_sync(5, 32 * (kSoftWarps + kAccWarps));
+  } else {
+    // ------------------------------------------------ block keys, accumulators
+    const int aw = warp - 2 - kSoftWarps, quad = warp & 3;
+    const int at = aw * 32 + lane;                     // 0 .. 127
+    const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    if (has_block) {
+      constexpr int kKeys = kBlkKeys / kAccWarps;
+      WarpRow<D> x[kKeys], y[kKeys];
+#pragma unroll
+      for (int e = 0; e < kKeys; ++e) {
+        const int key = aw + kAccWarps * e;
+        x[e].zero(), y[e].zero();
+        if (key < a.k) {
+          const size_t off = (((size_t)b * a.k + key) * a.Hkv + hkv) * D;
+          x[e].load(a.kb + off, lane);
+          y[e].load(a.vb + off, lane);
+        }
+      }
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < kKeys; ++e) {
+        const int key = aw + kAccWarps * e;
+        // Values that are not finite stay out of the product (a row that does not
+        // see them would multiply them by 0) and are added at the end.
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const uint32_t w = y[e].w[i];
+          const bool lo_bad = (w & 0x7f80u) == 0x7f80u, hi_bad = (w & 0x7f800000u) == 0x7f800000u;
+          bad |= lo_bad || hi_bad;
+          y[e].w[i] = (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
+        }
+        const float s = x[e].store(bk_s, key, kBlkKeys + key, lane);
+        if (lane == 0) bks_sh[key] = s;
+        const int byte = 2 * D / 32 * lane;            // of the values' row
+        const uint32_t va = swz<128>(bv_s + byte / 128 * C::kBlkSub, key, byte % 128 / 16) + byte % 16;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) st_shared_b32(va + 4 * i, y[e].w[i]);
+      }
+      if (bad) blk_bad = 1;
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&blk_ready);
+    }
+    float acc[R];                                      // of one dimension, against m_run
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = 0.f;
+    float m_run = -INFINITY;                           // of row `at`
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      if (ok && !mbar_wait(&o_full[j & 1], (j >> 1) & 1, a.err)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      bool moved = false;
+      if (ok && at < R) {
+        const float mt = mt_sh[j & 3][at], m_new = fmaxf(m_run, mt);
+        f_sh[j & 1][at] = mt == -INFINITY ? 0.f : exp2f(mt - m_new) * vr_sh[j & 3] * (1.f / kPScale);
+        fa_sh[j & 1][at] = m_run == -INFINITY ? 1.f : exp2f(m_run - m_new);
+        moved = m_run != -INFINITY && m_new != m_run;
+        m_run = m_new;
+      }
+      if (aw < (R + 31) / 32) {
+        const uint32_t any = __ballot_sync(0xffffffffu, moved);
+        if (R <= 32) {
+          if (lane == 0) fmoved_sh[j & 1] = any != 0;
+        } else if (lane == 0) {
+          reinterpret_cast<short*>(&fmoved_sh[j & 1])[aw] = any != 0;
+        }
+      }
+      bar_sync(3, 32 * kAccWarps);
+      if (!ok) continue;
+      tc_fence_after();
+      if (fmoved_sh[j & 1]) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[r] *= fa_sh[j & 1][r];
+      }
+      const uint32_t oa = tmem + lane_addr + kOCol + (uint32_t)((j & 1) * 2 * R);
+      // the block's product has no lo columns
+      const float lo_w = has_block && j == n - 1 ? 0.f : 1.f / kLoScale;
+#pragma unroll
+      for (int c = 0; c < R / 16; ++c) {
+        uint32_t h[16], lo[16];
+        tc_ld16(oa + 16 * c, h);
+        tc_ld16(oa + R + 16 * c, lo);
+        tc_wait_ld();
+        if (lo_w == 0.f) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) lo[e] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(&f_sh[j & 1][16 * c + e]);
+          const float ff[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc[16 * c + e + i] =
+                fmaf(fmaf(__uint_as_float(lo[e + i]), lo_w, __uint_as_float(h[e + i])), ff[i],
+                     acc[16 * c + e + i]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free[j & 1]);
+    }
+    bar_sync(5, 32 * (kSoftWarps + kAccWarps));
+    // ------------------------------------------------ epilogue
+    if (at < R) {
+      float sum = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        if (C::kRowGroups > 1 && g != at / RT) continue;
+        const int i = at % RT;
+        const float m = mref_sh[g][i];
+        const float lg = (red_sh[g][0][i] + red_sh[g][1][i]) + (red_sh[g][2][i] + red_sh[g][3][i]);
+        if (m != -INFINITY || lg != 0.f) sum += lg * exp2f(m - m_run);
+      }
+      f_sh[0][at] = n > 0 ? 1.f / sum : 0.f;
+      fa_sh[0][at] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
+    }
+    bar_sync(3, 32 * kAccWarps);
+    // M = 64 leaves 16 dimensions in the first half of every quadrant's lanes
+    const int d = D == 128 ? quad * 32 + lane : quad * 16 + (lane & 15);
+    const bool has_d = D == 128 || lane < 16;
+    float* part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
+    if (has_d) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int row = chunk * R + r;
+        if (row >= a.M) break;
+        float o = acc[r] * f_sh[0][r];
+        if (has_block && blk_bad)
+          for (int i = 0; i < vis_sh[r]; ++i) {
+            const float v = __bfloat162float(a.vb[(((size_t)b * a.k + i) * a.Hkv + hkv) * D + d]);
+            if (finite_size(v) == 0.f) o += v;
+          }
+        if (a.splits == 1)
+          a.out[(((size_t)b * a.k + row / a.G) * a.Hq + hkv * a.G + row % a.G) * D + d] = __float2bfloat16(o);
+        else
+          part[r * C::kPStride + d] = n > 0 ? o : 0.f;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tc_dealloc(tmem, kTmemCols);
+  }
+  if (a.splits == 1) return;
+  // ------------------------------------------------ merge in the cluster
+  // The CTAs of a cluster are the splits of one (sequence, KV head, chunk), each
+  // holding its normalised rows and their log2-sum-exps in shared memory; CTA
+  // `split` merges rows split, split + splits, ..., a warp a row.  The second
+  // barrier keeps shared memory alive until every CTA has read it.
+  cluster_sync_all();
+  {
+    constexpr int kPer = D / 32;
+    const uint32_t lse_s = smem_u32(&fa_sh[0][0]);
+    for (int r = split + a.splits * warp; r < R && chunk * R + r < a.M;
+         r += a.splits * (kThreads / 32)) {
+      const float l = lane < a.splits ? ld_cluster_f32(mapa_shared(lse_s + 4u * r, lane)) : -INFINITY;
+      float2 v[kMaxSplits][kPer / 2];
+#pragma unroll
+      for (int s = 0; s < kMaxSplits; ++s)
+        if (s < a.splits) {
+          const uint32_t src = mapa_shared(ring + 4u * (r * C::kPStride + kPer * lane), s);
+#pragma unroll
+          for (int c = 0; c < kPer / 2; ++c) v[s][c] = ld_cluster_v2(src + 8 * c);
+        }
+      const float mx = warp_max(l);
+      const float w = l == -INFINITY ? 0.f : exp2f(l - mx);
+      const float inv = 1.f / warp_sum(w);
+      float o[kPer];
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) o[c] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kMaxSplits; ++s) {
+        const float ws = __shfl_sync(0xffffffffu, w, s);
+        if (s < a.splits && !(ws == 0.f)) {
+#pragma unroll
+          for (int c = 0; c < kPer / 2; ++c) {
+            o[2 * c] = fmaf(ws, v[s][c].x, o[2 * c]);
+            o[2 * c + 1] = fmaf(ws, v[s][c].y, o[2 * c + 1]);
+          }
+        }
+      }
+      const int row = chunk * R + r;
+      __nv_bfloat16* dst =
+          a.out + (((size_t)b * a.k + row / a.G) * a.Hq + hkv * a.G + row % a.G) * D + kPer * lane;
+#pragma unroll
+      for (int c = 0; c < kPer; c += 2)
+        *reinterpret_cast<__nv_bfloat162*>(dst + c) = __floats2bfloat162_rn(o[c] * inv, o[c + 1] * inv);
+    }
+  }
+  cluster_sync_all();
+}
+
+struct Kernel {
+  const void* fn;
+  size_t smem;
+};
+template <int D>
+Kernel kernel_of(int R) {
+  if (R == 16) return {(const void*)paged_tc_kernel<D, 16>, Shape<D, 16>::kSmem};
+  if (R == 32) return {(const void*)paged_tc_kernel<D, 32>, Shape<D, 32>::kSmem};
+  return {(const void*)paged_tc_kernel<D, 64>, Shape<D, 64>::kSmem};
+}
+Kernel kernel_for(int D, int R) { return D == 128 ? kernel_of<128>(R) : kernel_of<64>(R); }
+
+}  // namespace
+
+namespace sbd {
+
+void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
+  p->rows = p->M <= 16 ? 16 : p->M <= 32 ? 32 : 64;
+  p->chunks = (p->M + p->rows - 1) / p->rows;
+  const Kernel kern = kernel_for(p->D, p->rows);
+  const long long jobs = (long long)p->B * p->Hkv * p->chunks;
+  const long long tiles = ((long long)p->max_pages * p->P + kTile - 1) / kTile + 1;
+  int s = 1;
+  if (num_splits > 0) {
+    for (s = num_splits < kMaxSplits ? num_splits : kMaxSplits; s > 1; --s)
+      if (cluster_slots(kern.fn, kThreads, kern.smem, s) > 0) break;
+  } else if (jobs > 0) {
+    // one wave of CTAs, the clusters of all jobs at once
+    long long most = num_sms() / jobs;
+    if (most > tiles) most = tiles;
+    for (s = most < kMaxSplits ? (int)most : kMaxSplits; s > 1; --s)
+      if (cluster_slots(kern.fn, kThreads, kern.smem, s) >= jobs) break;
+  }
+  p->splits = s < 1 ? 1 : s;
+  p->cluster = p->splits > 1;
+}
+
+sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st) {
+  const Kernel kern = kernel_for(p.D, p.rows);
+  // Codes as bytes: (D, tokens of a page, page and head); a copy is a page.
+  CUtensorMap tk, tv;
+  const uint64_t dims[3] = {(uint64_t)p.D, (uint64_t)p.P, (uint64_t)p.n_pages * p.Hkv};
+  const uint64_t strides[2] = {(uint64_t)p.D, (uint64_t)p.D * p.P};
+  const uint32_t box[3] = {(uint32_t)p.D, (uint32_t)p.P, 1};
+  const CUtensorMapSwizzle swizzle = p.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+  sbd_status s = encode_tensor_map(&tk, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, (void*)t.k_cache, dims,
+                                   strides, box, swizzle);
+  if (s != SBD_OK) return s;
+  s = encode_tensor_map(&tv, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, (void*)t.v_cache, dims, strides, box,
+                        swizzle);
+  if (s != SBD_OK) return s;
+  Args a;
+  a.q = (const __nv_bfloat16*)t.q;
+  a.kb = (const __nv_bfloat16*)t.kb;
+  a.vb = (const __nv_bfloat16*)t.vb;
+  a.ks = t.k_scale;
+  a.vs = t.v_scale;
+  a.table = t.table;
+  a.lens = t.lens;
+  a.out = (__nv_bfloat16*)t.out;
+  a.err = device_error_word();
+  a.B = p.B;
+  a.k = p.k;
+  a.Hq = p.Hq;
+  a.Hkv = p.Hkv;
+  a.G = p.G;
+  a.M = p.M;
+  a.max_pages = p.max_pages;
+  a.n_pages = p.n_pages;
+  a.n_causal = p.n_causal;
+  a.splits = p.splits;
+  a.chunks = p.chunks;
+  a.page_log2 = p.P == 16 ? 4 : p.P == 32 ? 5 : p.P == 64 ? 6 : 7;
+  // more CTAs than one wave: the longest sequences first (the pick costs B^2
+  // comparisons a CTA, hence the limit)
+  a.order = p.B > 1 && p.B <= 128 &&
+            (long long)p.B * p.Hkv * p.chunks * p.splits > num_sms();
+  a.scale_log2 = p.scale_log2;
+  s = allow_smem(kern.fn, kern.smem, "cudaFuncSetAttribute(paged_tc_kernel)");
+  if (s != SBD_OK) return s;
+  void* args[] = {(void*)&tk, (void*)&tv, (void*)&a};
+  return launch_pdl(kern.fn, dim3(p.splits, p.Hkv * p.chunks, p.B), dim3(kThreads), kern.smem, st,
+                    args, "paged_tc_kernel launch", p.splits);
+}
+
+}  // namespace sbd

@@ -35,13 +35,16 @@ sbd_status check_pool(int page_size, int n_pages) {
   return SBD_OK;
 }
 
-sbd_status check_heads(int n_kv_heads, int head_dim, int dtype) {
+sbd_status check_heads(int n_kv_heads, int n_pages, int head_dim, int dtype) {
   if (n_kv_heads < 1 || head_dim < 1)
     return fail(SBD_ERR_INVALID_ARG, "bad sizes: n_kv_heads=%d head_dim=%d", n_kv_heads, head_dim);
   if (dtype != SBD_DTYPE_F32 && dtype != SBD_DTYPE_BF16)
     return fail(SBD_ERR_INVALID_ARG, "unknown dtype %d", dtype);
   if (head_dim != 64 && head_dim != 128)
     return fail(SBD_ERR_UNSUPPORTED, "head_dim %d not in {64, 128}", head_dim);
+  if ((long long)n_pages * n_kv_heads > kMax32)
+    return fail(SBD_ERR_UNSUPPORTED, "n_pages * n_kv_heads = %lld >= 2^31",
+                (long long)n_pages * n_kv_heads);
   if (n_kv_heads > 65535) return fail(SBD_ERR_UNSUPPORTED, "n_kv_heads %d > 65535", n_kv_heads);
   return SBD_OK;
 }
@@ -51,7 +54,7 @@ sbd_status check_attn_q8_desc(const sbd_attn_q8_desc* d) {
   if (d->batch < 0 || d->block_k < 1 || d->n_q_heads < 1 || d->max_pages < 1)
     return fail(SBD_ERR_INVALID_ARG, "bad sizes: batch=%d block_k=%d n_q_heads=%d max_pages=%d",
                 d->batch, d->block_k, d->n_q_heads, d->max_pages);
-  sbd_status s = check_heads(d->n_kv_heads, d->head_dim, d->dtype);
+  sbd_status s = check_heads(d->n_kv_heads, d->n_pages, d->head_dim, d->dtype);
   if (s != SBD_OK) return s;
   s = check_pool(d->page_size, d->n_pages);
   if (s != SBD_OK) return s;
@@ -127,7 +130,7 @@ sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new
   if (!desc) return fail(SBD_ERR_INVALID_ARG, "desc is NULL");
   if (desc->tokens < 0 || desc->group < 1)
     return fail(SBD_ERR_INVALID_ARG, "bad sizes: tokens=%d group=%d", desc->tokens, desc->group);
-  sbd_status s = check_heads(desc->n_kv_heads, desc->head_dim, desc->dtype);
+  sbd_status s = check_heads(desc->n_kv_heads, desc->n_pages, desc->head_dim, desc->dtype);
   if (s != SBD_OK) return s;
   s = check_pool(desc->page_size, desc->n_pages);
   if (s != SBD_OK) return s;
