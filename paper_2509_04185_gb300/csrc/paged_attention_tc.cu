@@ -11,26 +11,24 @@
 //                                     B = the rows' hi codes, then their lo codes
 //   O[dim, (hi|lo) row] += V^T P^T    A = V tile (MN-major), B = P (MN-major)
 //
-// so that N = 2 R is what the call needs (R = 16, 32 or 64 packed rows of the KV
+// so that N follows the rows of the call (R = 16, 32 or 64 packed rows of the KV
 // head's group a CTA, r = i*G + g) and a thread of the softmax owns one key: its
-// page's scales are scalars of the thread, masks a comparison, the row's maximum
-// one redux a warp.
+// page's scales are scalars of the thread, masks a comparison, a row's maximum and
+// sum one redux a warp.
 //
 // P.  Probabilities span more octaves than two codes: next to a key that takes all
 // the weight, a thousand weak ones would vanish.  So P is relative to the maximum
 // of its own tile of 128 keys (times the value scale over the tile's largest, and
 // 2^8), every tile's product starts at zero, and four warps add it to fp32
-// accumulators in registers, weighted 2^(m_tile - m).  lo codes of P are scaled
-// by 2^5 and weighted back there.  No accumulator in tensor memory is ever
-// rescaled, and the softmax never waits for one.
+// accumulators in registers, weighted 2^(m_tile - m).  No accumulator in tensor
+// memory is ever rescaled, and the softmax never waits for one.
 //
 // Block keys (not cached, bf16) form the last tile: the keys split into code pairs
 // like the rows, two products for S; the values as they are against P in bf16
 // (kind::f16), since a row may see a single small value of a key.
 //
-// Warp roles: 0 pages and TMA, 1 tensor memory and MMA issue, 2-9 softmax, 10-13
-// block keys first, then the accumulators.  With R = 64 softmax warps 2-5 take
-// rows 0-31 of every tile and 6-9 rows 32-63; else they take alternate tiles.
+// Warp roles: 0 pages and TMA, 1 tensor memory and MMA issue, 2-9 softmax (two
+// groups of four on alternate tiles), 10-13 block keys first, then the accumulators.
 #include <math.h>
 
 #include "paged.cuh"
@@ -118,6 +116,18 @@ __device__ __forceinline__ float redux_max(float v) {
   return r;
 }
 
+// The same, NaN where any lane has it; and of two.
+__device__ __forceinline__ float redux_max_nan(float v) {
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+
 // Shared-memory operands of rows of `W` = 32, 64 or 128 bytes, swizzled over W:
 // 16-byte pieces of a row permuted by the row's place, the pattern repeating every
 // 8 rows (one 8 W-byte atom).
@@ -153,12 +163,6 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z),
                "r"(v.w)
                : "memory");
-}
-__device__ __forceinline__ void st_shared_b32(uint32_t addr, uint32_t v) {
-  asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-__device__ __forceinline__ void st_shared_b16(uint32_t addr, uint32_t v) {
-  asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"((uint16_t)v) : "memory");
 }
 __device__ __forceinline__ void bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
@@ -199,9 +203,13 @@ struct Args {
 
 template <int D, int R>
 struct Shape {
-  static constexpr int kRT = R < 32 ? R : 32;          // rows of a softmax thread
-  static constexpr int kRowGroups = R / kRT;
-  static constexpr int kTileGroups = 2 / kRowGroups;
+  // The rows' hi and lo codes side by side along N, or one after the other into the
+  // same columns of S.  An MMA of M = 128 takes 53 clocks up to N = 64 and 68 at N =
+  // 128, so the pair costs less side by side, but then the softmax reads two columns
+  // a row and adds them, and at R = 64 it sets the pace.
+  static constexpr bool kBeside = R < 64;
+  static constexpr int kNS = kBeside ? 2 * R : R;      // columns of S
+  static constexpr int kNO = 2 * R;                    // columns of O, bytes of a key's row of P
   static constexpr int kKV = kTile * D;                // a K or V tile
   static constexpr int kQ = 2 * R * D;
   static constexpr int kP = kTile * 2 * R;
@@ -210,7 +218,7 @@ struct Shape {
   static constexpr int kBlk = 2 * kBlkKeys * D;
   static constexpr int kBlkSub = kBlkKeys * 128;
   static constexpr int kFixed = 1024 + kQ + 2 * kP + 2 * kBlk;
-  static constexpr int kLeft = 227 * 1024 - 6 * 1024 - kFixed;     // 6 KB: barriers and tables
+  static constexpr int kLeft = 227 * 1024 - 15 * 1024 - kFixed;    // 15 KB: barriers and tables
   static constexpr int kStages = kLeft / (2 * kKV) < kMaxStages ? kLeft / (2 * kKV) : kMaxStages;
   static constexpr int kSmem = kFixed + kStages * 2 * kKV;
   static constexpr int kPStride = D + 4;               // floats of a partial row
@@ -218,90 +226,68 @@ struct Shape {
   static_assert(kBlk + kTile * D <= 2 * kBlk + kStages * 2 * kKV, "reads past the block's keys stay inside");
 };
 
-// x = s (hi + lo): the codes of n values of a row, s a power of two (inv = 1 / s).
-// What is not finite becomes NaN.
-__device__ __forceinline__ float finite_or_nan(float x) {
-  return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __int_as_float(0x7fffffff) : x;
-}
 __device__ __forceinline__ float finite_size(float x) {
   const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
   return u < 0x7f800000u ? __uint_as_float(u) : 0.f;
 }
-template <int N>
-__device__ __forceinline__ void split_codes(const float (&x)[N], float inv, uint32_t* hi, uint32_t* lo) {
-  float y[4] = {0.f, 0.f, 0.f, 0.f}, h[4];
-#pragma unroll
-  for (int e = 0; e < N; ++e) y[e] = finite_or_nan(x[e]) * inv;
-  *hi = e4m3x4(y[0], y[1], y[2], y[3]);
-  e4m3x4_values(*hi, h);
-  *lo = e4m3x4(y[0] - h[0], y[1] - h[1], y[2] - h[2], y[3] - h[3]);
-}
-// One row of D values over a warp, D / 32 a lane.
+// 16 consecutive bf16 values of a row; the D / 16 lanes of a row lie together.
 template <int D>
-struct WarpRow {
-  static constexpr int kN = D / 32;
-  uint32_t w[kN / 2];
-  __device__ __forceinline__ void load(const __nv_bfloat16* row, int lane) {
-    if constexpr (kN == 4) {
-      const uint2 v = *reinterpret_cast<const uint2*>(row + 4 * lane);
-      w[0] = v.x, w[1] = v.y;
-    } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(row + 2 * lane);
-    }
+struct Piece {
+  uint4 w[2];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    w[0] = reinterpret_cast<const uint4*>(p)[0];
+    w[1] = reinterpret_cast<const uint4*>(p)[1];
   }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int e = 0; e < kN / 2; ++e) w[e] = 0;
-  }
-  __device__ __forceinline__ void get(float (&x)[kN]) const {
-#pragma unroll
-    for (int e = 0; e < kN / 2; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
-  }
-  // Writes the codes into rows `hi_row` and `lo_row` of the operand at `base`;
-  // returns the scale.
-  __device__ __forceinline__ float store(uint32_t base, int hi_row, int lo_row, int lane) const {
-    float x[kN];
-    get(x);
+  __device__ __forceinline__ void zero() { w[0] = w[1] = make_uint4(0, 0, 0, 0); }
+  // x = s (hi + lo) for the row's scale s, which it returns: the codes become
+  // piece `c` of rows hi_row and lo_row of the operand at `base`.  What is not
+  // finite becomes NaN.
+  __device__ __forceinline__ float store(uint32_t base, int hi_row, int lo_row, int c) const {
+    float x[16];
+    const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
     float amax = 0.f;
 #pragma unroll
-    for (int e = 0; e < kN; ++e) amax = fmaxf(amax, finite_size(x[e]));
-    amax = redux_max(amax);
-    const float s = scale_for(amax);
-    uint32_t hi, lo;
-    split_codes<kN>(x, 1.f / s, &hi, &lo);
-    const int byte = kN * lane;
-    const uint32_t ha = swz<D>(base, hi_row, byte / 16) + byte % 16;
-    const uint32_t la = swz<D>(base, lo_row, byte / 16) + byte % 16;
-    if constexpr (kN == 4) {
-      st_shared_b32(ha, hi);
-      st_shared_b32(la, lo);
-    } else {
-      st_shared_b16(ha, hi);
-      st_shared_b16(la, lo);
+    for (int e = 0; e < 8; ++e) {
+      x[2 * e] = __uint_as_float(u[e] << 16);
+      x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+      amax = fmaxf(amax, fmaxf(finite_size(x[2 * e]), finite_size(x[2 * e + 1])));
     }
+#pragma unroll
+    for (int o = 1; o < D / 16; o *= 2) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const float s = scale_for(amax), inv = 1.f / s;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float y[4], h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v = x[4 * e + i];
+        y[i] = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? __int_as_float(0x7fffffff) : v * inv;
+      }
+      hi[e] = e4m3x4(y[0], y[1], y[2], y[3]);
+      e4m3x4_values(hi[e], h);
+      lo[e] = e4m3x4(y[0] - h[0], y[1] - h[1], y[2] - h[2], y[3] - h[3]);
+    }
+    st_shared_v4(swz<D>(base, hi_row, c), make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    st_shared_v4(swz<D>(base, lo_row, c), make_uint4(lo[0], lo[1], lo[2], lo[3]));
     return s;
   }
 };
 
-// v[i] of lane l becomes, in v[0], the sum over lanes of v[l % N].
-template <int N>
-__device__ __forceinline__ void sum_across(float (&v)[N], int lane) {
-  if constexpr (N == 16) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 16);
-  }
-#pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) {
-#pragma unroll
-    for (int i = 0; i < o; ++i) {
-      const bool up = lane & o;
-      const float send = up ? v[i] : v[i + o];
-      v[i] = (up ? v[i + o] : v[i]) + __shfl_xor_sync(0xffffffffu, send, o);
-    }
-  }
+// Four probabilities as code pairs.  The fp16 pattern of p in [0, 1], shifted right
+// by 7, is the e4m3 pattern of 2^8 p (the exponents are 8 apart, and so are the
+// subnormal steps), so a code is a rounded shift: hi = p to 4 bits, lo = 2^5 (p - hi)
+// to 4 more (exact in fp16, with a sign).  Together they hold p to 2^-9, and to
+// 2^-23 of the tile's largest.
+__device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, uint32_t* lo) {
+  auto bits = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
+  auto half2 = [](uint32_t x) { return *reinterpret_cast<const __half2*>(&x); };
+  const uint32_t a = bits(p01) + 0x00400040u, b = bits(p23) + 0x00400040u;
+  *hi = __byte_perm(a << 1, b << 1, 0x7531);
+  const __half2 up = __float2half2_rn(kLoScale);
+  const uint32_t c = bits(__hmul2(__hsub2(p01, half2(a & 0xff80ff80u)), up)) + 0x00400040u;
+  const uint32_t d = bits(__hmul2(__hsub2(p23, half2(b & 0xff80ff80u)), up)) + 0x00400040u;
+  *lo = __byte_perm(((c << 1) & 0x7fff7fffu) | (c & 0x80008000u), ((d << 1) & 0x7fff7fffu) | (d & 0x80008000u), 0x7531);
 }
 
 template <int D, int R>
@@ -309,11 +295,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
   using C = Shape<D, R>;
-  constexpr int RT = C::kRT, kStages = C::kStages;
-  constexpr uint32_t kTmemCols = 8 * R;                // S: 2 x 2 R, O: 2 x 2 R
-  constexpr uint32_t kOCol = 4 * R;
-  constexpr int kHandIn = 4 * C::kRowGroups;           // softmax warps of a tile
-  static_assert(R == 16 || R == 32 || R == 64, "N = 2 R is one swizzle atom");
+  constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
+  constexpr uint32_t kTmemCols = 8 * R;                // two buffers of S and of O
+  constexpr uint32_t kOCol = 2 * kNS;
+  constexpr int kOwn = (R + 31) / 32;                  // rows of a lane: lane, lane + 32
+  static_assert(R == 16 || R == 32 || R == 64, "a key's row of P is one swizzle atom");
 
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
@@ -321,17 +307,18 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
-  __shared__ float ks_sh[kMaxStages][8], vs_sh[kMaxStages][8], vref_sh[kMaxStages];
+  // a stage's page scales: of the keys; of the values over the tile's largest; that
+  __shared__ float ks_sh[kMaxStages][8], vw_sh[kMaxStages][8], vref_sh[kMaxStages];
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
-  __shared__ __align__(16) float red_sh[2][4][RT];     // a warp's maxima; at the end its sums
-  __shared__ __align__(16) float mq_sh[2][RT], g_sh[2][RT], al_sh[2][RT];
-  __shared__ int moved_sh[2];
+  __shared__ __align__(16) float red_sh[2][2][R][4];   // maxima by row and warp of a group, two tiles
+  __shared__ __align__(16) float mq_sh[kSoftWarps][R]; // a warp's copy of the tile's maxima
+  __shared__ __align__(16) uint32_t sum_sh[kSoftWarps][R];   // its sums of probabilities
   __shared__ float mt_sh[4][R], vr_sh[4];              // a tile's maxima and value reference
   __shared__ __align__(16) float f_sh[2][R], fa_sh[2][R];
-  __shared__ int fmoved_sh[2];
-  __shared__ float mref_sh[2][RT];
+  __shared__ int fmoved_sh[2][kOwn];
+  __shared__ float lsum_sh[kSoftWarps][R], mref_sh[2][R];
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_s = sbase, p_s = q_s + C::kQ;
@@ -349,8 +336,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 2);              // the product, and its issuer's view of the stage
-      mbar_init(&s_free[i], kHandIn);
-      mbar_init(&p_full[i], kHandIn);
+      mbar_init(&s_free[i], 4);
+      mbar_init(&p_full[i], 4);
       mbar_init(&o_full[i], 2);
       mbar_init(&o_free[i], kAccWarps);
     }
@@ -400,7 +387,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const int P = 1 << a.page_log2, per_tile = kTile >> a.page_log2;
     const int n_mine = n - (has_block ? 1 : 0);
     const int p_first = t_begin * per_tile;
-    const int p_end = (int)(((long long)min((t_begin + n_mine) * (long long)kTile, (long long)len) + P - 1) >> a.page_log2);
+    const int p_end = (int)((min((t_begin + n_mine) * (long long)kTile, (long long)len) + P - 1) >> a.page_log2);
     const int32_t* table = a.table + (size_t)b * a.max_pages;
     // Pages come in windows of 32, one a lane: ids a window ahead, their scales a
     // tile into the window before.  A page out of range lies past the tensor's
@@ -430,30 +417,31 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       const bool freed = mbar_wait(&kv_empty[stage], ((j / kStages) & 1) ^ 1, a.err);
       if (!__all_sync(0xffffffffu, freed)) break;
       const int valid = keys_of(j), n_pg = (valid + P - 1) >> a.page_log2;
-      const int src = w * per_tile + lane;   // lane i < n_pg: the tile's page i
-      const int pg = __shfl_sync(0xffffffffu, id, src & 31);
-      const float k_sc = __shfl_sync(0xffffffffu, ks, src & 31);
-      const float v_sc = __shfl_sync(0xffffffffu, vs, src & 31);
-      const float v_max = redux_max(lane < n_pg ? v_sc : 0.f);
-      if (lane < per_tile) {
-        ks_sh[stage][lane] = lane < n_pg ? k_sc : 0.f;
-        vs_sh[stage][lane] = lane < n_pg ? v_sc : 0.f;
-      }
-      if (lane == 0) vref_sh[stage] = v_max;
-      __syncwarp();
+      const int src = (w * per_tile + lane) & 31;      // lane i < n_pg: the tile's page i
+      const int pg = __shfl_sync(0xffffffffu, id, src);
+      // Values past the length may be anything (NaN); the products go on to the
+      // next multiple of 32 keys, so those become zeros once the copy is there.
       const bool tail = (valid & 31) != 0;
       uint64_t* bar = tail ? &tail_bar : &kv_full[stage];
-      if (lane == 0) mbar_arrive_expect_tx(bar, 2 * n_pg * P * D);
-      __syncwarp();
+      // The copies first; the scales (whose loads may still be on their way) are in
+      // place before the barrier's one arrival.
       if (lane < n_pg) {
         const int row = pg < a.n_pages ? pg * a.Hkv + hkv : a.n_pages * a.Hkv;
         tma_load_3d(k_tile(j) + lane * P * D, &tmap_k, bar, 0, 0, row);
         tma_load_3d(v_tile(j) + lane * P * D, &tmap_v, bar, 0, 0, row);
       }
       issued = j + 1;
+      const float k_sc = __shfl_sync(0xffffffffu, ks, src);
+      const float v_sc = __shfl_sync(0xffffffffu, vs, src);
+      const float v_max = redux_max(lane < n_pg ? v_sc : 0.f);
+      if (lane < n_pg) {
+        ks_sh[stage][lane] = k_sc;
+        vw_sh[stage][lane] = v_max > 0.f ? v_sc / v_max : v_sc * 0.f;
+      }
+      if (lane == 0) vref_sh[stage] = v_max;
+      __syncwarp();
+      if (lane == 0) mbar_arrive_expect_tx(bar, 2 * n_pg * P * D);
       if (tail) {
-        // Values past the length may be anything (NaN); the products go on to the
-        // next multiple of 32 keys, so those become zeros.
         mbar_wait(&tail_bar, 0, a.err);
         const int end = (valid + 31) & ~31;
         for (int c = lane; c < (end - valid) * (D / 16); c += 32)
@@ -471,47 +459,52 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     if (lane == 0 && n > 0) {
       bool ok = mbar_wait(&q_ready, 0, a.err);
       tc_fence_after();
-      const uint32_t id_s = idesc_f8(kTile, 2 * R, false), id_pv = idesc_f8(D, 2 * R, true);
+      const uint32_t id_s = idesc_f8(kTile, kNS, false), id_pv = idesc_f8(D, kNO, true);
+      constexpr int kPasses = C::kBeside ? 1 : 2;      // hi codes, then lo codes
       auto is_block = [&](int j) { return has_block && j == n - 1; };
       auto issue_s = [&](int j) {
-        const uint32_t d = tmem + (uint32_t)((j & 1) * 2 * R);
-        const int passes = is_block(j) ? 2 : 1;
-        for (int e = 0; e < passes; ++e) {
+        const uint32_t d = tmem + (uint32_t)((j & 1) * kNS);
+        const int parts = is_block(j) ? 2 : 1;
+        for (int e = 0; e < parts; ++e) {
           const uint32_t kt = is_block(j) ? bk_s + e * kBlkKeys * D : k_tile(j);
 #pragma unroll
-          for (int kk = 0; kk < D / 32; ++kk)
-            tc_mma_f8(d, desc<D>(kt + 32 * kk), desc<D>(q_s + 32 * kk), id_s, e > 0 || kk > 0);
+          for (int h = 0; h < kPasses; ++h)
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+              tc_mma_f8(d, desc<D>(kt + 32 * kk), desc<D>(q_s + h * R * D + 32 * kk), id_s,
+                        e > 0 || h > 0 || kk > 0);
         }
         tc_commit(&s_full[j & 1]);
         mbar_arrive(&s_full[j & 1]);
       };
       auto issue_pv = [&](int j) {
-        const uint32_t o = tmem + kOCol + (uint32_t)((j & 1) * 2 * R);
+        const uint32_t o = tmem + kOCol + (uint32_t)((j & 1) * kNO);
         const uint32_t pt = p_s + (j & 1) * C::kP;
         if (is_block(j)) {
 #pragma unroll
           for (int kk = 0; kk < kBlkKeys / 16; ++kk)
-            tc_mma_bf16(o, desc<128>(bv_s + kk * 16 * 128, C::kBlkSub), desc<2 * R>(pt + kk * 16 * 2 * R),
-                        idesc_bf16_mn(D, R), kk > 0);
+            tc_mma_bf16(o, desc<128>(bv_s + kk * 16 * 128, C::kBlkSub),
+                        desc<kNO>(pt + kk * 16 * kNO), idesc_bf16_mn(D, R), kk > 0);
         } else {
           const int steps = (keys_of(j) + 31) / 32;
           for (int kk = 0; kk < steps; ++kk)
-            tc_mma_f8(o, desc<D>(v_tile(j) + kk * 32 * D), desc<2 * R>(pt + kk * 32 * 2 * R), id_pv,
-                      kk > 0);
+            tc_mma_f8(o, desc<D>(v_tile(j) + kk * 32 * D), desc<kNO>(pt + kk * 32 * kNO), id_pv, kk > 0);
           tc_commit(&kv_empty[j % kStages]);
         }
         tc_commit(&o_full[j & 1]);
         mbar_arrive(&o_full[j & 1]);
       };
-      // Scores run up to two tiles ahead; whichever is ready first is issued.
+      // Scores run up to two tiles ahead of the products with V (a softmax group that
+      // hands in its P finds its next scores done); whichever is ready first is
+      // issued.
       int next_s = 0, next_pv = 0;
       uint64_t t0 = 0;
       for (uint32_t idle = 0; ok && next_pv < n;) {
         bool moved = false;
-        if (next_s < n && next_s < next_pv + 2 &&
+        if (next_s < n && next_s <= next_pv + 2 &&
+            mbar_poll_parity(&s_free[next_s & 1], ((next_s >> 1) & 1) ^ 1) &&
             (is_block(next_s) ? mbar_poll_parity(&blk_ready, 0)
-                              : mbar_poll_parity(&kv_full[next_s % kStages], (next_s / kStages) & 1)) &&
-            mbar_poll_parity(&s_free[next_s & 1], ((next_s >> 1) & 1) ^ 1)) {
+                              : mbar_poll_parity(&kv_full[next_s % kStages], (next_s / kStages) & 1))) {
           tc_fence_after();
           issue_s(next_s++);
           moved = true;
@@ -537,24 +530,19 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   } else if (warp < 2 + kSoftWarps) {
     // ------------------------------------------------ softmax warps
     const int sw = warp - 2, quad = warp & 3, grp = sw >> 2;
-    const int r0 = C::kRowGroups > 1 ? grp * RT : 0;   // first row of this thread
+    const int key = quad * 32 + lane;                  // of every tile
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     {
-      constexpr int kRows = R / kSoftWarps;
-      WarpRow<D> x[kRows];
-#pragma unroll
-      for (int e = 0; e < kRows; ++e) {
-        const int row = chunk * R + sw * kRows + e;
-        if (row < a.M)
-          x[e].load(a.q + (((size_t)b * a.k + row / a.G) * a.Hq + hkv * a.G + row % a.G) * D, lane);
-        else
-          x[e].zero();
-      }
-#pragma unroll
-      for (int e = 0; e < kRows; ++e) {
-        const int r = sw * kRows + e, i = (chunk * R + r) / a.G;
-        const float s = x[e].store(q_s, r, R + r, lane);
-        if (lane == 0) {
+      constexpr int kRowsTurn = 32 * kSoftWarps / (D / 16);
+      const int t = sw * 32 + lane, c = t % (D / 16);
+#pragma unroll 1
+      for (int r = t / (D / 16); r < R; r += kRowsTurn) {
+        const int row = chunk * R + r, i = row / a.G;
+        Piece<D> x;
+        x.zero();
+        if (row < a.M) x.load(a.q + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + 16 * c);
+        const float s = x.store(q_s, r, R + r, c);
+        if (c == 0) {
           c_sh[r] = s * a.scale_log2;
           vis_sh[r] = i < a.n_causal ? i + 1 : a.k;
         }
@@ -564,148 +552,176 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (lane == 0) mbar_arrive(&q_ready);
       bar_sync(4, 32 * kSoftWarps);                    // c and vis of all rows
     }
-    float l[RT];                                       // this key lane's sums, against m_ref
+    // A lane keeps the statistics of rows lane and lane + 32 over its warp's keys:
+    // the running maximum (the same in the four warps of a group) and the sum of
+    // probabilities against it.
+    float c_own[kOwn], m_ref[kOwn], l[kOwn];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) l[r] = 0.f;
-    float m_ref = -INFINITY;                           // of row r0 + lane, in the warp of quad 0
+    for (int e = 0; e < kOwn; ++e) {
+      c_own[e] = lane + 32 * e < R ? c_sh[lane + 32 * e] : 0.f;
+      m_ref[e] = -INFINITY;
+      l[e] = 0.f;
+    }
     bool ok = true;
-    const int j_first = C::kTileGroups > 1 ? grp : 0;
-    for (int j = j_first; j < n; j += C::kTileGroups) {
+    for (int j = grp; j < n; j += 2) {
       const bool blk = has_block && j == n - 1;
       const int stage = j % kStages, valid = keys_of(j);
-      const int key = quad * 32 + lane;
       const bool warp_has = quad * 32 < valid;
-      if (ok && !mbar_wait(&s_full[j & 1], (j >> 1) & 1, a.err)) ok = false;
+      if (ok && !mbar_wait(&s_full[grp], (j >> 1) & 1, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
-      float z[RT];
-      float vfac = 0.f, vref = 0.f;
+      float z[R];
+      float vw = 1.f, vref = 1.f;
       if (ok) {
         tc_fence_after();
-        float kf, vf;
-        if (blk) {
-          kf = bks_sh[key & 31];
-          vf = vref = 1.f;
-        } else {
-          kf = ks_sh[stage][key >> a.page_log2], vf = vs_sh[stage][key >> a.page_log2];
-          vref = vref_sh[stage];
-        }
-        vfac = vref > 0.f ? kPScale * (vf / vref) : vf * 0.f;
         if (warp_has) {
-          const uint32_t sa = tmem + lane_addr + (uint32_t)((j & 1) * 2 * R + r0);
+          float kf;
+          if (blk) {
+            kf = bks_sh[key & (kBlkKeys - 1)];
+          } else {
+            kf = ks_sh[stage][key >> a.page_log2];
+            vw = vw_sh[stage][key >> a.page_log2];
+            vref = vref_sh[stage];
+          }
+          const uint32_t sa = tmem + lane_addr + (uint32_t)(grp * kNS);
+          if constexpr (C::kBeside) {
+            uint32_t h[R / 16][16], lo[R / 16][16];
 #pragma unroll
-          for (int c = 0; c < RT / 16; ++c) {
-            uint32_t h[16], lo[16];
-            tc_ld16(sa + 16 * c, h);
-            tc_ld16(sa + R + 16 * c, lo);
+            for (int c = 0; c < R / 16; ++c) {
+              tc_ld16(sa + 16 * c, h[c]);
+              tc_ld16(sa + R + 16 * c, lo[c]);
+            }
             tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              z[16 * c + e] = (__uint_as_float(h[e]) + __uint_as_float(lo[e])) * kf;
+            for (int r = 0; r < R; ++r)
+              z[r] = (__uint_as_float(h[r / 16][r % 16]) + __uint_as_float(lo[r / 16][r % 16])) * kf;
+          } else {
+            uint32_t h[R / 16][16];
+#pragma unroll
+            for (int c = 0; c < R / 16; ++c) tc_ld16(sa + 16 * c, h[c]);
+            tc_wait_ld();
+#pragma unroll
+            for (int r = 0; r < R; ++r) z[r] = __uint_as_float(h[r / 16][r % 16]) * kf;
           }
           if (blk) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-              if (key >= vis_sh[r0 + r]) z[r] = -INFINITY;
+            for (int r = 0; r < R; ++r)
+              if (key >= vis_sh[r]) z[r] = -INFINITY;
           } else if (valid < quad * 32 + 32) {
+            const bool out = key >= valid;
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-              if (key >= valid) z[r] = -INFINITY;
+            for (int r = 0; r < R; ++r) z[r] = out ? -INFINITY : z[r];
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s_free[j & 1]);
+        if (lane == 0) mbar_arrive(&s_free[grp]);
         if (warp_has) {
+          // NaN propagates: a row with one has NaN statistics from here on
 #pragma unroll
-          for (int r = 0; r < RT; r += 4) {
-            const float4 m = make_float4(redux_max(z[r]), redux_max(z[r + 1]), redux_max(z[r + 2]),
-                                         redux_max(z[r + 3]));
-            if (lane == 0) *reinterpret_cast<float4*>(&red_sh[grp][quad][r]) = m;
+          for (int r = 0; r < R; ++r) {
+            const float m = redux_max_nan(z[r]);
+            if (lane == 0) red_sh[grp][(j >> 1) & 1][r][quad] = m;
           }
-        } else if (lane < RT) {
-          red_sh[grp][quad][lane] = -INFINITY;
+        } else {
+#pragma unroll
+          for (int e = 0; e < kOwn; ++e)
+            if (lane + 32 * e < R) red_sh[grp][(j >> 1) & 1][lane + 32 * e][quad] = -INFINITY;
         }
       }
       bar_sync(1 + grp, 128);
-      if (quad == 0) {
-        if (ok && lane < RT) {
-          const float mx = fmaxf(fmaxf(red_sh[grp][0][lane], red_sh[grp][1][lane]),
-                                 fmaxf(red_sh[grp][2][lane], red_sh[grp][3][lane]));
-          const float my = mx * c_sh[r0 + lane];       // the scale is positive
-          const float m_new = fmaxf(m_ref, my);
-          mq_sh[grp][lane] = my == -INFINITY ? 0.f : my;
-          g_sh[grp][lane] = my == -INFINITY ? 0.f : exp2f(my - m_new);
-          al_sh[grp][lane] = m_ref == -INFINITY ? 1.f : exp2f(m_ref - m_new);
-          mt_sh[j & 3][r0 + lane] = my;
-          if (lane == 0 && r0 == 0) vr_sh[j & 3] = vref;
-          const bool moved = m_new != m_ref && m_ref != -INFINITY;
-          m_ref = m_new;
-          const uint32_t any = __ballot_sync(RT == 32 ? 0xffffffffu : 0xffffu, moved);
-          if (lane == 0) moved_sh[grp] = any != 0;
+      float my[kOwn];
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e) {
+        my[e] = -INFINITY;
+        if (lane + 32 * e < R) {
+          const float4 x = *reinterpret_cast<const float4*>(red_sh[grp][(j >> 1) & 1][lane + 32 * e]);
+          my[e] = max_nan(max_nan(x.x, x.y), max_nan(x.z, x.w)) * c_own[e];   // c > 0
+          mq_sh[sw][lane + 32 * e] = my[e] == -INFINITY ? 0.f : -my[e];
         }
       }
-      bar_sync(1 + grp, 128);
+      __syncwarp();
       // the P buffer is free once the product before last is done
-      if (ok && !mbar_wait(&o_full[j & 1], ((j >> 1) & 1) ^ 1, a.err)) ok = false;
+      if (ok && !mbar_wait(&o_full[grp], ((j >> 1) & 1) ^ 1, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) continue;
-      if (moved_sh[grp]) {
+      // (and then the accumulators are done with the maxima of four tiles ago)
+      if (quad == 0) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) l[r] *= al_sh[grp][r];
+        for (int e = 0; e < kOwn; ++e)
+          if (lane + 32 * e < R) mt_sh[j & 3][lane + 32 * e] = my[e];
+        if (lane == 0) vr_sh[j & 3] = vref;
       }
       if (warp_has) {
-        const uint32_t pb = p_s + (j & 1) * C::kP;
+        const uint32_t pb = p_s + grp * C::kP;
+        const __half2 vw2 = __float2half2_rn(vw);
+        auto probs = [&](int r, float (&p)[4], uint32_t* sums) {
+          const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r]);
+          const float4 mq = *reinterpret_cast<const float4*>(&mq_sh[sw][r]);
+          p[0] = ex2_ftz(fmaf(z[r], cc.x, mq.x));
+          p[1] = ex2_ftz(fmaf(z[r + 1], cc.y, mq.y));
+          p[2] = ex2_ftz(fmaf(z[r + 2], cc.z, mq.z));
+          p[3] = ex2_ftz(fmaf(z[r + 3], cc.w, mq.w));
+          // Sums over the warp's keys in fixed point: the pattern of 1 + p counts p in
+          // steps of 2^-23, 32 of them stay below 2^28 (modulo the patterns of 1).
 #pragma unroll
-        for (int c = 0; c < RT / 16; ++c) {
-          uint32_t hi[4], lo[4];
+          for (int i = 0; i < 4; ++i) sums[i] = __reduce_add_sync(0xffffffffu, __float_as_uint(p[i] + 1.f));
+        };
+        if (!blk) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 16 * c + 4 * e;
-            const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r0 + r]);
-            const float4 mq = *reinterpret_cast<const float4*>(&mq_sh[grp][r]);
-            const float4 gg = *reinterpret_cast<const float4*>(&g_sh[grp][r]);
-            float p[4], h[4];
-            p[0] = ex2_ftz(fmaf(z[r], cc.x, -mq.x));
-            p[1] = ex2_ftz(fmaf(z[r + 1], cc.y, -mq.y));
-            p[2] = ex2_ftz(fmaf(z[r + 2], cc.z, -mq.z));
-            p[3] = ex2_ftz(fmaf(z[r + 3], cc.w, -mq.w));
-            l[r] = fmaf(p[0], gg.x, l[r]);
-            l[r + 1] = fmaf(p[1], gg.y, l[r + 1]);
-            l[r + 2] = fmaf(p[2], gg.z, l[r + 2]);
-            l[r + 3] = fmaf(p[3], gg.w, l[r + 3]);
+          for (int c = 0; c < R / 16; ++c) {
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] *= vfac;
-            if (blk) {                                 // bf16, two rows a word
-              hi[e] = pack_bf16(p[0], p[1]);
-              lo[e] = pack_bf16(p[2], p[3]);
-              continue;
+            for (int e = 0; e < 4; ++e) {
+              float p[4];
+              uint32_t sums[4];
+              probs(16 * c + 4 * e, p, sums);
+              if (lane == 0)
+                *reinterpret_cast<uint4*>(&sum_sh[sw][16 * c + 4 * e]) = make_uint4(sums[0], sums[1], sums[2], sums[3]);
+              const __half2 a2 = __hmul2(__floats2half2_rn(p[0], p[1]), vw2);
+              const __half2 b2 = __hmul2(__floats2half2_rn(p[2], p[3]), vw2);
+              p_codes(a2, b2, &hi[e], &lo[e]);
             }
-            hi[e] = e4m3x4(p[0], p[1], p[2], p[3]);
-            e4m3x4_values(hi[e], h);
-            lo[e] = e4m3x4((p[0] - h[0]) * kLoScale, (p[1] - h[1]) * kLoScale,
-                           (p[2] - h[2]) * kLoScale, (p[3] - h[3]) * kLoScale);
+            const uint4 h4 = make_uint4(hi[0], hi[1], hi[2], hi[3]), l4 = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            st_shared_v4(swz<kNO>(pb, key, c), h4);
+            st_shared_v4(swz<kNO>(pb, key, R / 16 + c), l4);
           }
-          if (blk) {
-            const int piece = (r0 + 16 * c) / 8;
-            st_shared_v4(swz<2 * R>(pb, key, piece), make_uint4(hi[0], lo[0], hi[1], lo[1]));
-            st_shared_v4(swz<2 * R>(pb, key, piece + 1), make_uint4(hi[2], lo[2], hi[3], lo[3]));
-            continue;
+        } else {
+#pragma unroll
+          for (int r = 0; r < R; r += 8) {
+            float p[4], q[4];
+            uint32_t sums[4], more[4];
+            probs(r, p, sums);
+            probs(r + 4, q, more);
+            if (lane == 0) {
+              *reinterpret_cast<uint4*>(&sum_sh[sw][r]) = make_uint4(sums[0], sums[1], sums[2], sums[3]);
+              *reinterpret_cast<uint4*>(&sum_sh[sw][r + 4]) = make_uint4(more[0], more[1], more[2], more[3]);
+            }
+            st_shared_v4(swz<kNO>(pb, key, r / 8),
+                         make_uint4(pack_bf16(p[0] * kPScale, p[1] * kPScale), pack_bf16(p[2] * kPScale, p[3] * kPScale),
+                                    pack_bf16(q[0] * kPScale, q[1] * kPScale), pack_bf16(q[2] * kPScale, q[3] * kPScale)));
           }
-          st_shared_v4(swz<2 * R>(pb, key, r0 / 16 + c), make_uint4(hi[0], hi[1], hi[2], hi[3]));
-          st_shared_v4(swz<2 * R>(pb, key, R / 16 + r0 / 16 + c), make_uint4(lo[0], lo[1], lo[2], lo[3]));
         }
         fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[j & 1]);
+      if (lane == 0) mbar_arrive(&p_full[grp]);
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e) {
+        if (lane + 32 * e >= R) continue;
+        const float m_new = max_nan(m_ref[e], my[e]);
+        const float keep = m_ref[e] == -INFINITY ? 0.f : ex2_ftz(m_ref[e] - m_new);
+        const float add = warp_has ? (float)(sum_sh[sw][lane + 32 * e] - 32u * 0x3f800000u) * (1.f / (1 << 23)) : 0.f;
+        l[e] = fmaf(l[e], keep, my[e] == -INFINITY ? 0.f : add * ex2_ftz(my[e] - m_new));
+        m_ref[e] = m_new;
+      }
     }
     grid_dependents_launch();
-    sum_across<RT>(l, lane);
-    bar_sync(1 + grp, 128);                            // the last maxima have been read
-    if (lane < RT) {
-      red_sh[grp][quad][lane] = l[0];
-      if (quad == 0) mref_sh[grp][lane] = m_ref;
-    }
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e)
+      if (lane + 32 * e < R) {
+        lsum_sh[sw][lane + 32 * e] = l[e];
+        if (quad == 0) mref_sh[grp][lane + 32 * e] = m_ref[e];
+      }
     bar_sync(5, 32 * (kSoftWarps + kAccWarps));
   } else {
     // ------------------------------------------------ block keys, accumulators
@@ -713,37 +729,31 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const int at = aw * 32 + lane;                     // 0 .. 127
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     if (has_block) {
-      constexpr int kKeys = kBlkKeys / kAccWarps;
-      WarpRow<D> x[kKeys], y[kKeys];
-#pragma unroll
-      for (int e = 0; e < kKeys; ++e) {
-        const int key = aw + kAccWarps * e;
-        x[e].zero(), y[e].zero();
-        if (key < a.k) {
-          const size_t off = (((size_t)b * a.k + key) * a.Hkv + hkv) * D;
-          x[e].load(a.kb + off, lane);
-          y[e].load(a.vb + off, lane);
-        }
-      }
+      constexpr int kRowsTurn = 32 * kAccWarps / (D / 16);
+      const int c = at % (D / 16);
       bool bad = false;
-#pragma unroll
-      for (int e = 0; e < kKeys; ++e) {
-        const int key = aw + kAccWarps * e;
+#pragma unroll 1
+      for (int key = at / (D / 16); key < kBlkKeys; key += kRowsTurn) {
+        Piece<D> x, y;
+        x.zero(), y.zero();
+        if (key < a.k) {
+          const size_t off = (((size_t)b * a.k + key) * a.Hkv + hkv) * D + 16 * c;
+          x.load(a.kb + off);
+          y.load(a.vb + off);
+        }
+        const float s = x.store(bk_s, key, kBlkKeys + key, c);
+        if (c == 0) bks_sh[key] = s;
         // Values that are not finite stay out of the product (a row that does not
         // see them would multiply them by 0) and are added at the end.
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const uint32_t w = y[e].w[i];
+        auto finite2 = [&](uint32_t w) {
           const bool lo_bad = (w & 0x7f80u) == 0x7f80u, hi_bad = (w & 0x7f800000u) == 0x7f800000u;
           bad |= lo_bad || hi_bad;
-          y[e].w[i] = (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
-        }
-        const float s = x[e].store(bk_s, key, kBlkKeys + key, lane);
-        if (lane == 0) bks_sh[key] = s;
-        const int byte = 2 * D / 32 * lane;            // of the values' row
-        const uint32_t va = swz<128>(bv_s + byte / 128 * C::kBlkSub, key, byte % 128 / 16) + byte % 16;
+          return (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
+        };
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) st_shared_b32(va + 4 * i, y[e].w[i]);
+        for (int e = 0; e < 2; ++e)                    // 8 dimensions each
+          st_shared_v4(swz<128>(bv_s + (2 * c + e) / 8 * C::kBlkSub, key, (2 * c + e) % 8),
+                       make_uint4(finite2(y.w[e].x), finite2(y.w[e].y), finite2(y.w[e].z), finite2(y.w[e].w)));
       }
       if (bad) blk_bad = 1;
       fence_proxy_async_smem();
@@ -756,58 +766,56 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     float m_run = -INFINITY;                           // of row `at`
     bool ok = true;
     for (int j = 0; j < n; ++j) {
-      if (ok && !mbar_wait(&o_full[j & 1], (j >> 1) & 1, a.err)) ok = false;
+      const int buf = j & 1;
+      const bool blk = has_block && j == n - 1;
+      if (ok && !mbar_wait(&o_full[buf], (j >> 1) & 1, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       bool moved = false;
       if (ok && at < R) {
-        const float mt = mt_sh[j & 3][at], m_new = fmaxf(m_run, mt);
-        f_sh[j & 1][at] = mt == -INFINITY ? 0.f : exp2f(mt - m_new) * vr_sh[j & 3] * (1.f / kPScale);
-        fa_sh[j & 1][at] = m_run == -INFINITY ? 1.f : exp2f(m_run - m_new);
+        const float mt = mt_sh[j & 3][at], m_new = max_nan(m_run, mt);
+        f_sh[buf][at] = mt == -INFINITY ? 0.f : ex2_ftz(mt - m_new) * vr_sh[j & 3] * (1.f / kPScale);
+        fa_sh[buf][at] = m_run == -INFINITY ? 1.f : ex2_ftz(m_run - m_new);
         moved = m_run != -INFINITY && m_new != m_run;
         m_run = m_new;
       }
-      if (aw < (R + 31) / 32) {
+      if (aw < kOwn) {
         const uint32_t any = __ballot_sync(0xffffffffu, moved);
-        if (R <= 32) {
-          if (lane == 0) fmoved_sh[j & 1] = any != 0;
-        } else if (lane == 0) {
-          reinterpret_cast<short*>(&fmoved_sh[j & 1])[aw] = any != 0;
-        }
+        if (lane == 0) fmoved_sh[buf][aw] = any != 0;
       }
       bar_sync(3, 32 * kAccWarps);
       if (!ok) continue;
       tc_fence_after();
-      if (fmoved_sh[j & 1]) {
+      if (fmoved_sh[buf][0] | fmoved_sh[buf][kOwn - 1]) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) acc[r] *= fa_sh[j & 1][r];
+        for (int r = 0; r < R; r += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(&fa_sh[buf][r]);
+          acc[r] *= x.x, acc[r + 1] *= x.y, acc[r + 2] *= x.z, acc[r + 3] *= x.w;
+        }
       }
-      const uint32_t oa = tmem + lane_addr + kOCol + (uint32_t)((j & 1) * 2 * R);
-      // the block's product has no lo columns
-      const float lo_w = has_block && j == n - 1 ? 0.f : 1.f / kLoScale;
+      const uint32_t oa = tmem + lane_addr + kOCol + (uint32_t)(buf * kNO);
 #pragma unroll
       for (int c = 0; c < R / 16; ++c) {
         uint32_t h[16], lo[16];
         tc_ld16(oa + 16 * c, h);
         tc_ld16(oa + R + 16 * c, lo);
         tc_wait_ld();
-        if (lo_w == 0.f) {
+        if (!blk) {                                    // the block's product has no lo columns
 #pragma unroll
-          for (int e = 0; e < 16; ++e) lo[e] = 0;
+          for (int e = 0; e < 16; ++e)
+            h[e] = __float_as_uint(fmaf(__uint_as_float(lo[e]), 1.f / kLoScale, __uint_as_float(h[e])));
         }
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(&f_sh[j & 1][16 * c + e]);
-          const float ff[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            acc[16 * c + e + i] =
-                fmaf(fmaf(__uint_as_float(lo[e + i]), lo_w, __uint_as_float(h[e + i])), ff[i],
-                     acc[16 * c + e + i]);
+          const float4 f = *reinterpret_cast<const float4*>(&f_sh[buf][16 * c + e]);
+          acc[16 * c + e] = fmaf(__uint_as_float(h[e]), f.x, acc[16 * c + e]);
+          acc[16 * c + e + 1] = fmaf(__uint_as_float(h[e + 1]), f.y, acc[16 * c + e + 1]);
+          acc[16 * c + e + 2] = fmaf(__uint_as_float(h[e + 2]), f.z, acc[16 * c + e + 2]);
+          acc[16 * c + e + 3] = fmaf(__uint_as_float(h[e + 3]), f.w, acc[16 * c + e + 3]);
         }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&o_free[j & 1]);
+      if (lane == 0) mbar_arrive(&o_free[buf]);
     }
     bar_sync(5, 32 * (kSoftWarps + kAccWarps));
     // ------------------------------------------------ epilogue
@@ -815,35 +823,53 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       float sum = 0.f;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        if (C::kRowGroups > 1 && g != at / RT) continue;
-        const int i = at % RT;
-        const float m = mref_sh[g][i];
-        const float lg = (red_sh[g][0][i] + red_sh[g][1][i]) + (red_sh[g][2][i] + red_sh[g][3][i]);
-        if (m != -INFINITY || lg != 0.f) sum += lg * exp2f(m - m_run);
+        const float m = mref_sh[g][at];
+        if (m == -INFINITY) continue;                  // no tile
+        sum += ((lsum_sh[4 * g][at] + lsum_sh[4 * g + 1][at]) +
+                (lsum_sh[4 * g + 2][at] + lsum_sh[4 * g + 3][at])) * ex2_ftz(m - m_run);
       }
       f_sh[0][at] = n > 0 ? 1.f / sum : 0.f;
       fa_sh[0][at] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
     }
     bar_sync(3, 32 * kAccWarps);
-    // M = 64 leaves 16 dimensions in the first half of every quadrant's lanes
+    // The normalised rows through shared memory (the ring is idle), then out 8
+    // dimensions a thread.  M = 64 leaves 16 dimensions in the first half of every
+    // quadrant's lanes.
     const int d = D == 128 ? quad * 32 + lane : quad * 16 + (lane & 15);
-    const bool has_d = D == 128 || lane < 16;
     float* part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
-    if (has_d) {
+    if (D == 128 || lane < 16) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int row = chunk * R + r;
+      for (int r = 0; r < R; r += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(&f_sh[0][r]);
+        part[r * C::kPStride + d] = acc[r] * f.x;
+        part[(r + 1) * C::kPStride + d] = acc[r + 1] * f.y;
+        part[(r + 2) * C::kPStride + d] = acc[r + 2] * f.z;
+        part[(r + 3) * C::kPStride + d] = acc[r + 3] * f.w;
+      }
+    }
+    bar_sync(3, 32 * kAccWarps);
+    if (has_block && blk_bad) {
+#pragma unroll 1
+      for (int e = at; e < R * D; e += 32 * kAccWarps) {
+        const int r = e / D, dd = e % D;
+        float o = part[r * C::kPStride + dd];
+        for (int i = 0; i < vis_sh[r]; ++i) {
+          const float v = __bfloat162float(a.vb[(((size_t)b * a.k + i) * a.Hkv + hkv) * D + dd]);
+          if (!(fabsf(v) < INFINITY)) o += v;
+        }
+        part[r * C::kPStride + dd] = o;
+      }
+      bar_sync(3, 32 * kAccWarps);
+    }
+    if (a.splits == 1) {
+#pragma unroll 1
+      for (int e = at; e < R * (D / 8); e += 32 * kAccWarps) {
+        const int r = e / (D / 8), c = e % (D / 8), row = chunk * R + r, i = row / a.G;
         if (row >= a.M) break;
-        float o = acc[r] * f_sh[0][r];
-        if (has_block && blk_bad)
-          for (int i = 0; i < vis_sh[r]; ++i) {
-            const float v = __bfloat162float(a.vb[(((size_t)b * a.k + i) * a.Hkv + hkv) * D + d]);
-            if (finite_size(v) == 0.f) o += v;
-          }
-        if (a.splits == 1)
-          a.out[(((size_t)b * a.k + row / a.G) * a.Hq + hkv * a.G + row % a.G) * D + d] = __float2bfloat16(o);
-        else
-          part[r * C::kPStride + d] = n > 0 ? o : 0.f;
+        const float* src = part + r * C::kPStride + 8 * c;
+        const float4 x = *reinterpret_cast<const float4*>(src), y = *reinterpret_cast<const float4*>(src + 4);
+        *reinterpret_cast<uint4*>(a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + 8 * c) =
+            make_uint4(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w), pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
       }
     }
   }
@@ -863,6 +889,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   {
     constexpr int kPer = D / 32;
     const uint32_t lse_s = smem_u32(&fa_sh[0][0]);
+#pragma unroll 1
     for (int r = split + a.splits * warp; r < R && chunk * R + r < a.M;
          r += a.splits * (kThreads / 32)) {
       const float l = lane < a.splits ? ld_cluster_f32(mapa_shared(lse_s + 4u * r, lane)) : -INFINITY;
@@ -891,9 +918,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           }
         }
       }
-      const int row = chunk * R + r;
+      const int row = chunk * R + r, i = row / a.G;
       __nv_bfloat16* dst =
-          a.out + (((size_t)b * a.k + row / a.G) * a.Hq + hkv * a.G + row % a.G) * D + kPer * lane;
+          a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + kPer * lane;
 #pragma unroll
       for (int c = 0; c < kPer; c += 2)
         *reinterpret_cast<__nv_bfloat162*>(dst + c) = __floats2bfloat162_rn(o[c] * inv, o[c + 1] * inv);
