@@ -27,8 +27,9 @@
 // like the rows, two products for S; the values as they are against P in bf16
 // (kind::f16), since a row may see a single small value of a key.
 //
-// Warp roles: 0 pages and TMA, 1 tensor memory and MMA issue, 2-9 softmax (two
-// groups of four on alternate tiles), 10-13 block keys first, then the accumulators.
+// Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
+// O, 3-10 softmax (two groups of four on alternate tiles), 11-14 block keys first,
+// then the accumulators.
 #include <math.h>
 
 #include "paged.cuh"
@@ -40,7 +41,7 @@ using namespace sbd_dev;
 constexpr int kTile = 128;                   // keys
 constexpr int kSoftWarps = 8;
 constexpr int kAccWarps = 4;
-constexpr int kThreads = 32 * (2 + kSoftWarps + kAccWarps);
+constexpr int kThreads = 32 * (3 + kSoftWarps + kAccWarps);
 constexpr int kMaxStages = 8;
 constexpr int kBlkKeys = 32;                 // block keys, padded
 constexpr int kMaxSplits = 16;
@@ -64,6 +65,11 @@ __device__ __forceinline__ void tc_fence_before() {
 }
 __device__ __forceinline__ void tc_fence_after() {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
 }
 __device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
                                           uint32_t idesc, uint32_t accumulate) {
@@ -335,10 +341,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       mbar_init(&kv_empty[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&s_full[i], 2);              // the product, and its issuer's view of the stage
+      mbar_init(&s_full[i], 1);
       mbar_init(&s_free[i], 4);
       mbar_init(&p_full[i], 4);
-      mbar_init(&o_full[i], 2);
+      mbar_init(&o_full[i], 2);              // the product, and the tile's maxima
       mbar_init(&o_free[i], kAccWarps);
     }
     mbar_init(&q_ready, kSoftWarps);
@@ -455,81 +461,79 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     for (int j = max(0, issued - kStages); j < issued; ++j)
       mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
   } else if (warp == 1) {
-    // ------------------------------------------------ MMA issuer
-    if (lane == 0 && n > 0) {
-      bool ok = mbar_wait(&q_ready, 0, a.err);
+    // ------------------------------------------------ S = K Q^T
+    // Two tiles ahead of the softmax group that reads it.  The whole warp runs the
+    // loop (descriptors stay in uniform registers) and one lane issues.
+    const bool leader = elect_one();
+    bool ok = n > 0 && mbar_wait(&q_ready, 0, a.err);
+    const uint32_t id_s = idesc_f8(kTile, kNS, false);
+    constexpr int kPasses = C::kBeside ? 1 : 2;        // hi codes, then lo codes
+    const uint64_t qd = desc<D>(q_s);
+    for (int j = 0; j < n && ok; ++j) {
+      const bool blk = has_block && j == n - 1;
+      ok = mbar_wait(&s_free[j & 1], ((j >> 1) & 1) ^ 1, a.err) &&
+           (blk ? mbar_wait(&blk_ready, 0, a.err)
+                : mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err));
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
       tc_fence_after();
-      const uint32_t id_s = idesc_f8(kTile, kNS, false), id_pv = idesc_f8(D, kNO, true);
-      constexpr int kPasses = C::kBeside ? 1 : 2;      // hi codes, then lo codes
-      auto is_block = [&](int j) { return has_block && j == n - 1; };
-      auto issue_s = [&](int j) {
-        const uint32_t d = tmem + (uint32_t)((j & 1) * kNS);
-        const int parts = is_block(j) ? 2 : 1;
-        for (int e = 0; e < parts; ++e) {
-          const uint32_t kt = is_block(j) ? bk_s + e * kBlkKeys * D : k_tile(j);
+      const uint32_t d = tmem + (uint32_t)((j & 1) * kNS);
+      const uint64_t kd = desc<D>(blk ? bk_s : k_tile(j));
+      if (leader) {
+#pragma unroll
+        for (int h = 0; h < kPasses; ++h)
+#pragma unroll
+          for (int kk = 0; kk < D / 32; ++kk)
+            tc_mma_f8(d, kd + 2 * kk, qd + (h * R * D / 16 + 2 * kk), id_s, h > 0 || kk > 0);
+        if (blk) {                                     // the block keys' lo codes
 #pragma unroll
           for (int h = 0; h < kPasses; ++h)
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk)
-              tc_mma_f8(d, desc<D>(kt + 32 * kk), desc<D>(q_s + h * R * D + 32 * kk), id_s,
-                        e > 0 || h > 0 || kk > 0);
+              tc_mma_f8(d, kd + (kBlkKeys * D / 16 + 2 * kk), qd + (h * R * D / 16 + 2 * kk), id_s, 1);
         }
         tc_commit(&s_full[j & 1]);
-        mbar_arrive(&s_full[j & 1]);
-      };
-      auto issue_pv = [&](int j) {
-        const uint32_t o = tmem + kOCol + (uint32_t)((j & 1) * kNO);
-        const uint32_t pt = p_s + (j & 1) * C::kP;
-        if (is_block(j)) {
+      }
+      __syncwarp();
+    }
+  } else if (warp == 2) {
+    // ------------------------------------------------ O = V^T P^T
+    const bool leader = elect_one();
+    bool ok = true;
+    const uint32_t id_pv = idesc_f8(D, kNO, true);
+    for (int j = 0; j < n && ok; ++j) {
+      const bool blk = has_block && j == n - 1;
+      ok = mbar_wait(&o_free[j & 1], ((j >> 1) & 1) ^ 1, a.err) &&
+           mbar_wait(&p_full[j & 1], (j >> 1) & 1, a.err);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t o = tmem + kOCol + (uint32_t)((j & 1) * kNO);
+      const uint64_t pd = desc<kNO>(p_s + (j & 1) * C::kP);
+      if (blk) {
+        const uint64_t vd = desc<128>(bv_s, C::kBlkSub);
+        if (leader) {
 #pragma unroll
           for (int kk = 0; kk < kBlkKeys / 16; ++kk)
-            tc_mma_bf16(o, desc<128>(bv_s + kk * 16 * 128, C::kBlkSub),
-                        desc<kNO>(pt + kk * 16 * kNO), idesc_bf16_mn(D, R), kk > 0);
-        } else {
-          const int steps = (keys_of(j) + 31) / 32;
-          for (int kk = 0; kk < steps; ++kk)
-            tc_mma_f8(o, desc<D>(v_tile(j) + kk * 32 * D), desc<kNO>(pt + kk * 32 * kNO), id_pv, kk > 0);
+            tc_mma_bf16(o, vd + kk * 128, pd + kk * kNO, idesc_bf16_mn(D, R), kk > 0);
+          tc_commit(&o_full[j & 1]);
+        }
+      } else {
+        const uint64_t vd = desc<D>(v_tile(j));
+        const int steps = (keys_of(j) + 31) / 32;
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < kTile / 32; ++kk)
+            if (kk < steps) tc_mma_f8(o, vd + kk * 2 * D, pd + kk * 2 * kNO, id_pv, kk > 0);
           tc_commit(&kv_empty[j % kStages]);
-        }
-        tc_commit(&o_full[j & 1]);
-        mbar_arrive(&o_full[j & 1]);
-      };
-      // Scores run up to two tiles ahead of the products with V (a softmax group that
-      // hands in its P finds its next scores done); whichever is ready first is
-      // issued.
-      int next_s = 0, next_pv = 0;
-      uint64_t t0 = 0;
-      for (uint32_t idle = 0; ok && next_pv < n;) {
-        bool moved = false;
-        if (next_s < n && next_s <= next_pv + 2 &&
-            mbar_poll_parity(&s_free[next_s & 1], ((next_s >> 1) & 1) ^ 1) &&
-            (is_block(next_s) ? mbar_poll_parity(&blk_ready, 0)
-                              : mbar_poll_parity(&kv_full[next_s % kStages], (next_s / kStages) & 1))) {
-          tc_fence_after();
-          issue_s(next_s++);
-          moved = true;
-        }
-        if (next_pv < next_s && mbar_poll_parity(&p_full[next_pv & 1], (next_pv >> 1) & 1) &&
-            mbar_poll_parity(&o_free[next_pv & 1], ((next_pv >> 1) & 1) ^ 1)) {
-          tc_fence_after();
-          issue_pv(next_pv++);
-          moved = true;
-        }
-        if (moved) {
-          idle = 0;
-        } else if ((++idle & 63u) == 0) {            // bounded, as mbar_wait
-          const uint64_t now = globaltimer();
-          if (idle == 64) t0 = now;
-          if (now - t0 > kWaitLimitNs) {
-            record_error(a.err, SBD_DEVERR_TIMEOUT);
-            ok = false;
-          }
+          tc_commit(&o_full[j & 1]);
         }
       }
+      __syncwarp();
     }
-  } else if (warp < 2 + kSoftWarps) {
+  } else if (warp < 3 + kSoftWarps) {
     // ------------------------------------------------ softmax warps
-    const int sw = warp - 2, quad = warp & 3, grp = sw >> 2;
+    const int sw = warp - 3, quad = warp & 3, grp = sw >> 2;
     const int key = quad * 32 + lane;                  // of every tile
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     {
@@ -567,21 +571,23 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       const bool blk = has_block && j == n - 1;
       const int stage = j % kStages, valid = keys_of(j);
       const bool warp_has = quad * 32 < valid;
+      // the scales come with the stage, which stays until P is handed in
+      if (ok && !(blk ? mbar_wait(&blk_ready, 0, a.err) : mbar_wait(&kv_full[stage], (j / kStages) & 1, a.err)))
+        ok = false;
+      float z[R];
+      float kf = 0.f, vw = 1.f, vref = 1.f;
+      if (blk) {
+        kf = bks_sh[key & (kBlkKeys - 1)];
+      } else if (warp_has) {
+        kf = ks_sh[stage][key >> a.page_log2];
+        vw = vw_sh[stage][key >> a.page_log2];
+        vref = vref_sh[stage];
+      }
       if (ok && !mbar_wait(&s_full[grp], (j >> 1) & 1, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
-      float z[R];
-      float vw = 1.f, vref = 1.f;
       if (ok) {
         tc_fence_after();
         if (warp_has) {
-          float kf;
-          if (blk) {
-            kf = bks_sh[key & (kBlkKeys - 1)];
-          } else {
-            kf = ks_sh[stage][key >> a.page_log2];
-            vw = vw_sh[stage][key >> a.page_log2];
-            vref = vref_sh[stage];
-          }
           const uint32_t sa = tmem + lane_addr + (uint32_t)(grp * kNS);
           if constexpr (C::kBeside) {
             uint32_t h[R / 16][16], lo[R / 16][16];
@@ -650,6 +656,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         for (int e = 0; e < kOwn; ++e)
           if (lane + 32 * e < R) mt_sh[j & 3][lane + 32 * e] = my[e];
         if (lane == 0) vr_sh[j & 3] = vref;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&o_full[grp]);
       }
       if (warp_has) {
         const uint32_t pb = p_s + grp * C::kP;
@@ -725,7 +733,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     bar_sync(5, 32 * (kSoftWarps + kAccWarps));
   } else {
     // ------------------------------------------------ block keys, accumulators
-    const int aw = warp - 2 - kSoftWarps, quad = warp & 3;
+    const int aw = warp - 3 - kSoftWarps, quad = warp & 3;
     const int at = aw * 32 + lane;                     // 0 .. 127
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     if (has_block) {
