@@ -170,6 +170,12 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
                "r"(v.w)
                : "memory");
 }
+// The same without a branch (what it stores is the warp's, one lane does it).
+__device__ __forceinline__ void st_shared_v4_if(bool p, uint32_t addr, float x, float y, float z, float w) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t@q st.shared.v4.f32 [%0], {%1,%2,%3,%4};\n\t}"
+               ::"r"(addr), "f"(x), "f"(y), "f"(z), "f"(w), "r"((uint32_t)p)
+               : "memory");
+}
 __device__ __forceinline__ void bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
@@ -318,9 +324,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
-  __shared__ __align__(16) float red_sh[2][2][R][4];   // maxima by row and warp of a group, two tiles
+  __shared__ __align__(16) float red_sh[2][2][4][R];   // maxima of a group's warps, two tiles
+  __shared__ __align__(16) float sum_sh[kSoftWarps][R];  // a warp's sums of probabilities
   __shared__ __align__(16) float mq_sh[kSoftWarps][R]; // a warp's copy of the tile's maxima
-  __shared__ __align__(16) uint32_t sum_sh[kSoftWarps][R];   // its sums of probabilities
   __shared__ float mt_sh[4][R], vr_sh[4];              // a tile's maxima and value reference
   __shared__ __align__(16) float f_sh[2][R], fa_sh[2][R];
   __shared__ int fmoved_sh[2][kOwn];
@@ -559,10 +565,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     // A lane keeps the statistics of rows lane and lane + 32 over its warp's keys:
     // the running maximum (the same in the four warps of a group) and the sum of
     // probabilities against it.
+    const int own = lane % (R < 32 ? R : 32);          // (R = 16: two lanes a row)
     float c_own[kOwn], m_ref[kOwn], l[kOwn];
 #pragma unroll
     for (int e = 0; e < kOwn; ++e) {
-      c_own[e] = lane + 32 * e < R ? c_sh[lane + 32 * e] : 0.f;
+      c_own[e] = c_sh[own + 32 * e];
       m_ref[e] = -INFINITY;
       l[e] = 0.f;
     }
@@ -621,29 +628,26 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[grp]);
+        // NaN propagates: a row with one has NaN statistics from here on
         if (warp_has) {
-          // NaN propagates: a row with one has NaN statistics from here on
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const float m = redux_max_nan(z[r]);
-            if (lane == 0) red_sh[grp][(j >> 1) & 1][r][quad] = m;
-          }
+          for (int r = 0; r < R; r += 4)
+            st_shared_v4_if(lane == 0, smem_u32(&red_sh[grp][(j >> 1) & 1][quad][r]),
+                            redux_max_nan(z[r]), redux_max_nan(z[r + 1]), redux_max_nan(z[r + 2]),
+                            redux_max_nan(z[r + 3]));
         } else {
 #pragma unroll
-          for (int e = 0; e < kOwn; ++e)
-            if (lane + 32 * e < R) red_sh[grp][(j >> 1) & 1][lane + 32 * e][quad] = -INFINITY;
+          for (int e = 0; e < kOwn; ++e) red_sh[grp][(j >> 1) & 1][quad][own + 32 * e] = -INFINITY;
         }
       }
       bar_sync(1 + grp, 128);
       float my[kOwn];
 #pragma unroll
       for (int e = 0; e < kOwn; ++e) {
-        my[e] = -INFINITY;
-        if (lane + 32 * e < R) {
-          const float4 x = *reinterpret_cast<const float4*>(red_sh[grp][(j >> 1) & 1][lane + 32 * e]);
-          my[e] = max_nan(max_nan(x.x, x.y), max_nan(x.z, x.w)) * c_own[e];   // c > 0
-          mq_sh[sw][lane + 32 * e] = my[e] == -INFINITY ? 0.f : -my[e];
-        }
+        const float(*x)[R] = red_sh[grp][(j >> 1) & 1];
+        const int r = own + 32 * e;
+        my[e] = max_nan(max_nan(x[0][r], x[1][r]), max_nan(x[2][r], x[3][r])) * c_own[e];   // c > 0
+        mq_sh[sw][own + 32 * e] = my[e] == -INFINITY ? 0.f : -my[e];
       }
       __syncwarp();
       // the P buffer is free once the product before last is done
@@ -653,8 +657,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       // (and then the accumulators are done with the maxima of four tiles ago)
       if (quad == 0) {
 #pragma unroll
-        for (int e = 0; e < kOwn; ++e)
-          if (lane + 32 * e < R) mt_sh[j & 3][lane + 32 * e] = my[e];
+        for (int e = 0; e < kOwn; ++e) mt_sh[j & 3][own + 32 * e] = my[e];
         if (lane == 0) vr_sh[j & 3] = vref;
         __syncwarp();
         if (lane == 0) mbar_arrive(&o_full[grp]);
@@ -662,7 +665,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (warp_has) {
         const uint32_t pb = p_s + grp * C::kP;
         const __half2 vw2 = __float2half2_rn(vw);
-        auto probs = [&](int r, float (&p)[4], uint32_t* sums) {
+        auto probs = [&](int r, float (&p)[4]) {
           const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r]);
           const float4 mq = *reinterpret_cast<const float4*>(&mq_sh[sw][r]);
           p[0] = ex2_ftz(fmaf(z[r], cc.x, mq.x));
@@ -671,8 +674,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           p[3] = ex2_ftz(fmaf(z[r + 3], cc.w, mq.w));
           // Sums over the warp's keys in fixed point: the pattern of 1 + p counts p in
           // steps of 2^-23, 32 of them stay below 2^28 (modulo the patterns of 1).
+          uint32_t n1[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sums[i] = __reduce_add_sync(0xffffffffu, __float_as_uint(p[i] + 1.f));
+          for (int i = 0; i < 4; ++i) n1[i] = __reduce_add_sync(0xffffffffu, __float_as_uint(p[i] + 1.f));
+          st_shared_v4_if(lane == 0, smem_u32(&sum_sh[sw][r]), __uint_as_float(n1[0]),
+                          __uint_as_float(n1[1]), __uint_as_float(n1[2]), __uint_as_float(n1[3]));
         };
         if (!blk) {
 #pragma unroll
@@ -681,10 +687,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float p[4];
-              uint32_t sums[4];
-              probs(16 * c + 4 * e, p, sums);
-              if (lane == 0)
-                *reinterpret_cast<uint4*>(&sum_sh[sw][16 * c + 4 * e]) = make_uint4(sums[0], sums[1], sums[2], sums[3]);
+              probs(16 * c + 4 * e, p);
               const __half2 a2 = __hmul2(__floats2half2_rn(p[0], p[1]), vw2);
               const __half2 b2 = __hmul2(__floats2half2_rn(p[2], p[3]), vw2);
               p_codes(a2, b2, &hi[e], &lo[e]);
@@ -697,13 +700,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
 #pragma unroll
           for (int r = 0; r < R; r += 8) {
             float p[4], q[4];
-            uint32_t sums[4], more[4];
-            probs(r, p, sums);
-            probs(r + 4, q, more);
-            if (lane == 0) {
-              *reinterpret_cast<uint4*>(&sum_sh[sw][r]) = make_uint4(sums[0], sums[1], sums[2], sums[3]);
-              *reinterpret_cast<uint4*>(&sum_sh[sw][r + 4]) = make_uint4(more[0], more[1], more[2], more[3]);
-            }
+            probs(r, p);
+            probs(r + 4, q);
             st_shared_v4(swz<kNO>(pb, key, r / 8),
                          make_uint4(pack_bf16(p[0] * kPScale, p[1] * kPScale), pack_bf16(p[2] * kPScale, p[3] * kPScale),
                                     pack_bf16(q[0] * kPScale, q[1] * kPScale), pack_bf16(q[2] * kPScale, q[3] * kPScale)));
@@ -715,21 +713,20 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (lane == 0) mbar_arrive(&p_full[grp]);
 #pragma unroll
       for (int e = 0; e < kOwn; ++e) {
-        if (lane + 32 * e >= R) continue;
         const float m_new = max_nan(m_ref[e], my[e]);
         const float keep = m_ref[e] == -INFINITY ? 0.f : ex2_ftz(m_ref[e] - m_new);
-        const float add = warp_has ? (float)(sum_sh[sw][lane + 32 * e] - 32u * 0x3f800000u) * (1.f / (1 << 23)) : 0.f;
+        const uint32_t steps = __float_as_uint(sum_sh[sw][own + 32 * e]) - 32u * 0x3f800000u;
+        const float add = warp_has ? (float)steps * (1.f / (1 << 23)) : 0.f;
         l[e] = fmaf(l[e], keep, my[e] == -INFINITY ? 0.f : add * ex2_ftz(my[e] - m_new));
         m_ref[e] = m_new;
       }
     }
     grid_dependents_launch();
 #pragma unroll
-    for (int e = 0; e < kOwn; ++e)
-      if (lane + 32 * e < R) {
-        lsum_sh[sw][lane + 32 * e] = l[e];
-        if (quad == 0) mref_sh[grp][lane + 32 * e] = m_ref[e];
-      }
+    for (int e = 0; e < kOwn; ++e) {
+      lsum_sh[sw][own + 32 * e] = l[e];
+      if (quad == 0) mref_sh[grp][own + 32 * e] = m_ref[e];
+    }
     bar_sync(5, 32 * (kSoftWarps + kAccWarps));
   } else {
     // ------------------------------------------------ block keys, accumulators
