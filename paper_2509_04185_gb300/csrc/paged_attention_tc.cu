@@ -28,7 +28,10 @@
 // (kind::f16), since a row may see a single small value of a key.
 //
 // Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
-// O, 3-10 softmax (two groups of four on alternate tiles), 11-14 block keys first,
+// O; from 4 the softmax, groups of four warps, two on alternate tiles or, above 16
+// rows, four on alternate tiles and halves of the rows (with two groups of 64 rows a
+// thread the two warps of a scheduler could not keep its pipes busy: 29 clocks a row
+// and warp, the sum of what each pipe needs); the last four the block keys first,
 // then the accumulators.
 #include <math.h>
 
@@ -39,9 +42,6 @@ namespace {
 using namespace sbd_dev;
 
 constexpr int kTile = 128;                   // keys
-constexpr int kSoftWarps = 8;
-constexpr int kAccWarps = 4;
-constexpr int kThreads = 32 * (3 + kSoftWarps + kAccWarps);
 constexpr int kMaxStages = 8;
 constexpr int kBlkKeys = 32;                 // block keys, padded
 constexpr int kMaxSplits = 16;
@@ -222,6 +222,14 @@ struct Shape {
   static constexpr bool kBeside = R < 64;
   static constexpr int kNS = kBeside ? 2 * R : R;      // columns of S
   static constexpr int kNO = 2 * R;                    // columns of O, bytes of a key's row of P
+  // A softmax group of four warps takes every other tile, all rows or half of them.
+  static constexpr int kHalves = R > 16 ? 2 : 1;
+  static constexpr int kRT = R / kHalves;              // rows of a softmax thread
+  static constexpr int kSoftWarps = 8 * kHalves;
+  // Four warps hold the accumulators of 32 rows at most, a dimension a thread.
+  static constexpr int kRA = R < 32 ? R : 32;
+  static constexpr int kAccWarps = 4 * (R / kRA);
+  static constexpr int kThreads = 32 * (4 + kSoftWarps + kAccWarps);
   static constexpr int kKV = kTile * D;                // a K or V tile
   static constexpr int kQ = 2 * R * D;
   static constexpr int kP = kTile * 2 * R;
@@ -303,14 +311,15 @@ __device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, 
 }
 
 template <int D, int R>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<D, R>::kThreads, 1)
 paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
   using C = Shape<D, R>;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
+  constexpr int kHalves = C::kHalves, RT = C::kRT, kSoftWarps = C::kSoftWarps;
+  constexpr int RA = C::kRA, kAccWarps = C::kAccWarps;
   constexpr uint32_t kTmemCols = 8 * R;                // two buffers of S and of O
   constexpr uint32_t kOCol = 2 * kNS;
-  constexpr int kOwn = (R + 31) / 32;                  // rows of a lane: lane, lane + 32
   static_assert(R == 16 || R == 32 || R == 64, "a key's row of P is one swizzle atom");
 
   extern __shared__ uint8_t smem_raw[];
@@ -325,12 +334,12 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
   __shared__ __align__(16) float red_sh[2][2][4][R];   // maxima of a group's warps, two tiles
-  __shared__ __align__(16) float sum_sh[kSoftWarps][R];  // a warp's sums of probabilities
-  __shared__ __align__(16) float mq_sh[kSoftWarps][R]; // a warp's copy of the tile's maxima
+  __shared__ __align__(16) float sum_sh[kSoftWarps][RT]; // a warp's sums of probabilities
+  __shared__ __align__(16) float mq_sh[kSoftWarps][RT]; // a warp's copy of the tile's maxima, negated
   __shared__ float mt_sh[4][R], vr_sh[4];              // a tile's maxima and value reference
   __shared__ __align__(16) float f_sh[2][R], fa_sh[2][R];
-  __shared__ int fmoved_sh[2][kOwn];
-  __shared__ float lsum_sh[kSoftWarps][R], mref_sh[2][R];
+  __shared__ int fmoved_sh[2][2];
+  __shared__ float lsum_sh[kSoftWarps][RT], mref_sh[2][R];
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_s = sbase, p_s = q_s + C::kQ;
@@ -348,9 +357,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&s_free[i], 4);
-      mbar_init(&p_full[i], 4);
-      mbar_init(&o_full[i], 2);              // the product, and the tile's maxima
+      mbar_init(&s_free[i], 4 * kHalves);
+      mbar_init(&p_full[i], 4 * kHalves);
+      mbar_init(&o_full[i], 1 + kHalves);    // the product, and the tile's maxima
       mbar_init(&o_free[i], kAccWarps);
     }
     mbar_init(&q_ready, kSoftWarps);
@@ -537,9 +546,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       }
       __syncwarp();
     }
-  } else if (warp < 3 + kSoftWarps) {
+  } else if (warp >= 4 && warp < 4 + kSoftWarps) {
     // ------------------------------------------------ softmax warps
-    const int sw = warp - 3, quad = warp & 3, grp = sw >> 2;
+    const int sw = warp - 4, quad = warp & 3, grp = sw / (4 * kHalves);
+    const int r0 = sw / 4 % kHalves * RT;              // its rows: r0 .. r0 + RT - 1
     const int key = quad * 32 + lane;                  // of every tile
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     {
@@ -560,19 +570,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_ready);
-      bar_sync(4, 32 * kSoftWarps);                    // c and vis of all rows
+      bar_sync(5, 32 * kSoftWarps);                    // c and vis of all rows
     }
-    // A lane keeps the statistics of rows lane and lane + 32 over its warp's keys:
-    // the running maximum (the same in the four warps of a group) and the sum of
-    // probabilities against it.
-    const int own = lane % (R < 32 ? R : 32);          // (R = 16: two lanes a row)
-    float c_own[kOwn], m_ref[kOwn], l[kOwn];
-#pragma unroll
-    for (int e = 0; e < kOwn; ++e) {
-      c_own[e] = c_sh[own + 32 * e];
-      m_ref[e] = -INFINITY;
-      l[e] = 0.f;
-    }
+    // A lane keeps the statistics of one row over its warp's keys: the running
+    // maximum (the same in the four warps of a group) and the sum of probabilities
+    // against it.  (RT = 16: two lanes a row.)
+    const int own = lane % RT;
+    const float c_own = c_sh[r0 + own];
+    float m_ref = -INFINITY, l = 0.f;
     bool ok = true;
     for (int j = grp; j < n; j += 2) {
       const bool blk = has_block && j == n - 1;
@@ -581,7 +586,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       // the scales come with the stage, which stays until P is handed in
       if (ok && !(blk ? mbar_wait(&blk_ready, 0, a.err) : mbar_wait(&kv_full[stage], (j / kStages) & 1, a.err)))
         ok = false;
-      float z[R];
+      float z[RT];
       float kf = 0.f, vw = 1.f, vref = 1.f;
       if (blk) {
         kf = bks_sh[key & (kBlkKeys - 1)];
@@ -595,34 +600,31 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (ok) {
         tc_fence_after();
         if (warp_has) {
-          const uint32_t sa = tmem + lane_addr + (uint32_t)(grp * kNS);
-          if constexpr (C::kBeside) {
-            uint32_t h[R / 16][16], lo[R / 16][16];
+          const uint32_t sa = tmem + lane_addr + (uint32_t)(grp * kNS + r0);
+          uint32_t h[RT / 16][16];
 #pragma unroll
-            for (int c = 0; c < R / 16; ++c) {
-              tc_ld16(sa + 16 * c, h[c]);
-              tc_ld16(sa + R + 16 * c, lo[c]);
-            }
+          for (int c = 0; c < RT / 16; ++c) tc_ld16(sa + 16 * c, h[c]);
+          if constexpr (C::kBeside) {
+            uint32_t lo[RT / 16][16];
+#pragma unroll
+            for (int c = 0; c < RT / 16; ++c) tc_ld16(sa + R + 16 * c, lo[c]);
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < RT; ++r)
               z[r] = (__uint_as_float(h[r / 16][r % 16]) + __uint_as_float(lo[r / 16][r % 16])) * kf;
           } else {
-            uint32_t h[R / 16][16];
-#pragma unroll
-            for (int c = 0; c < R / 16; ++c) tc_ld16(sa + 16 * c, h[c]);
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < R; ++r) z[r] = __uint_as_float(h[r / 16][r % 16]) * kf;
+            for (int r = 0; r < RT; ++r) z[r] = __uint_as_float(h[r / 16][r % 16]) * kf;
           }
           if (blk) {
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-              if (key >= vis_sh[r]) z[r] = -INFINITY;
+            for (int r = 0; r < RT; ++r)
+              if (key >= vis_sh[r0 + r]) z[r] = -INFINITY;
           } else if (valid < quad * 32 + 32) {
             const bool out = key >= valid;
 #pragma unroll
-            for (int r = 0; r < R; ++r) z[r] = out ? -INFINITY : z[r];
+            for (int r = 0; r < RT; ++r) z[r] = out ? -INFINITY : z[r];
           }
         }
         tc_fence_before();
@@ -631,24 +633,19 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         // NaN propagates: a row with one has NaN statistics from here on
         if (warp_has) {
 #pragma unroll
-          for (int r = 0; r < R; r += 4)
-            st_shared_v4_if(lane == 0, smem_u32(&red_sh[grp][(j >> 1) & 1][quad][r]),
+          for (int r = 0; r < RT; r += 4)
+            st_shared_v4_if(lane == 0, smem_u32(&red_sh[grp][(j >> 1) & 1][quad][r0 + r]),
                             redux_max_nan(z[r]), redux_max_nan(z[r + 1]), redux_max_nan(z[r + 2]),
                             redux_max_nan(z[r + 3]));
         } else {
-#pragma unroll
-          for (int e = 0; e < kOwn; ++e) red_sh[grp][(j >> 1) & 1][quad][own + 32 * e] = -INFINITY;
+          red_sh[grp][(j >> 1) & 1][quad][r0 + own] = -INFINITY;
         }
       }
-      bar_sync(1 + grp, 128);
-      float my[kOwn];
-#pragma unroll
-      for (int e = 0; e < kOwn; ++e) {
-        const float(*x)[R] = red_sh[grp][(j >> 1) & 1];
-        const int r = own + 32 * e;
-        my[e] = max_nan(max_nan(x[0][r], x[1][r]), max_nan(x[2][r], x[3][r])) * c_own[e];   // c > 0
-        mq_sh[sw][own + 32 * e] = my[e] == -INFINITY ? 0.f : -my[e];
-      }
+      bar_sync(1 + sw / 4, 128);
+      const float(*x)[R] = red_sh[grp][(j >> 1) & 1];
+      const float my = max_nan(max_nan(x[0][r0 + own], x[1][r0 + own]), max_nan(x[2][r0 + own], x[3][r0 + own])) *
+                       c_own;                          // c > 0
+      mq_sh[sw][own] = my == -INFINITY ? 0.f : -my;
       __syncwarp();
       // the P buffer is free once the product before last is done
       if (ok && !mbar_wait(&o_full[grp], ((j >> 1) & 1) ^ 1, a.err)) ok = false;
@@ -656,9 +653,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (!ok) continue;
       // (and then the accumulators are done with the maxima of four tiles ago)
       if (quad == 0) {
-#pragma unroll
-        for (int e = 0; e < kOwn; ++e) mt_sh[j & 3][own + 32 * e] = my[e];
-        if (lane == 0) vr_sh[j & 3] = vref;
+        mt_sh[j & 3][r0 + own] = my;
+        if (lane == 0 && r0 == 0) vr_sh[j & 3] = vref;
         __syncwarp();
         if (lane == 0) mbar_arrive(&o_full[grp]);
       }
@@ -666,7 +662,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         const uint32_t pb = p_s + grp * C::kP;
         const __half2 vw2 = __float2half2_rn(vw);
         auto probs = [&](int r, float (&p)[4]) {
-          const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r]);
+          const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r0 + r]);
           const float4 mq = *reinterpret_cast<const float4*>(&mq_sh[sw][r]);
           p[0] = ex2_ftz(fmaf(z[r], cc.x, mq.x));
           p[1] = ex2_ftz(fmaf(z[r + 1], cc.y, mq.y));
@@ -682,7 +678,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         };
         if (!blk) {
 #pragma unroll
-          for (int c = 0; c < R / 16; ++c) {
+          for (int c = 0; c < RT / 16; ++c) {
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -692,17 +688,16 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
               const __half2 b2 = __hmul2(__floats2half2_rn(p[2], p[3]), vw2);
               p_codes(a2, b2, &hi[e], &lo[e]);
             }
-            const uint4 h4 = make_uint4(hi[0], hi[1], hi[2], hi[3]), l4 = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            st_shared_v4(swz<kNO>(pb, key, c), h4);
-            st_shared_v4(swz<kNO>(pb, key, R / 16 + c), l4);
+            st_shared_v4(swz<kNO>(pb, key, r0 / 16 + c), make_uint4(hi[0], hi[1], hi[2], hi[3]));
+            st_shared_v4(swz<kNO>(pb, key, (R + r0) / 16 + c), make_uint4(lo[0], lo[1], lo[2], lo[3]));
           }
         } else {
 #pragma unroll
-          for (int r = 0; r < R; r += 8) {
+          for (int r = 0; r < RT; r += 8) {
             float p[4], q[4];
             probs(r, p);
             probs(r + 4, q);
-            st_shared_v4(swz<kNO>(pb, key, r / 8),
+            st_shared_v4(swz<kNO>(pb, key, (r0 + r) / 8),
                          make_uint4(pack_bf16(p[0] * kPScale, p[1] * kPScale), pack_bf16(p[2] * kPScale, p[3] * kPScale),
                                     pack_bf16(q[0] * kPScale, q[1] * kPScale), pack_bf16(q[2] * kPScale, q[3] * kPScale)));
           }
@@ -711,27 +706,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&p_full[grp]);
-#pragma unroll
-      for (int e = 0; e < kOwn; ++e) {
-        const float m_new = max_nan(m_ref[e], my[e]);
-        const float keep = m_ref[e] == -INFINITY ? 0.f : ex2_ftz(m_ref[e] - m_new);
-        const uint32_t steps = __float_as_uint(sum_sh[sw][own + 32 * e]) - 32u * 0x3f800000u;
-        const float add = warp_has ? (float)steps * (1.f / (1 << 23)) : 0.f;
-        l[e] = fmaf(l[e], keep, my[e] == -INFINITY ? 0.f : add * ex2_ftz(my[e] - m_new));
-        m_ref[e] = m_new;
-      }
+      const float m_new = max_nan(m_ref, my);
+      const float keep = m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - m_new);
+      const uint32_t steps = __float_as_uint(sum_sh[sw][own]) - 32u * 0x3f800000u;
+      const float add = warp_has ? (float)steps * (1.f / (1 << 23)) : 0.f;
+      l = fmaf(l, keep, my == -INFINITY ? 0.f : add * ex2_ftz(my - m_new));
+      m_ref = m_new;
     }
     grid_dependents_launch();
-#pragma unroll
-    for (int e = 0; e < kOwn; ++e) {
-      lsum_sh[sw][own + 32 * e] = l[e];
-      if (quad == 0) mref_sh[grp][own + 32 * e] = m_ref[e];
-    }
-    bar_sync(5, 32 * (kSoftWarps + kAccWarps));
-  } else {
+    lsum_sh[sw][own] = l;
+    if (quad == 0) mref_sh[grp][r0 + own] = m_ref;
+    bar_sync(6, 32 * (kSoftWarps + kAccWarps));
+  } else if (warp >= 4 + kSoftWarps) {
     // ------------------------------------------------ block keys, accumulators
-    const int aw = warp - 3 - kSoftWarps, quad = warp & 3;
-    const int at = aw * 32 + lane;                     // 0 .. 127
+    const int aw = warp - 4 - kSoftWarps, quad = warp & 3;
+    const int at = aw * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     if (has_block) {
       constexpr int kRowsTurn = 32 * kAccWarps / (D / 16);
@@ -765,10 +754,12 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       __syncwarp();
       if (lane == 0) mbar_arrive(&blk_ready);
     }
-    float acc[R];                                      // of one dimension, against m_run
+    const int ra = aw / 4 * RA, mine = at % 128;       // rows ra .. ra + RA - 1; thread `mine` keeps one's maximum
+    const bool keeps = mine < RA;
+    float acc[RA];                                     // of one dimension, against m_run
 #pragma unroll
-    for (int r = 0; r < R; ++r) acc[r] = 0.f;
-    float m_run = -INFINITY;                           // of row `at`
+    for (int r = 0; r < RA; ++r) acc[r] = 0.f;
+    float m_run = -INFINITY;                           // of row ra + mine
     bool ok = true;
     for (int j = 0; j < n; ++j) {
       const int buf = j & 1;
@@ -776,30 +767,30 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (ok && !mbar_wait(&o_full[buf], (j >> 1) & 1, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       bool moved = false;
-      if (ok && at < R) {
-        const float mt = mt_sh[j & 3][at], m_new = max_nan(m_run, mt);
-        f_sh[buf][at] = mt == -INFINITY ? 0.f : ex2_ftz(mt - m_new) * vr_sh[j & 3] * (1.f / kPScale);
-        fa_sh[buf][at] = m_run == -INFINITY ? 1.f : ex2_ftz(m_run - m_new);
+      if (ok && keeps) {
+        const float mt = mt_sh[j & 3][ra + mine], m_new = max_nan(m_run, mt);
+        f_sh[buf][ra + mine] = mt == -INFINITY ? 0.f : ex2_ftz(mt - m_new) * vr_sh[j & 3] * (1.f / kPScale);
+        fa_sh[buf][ra + mine] = m_run == -INFINITY ? 1.f : ex2_ftz(m_run - m_new);
         moved = m_run != -INFINITY && m_new != m_run;
         m_run = m_new;
       }
-      if (aw < kOwn) {
+      if (aw % 4 == 0) {
         const uint32_t any = __ballot_sync(0xffffffffu, moved);
-        if (lane == 0) fmoved_sh[buf][aw] = any != 0;
+        if (lane == 0) fmoved_sh[buf][aw / 4] = any != 0;
       }
-      bar_sync(3, 32 * kAccWarps);
+      bar_sync(7 + aw / 4, 128);
       if (!ok) continue;
       tc_fence_after();
-      if (fmoved_sh[buf][0] | fmoved_sh[buf][kOwn - 1]) {
+      if (fmoved_sh[buf][aw / 4]) {
 #pragma unroll
-        for (int r = 0; r < R; r += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(&fa_sh[buf][r]);
+        for (int r = 0; r < RA; r += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(&fa_sh[buf][ra + r]);
           acc[r] *= x.x, acc[r + 1] *= x.y, acc[r + 2] *= x.z, acc[r + 3] *= x.w;
         }
       }
-      const uint32_t oa = tmem + lane_addr + kOCol + (uint32_t)(buf * kNO);
+      const uint32_t oa = tmem + lane_addr + kOCol + (uint32_t)(buf * kNO + ra);
 #pragma unroll
-      for (int c = 0; c < R / 16; ++c) {
+      for (int c = 0; c < RA / 16; ++c) {
         uint32_t h[16], lo[16];
         tc_ld16(oa + 16 * c, h);
         tc_ld16(oa + R + 16 * c, lo);
@@ -811,7 +802,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         }
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(&f_sh[buf][16 * c + e]);
+          const float4 f = *reinterpret_cast<const float4*>(&f_sh[buf][ra + 16 * c + e]);
           acc[16 * c + e] = fmaf(__uint_as_float(h[e]), f.x, acc[16 * c + e]);
           acc[16 * c + e + 1] = fmaf(__uint_as_float(h[e + 1]), f.y, acc[16 * c + e + 1]);
           acc[16 * c + e + 2] = fmaf(__uint_as_float(h[e + 2]), f.z, acc[16 * c + e + 2]);
@@ -822,21 +813,22 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free[buf]);
     }
-    bar_sync(5, 32 * (kSoftWarps + kAccWarps));
+    bar_sync(6, 32 * (kSoftWarps + kAccWarps));
     // ------------------------------------------------ epilogue
-    if (at < R) {
+    if (keeps) {
+      const int r = ra + mine, i = r % RT;
       float sum = 0.f;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        const float m = mref_sh[g][at];
+        const float m = mref_sh[g][r];
         if (m == -INFINITY) continue;                  // no tile
-        sum += ((lsum_sh[4 * g][at] + lsum_sh[4 * g + 1][at]) +
-                (lsum_sh[4 * g + 2][at] + lsum_sh[4 * g + 3][at])) * ex2_ftz(m - m_run);
+        const float(*lw)[RT] = lsum_sh + 4 * (g * kHalves + r / RT);
+        sum += ((lw[0][i] + lw[1][i]) + (lw[2][i] + lw[3][i])) * ex2_ftz(m - m_run);
       }
-      f_sh[0][at] = n > 0 ? 1.f / sum : 0.f;
-      fa_sh[0][at] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
+      f_sh[0][r] = n > 0 ? 1.f / sum : 0.f;
+      fa_sh[0][r] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
     }
-    bar_sync(3, 32 * kAccWarps);
+    bar_sync(7 + aw / 4, 128);
     // The normalised rows through shared memory (the ring is idle), then out 8
     // dimensions a thread.  M = 64 leaves 16 dimensions in the first half of every
     // quadrant's lanes.
@@ -844,15 +836,16 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     float* part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
     if (D == 128 || lane < 16) {
 #pragma unroll
-      for (int r = 0; r < R; r += 4) {
-        const float4 f = *reinterpret_cast<const float4*>(&f_sh[0][r]);
-        part[r * C::kPStride + d] = acc[r] * f.x;
-        part[(r + 1) * C::kPStride + d] = acc[r + 1] * f.y;
-        part[(r + 2) * C::kPStride + d] = acc[r + 2] * f.z;
-        part[(r + 3) * C::kPStride + d] = acc[r + 3] * f.w;
+      for (int r = 0; r < RA; r += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(&f_sh[0][ra + r]);
+        float* dst = part + (ra + r) * C::kPStride + d;
+        dst[0] = acc[r] * f.x;
+        dst[C::kPStride] = acc[r + 1] * f.y;
+        dst[2 * C::kPStride] = acc[r + 2] * f.z;
+        dst[3 * C::kPStride] = acc[r + 3] * f.w;
       }
     }
-    bar_sync(3, 32 * kAccWarps);
+    bar_sync(9, 32 * kAccWarps);
     if (has_block && blk_bad) {
 #pragma unroll 1
       for (int e = at; e < R * D; e += 32 * kAccWarps) {
@@ -864,7 +857,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         }
         part[r * C::kPStride + dd] = o;
       }
-      bar_sync(3, 32 * kAccWarps);
+      bar_sync(9, 32 * kAccWarps);
     }
     if (a.splits == 1) {
 #pragma unroll 1
@@ -896,7 +889,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const uint32_t lse_s = smem_u32(&fa_sh[0][0]);
 #pragma unroll 1
     for (int r = split + a.splits * warp; r < R && chunk * R + r < a.M;
-         r += a.splits * (kThreads / 32)) {
+         r += a.splits * (C::kThreads / 32)) {
       const float l = lane < a.splits ? ld_cluster_f32(mapa_shared(lse_s + 4u * r, lane)) : -INFINITY;
       float2 v[kMaxSplits][kPer / 2];
 #pragma unroll
@@ -937,12 +930,15 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
 struct Kernel {
   const void* fn;
   size_t smem;
+  int threads;
 };
+template <int D, int R>
+Kernel instance() {
+  return {(const void*)paged_tc_kernel<D, R>, Shape<D, R>::kSmem, Shape<D, R>::kThreads};
+}
 template <int D>
 Kernel kernel_of(int R) {
-  if (R == 16) return {(const void*)paged_tc_kernel<D, 16>, Shape<D, 16>::kSmem};
-  if (R == 32) return {(const void*)paged_tc_kernel<D, 32>, Shape<D, 32>::kSmem};
-  return {(const void*)paged_tc_kernel<D, 64>, Shape<D, 64>::kSmem};
+  return R == 16 ? instance<D, 16>() : R == 32 ? instance<D, 32>() : instance<D, 64>();
 }
 Kernel kernel_for(int D, int R) { return D == 128 ? kernel_of<128>(R) : kernel_of<64>(R); }
 
@@ -959,13 +955,13 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
   int s = 1;
   if (num_splits > 0) {
     for (s = num_splits < kMaxSplits ? num_splits : kMaxSplits; s > 1; --s)
-      if (cluster_slots(kern.fn, kThreads, kern.smem, s) > 0) break;
+      if (cluster_slots(kern.fn, kern.threads, kern.smem, s) > 0) break;
   } else if (jobs > 0) {
     // one wave of CTAs, the clusters of all jobs at once
     long long most = num_sms() / jobs;
     if (most > tiles) most = tiles;
     for (s = most < kMaxSplits ? (int)most : kMaxSplits; s > 1; --s)
-      if (cluster_slots(kern.fn, kThreads, kern.smem, s) >= jobs) break;
+      if (cluster_slots(kern.fn, kern.threads, kern.smem, s) >= jobs) break;
   }
   p->splits = s < 1 ? 1 : s;
   p->cluster = p->splits > 1;
@@ -1015,7 +1011,7 @@ sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStre
   s = allow_smem(kern.fn, kern.smem, "cudaFuncSetAttribute(paged_tc_kernel)");
   if (s != SBD_OK) return s;
   void* args[] = {(void*)&tk, (void*)&tv, (void*)&a};
-  return launch_pdl(kern.fn, dim3(p.splits, p.Hkv * p.chunks, p.B), dim3(kThreads), kern.smem, st,
+  return launch_pdl(kern.fn, dim3(p.splits, p.Hkv * p.chunks, p.B), dim3(kern.threads), kern.smem, st,
                     args, "paged_tc_kernel launch", p.splits);
 }
 
