@@ -16,23 +16,24 @@
 // page's scales are scalars of the thread, masks a comparison, a row's maximum and
 // sum one redux a warp.
 //
+// Tiles go in steps of two (256 keys): what a step costs by row and not by key --
+// redux, the row's scale and maximum from shared memory, the accumulators -- is all
+// on the path to shared memory that sets the pace from 32 rows on.
+//
 // P.  Probabilities span more octaves than two codes: next to a key that takes all
 // the weight, a thousand weak ones would vanish.  So P is relative to the maximum
-// of its own tile of 128 keys (times the value scale over the tile's largest, and
-// 2^8), every tile's product starts at zero, and four warps add it to fp32
-// accumulators in registers, weighted 2^(m_tile - m).  No accumulator in tensor
-// memory is ever rescaled, and the softmax never waits for one.
+// of its own step (times the value scale over the step's largest, and 2^8), every
+// step's product starts at zero, and four or eight warps add it to fp32 accumulators
+// in registers, weighted 2^(m_step - m).  No accumulator in tensor memory is ever
+// rescaled, and the softmax never waits for one.
 //
-// Block keys (not cached, bf16) form the last tile: the keys split into code pairs
+// Block keys (not cached, bf16) form the last step: the keys split into code pairs
 // like the rows, two products for S; the values as they are against P in bf16
 // (kind::f16), since a row may see a single small value of a key.
 //
 // Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
-// O; from 4 the softmax, groups of four warps, two on alternate tiles or, above 16
-// rows, four on alternate tiles and halves of the rows (with two groups of 64 rows a
-// thread the two warps of a scheduler could not keep its pipes busy: 29 clocks a row
-// and warp, the sum of what each pipe needs); the last four the block keys first,
-// then the accumulators.
+// O; from 4 the softmax, four warps for 16 rows of a step; the last four or eight the
+// block keys first, then the accumulators.
 #include <math.h>
 
 #include "paged.cuh"
@@ -41,7 +42,8 @@ namespace {
 
 using namespace sbd_dev;
 
-constexpr int kTile = 128;                   // keys
+constexpr int kTile = 128;                   // keys of an MMA; a step is two tiles
+constexpr int kRT = 16;                      // rows of a softmax thread
 constexpr int kMaxStages = 8;
 constexpr int kBlkKeys = 32;                 // block keys, padded
 constexpr int kMaxSplits = 16;
@@ -220,28 +222,36 @@ struct Shape {
   // 128, so the pair costs less side by side, but then the softmax reads two columns
   // a row and adds them, and at R = 64 it sets the pace.
   static constexpr bool kBeside = R < 64;
-  static constexpr int kNS = kBeside ? 2 * R : R;      // columns of S
+  static constexpr int kNS = kBeside ? 2 * R : R;      // columns of a tile's S
   static constexpr int kNO = 2 * R;                    // columns of O, bytes of a key's row of P
-  // A softmax group of four warps takes every other tile, all rows or half of them.
-  static constexpr int kHalves = R > 16 ? 2 : 1;
-  static constexpr int kRT = R / kHalves;              // rows of a softmax thread
-  static constexpr int kSoftWarps = 8 * kHalves;
+  static constexpr int kOCol = 4 * kNS;                // S: two buffers of two tiles
+  static constexpr int kTmemCols = kOCol + 2 * kNO <= 256 ? 256 : 512;
+  // Four softmax warps take 16 rows of a step; all the rows of a step are the parts'
+  // together, and with few rows two sets of parts take alternate steps.
+  static constexpr int kParts = R / kRT;
+  static constexpr int kGroups = R < 64 ? 2 : 1;
+  static constexpr int kSoftWarps = 4 * kParts * kGroups;
   // Four warps hold the accumulators of 32 rows at most, a dimension a thread.
   static constexpr int kRA = R < 32 ? R : 32;
   static constexpr int kAccWarps = 4 * (R / kRA);
   static constexpr int kThreads = 32 * (4 + kSoftWarps + kAccWarps);
   static constexpr int kKV = kTile * D;                // a K or V tile
   static constexpr int kQ = 2 * R * D;
-  static constexpr int kP = kTile * 2 * R;
+  // P of a tile takes the place of its K, which is dead by then, where it fits.
+  static constexpr int kP = kTile * kNO;
+  static constexpr bool kPInK = kP <= kKV;
+  static constexpr int kPBlk = kBlkKeys * kNO;         // the block's P
   // The block's keys (hi rows, then lo rows), or its values (bf16, 64 dimensions
   // a sub-tile).
   static constexpr int kBlk = 2 * kBlkKeys * D;
   static constexpr int kBlkSub = kBlkKeys * 128;
-  static constexpr int kFixed = 1024 + kQ + 2 * kP + 2 * kBlk;
-  static constexpr int kLeft = 227 * 1024 - 15 * 1024 - kFixed;    // 15 KB: barriers and tables
+  static constexpr int kFixed = 1024 + kQ + (kPInK ? 0 : 4 * kP) + kPBlk + 2 * kBlk;
+  static constexpr int kLeft = 227 * 1024 - 12 * 1024 - kFixed;    // 12 KB: barriers and tables
   static constexpr int kStages = kLeft / (2 * kKV) < kMaxStages ? kLeft / (2 * kKV) : kMaxStages;
   static constexpr int kSmem = kFixed + kStages * 2 * kKV;
   static constexpr int kPStride = D + 4;               // floats of a partial row
+  static_assert(kStages >= 4, "two steps of two tiles");
+  static_assert(kPBlk % 1024 == 0, "operands begin on 1 KB");
   static_assert(R * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
   static_assert(kBlk + kTile * D <= 2 * kBlk + kStages * 2 * kKV, "reads past the block's keys stay inside");
 };
@@ -316,10 +326,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
   using C = Shape<D, R>;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
-  constexpr int kHalves = C::kHalves, RT = C::kRT, kSoftWarps = C::kSoftWarps;
+  constexpr int kParts = C::kParts, kGroups = C::kGroups, kSoftWarps = C::kSoftWarps;
   constexpr int RA = C::kRA, kAccWarps = C::kAccWarps;
-  constexpr uint32_t kTmemCols = 8 * R;                // two buffers of S and of O
-  constexpr uint32_t kOCol = 2 * kNS;
   static_assert(R == 16 || R == 32 || R == 64, "a key's row of P is one swizzle atom");
 
   extern __shared__ uint8_t smem_raw[];
@@ -328,25 +336,27 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
-  // a stage's page scales: of the keys; of the values over the tile's largest; that
+  // a stage's page scales: of the keys; of the values over their step's largest; that
   __shared__ float ks_sh[kMaxStages][8], vw_sh[kMaxStages][8], vref_sh[kMaxStages];
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
-  __shared__ __align__(16) float red_sh[2][2][4][R];   // maxima of a group's warps, two tiles
-  __shared__ __align__(16) float sum_sh[kSoftWarps][RT]; // a warp's sums of probabilities
-  __shared__ __align__(16) float mq_sh[kSoftWarps][RT]; // a warp's copy of the tile's maxima, negated
-  __shared__ float mt_sh[4][R], vr_sh[4];              // a tile's maxima and value reference
+  __shared__ __align__(16) float red_sh[kSoftWarps / 4][2][4][kRT];  // maxima of four warps, two steps
+  __shared__ __align__(16) float sum_sh[kSoftWarps][kRT];            // a warp's sums of probabilities
+  __shared__ __align__(16) float mq_sh[kSoftWarps][kRT];             // a warp's copy of the step's maxima, negated
+  __shared__ float mt_sh[4][R], vr_sh[4];              // a step's maxima and value reference
   __shared__ __align__(16) float f_sh[2][R], fa_sh[2][R];
   __shared__ int fmoved_sh[2][2];
-  __shared__ float lsum_sh[kSoftWarps][RT], mref_sh[2][R];
+  __shared__ float lsum_sh[kSoftWarps][kRT], mref_sh[kGroups][R];
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_s = sbase, p_s = q_s + C::kQ;
-  const uint32_t bk_s = p_s + 2 * C::kP, bv_s = bk_s + C::kBlk;
+  const uint32_t q_s = sbase, pblk_s = q_s + C::kQ, p_s = pblk_s + C::kPBlk;
+  const uint32_t bk_s = p_s + (C::kPInK ? 0 : 4 * C::kP), bv_s = bk_s + C::kBlk;
   const uint32_t ring = bv_s + C::kBlk;
   auto k_tile = [&](int j) { return ring + (uint32_t)(j % kStages) * 2 * C::kKV; };
   auto v_tile = [&](int j) { return k_tile(j) + C::kKV; };
+  // P of local tile j
+  auto p_tile = [&](int j) { return C::kPInK ? k_tile(j) : p_s + (uint32_t)(j & 3) * C::kP; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
@@ -357,9 +367,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&s_free[i], 4 * kHalves);
-      mbar_init(&p_full[i], 4 * kHalves);
-      mbar_init(&o_full[i], 1 + kHalves);    // the product, and the tile's maxima
+      mbar_init(&s_free[i], 4 * kParts);
+      mbar_init(&p_full[i], 4 * kParts);
+      mbar_init(&o_full[i], 1 + kParts);     // the product, and the step's maxima
       mbar_init(&o_free[i], kAccWarps);
     }
     mbar_init(&q_ready, kSoftWarps);
@@ -377,7 +387,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     __syncthreads();
   }
   const int b = a.order ? b_pick : (int)blockIdx.z;
-  if (warp == 1) tc_alloc(&tmem_base_sh, kTmemCols);
+  if (warp == 1) tc_alloc(&tmem_base_sh, C::kTmemCols);
   int len = a.lens[b];
   if (len < 0 || len > cap) {
     if (threadIdx.x == 0 && split == 0 && blockIdx.y == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
@@ -387,13 +397,12 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   const int n_tiles = n_cache + 1;
   const int t_begin = (int)((long long)split * n_tiles / a.splits);
   const int t_end = (int)((long long)(split + 1) * n_tiles / a.splits);
-  const int n = t_end - t_begin;             // tiles of this CTA
-  const bool has_block = t_end == n_tiles && n > 0;
-  // keys of local tile j (the block's tile comes last)
-  auto keys_of = [&](int j) {
-    const int t = t_begin + j;
-    return t < n_cache ? min(kTile, len - t * kTile) : a.k;
-  };
+  const bool has_block = t_end == n_tiles && t_end > t_begin;
+  // This CTA's cache tiles, two a step, and the block's keys as a last step.
+  const int nc = t_end - t_begin - (has_block ? 1 : 0);
+  const int n = (nc + 1) / 2 + (has_block ? 1 : 0);
+  // keys of local cache tile j
+  auto keys_of = [&](int j) { return max(0, min(kTile, j < nc ? len - (t_begin + j) * kTile : 0)); };
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -406,9 +415,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       tma_prefetch_desc(&tmap_v);
     }
     const int P = 1 << a.page_log2, per_tile = kTile >> a.page_log2;
-    const int n_mine = n - (has_block ? 1 : 0);
     const int p_first = t_begin * per_tile;
-    const int p_end = (int)((min((t_begin + n_mine) * (long long)kTile, (long long)len) + P - 1) >> a.page_log2);
+    const int p_end = (int)((min((t_begin + nc) * (long long)kTile, (long long)len) + P - 1) >> a.page_log2);
     const int32_t* table = a.table + (size_t)b * a.max_pages;
     // Pages come in windows of 32, one a lane: ids a window ahead, their scales a
     // tile into the window before.  A page out of range lies past the tensor's
@@ -427,7 +435,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     float ks = scale_at(a.ks, id), vs = scale_at(a.vs, id), ks_next = 0.f, vs_next = 0.f;
     const int per_window = 32 / per_tile;
     int issued = 0;
-    for (int j = 0; j < n_mine; ++j) {
+    for (int j = 0; j < nc; ++j) {
       const int w = j % per_window;
       if (w == 0 && j > 0) {
         id = id_next, ks = ks_next, vs = vs_next;
@@ -454,7 +462,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       issued = j + 1;
       const float k_sc = __shfl_sync(0xffffffffu, ks, src);
       const float v_sc = __shfl_sync(0xffffffffu, vs, src);
-      const float v_max = redux_max(lane < n_pg ? v_sc : 0.f);
+      // the largest value scale of the step's pages (lanes without a page have 0)
+      const int pair = (w & ~1) * per_tile;
+      const float v_max = redux_max(lane >= pair && lane < pair + 2 * per_tile ? vs : 0.f);
       if (lane < n_pg) {
         ks_sh[stage][lane] = k_sc;
         vw_sh[stage][lane] = v_max > 0.f ? v_sc / v_max : v_sc * 0.f;
@@ -477,38 +487,42 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
   } else if (warp == 1) {
     // ------------------------------------------------ S = K Q^T
-    // Two tiles ahead of the softmax group that reads it.  The whole warp runs the
-    // loop (descriptors stay in uniform registers) and one lane issues.
+    // Ahead of the softmax by the second buffer.  The whole warp runs the loop
+    // (descriptors stay in uniform registers) and one lane issues.
     const bool leader = elect_one();
     bool ok = n > 0 && mbar_wait(&q_ready, 0, a.err);
     const uint32_t id_s = idesc_f8(kTile, kNS, false);
     constexpr int kPasses = C::kBeside ? 1 : 2;        // hi codes, then lo codes
     const uint64_t qd = desc<D>(q_s);
-    for (int j = 0; j < n && ok; ++j) {
-      const bool blk = has_block && j == n - 1;
-      ok = mbar_wait(&s_free[j & 1], ((j >> 1) & 1) ^ 1, a.err) &&
-           (blk ? mbar_wait(&blk_ready, 0, a.err)
-                : mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err));
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)((j & 1) * kNS);
-      const uint64_t kd = desc<D>(blk ? bk_s : k_tile(j));
-      if (leader) {
+    auto product = [&](uint32_t d, uint64_t kd, bool add) {
 #pragma unroll
-        for (int h = 0; h < kPasses; ++h)
+      for (int h = 0; h < kPasses; ++h)
 #pragma unroll
-          for (int kk = 0; kk < D / 32; ++kk)
-            tc_mma_f8(d, kd + 2 * kk, qd + (h * R * D / 16 + 2 * kk), id_s, h > 0 || kk > 0);
-        if (blk) {                                     // the block keys' lo codes
-#pragma unroll
-          for (int h = 0; h < kPasses; ++h)
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-              tc_mma_f8(d, kd + (kBlkKeys * D / 16 + 2 * kk), qd + (h * R * D / 16 + 2 * kk), id_s, 1);
+        for (int kk = 0; kk < D / 32; ++kk)
+          tc_mma_f8(d, kd + 2 * kk, qd + (h * R * D / 16 + 2 * kk), id_s, add || h > 0 || kk > 0);
+    };
+    for (int i = 0; i < n && ok; ++i) {
+      const uint32_t d = tmem + (uint32_t)((i & 1) * 2 * kNS);
+      ok = mbar_wait(&s_free[i & 1], ((i >> 1) & 1) ^ 1, a.err);
+      if (has_block && i == n - 1) {
+        ok = ok && mbar_wait(&blk_ready, 0, a.err);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        if (leader) {                                  // the keys' hi codes, then their lo codes
+          product(d, desc<D>(bk_s), false);
+          product(d, desc<D>(bk_s + kBlkKeys * D), true);
         }
-        tc_commit(&s_full[j & 1]);
+      } else {
+        for (int j = 2 * i; j < min(nc, 2 * i + 2) && ok; ++j) {
+          ok = mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
+          ok = __all_sync(0xffffffffu, ok);
+          tc_fence_after();
+          if (leader && ok) product(d + (uint32_t)((j & 1) * kNS), desc<D>(k_tile(j)), false);
+        }
+        if (!ok) break;
       }
+      if (leader) tc_commit(&s_full[i & 1]);
       __syncwarp();
     }
   } else if (warp == 2) {
@@ -516,41 +530,40 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const bool leader = elect_one();
     bool ok = true;
     const uint32_t id_pv = idesc_f8(D, kNO, true);
-    for (int j = 0; j < n && ok; ++j) {
-      const bool blk = has_block && j == n - 1;
-      ok = mbar_wait(&o_free[j & 1], ((j >> 1) & 1) ^ 1, a.err) &&
-           mbar_wait(&p_full[j & 1], (j >> 1) & 1, a.err);
+    for (int i = 0; i < n && ok; ++i) {
+      ok = mbar_wait(&o_free[i & 1], ((i >> 1) & 1) ^ 1, a.err) &&
+           mbar_wait(&p_full[i & 1], (i >> 1) & 1, a.err);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t o = tmem + kOCol + (uint32_t)((j & 1) * kNO);
-      const uint64_t pd = desc<kNO>(p_s + (j & 1) * C::kP);
-      if (blk) {
-        const uint64_t vd = desc<128>(bv_s, C::kBlkSub);
+      const uint32_t o = tmem + C::kOCol + (uint32_t)((i & 1) * kNO);
+      if (has_block && i == n - 1) {
+        const uint64_t vd = desc<128>(bv_s, C::kBlkSub), pd = desc<kNO>(pblk_s);
         if (leader) {
 #pragma unroll
           for (int kk = 0; kk < kBlkKeys / 16; ++kk)
             tc_mma_bf16(o, vd + kk * 128, pd + kk * kNO, idesc_bf16_mn(D, R), kk > 0);
-          tc_commit(&o_full[j & 1]);
         }
       } else {
-        const uint64_t vd = desc<D>(v_tile(j));
-        const int steps = (keys_of(j) + 31) / 32;
-        if (leader) {
+        for (int j = 2 * i; j < min(nc, 2 * i + 2); ++j) {
+          const uint64_t vd = desc<D>(v_tile(j)), pd = desc<kNO>(p_tile(j));
+          const int steps = (keys_of(j) + 31) / 32;
+          if (leader) {
 #pragma unroll
-          for (int kk = 0; kk < kTile / 32; ++kk)
-            if (kk < steps) tc_mma_f8(o, vd + kk * 2 * D, pd + kk * 2 * kNO, id_pv, kk > 0);
-          tc_commit(&kv_empty[j % kStages]);
-          tc_commit(&o_full[j & 1]);
+            for (int kk = 0; kk < kTile / 32; ++kk)
+              if (kk < steps) tc_mma_f8(o, vd + kk * 2 * D, pd + kk * 2 * kNO, id_pv, (j & 1) || kk > 0);
+            tc_commit(&kv_empty[j % kStages]);
+          }
         }
       }
+      if (leader) tc_commit(&o_full[i & 1]);
       __syncwarp();
     }
   } else if (warp >= 4 && warp < 4 + kSoftWarps) {
     // ------------------------------------------------ softmax warps
-    const int sw = warp - 4, quad = warp & 3, grp = sw / (4 * kHalves);
-    const int r0 = sw / 4 % kHalves * RT;              // its rows: r0 .. r0 + RT - 1
-    const int key = quad * 32 + lane;                  // of every tile
+    const int sw = warp - 4, quad = warp & 3, grp = sw / (4 * kParts);
+    const int r0 = sw / 4 % kParts * kRT;              // its rows: r0 .. r0 + 15
+    const int key = quad * 32 + lane;                  // of both tiles
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     {
       constexpr int kRowsTurn = 32 * kSoftWarps / (D / 16);
@@ -563,7 +576,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         if (row < a.M) x.load(a.q + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + 16 * c);
         const float s = x.store(q_s, r, R + r, c);
         if (c == 0) {
-          c_sh[r] = s * a.scale_log2;
+          c_sh[r] = fmaxf(s * a.scale_log2, 1.17549435e-38f);   // > 0: masked scores stay -inf
           vis_sh[r] = i < a.n_causal ? i + 1 : a.k;
         }
       }
@@ -572,132 +585,143 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (lane == 0) mbar_arrive(&q_ready);
       bar_sync(5, 32 * kSoftWarps);                    // c and vis of all rows
     }
-    // A lane keeps the statistics of one row over its warp's keys: the running
-    // maximum (the same in the four warps of a group) and the sum of probabilities
-    // against it.  (RT = 16: two lanes a row.)
-    const int own = lane % RT;
+    // A lane keeps the statistics of one row (two lanes a row) over its warp's keys:
+    // the running maximum (the same in the four warps of a part) and the sum of
+    // probabilities against it.
+    const int own = lane % kRT;
     const float c_own = c_sh[r0 + own];
     float m_ref = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int j = grp; j < n; j += 2) {
-      const bool blk = has_block && j == n - 1;
-      const int stage = j % kStages, valid = keys_of(j);
-      const bool warp_has = quad * 32 < valid;
-      // the scales come with the stage, which stays until P is handed in
-      if (ok && !(blk ? mbar_wait(&blk_ready, 0, a.err) : mbar_wait(&kv_full[stage], (j / kStages) & 1, a.err)))
+    for (int i = grp; i < n; i += kGroups) {
+      const int buf = i & 1, phase = (i >> 1) & 1;
+      const bool blk = has_block && i == n - 1;
+      const int j0 = 2 * i, st0 = j0 % kStages, st1 = (j0 + 1) % kStages;
+      const int valid0 = blk ? a.k : keys_of(j0), valid1 = blk ? 0 : keys_of(j0 + 1);
+      const bool has0 = quad * 32 < valid0, has1 = quad * 32 < valid1;
+      // the scales come with the stages, which stay until P is handed in
+      if (ok && !(blk ? mbar_wait(&blk_ready, 0, a.err) : mbar_wait(&kv_full[st0], (j0 / kStages) & 1, a.err)))
         ok = false;
-      float z[RT];
-      float kf = 0.f, vw = 1.f, vref = 1.f;
+      if (ok && valid1 > 0 && !mbar_wait(&kv_full[st1], ((j0 + 1) / kStages) & 1, a.err)) ok = false;
+      float kf0 = 0.f, kf1 = 0.f, vw0 = 1.f, vw1 = 1.f, vref = 1.f;
       if (blk) {
-        kf = bks_sh[key & (kBlkKeys - 1)];
-      } else if (warp_has) {
-        kf = ks_sh[stage][key >> a.page_log2];
-        vw = vw_sh[stage][key >> a.page_log2];
-        vref = vref_sh[stage];
+        kf0 = bks_sh[key & (kBlkKeys - 1)];
+      } else {
+        const int pg = key >> a.page_log2;
+        if (has0) kf0 = ks_sh[st0][pg], vw0 = vw_sh[st0][pg];
+        if (has1) kf1 = ks_sh[st1][pg], vw1 = vw_sh[st1][pg];
+        vref = vref_sh[st0];
       }
-      if (ok && !mbar_wait(&s_full[grp], (j >> 1) & 1, a.err)) ok = false;
+      if (ok && !mbar_wait(&s_full[buf], phase, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
+      float z0[kRT], z1[kRT];
+#pragma unroll
+      for (int r = 0; r < kRT; ++r) z1[r] = -INFINITY;
       if (ok) {
         tc_fence_after();
-        if (warp_has) {
-          const uint32_t sa = tmem + lane_addr + (uint32_t)(grp * kNS + r0);
-          uint32_t h[RT / 16][16];
+        const uint32_t sa = tmem + lane_addr + (uint32_t)(buf * 2 * kNS + r0);
+        auto scores = [&](float (&z)[kRT], uint32_t col, float kf) {
+          uint32_t h[16], lo[16];
+          tc_ld16(col, h);
+          if constexpr (C::kBeside) tc_ld16(col + R, lo);
+          tc_wait_ld();
 #pragma unroll
-          for (int c = 0; c < RT / 16; ++c) tc_ld16(sa + 16 * c, h[c]);
-          if constexpr (C::kBeside) {
-            uint32_t lo[RT / 16][16];
-#pragma unroll
-            for (int c = 0; c < RT / 16; ++c) tc_ld16(sa + R + 16 * c, lo[c]);
-            tc_wait_ld();
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-              z[r] = (__uint_as_float(h[r / 16][r % 16]) + __uint_as_float(lo[r / 16][r % 16])) * kf;
-          } else {
-            tc_wait_ld();
-#pragma unroll
-            for (int r = 0; r < RT; ++r) z[r] = __uint_as_float(h[r / 16][r % 16]) * kf;
+          for (int r = 0; r < kRT; ++r) {
+            float x = __uint_as_float(h[r]);
+            if constexpr (C::kBeside) x += __uint_as_float(lo[r]);
+            z[r] = x * kf;
           }
+        };
+        if (has0) {
+          scores(z0, sa, kf0);
           if (blk) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-              if (key >= vis_sh[r0 + r]) z[r] = -INFINITY;
-          } else if (valid < quad * 32 + 32) {
-            const bool out = key >= valid;
+            for (int r = 0; r < kRT; ++r)
+              if (key >= vis_sh[r0 + r]) z0[r] = -INFINITY;
+          } else if (valid0 < quad * 32 + 32) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) z[r] = out ? -INFINITY : z[r];
+            for (int r = 0; r < kRT; ++r) z0[r] = key >= valid0 ? -INFINITY : z0[r];
+          }
+        }
+        if (has1) {
+          scores(z1, sa + kNS, kf1);
+          if (valid1 < quad * 32 + 32) {
+#pragma unroll
+            for (int r = 0; r < kRT; ++r) z1[r] = key >= valid1 ? -INFINITY : z1[r];
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s_free[grp]);
+        if (lane == 0) mbar_arrive(&s_free[buf]);
         // NaN propagates: a row with one has NaN statistics from here on
-        if (warp_has) {
+        if (has0) {
 #pragma unroll
-          for (int r = 0; r < RT; r += 4)
-            st_shared_v4_if(lane == 0, smem_u32(&red_sh[grp][(j >> 1) & 1][quad][r0 + r]),
-                            redux_max_nan(z[r]), redux_max_nan(z[r + 1]), redux_max_nan(z[r + 2]),
-                            redux_max_nan(z[r + 3]));
+          for (int r = 0; r < kRT; r += 4)
+            st_shared_v4_if(lane == 0, smem_u32(&red_sh[sw / 4][(i / kGroups) & 1][quad][r]),
+                            redux_max_nan(max_nan(z0[r], z1[r])), redux_max_nan(max_nan(z0[r + 1], z1[r + 1])),
+                            redux_max_nan(max_nan(z0[r + 2], z1[r + 2])),
+                            redux_max_nan(max_nan(z0[r + 3], z1[r + 3])));
         } else {
-          red_sh[grp][(j >> 1) & 1][quad][r0 + own] = -INFINITY;
+          red_sh[sw / 4][(i / kGroups) & 1][quad][own] = -INFINITY;
         }
       }
       bar_sync(1 + sw / 4, 128);
-      const float(*x)[R] = red_sh[grp][(j >> 1) & 1];
-      const float my = max_nan(max_nan(x[0][r0 + own], x[1][r0 + own]), max_nan(x[2][r0 + own], x[3][r0 + own])) *
-                       c_own;                          // c > 0
+      const float(*x)[kRT] = red_sh[sw / 4][(i / kGroups) & 1];
+      const float my = max_nan(max_nan(x[0][own], x[1][own]), max_nan(x[2][own], x[3][own])) * c_own;   // c > 0
       mq_sh[sw][own] = my == -INFINITY ? 0.f : -my;
       __syncwarp();
-      // the P buffer is free once the product before last is done
-      if (ok && !mbar_wait(&o_full[grp], ((j >> 1) & 1) ^ 1, a.err)) ok = false;
+      // The phase of this buffer's last product is over (and so are the accumulators
+      // with the maxima of four steps ago, and the product with its P).
+      if (ok && !mbar_wait(&o_full[buf], phase ^ 1, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) continue;
-      // (and then the accumulators are done with the maxima of four tiles ago)
       if (quad == 0) {
-        mt_sh[j & 3][r0 + own] = my;
-        if (lane == 0 && r0 == 0) vr_sh[j & 3] = vref;
+        mt_sh[i & 3][r0 + own] = my;
+        if (lane == 0 && r0 == 0) vr_sh[i & 3] = vref;
         __syncwarp();
-        if (lane == 0) mbar_arrive(&o_full[grp]);
+        if (lane == 0) mbar_arrive(&o_full[buf]);
       }
-      if (warp_has) {
-        const uint32_t pb = p_s + grp * C::kP;
-        const __half2 vw2 = __float2half2_rn(vw);
-        auto probs = [&](int r, float (&p)[4]) {
-          const float4 cc = *reinterpret_cast<const float4*>(&c_sh[r0 + r]);
-          const float4 mq = *reinterpret_cast<const float4*>(&mq_sh[sw][r]);
-          p[0] = ex2_ftz(fmaf(z[r], cc.x, mq.x));
-          p[1] = ex2_ftz(fmaf(z[r + 1], cc.y, mq.y));
-          p[2] = ex2_ftz(fmaf(z[r + 2], cc.z, mq.z));
-          p[3] = ex2_ftz(fmaf(z[r + 3], cc.w, mq.w));
-          // Sums over the warp's keys in fixed point: the pattern of 1 + p counts p in
-          // steps of 2^-23, 32 of them stay below 2^28 (modulo the patterns of 1).
+      if (has0) {
+        // p of four rows, and their sums over the warp's keys in fixed point: the
+        // pattern of 1 + x counts x in steps of 2^-23, 32 of them stay below 2^28
+        // (modulo the patterns of 1).
+        auto probs = [&](int r, float (&p)[4], float (&q)[4]) {
+          const float4 c4 = *reinterpret_cast<const float4*>(&c_sh[r0 + r]);
+          const float4 m4 = *reinterpret_cast<const float4*>(&mq_sh[sw][r]);
+          const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, mq[4] = {m4.x, m4.y, m4.z, m4.w};
           uint32_t n1[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) n1[i] = __reduce_add_sync(0xffffffffu, __float_as_uint(p[i] + 1.f));
+          for (int e = 0; e < 4; ++e) {
+            p[e] = ex2_ftz(fmaf(z0[r + e], cc[e], mq[e]));
+            q[e] = ex2_ftz(fmaf(z1[r + e], cc[e], mq[e]));
+            n1[e] = __reduce_add_sync(0xffffffffu, __float_as_uint(fmaf(p[e] + q[e], 0.5f, 1.f)));
+          }
           st_shared_v4_if(lane == 0, smem_u32(&sum_sh[sw][r]), __uint_as_float(n1[0]),
                           __uint_as_float(n1[1]), __uint_as_float(n1[2]), __uint_as_float(n1[3]));
         };
         if (!blk) {
+          const __half2 w0 = __float2half2_rn(vw0), w1 = __float2half2_rn(vw1);
+          uint32_t hi0[4], lo0[4], hi1[4], lo1[4];
 #pragma unroll
-          for (int c = 0; c < RT / 16; ++c) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float p[4];
-              probs(16 * c + 4 * e, p);
-              const __half2 a2 = __hmul2(__floats2half2_rn(p[0], p[1]), vw2);
-              const __half2 b2 = __hmul2(__floats2half2_rn(p[2], p[3]), vw2);
-              p_codes(a2, b2, &hi[e], &lo[e]);
-            }
-            st_shared_v4(swz<kNO>(pb, key, r0 / 16 + c), make_uint4(hi[0], hi[1], hi[2], hi[3]));
-            st_shared_v4(swz<kNO>(pb, key, (R + r0) / 16 + c), make_uint4(lo[0], lo[1], lo[2], lo[3]));
+          for (int e = 0; e < 4; ++e) {
+            float p[4], q[4];
+            probs(4 * e, p, q);
+            p_codes(__hmul2(__floats2half2_rn(p[0], p[1]), w0), __hmul2(__floats2half2_rn(p[2], p[3]), w0), &hi0[e], &lo0[e]);
+            p_codes(__hmul2(__floats2half2_rn(q[0], q[1]), w1), __hmul2(__floats2half2_rn(q[2], q[3]), w1), &hi1[e], &lo1[e]);
+          }
+          const uint32_t p0 = p_tile(j0), p1 = p_tile(j0 + 1);
+          st_shared_v4(swz<kNO>(p0, key, r0 / 16), make_uint4(hi0[0], hi0[1], hi0[2], hi0[3]));
+          st_shared_v4(swz<kNO>(p0, key, (R + r0) / 16), make_uint4(lo0[0], lo0[1], lo0[2], lo0[3]));
+          if (has1) {
+            st_shared_v4(swz<kNO>(p1, key, r0 / 16), make_uint4(hi1[0], hi1[1], hi1[2], hi1[3]));
+            st_shared_v4(swz<kNO>(p1, key, (R + r0) / 16), make_uint4(lo1[0], lo1[1], lo1[2], lo1[3]));
           }
         } else {
 #pragma unroll
-          for (int r = 0; r < RT; r += 8) {
-            float p[4], q[4];
-            probs(r, p);
-            probs(r + 4, q);
-            st_shared_v4(swz<kNO>(pb, key, (r0 + r) / 8),
+          for (int r = 0; r < kRT; r += 8) {
+            float p[4], q[4], zero[4];
+            probs(r, p, zero);
+            probs(r + 4, q, zero);
+            st_shared_v4(swz<kNO>(pblk_s, key, (r0 + r) / 8),
                          make_uint4(pack_bf16(p[0] * kPScale, p[1] * kPScale), pack_bf16(p[2] * kPScale, p[3] * kPScale),
                                     pack_bf16(q[0] * kPScale, q[1] * kPScale), pack_bf16(q[2] * kPScale, q[3] * kPScale)));
           }
@@ -705,11 +729,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[grp]);
+      if (lane == 0) mbar_arrive(&p_full[buf]);
       const float m_new = max_nan(m_ref, my);
       const float keep = m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - m_new);
       const uint32_t steps = __float_as_uint(sum_sh[sw][own]) - 32u * 0x3f800000u;
-      const float add = warp_has ? (float)steps * (1.f / (1 << 23)) : 0.f;
+      const float add = has0 ? (float)steps * (1.f / (1 << 22)) : 0.f;
       l = fmaf(l, keep, my == -INFINITY ? 0.f : add * ex2_ftz(my - m_new));
       m_ref = m_new;
     }
@@ -788,7 +812,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           acc[r] *= x.x, acc[r + 1] *= x.y, acc[r + 2] *= x.z, acc[r + 3] *= x.w;
         }
       }
-      const uint32_t oa = tmem + lane_addr + kOCol + (uint32_t)(buf * kNO + ra);
+      const uint32_t oa = tmem + lane_addr + C::kOCol + (uint32_t)(buf * kNO + ra);
 #pragma unroll
       for (int c = 0; c < RA / 16; ++c) {
         uint32_t h[16], lo[16];
@@ -816,13 +840,13 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     bar_sync(6, 32 * (kSoftWarps + kAccWarps));
     // ------------------------------------------------ epilogue
     if (keeps) {
-      const int r = ra + mine, i = r % RT;
+      const int r = ra + mine, i = r % kRT;
       float sum = 0.f;
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
+      for (int g = 0; g < kGroups; ++g) {
         const float m = mref_sh[g][r];
-        if (m == -INFINITY) continue;                  // no tile
-        const float(*lw)[RT] = lsum_sh + 4 * (g * kHalves + r / RT);
+        if (m == -INFINITY) continue;                  // no step
+        const float(*lw)[kRT] = lsum_sh + 4 * (g * kParts + r / kRT);
         sum += ((lw[0][i] + lw[1][i]) + (lw[2][i] + lw[3][i])) * ex2_ftz(m - m_run);
       }
       f_sh[0][r] = n > 0 ? 1.f / sum : 0.f;
@@ -875,7 +899,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tc_dealloc(tmem, kTmemCols);
+    tc_dealloc(tmem, C::kTmemCols);
   }
   if (a.splits == 1) return;
   // ------------------------------------------------ merge in the cluster
