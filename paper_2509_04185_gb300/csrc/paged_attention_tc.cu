@@ -23,17 +23,17 @@
 // P.  Probabilities span more octaves than two codes: next to a key that takes all
 // the weight, a thousand weak ones would vanish.  So P is relative to the maximum
 // of its own step (times the value scale over the step's largest, and 2^8), every
-// step's product starts at zero, and four or eight warps add it to fp32 accumulators
-// in registers, weighted 2^(m_step - m).  No accumulator in tensor memory is ever
-// rescaled, and the softmax never waits for one.
+// step's product starts at zero, and the softmax warps add the product of the step
+// before to fp32 accumulators in registers (16 rows, a dimension a thread), weighted
+// 2^(m_step - m).  No accumulator in tensor memory is ever rescaled, and no warp
+// waits for a product that has just been asked for.
 //
 // Block keys (not cached, bf16) form the last step: the keys split into code pairs
 // like the rows, two products for S; the values as they are against P in bf16
 // (kind::f16), since a row may see a single small value of a key.
 //
 // Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
-// O; from 4 the softmax, four warps for 16 rows of a step; the last four or eight the
-// block keys first, then the accumulators.
+// O; from 3 the softmax and the accumulators, four warps for 16 rows of a step.
 #include <math.h>
 
 #include "paged.cuh"
@@ -44,6 +44,7 @@ using namespace sbd_dev;
 
 constexpr int kTile = 128;                   // keys of an MMA; a step is two tiles
 constexpr int kRT = 16;                      // rows of a softmax thread
+constexpr int kControl = 3;                  // warps: pages and TMA, products S, products O
 constexpr int kMaxStages = 8;
 constexpr int kBlkKeys = 32;                 // block keys, padded
 constexpr int kMaxSplits = 16;
@@ -105,6 +106,12 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
         "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
+}
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+                 "=r"(r[7])
+               : "r"(taddr));
 }
 __device__ __forceinline__ void tc_wait_ld() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -231,10 +238,7 @@ struct Shape {
   static constexpr int kParts = R / kRT;
   static constexpr int kGroups = R < 64 ? 2 : 1;
   static constexpr int kSoftWarps = 4 * kParts * kGroups;
-  // Four warps hold the accumulators of 32 rows at most, a dimension a thread.
-  static constexpr int kRA = R < 32 ? R : 32;
-  static constexpr int kAccWarps = 4 * (R / kRA);
-  static constexpr int kThreads = 32 * (4 + kSoftWarps + kAccWarps);
+  static constexpr int kThreads = 32 * (kControl + kSoftWarps);
   static constexpr int kKV = kTile * D;                // a K or V tile
   static constexpr int kQ = 2 * R * D;
   // P of a tile takes the place of its K, which is dead by then, where it fits.
@@ -327,12 +331,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   using C = Shape<D, R>;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
   constexpr int kParts = C::kParts, kGroups = C::kGroups, kSoftWarps = C::kSoftWarps;
-  constexpr int RA = C::kRA, kAccWarps = C::kAccWarps;
   static_assert(R == 16 || R == 32 || R == 64, "a key's row of P is one swizzle atom");
 
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
-  __shared__ __align__(8) uint64_t s_full[2], s_free[2], p_full[2], o_full[2], o_free[2];
+  __shared__ __align__(8) uint64_t s_full[2], s_free[2], p_full[4], o_full[2], o_free[2];
   __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
@@ -344,10 +347,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(16) float red_sh[kSoftWarps / 4][2][4][kRT];  // maxima of four warps, two steps
   __shared__ __align__(16) float sum_sh[kSoftWarps][kRT];            // a warp's sums of probabilities
   __shared__ __align__(16) float mq_sh[kSoftWarps][kRT];             // a warp's copy of the step's maxima, negated
-  __shared__ float mt_sh[4][R], vr_sh[4];              // a step's maxima and value reference
-  __shared__ __align__(16) float f_sh[2][R], fa_sh[2][R];
-  __shared__ int fmoved_sh[2][2];
-  __shared__ float lsum_sh[kSoftWarps][kRT], mref_sh[kGroups][R];
+  __shared__ __align__(16) float f_sh[kSoftWarps][2][kRT];           // its rows' weights: of a step's product, of what was before
+  __shared__ float lsum_sh[kSoftWarps][kRT], mref_sh[kGroups][R], lse_sh[R];
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_s = sbase, pblk_s = q_s + C::kQ, p_s = pblk_s + C::kPBlk;
@@ -366,14 +367,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       mbar_init(&kv_empty[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&s_full[i], 1);
+      mbar_init(&s_full[i], 2);              // the product, and its issuer's view of the scales
       mbar_init(&s_free[i], 4 * kParts);
-      mbar_init(&p_full[i], 4 * kParts);
-      mbar_init(&o_full[i], 1 + kParts);     // the product, and the step's maxima
-      mbar_init(&o_free[i], kAccWarps);
+      mbar_init(&o_full[i], 1);
+      mbar_init(&o_free[i], 4 * kParts);
     }
+    for (int i = 0; i < 4; ++i) mbar_init(&p_full[i], 4 * kParts);
     mbar_init(&q_ready, kSoftWarps);
-    mbar_init(&blk_ready, kAccWarps);
+    mbar_init(&blk_ready, kSoftWarps);
     mbar_init(&tail_bar, 1);
     blk_bad = 0;
     fence_mbar_init();
@@ -522,7 +523,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         }
         if (!ok) break;
       }
-      if (leader) tc_commit(&s_full[i & 1]);
+      if (leader) {
+        tc_commit(&s_full[i & 1]);
+        mbar_arrive(&s_full[i & 1]);
+      }
       __syncwarp();
     }
   } else if (warp == 2) {
@@ -532,7 +536,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const uint32_t id_pv = idesc_f8(D, kNO, true);
     for (int i = 0; i < n && ok; ++i) {
       ok = mbar_wait(&o_free[i & 1], ((i >> 1) & 1) ^ 1, a.err) &&
-           mbar_wait(&p_full[i & 1], (i >> 1) & 1, a.err);
+           mbar_wait(&p_full[i & 3], (i >> 2) & 1, a.err);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -559,17 +563,18 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (leader) tc_commit(&o_full[i & 1]);
       __syncwarp();
     }
-  } else if (warp >= 4 && warp < 4 + kSoftWarps) {
-    // ------------------------------------------------ softmax warps
-    const int sw = warp - 4, quad = warp & 3, grp = sw / (4 * kParts);
+  } else {
+    // ------------------------------------------------ softmax and accumulators
+    const int sw = warp - kControl, quad = warp & 3, grp = sw / (4 * kParts);
     const int r0 = sw / 4 % kParts * kRT;              // its rows: r0 .. r0 + 15
     const int key = quad * 32 + lane;                  // of both tiles
+    const int at = sw * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    constexpr int kRowsTurn = 32 * kSoftWarps / (D / 16);
     {
-      constexpr int kRowsTurn = 32 * kSoftWarps / (D / 16);
-      const int t = sw * 32 + lane, c = t % (D / 16);
+      const int c = at % (D / 16);
 #pragma unroll 1
-      for (int r = t / (D / 16); r < R; r += kRowsTurn) {
+      for (int r = at / (D / 16); r < R; r += kRowsTurn) {
         const int row = chunk * R + r, i = row / a.G;
         Piece<D> x;
         x.zero();
@@ -585,68 +590,144 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (lane == 0) mbar_arrive(&q_ready);
       bar_sync(5, 32 * kSoftWarps);                    // c and vis of all rows
     }
+    if (has_block) {
+      const int c = at % (D / 16);
+      bool bad = false;
+#pragma unroll 1
+      for (int key = at / (D / 16); key < kBlkKeys; key += kRowsTurn) {
+        Piece<D> x, y;
+        x.zero(), y.zero();
+        if (key < a.k) {
+          const size_t off = (((size_t)b * a.k + key) * a.Hkv + hkv) * D + 16 * c;
+          x.load(a.kb + off);
+          y.load(a.vb + off);
+        }
+        const float s = x.store(bk_s, key, kBlkKeys + key, c);
+        if (c == 0) bks_sh[key] = s;
+        // Values that are not finite stay out of the product (a row that does not
+        // see them would multiply them by 0) and are added at the end.
+        auto finite2 = [&](uint32_t w) {
+          const bool lo_bad = (w & 0x7f80u) == 0x7f80u, hi_bad = (w & 0x7f800000u) == 0x7f800000u;
+          bad |= lo_bad || hi_bad;
+          return (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
+        };
+#pragma unroll
+        for (int e = 0; e < 2; ++e)                    // 8 dimensions each
+          st_shared_v4(swz<128>(bv_s + (2 * c + e) / 8 * C::kBlkSub, key, (2 * c + e) % 8),
+                       make_uint4(finite2(y.w[e].x), finite2(y.w[e].y), finite2(y.w[e].z), finite2(y.w[e].w)));
+      }
+      if (bad) blk_bad = 1;
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&blk_ready);
+    }
     // A lane keeps the statistics of one row (two lanes a row) over its warp's keys:
     // the running maximum (the same in the four warps of a part) and the sum of
-    // probabilities against it.
+    // probabilities against it.  A thread also keeps the accumulators of its warp's
+    // rows for one dimension, against the same maximum.
     const int own = lane % kRT;
     const float c_own = c_sh[r0 + own];
     float m_ref = -INFINITY, l = 0.f;
-    bool ok = true;
+    float acc[kRT];
+#pragma unroll
+    for (int r = 0; r < kRT; ++r) acc[r] = 0.f;
+    bool ok = true, moved = false;
+    // Adds the product of step i, whose weights f_sh holds.
+    auto add_product = [&](int i) {
+      if (ok && !mbar_wait(&o_full[i & 1], (i >> 1) & 1, a.err)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t oa = tmem + lane_addr + C::kOCol + (uint32_t)((i & 1) * kNO + r0);
+      const bool blk = has_block && i == n - 1;
+      if (moved) {
+#pragma unroll
+        for (int r = 0; r < kRT; r += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(&f_sh[sw][1][r]);
+          acc[r] *= x.x, acc[r + 1] *= x.y, acc[r + 2] *= x.z, acc[r + 3] *= x.w;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < kRT; c += 8) {
+        uint32_t h[8], lo[8];
+        tc_ld8(oa + c, h);
+        tc_ld8(oa + R + c, lo);
+        tc_wait_ld();
+        if (blk) {                                     // the block's product has no lo columns
+#pragma unroll
+          for (int e = 0; e < 8; ++e) lo[e] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const float4 f4 = *reinterpret_cast<const float4*>(&f_sh[sw][0][c + e]);
+          const float f[4] = {f4.x, f4.y, f4.z, f4.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            acc[c + e + q] = fmaf(fmaf(__uint_as_float(lo[e + q]), 1.f / kLoScale, __uint_as_float(h[e + q])), f[q],
+                                  acc[c + e + q]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free[i & 1]);
+    };
     for (int i = grp; i < n; i += kGroups) {
       const int buf = i & 1, phase = (i >> 1) & 1;
       const bool blk = has_block && i == n - 1;
       const int j0 = 2 * i, st0 = j0 % kStages, st1 = (j0 + 1) % kStages;
       const int valid0 = blk ? a.k : keys_of(j0), valid1 = blk ? 0 : keys_of(j0 + 1);
       const bool has0 = quad * 32 < valid0, has1 = quad * 32 < valid1;
-      // the scales come with the stages, which stay until P is handed in
-      if (ok && !(blk ? mbar_wait(&blk_ready, 0, a.err) : mbar_wait(&kv_full[st0], (j0 / kStages) & 1, a.err)))
-        ok = false;
-      if (ok && valid1 > 0 && !mbar_wait(&kv_full[st1], ((j0 + 1) / kStages) & 1, a.err)) ok = false;
-      float kf0 = 0.f, kf1 = 0.f, vw0 = 1.f, vw1 = 1.f, vref = 1.f;
-      if (blk) {
-        kf0 = bks_sh[key & (kBlkKeys - 1)];
-      } else {
-        const int pg = key >> a.page_log2;
-        if (has0) kf0 = ks_sh[st0][pg], vw0 = vw_sh[st0][pg];
-        if (has1) kf1 = ks_sh[st1][pg], vw1 = vw_sh[st1][pg];
-        vref = vref_sh[st0];
-      }
       if (ok && !mbar_wait(&s_full[buf], phase, a.err)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       float z0[kRT], z1[kRT];
-#pragma unroll
-      for (int r = 0; r < kRT; ++r) z1[r] = -INFINITY;
+      float vw0 = 1.f, vw1 = 1.f, vref = 1.f;
       if (ok) {
         tc_fence_after();
-        const uint32_t sa = tmem + lane_addr + (uint32_t)(buf * 2 * kNS + r0);
-        auto scores = [&](float (&z)[kRT], uint32_t col, float kf) {
-          uint32_t h[16], lo[16];
-          tc_ld16(col, h);
-          if constexpr (C::kBeside) tc_ld16(col + R, lo);
-          tc_wait_ld();
-#pragma unroll
-          for (int r = 0; r < kRT; ++r) {
-            float x = __uint_as_float(h[r]);
-            if constexpr (C::kBeside) x += __uint_as_float(lo[r]);
-            z[r] = x * kf;
-          }
-        };
         if (has0) {
-          scores(z0, sa, kf0);
+          // (the scales come with the stages, which stay until P is handed in)
+          float kf0 = 0.f, kf1 = 0.f;
+          if (blk) {
+            kf0 = bks_sh[key & (kBlkKeys - 1)];
+          } else {
+            const int pg = key >> a.page_log2;
+            kf0 = ks_sh[st0][pg], vw0 = vw_sh[st0][pg], vref = vref_sh[st0];
+            if (has1) kf1 = ks_sh[st1][pg], vw1 = vw_sh[st1][pg];
+          }
+          // Both tiles' columns are read, also where the second has no keys.
+          const uint32_t sa = tmem + lane_addr + (uint32_t)(buf * 2 * kNS + r0);
+          if constexpr (C::kBeside) {
+            uint32_t h[16], lo[16];
+            tc_ld16(sa, h);
+            tc_ld16(sa + R, lo);
+            tc_wait_ld();
+#pragma unroll
+            for (int r = 0; r < kRT; ++r) z0[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf0;
+            tc_ld16(sa + kNS, h);
+            tc_ld16(sa + kNS + R, lo);
+            tc_wait_ld();
+#pragma unroll
+            for (int r = 0; r < kRT; ++r) z1[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf1;
+          } else {
+            uint32_t h0[16], h1[16];
+            tc_ld16(sa, h0);
+            tc_ld16(sa + kNS, h1);
+            tc_wait_ld();
+#pragma unroll
+            for (int r = 0; r < kRT; ++r) {
+              z0[r] = __uint_as_float(h0[r]) * kf0;
+              z1[r] = __uint_as_float(h1[r]) * kf1;
+            }
+          }
           if (blk) {
 #pragma unroll
-            for (int r = 0; r < kRT; ++r)
-              if (key >= vis_sh[r0 + r]) z0[r] = -INFINITY;
+            for (int r = 0; r < kRT; ++r) z0[r] = key < vis_sh[r0 + r] ? z0[r] : -INFINITY;
           } else if (valid0 < quad * 32 + 32) {
 #pragma unroll
-            for (int r = 0; r < kRT; ++r) z0[r] = key >= valid0 ? -INFINITY : z0[r];
+            for (int r = 0; r < kRT; ++r) z0[r] = key < valid0 ? z0[r] : -INFINITY;
           }
-        }
-        if (has1) {
-          scores(z1, sa + kNS, kf1);
           if (valid1 < quad * 32 + 32) {
 #pragma unroll
-            for (int r = 0; r < kRT; ++r) z1[r] = key >= valid1 ? -INFINITY : z1[r];
+            for (int r = 0; r < kRT; ++r) z1[r] = key < valid1 ? z1[r] : -INFINITY;
           }
         }
         tc_fence_before();
@@ -665,21 +746,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         }
       }
       bar_sync(1 + sw / 4, 128);
+      if (!ok) continue;
       const float(*x)[kRT] = red_sh[sw / 4][(i / kGroups) & 1];
       const float my = max_nan(max_nan(x[0][own], x[1][own]), max_nan(x[2][own], x[3][own])) * c_own;   // c > 0
       mq_sh[sw][own] = my == -INFINITY ? 0.f : -my;
       __syncwarp();
-      // The phase of this buffer's last product is over (and so are the accumulators
-      // with the maxima of four steps ago, and the product with its P).
-      if (ok && !mbar_wait(&o_full[buf], phase ^ 1, a.err)) ok = false;
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) continue;
-      if (quad == 0) {
-        mt_sh[i & 3][r0 + own] = my;
-        if (lane == 0 && r0 == 0) vr_sh[i & 3] = vref;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&o_full[buf]);
-      }
       if (has0) {
         // p of four rows, and their sums over the warp's keys in fixed point: the
         // pattern of 1 + x counts x in steps of 2^-23, 32 of them stay below 2^28
@@ -729,150 +800,70 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[buf]);
+      if (lane == 0) mbar_arrive(&p_full[i & 3]);
+      // The step before's product, done by now.  (A warp is past it before it hands
+      // in its next P but one, so no phase of p_full is ever two behind.)
+      if (i >= kGroups) add_product(i - kGroups);
       const float m_new = max_nan(m_ref, my);
       const float keep = m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - m_new);
+      const float g = my == -INFINITY ? 0.f : ex2_ftz(my - m_new);
       const uint32_t steps = __float_as_uint(sum_sh[sw][own]) - 32u * 0x3f800000u;
-      const float add = has0 ? (float)steps * (1.f / (1 << 22)) : 0.f;
-      l = fmaf(l, keep, my == -INFINITY ? 0.f : add * ex2_ftz(my - m_new));
+      l = fmaf(l, keep, has0 ? (float)steps * (1.f / (1 << 22)) * g : 0.f);
+      __syncwarp();                                    // f of the step before is read
+      if (!has0) vref = blk ? 1.f : vref_sh[st0];
+      f_sh[sw][0][own] = g * vref * (1.f / kPScale);
+      f_sh[sw][1][own] = keep;
+      moved = __any_sync(0xffffffffu, m_new != m_ref && m_ref != -INFINITY);
       m_ref = m_new;
+      __syncwarp();
     }
+    if (n > grp) add_product(n - 1 - (n - 1 - grp) % kGroups);
     grid_dependents_launch();
+    // ------------------------------------------------ epilogue
     lsum_sh[sw][own] = l;
     if (quad == 0) mref_sh[grp][r0 + own] = m_ref;
-    bar_sync(6, 32 * (kSoftWarps + kAccWarps));
-  } else if (warp >= 4 + kSoftWarps) {
-    // ------------------------------------------------ block keys, accumulators
-    const int aw = warp - 4 - kSoftWarps, quad = warp & 3;
-    const int at = aw * 32 + lane;
-    const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
-    if (has_block) {
-      constexpr int kRowsTurn = 32 * kAccWarps / (D / 16);
-      const int c = at % (D / 16);
-      bool bad = false;
-#pragma unroll 1
-      for (int key = at / (D / 16); key < kBlkKeys; key += kRowsTurn) {
-        Piece<D> x, y;
-        x.zero(), y.zero();
-        if (key < a.k) {
-          const size_t off = (((size_t)b * a.k + key) * a.Hkv + hkv) * D + 16 * c;
-          x.load(a.kb + off);
-          y.load(a.vb + off);
-        }
-        const float s = x.store(bk_s, key, kBlkKeys + key, c);
-        if (c == 0) bks_sh[key] = s;
-        // Values that are not finite stay out of the product (a row that does not
-        // see them would multiply them by 0) and are added at the end.
-        auto finite2 = [&](uint32_t w) {
-          const bool lo_bad = (w & 0x7f80u) == 0x7f80u, hi_bad = (w & 0x7f800000u) == 0x7f800000u;
-          bad |= lo_bad || hi_bad;
-          return (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
-        };
-#pragma unroll
-        for (int e = 0; e < 2; ++e)                    // 8 dimensions each
-          st_shared_v4(swz<128>(bv_s + (2 * c + e) / 8 * C::kBlkSub, key, (2 * c + e) % 8),
-                       make_uint4(finite2(y.w[e].x), finite2(y.w[e].y), finite2(y.w[e].z), finite2(y.w[e].w)));
-      }
-      if (bad) blk_bad = 1;
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&blk_ready);
-    }
-    const int ra = aw / 4 * RA, mine = at % 128;       // rows ra .. ra + RA - 1; thread `mine` keeps one's maximum
-    const bool keeps = mine < RA;
-    float acc[RA];                                     // of one dimension, against m_run
-#pragma unroll
-    for (int r = 0; r < RA; ++r) acc[r] = 0.f;
-    float m_run = -INFINITY;                           // of row ra + mine
-    bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      const int buf = j & 1;
-      const bool blk = has_block && j == n - 1;
-      if (ok && !mbar_wait(&o_full[buf], (j >> 1) & 1, a.err)) ok = false;
-      ok = __all_sync(0xffffffffu, ok);
-      bool moved = false;
-      if (ok && keeps) {
-        const float mt = mt_sh[j & 3][ra + mine], m_new = max_nan(m_run, mt);
-        f_sh[buf][ra + mine] = mt == -INFINITY ? 0.f : ex2_ftz(mt - m_new) * vr_sh[j & 3] * (1.f / kPScale);
-        fa_sh[buf][ra + mine] = m_run == -INFINITY ? 1.f : ex2_ftz(m_run - m_new);
-        moved = m_run != -INFINITY && m_new != m_run;
-        m_run = m_new;
-      }
-      if (aw % 4 == 0) {
-        const uint32_t any = __ballot_sync(0xffffffffu, moved);
-        if (lane == 0) fmoved_sh[buf][aw / 4] = any != 0;
-      }
-      bar_sync(7 + aw / 4, 128);
-      if (!ok) continue;
-      tc_fence_after();
-      if (fmoved_sh[buf][aw / 4]) {
-#pragma unroll
-        for (int r = 0; r < RA; r += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(&fa_sh[buf][ra + r]);
-          acc[r] *= x.x, acc[r + 1] *= x.y, acc[r + 2] *= x.z, acc[r + 3] *= x.w;
-        }
-      }
-      const uint32_t oa = tmem + lane_addr + C::kOCol + (uint32_t)(buf * kNO + ra);
-#pragma unroll
-      for (int c = 0; c < RA / 16; ++c) {
-        uint32_t h[16], lo[16];
-        tc_ld16(oa + 16 * c, h);
-        tc_ld16(oa + R + 16 * c, lo);
-        tc_wait_ld();
-        if (!blk) {                                    // the block's product has no lo columns
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            h[e] = __float_as_uint(fmaf(__uint_as_float(lo[e]), 1.f / kLoScale, __uint_as_float(h[e])));
-        }
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(&f_sh[buf][ra + 16 * c + e]);
-          acc[16 * c + e] = fmaf(__uint_as_float(h[e]), f.x, acc[16 * c + e]);
-          acc[16 * c + e + 1] = fmaf(__uint_as_float(h[e + 1]), f.y, acc[16 * c + e + 1]);
-          acc[16 * c + e + 2] = fmaf(__uint_as_float(h[e + 2]), f.z, acc[16 * c + e + 2]);
-          acc[16 * c + e + 3] = fmaf(__uint_as_float(h[e + 3]), f.w, acc[16 * c + e + 3]);
-        }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&o_free[buf]);
-    }
-    bar_sync(6, 32 * (kSoftWarps + kAccWarps));
-    // ------------------------------------------------ epilogue
-    if (keeps) {
-      const int r = ra + mine, i = r % kRT;
-      float sum = 0.f;
+    bar_sync(5, 32 * kSoftWarps);
+    {
+      const int r = r0 + own;
+      float m_run = mref_sh[0][r], sum = 0.f;
+      if constexpr (kGroups > 1) m_run = max_nan(m_run, mref_sh[1][r]);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         const float m = mref_sh[g][r];
         if (m == -INFINITY) continue;                  // no step
-        const float(*lw)[kRT] = lsum_sh + 4 * (g * kParts + r / kRT);
-        sum += ((lw[0][i] + lw[1][i]) + (lw[2][i] + lw[3][i])) * ex2_ftz(m - m_run);
+        const float(*lw)[kRT] = lsum_sh + 4 * (g * kParts + r0 / kRT);
+        sum += ((lw[0][own] + lw[1][own]) + (lw[2][own] + lw[3][own])) * ex2_ftz(m - m_run);
       }
-      f_sh[0][r] = n > 0 ? 1.f / sum : 0.f;
-      fa_sh[0][r] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
+      __syncwarp();
+      f_sh[sw][0][own] = m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - m_run) / sum;
+      if (quad == 0 && grp == 0) lse_sh[r] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
+      __syncwarp();
     }
-    bar_sync(7 + aw / 4, 128);
-    // The normalised rows through shared memory (the ring is idle), then out 8
-    // dimensions a thread.  M = 64 leaves 16 dimensions in the first half of every
-    // quadrant's lanes.
+    // The normalised rows through shared memory (the ring is idle: every product
+    // has been waited for), then out 8 dimensions a thread.  M = 64 leaves 16
+    // dimensions in the first half of every quadrant's lanes.
     const int d = D == 128 ? quad * 32 + lane : quad * 16 + (lane & 15);
-    float* part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
-    if (D == 128 || lane < 16) {
+    float* part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw))) + d;
 #pragma unroll
-      for (int r = 0; r < RA; r += 4) {
-        const float4 f = *reinterpret_cast<const float4*>(&f_sh[0][ra + r]);
-        float* dst = part + (ra + r) * C::kPStride + d;
-        dst[0] = acc[r] * f.x;
-        dst[C::kPStride] = acc[r + 1] * f.y;
-        dst[2 * C::kPStride] = acc[r + 2] * f.z;
-        dst[3 * C::kPStride] = acc[r + 3] * f.w;
+    for (int g = 0; g < kGroups; ++g) {
+      if (g == grp && (D == 128 || lane < 16)) {
+#pragma unroll
+        for (int r = 0; r < kRT; r += 4) {
+          const float4 f4 = *reinterpret_cast<const float4*>(&f_sh[sw][0][r]);
+          const float f[4] = {f4.x, f4.y, f4.z, f4.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float* dst = part + (r0 + r + q) * C::kPStride;
+            *dst = g == 0 ? acc[r + q] * f[q] : fmaf(acc[r + q], f[q], *dst);
+          }
+        }
       }
+      bar_sync(5, 32 * kSoftWarps);
     }
-    bar_sync(9, 32 * kAccWarps);
+    part -= d;
     if (has_block && blk_bad) {
 #pragma unroll 1
-      for (int e = at; e < R * D; e += 32 * kAccWarps) {
+      for (int e = at; e < R * D; e += 32 * kSoftWarps) {
         const int r = e / D, dd = e % D;
         float o = part[r * C::kPStride + dd];
         for (int i = 0; i < vis_sh[r]; ++i) {
@@ -881,11 +872,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         }
         part[r * C::kPStride + dd] = o;
       }
-      bar_sync(9, 32 * kAccWarps);
+      bar_sync(5, 32 * kSoftWarps);
     }
     if (a.splits == 1) {
 #pragma unroll 1
-      for (int e = at; e < R * (D / 8); e += 32 * kAccWarps) {
+      for (int e = at; e < R * (D / 8); e += 32 * kSoftWarps) {
         const int r = e / (D / 8), c = e % (D / 8), row = chunk * R + r, i = row / a.G;
         if (row >= a.M) break;
         const float* src = part + r * C::kPStride + 8 * c;
@@ -910,7 +901,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   cluster_sync_all();
   {
     constexpr int kPer = D / 32;
-    const uint32_t lse_s = smem_u32(&fa_sh[0][0]);
+    const uint32_t lse_s = smem_u32(lse_sh);
 #pragma unroll 1
     for (int r = split + a.splits * warp; r < R && chunk * R + r < a.M;
          r += a.splits * (C::kThreads / 32)) {
