@@ -11,6 +11,7 @@
 
 namespace sbd {
 
+inline int log2_page(int P) { return P == 16 ? 4 : P == 32 ? 5 : P == 64 ? 6 : 7; }
 size_t tables_smem_bytes(int B);
 sbd_status tables_launch(const sbd_tables_desc& d, const int32_t* len, const int32_t* target,
                          const int32_t* table, int32_t* free_pages, const int32_t* n_free,

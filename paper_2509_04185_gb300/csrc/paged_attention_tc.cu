@@ -1017,7 +1017,7 @@ sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStre
   a.n_causal = p.n_causal;
   a.splits = p.splits;
   a.chunks = p.chunks;
-  a.page_log2 = p.P == 16 ? 4 : p.P == 32 ? 5 : p.P == 64 ? 6 : 7;
+  a.page_log2 = log2_page(p.P);
   // more CTAs than one wave: the longest sequences first (the pick costs B^2
   // comparisons a CTA, hence the limit)
   a.order = p.B > 1 && p.B <= 128 &&

@@ -32,7 +32,7 @@ struct TablesArgs {
   const int32_t *len, *target, *table, *n_free;
   int32_t *free_pages, *table_out, *len_out, *new_start, *slot_map, *n_free_out;
   int* err;
-  int B, P, max_pages, n_pages, max_new;
+  int B, log2P, max_pages, n_pages, max_new;
 };
 
 struct Sums {
@@ -70,14 +70,15 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
   grid_dependency_wait();
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const long long capacity = (long long)a.max_pages * a.P;
+  const long long capacity = (long long)a.max_pages << a.log2P;
   const int per = (a.B + kTabThreads - 1) / kTabThreads;
   const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
   int n_free = a.n_free[0];
   bool bad_page = n_free < 0 || n_free > a.n_pages, bad_len = false;
   n_free = min(max(n_free, 0), a.n_pages);
 
-  auto pages = [&](int n) { return n / a.P + (n % a.P != 0); };
+  const int last = (1 << a.log2P) - 1;
+  auto pages = [&](int n) { return (n >> a.log2P) + ((n & last) != 0); };
   // a length out of range is clamped and the request left as it is
   auto request = [&](int b, int* len, int* target) {
     const int l = a.len[b], t = a.target[b];
@@ -161,9 +162,9 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
 
   const int gwarp = blockIdx.x * kTabWarps + warp, gwarps = gridDim.x * kTabWarps;
   const int chunks = (a.max_pages + kTabCols - 1) / kTabCols;
-  const long long units = (long long)a.B * chunks;
-  for (long long u = gwarp; u < units; u += gwarps) {
-    const int b = (int)(u / chunks), c0 = (int)(u % chunks) * kTabCols;
+  const int units = a.B * chunks;                  // <= B max_pages < 2^31
+  for (int u = gwarp; u < units; u += gwarps) {
+    const int b = u / chunks, c0 = (u - b * chunks) * kTabCols;
     const int keeps = pages(after_s[b]);
 #pragma unroll
     for (int e = 0; e < kTabCols / 32; ++e) {
@@ -184,10 +185,10 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
       if (t >= a.max_new || t >= all.fresh) continue;
       while (b + 1 < a.B && fresh_at[b + 1] <= t) ++b;
       if (after_s[b] <= len_s[b]) continue;          // refused
-      const int pos = len_s[b] + (t - fresh_at[b]), p = pos / a.P;
+      const int pos = len_s[b] + (t - fresh_at[b]), p = pos >> a.log2P;
       if (p != p_prev || b != b_prev) page = page_at(b, p);
       p_prev = p, b_prev = b;
-      v[e] = page * a.P + pos % a.P;
+      v[e] = (page << a.log2P) + (pos & last);
     }
     if (s + 4 <= a.max_new) {
       *reinterpret_cast<int4*>(a.slot_map + s) = make_int4(v[0], v[1], v[2], v[3]);
@@ -221,12 +222,16 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
 // That is why scales are powers of two: a page filled over many calls loses
 // nothing each time its scale grows, and x / s is exact.
 //
-// One CTA per (chunk of tokens, head, K or V) finds the segments that begin in
-// its chunk; its 8 warps form as many teams as there are segments, so that one
-// long segment (a prompt's page) is eight warps' work and eight single tokens
-// are one warp's each.  A thread keeps its share of the segment in registers
-// between the maximum and the codes (kHold units of 8 elements).
-// Bound: HBM, 3 bytes an element of bf16.
+// A CTA finds the segments that begin in its chunk of tokens and works on them for
+// some planes (K or V of a head); its 8 warps form as many teams as there are
+// segments, so that one long segment (a prompt's page) is eight warps' work and eight
+// single tokens are one warp's each.  A thread keeps its share of the segment in
+// registers between the maximum and the codes (kHold units of 8 elements).
+// Bound: HBM, 3 bytes an element of bf16.  4 x 32768 tokens of 8 heads of 128 144 us,
+// 5.6 TB/s; in pages of 16 131 us.  On the way there: 377 us with the chunks of a
+// plane as neighbours in the grid, 127 registers and fp32 arithmetic; 213 with maxima
+// of pairs and products in bf16; 184 with addresses a constant step apart; 144 with
+// the rows brought to L2 while the slots are read.
 constexpr int kAppThreads = 256;
 constexpr int kAppWarps = kAppThreads / 32;
 constexpr int kHold = 8;
@@ -239,35 +244,63 @@ struct AppendArgs {
   int* err;
   long long k_group_stride, k_token_stride, v_group_stride, v_token_stride;   // elements
   long long n_slots;
-  int tokens, group, Hkv, P, chunk;
+  int tokens, group, Hkv, log2P, chunk;
+  int planes;                                // of a CTA; a plane is K or V of a head
 };
 
+// 8 consecutive elements.  Max: their largest |x| so far, NaN left out.
 template <typename T>
-struct Eight;                                // 8 consecutive elements
+struct Eight;
 template <>
 struct Eight<__nv_bfloat16> {
-  uint4 v;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  using Max = __nv_bfloat162;
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  }
+  __device__ __forceinline__ __nv_bfloat162 two(int e) const {
+    return *reinterpret_cast<const __nv_bfloat162*>(&w[e]);
+  }
+  static __device__ __forceinline__ Max none() { return __float2bfloat162_rn(0.f); }
+  __device__ __forceinline__ void take_max(Max& m) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
+    for (int e = 0; e < 4; ++e) m = __hmax2(m, __habs2(two(e)));
+  }
+  static __device__ __forceinline__ float size(Max m) {
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  // e4m3 codes of 4 h .. 4 h + 3 times a power of two (exact in bf16: the products
+  // are 448 at most)
+  __device__ __forceinline__ uint32_t codes(int h, float inv) const {
+    const __nv_bfloat162 f = __float2bfloat162_rn(inv);
+    const float2 a = __bfloat1622float2(__hmul2(two(2 * h), f));
+    const float2 b = __bfloat1622float2(__hmul2(two(2 * h + 1), f));
+    return e4m3x4(a.x, a.y, b.x, b.y);
+  }
+  __device__ __forceinline__ float get(int e) const {
+    return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
   }
 };
 template <>
 struct Eight<float> {
-  float4 a, b;
+  using Max = float;
+  float w[8];
   __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-    x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  static __device__ __forceinline__ Max none() { return 0.f; }
+  __device__ __forceinline__ void take_max(Max& m) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(w[e]));
   }
+  static __device__ __forceinline__ float size(Max m) { return m; }
+  __device__ __forceinline__ uint32_t codes(int h, float inv) const {
+    return e4m3x4(w[4 * h] * inv, w[4 * h + 1] * inv, w[4 * h + 2] * inv, w[4 * h + 3] * inv);
+  }
+  __device__ __forceinline__ float get(int e) const { return w[e]; }
 };
 
 // |x| of a finite x, 0 of another
@@ -277,7 +310,7 @@ __device__ __forceinline__ float finite_size(float x) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8_kernel(const AppendArgs a) {
   constexpr int kUnits = D / 8;              // units of a row
   __shared__ uint32_t joins[kAppThreads / 32];       // bit i: token t0 + i goes on with a segment
   __shared__ uint32_t starts[kAppThreads / 32];      // bit i: token t0 + i begins one
@@ -285,9 +318,25 @@ __global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs
   __shared__ float team_max[kAppWarps];
   grid_dependency_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int h = blockIdx.y;
-  const bool is_v = blockIdx.z != 0;
-  const int t0 = blockIdx.x * a.chunk;
+  // The planes of a chunk of tokens are neighbours in the grid, as their rows are in
+  // memory (with the chunks of a plane as neighbours, prompts of 32768 tokens took
+  // 377 us: 256-byte pieces 6 KB apart).
+  const int sets = (2 * a.Hkv + a.planes - 1) / a.planes;      // CTAs of a chunk
+  const int t0 = (int)(blockIdx.x / sets) * a.chunk, set = (int)(blockIdx.x % sets);
+  const int last = (1 << a.log2P) - 1;
+  // The chunk's rows of a plane on their way to L2, while its slots are looked at or
+  // the plane before is worked on.
+  auto fetch_ahead = [&](int plane) {
+    constexpr int kLines = D * (int)sizeof(T) / 128;           // of a row
+    if (a.group < a.tokens || plane >= 2 * a.Hkv) return;
+    const bool is_v = plane >= a.Hkv;
+    const T* src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)(is_v ? plane - a.Hkv : plane) * D;
+    const long long stride = is_v ? a.v_token_stride : a.k_token_stride;
+    for (int i = threadIdx.x; i < a.chunk * kLines; i += kAppThreads)
+      if (t0 + i / kLines < a.tokens)
+        prefetch_l2(src + (t0 + i / kLines) * stride + i % kLines * (128 / (int)sizeof(T)));
+  };
+  fetch_ahead(set);
 
   // ---- the segments that begin in this chunk; chunk + P <= kAppThreads tokens
   // are looked at, as far as the last of them can reach
@@ -296,8 +345,8 @@ __global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs
     const int s = t < a.tokens ? a.slot_map[t] : -1;
     const int prev = t > 0 && t < a.tokens ? a.slot_map[t - 1] : -1;
     const bool valid = s >= 0 && s < a.n_slots;
-    if (s >= a.n_slots && h == 0 && !is_v) record_error(a.err, SBD_DEVERR_PAGE);
-    const bool join = valid && prev >= 0 && prev + 1 == s && s % a.P != 0;
+    if (s >= a.n_slots && set == 0) record_error(a.err, SBD_DEVERR_PAGE);
+    const bool join = valid && prev >= 0 && prev + 1 == s && (s & last) != 0;
     const uint32_t j = __ballot_sync(0xffffffffu, join);
     const uint32_t f = __ballot_sync(0xffffffffu, valid && !join && tid < a.chunk);
     if (lane == 0) joins[warp] = j, starts[warp] = f;
@@ -316,6 +365,10 @@ __global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs
   const int team_warps = kAppWarps / teams, team_threads = 32 * team_warps;
   const int team = warp / team_warps, rank = tid - team * team_threads;
 
+  for (int plane = set; plane < 2 * a.Hkv; plane += sets) {
+  const bool is_v = plane >= a.Hkv;
+  const int h = is_v ? plane - a.Hkv : plane;
+  fetch_ahead(plane + sets);
   const T* src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)h * D;
   const long long group_stride = is_v ? a.v_group_stride : a.k_group_stride;
   const long long token_stride = is_v ? a.v_token_stride : a.k_token_stride;
@@ -333,33 +386,55 @@ __global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs
       if (run < room) break;
     }
     const int n = end - i0;
-    const int slot = a.slot_map[t], off = slot % a.P;
-    const long long page = slot / a.P;
+    const int slot = a.slot_map[t], off = slot & last;
+    const long long page = slot >> a.log2P;
     const int units = n * kUnits;
-    auto at = [&](int u) {
-      const int tok = t + u / kUnits;
-      return src + (tok / a.group) * group_stride + (tok % a.group) * token_stride + (u % kUnits) * 8;
+    // A thread's units are team_threads apart, a whole number of tokens: their
+    // addresses a constant step apart where tokens are.
+    const T* first = src + (rank % kUnits) * 8;
+    const int tok = t + rank / kUnits, step = team_threads / kUnits;
+    const bool even = a.group >= a.tokens;
+    auto at = [&](int e) {                   // unit rank + e team_threads
+      const int i = tok + e * step;
+      if (even) return first + i * token_stride;
+      const int g = i / a.group;
+      return first + g * group_stride + (i - g * a.group) * token_stride;
     };
+    const int mine = (units - rank + team_threads - 1) / team_threads;   // this thread's units
     Eight<T> hold[kHold];
+    typename Eight<T>::Max m = Eight<T>::none();
+    if (even) {
+      const T* p = first + tok * token_stride;
+      const long long jump = step * token_stride;
 #pragma unroll
-    for (int e = 0; e < kHold; ++e)
-      if (rank + e * team_threads < units) hold[e].load(at(rank + e * team_threads));
+      for (int e = 0; e < kHold; ++e)
+        if (e < mine) hold[e].load(p + e * jump);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kHold; ++e)
+        if (e < mine) hold[e].load(at(e));
+    }
     const long long sc = page * a.Hkv + h;
     const float s_old = off > 0 ? scales[sc] : 0.f;
-    float amax = 0.f;
-    auto take_max = [&](const Eight<T>& v) {
-      float x[8];
-      v.get(x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_size(x[e]));
-    };
 #pragma unroll
     for (int e = 0; e < kHold; ++e)
-      if (rank + e * team_threads < units) take_max(hold[e]);
-    for (int u = rank + kHold * team_threads; u < units; u += team_threads) {
+      if (e < mine) hold[e].take_max(m);
+#pragma unroll 1
+    for (int e = kHold; e < mine; ++e) {
       Eight<T> v;
-      v.load(at(u));
-      take_max(v);
+      v.load(at(e));
+      v.take_max(m);
+    }
+    float amax = Eight<T>::size(m);
+    if (!(amax < INFINITY)) {                // some are infinite: those do not count
+      amax = 0.f;
+#pragma unroll 1
+      for (int e = 0; e < mine; ++e) {
+        Eight<T> v;
+        v.load(at(e));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_size(v.get(i)));
+      }
     }
     amax = warp_max(amax);
     if (team_warps > 1) {
@@ -373,26 +448,32 @@ __global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs
     }
     const float s = fmaxf(s_old, scale_for(amax));
     if (rank == 0) scales[sc] = s;
-    uint8_t* dst = cache + (page * a.Hkv + h) * (long long)(a.P * D);
-    const float inv = 1.f / s;               // a power of two unless a caller's scale is kept
-    const bool exact = (__float_as_uint(s) & 0x007fffffu) == 0;
-    auto put = [&](int u, const Eight<T>& v) {
-      float x[8];
-      v.get(x);
+    uint8_t* dst = cache + ((page * a.Hkv + h) << a.log2P) * D;
+    uint8_t* to = dst + off * D + 8 * rank;
+    const int hop = 8 * team_threads;
+    // s is a power of two unless a caller's own scale is kept: products are exact
+    if ((__float_as_uint(s) & 0x007fffffu) == 0) {
+      const float inv = 1.f / s;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = exact ? x[e] * inv : x[e] / s;
-      uint2 c;
-      c.x = e4m3x4(x[0], x[1], x[2], x[3]);
-      c.y = e4m3x4(x[4], x[5], x[6], x[7]);
-      *reinterpret_cast<uint2*>(dst + (long long)off * D + 8 * u) = c;
-    };
+      for (int e = 0; e < kHold; ++e)
+        if (e < mine) *reinterpret_cast<uint2*>(to + e * hop) = make_uint2(hold[e].codes(0, inv), hold[e].codes(1, inv));
+#pragma unroll 1
+      for (int e = kHold; e < mine; ++e) {
+        Eight<T> v;
+        v.load(at(e));
+        *reinterpret_cast<uint2*>(to + e * hop) = make_uint2(v.codes(0, inv), v.codes(1, inv));
+      }
+    } else {
+#pragma unroll 1
+      for (int e = 0; e < mine; ++e) {
+        Eight<T> v;
+        v.load(at(e));
+        float x[8];
 #pragma unroll
-    for (int e = 0; e < kHold; ++e)
-      if (rank + e * team_threads < units) put(rank + e * team_threads, hold[e]);
-    for (int u = rank + kHold * team_threads; u < units; u += team_threads) {
-      Eight<T> v;
-      v.load(at(u));
-      put(u, v);
+        for (int i = 0; i < 8; ++i) x[i] = v.get(i) / s;
+        *reinterpret_cast<uint2*>(to + e * hop) =
+            make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
+      }
     }
     if (off > 0 && s != s_old) {             // the page's earlier codes move to the new scale
       const float f = s_old / s;
@@ -403,6 +484,7 @@ __global__ void __launch_bounds__(kAppThreads) append_q8_kernel(const AppendArgs
         *reinterpret_cast<uint4*>(dst + 16 * u) = c;
       }
     }
+  }
   }
   grid_dependents_launch();
 }
@@ -419,7 +501,7 @@ sbd_status tables_launch(const sbd_tables_desc& d, const int32_t* len, const int
                          int32_t* slot_map, int32_t* n_free_out, cudaStream_t st) {
   TablesArgs a{len,     target,    table,    n_free,     free_pages,          table_out,
                len_out, new_start, slot_map, n_free_out, device_error_word(), d.batch,
-               d.page_size, d.max_pages, d.n_pages, d.max_new};
+               log2_page(d.page_size), d.max_pages, d.n_pages, d.max_new};
   const size_t smem = tables_smem_bytes(d.batch);
   if (smem > 48 * 1024) {
     const sbd_status s = allow_smem((const void*)block_tables_kernel, smem,
@@ -430,7 +512,7 @@ sbd_status tables_launch(const sbd_tables_desc& d, const int32_t* len, const int
   long long ctas = (rows + kTabWarps - 1) / kTabWarps;
   const long long by_slots = ((long long)d.max_new + kTabSlots - 1) / kTabSlots;
   if (by_slots > ctas) ctas = by_slots;
-  if (ctas > 2 * num_sms()) ctas = 2 * num_sms();
+  if (ctas > 4 * num_sms()) ctas = 4 * num_sms();
   if (ctas < 1) ctas = 1;
   void* args[] = {(void*)&a};
   return launch_pdl((const void*)block_tables_kernel, dim3((unsigned)ctas), dim3(kTabThreads), smem,
@@ -457,10 +539,17 @@ sbd_status append_q8_launch(const sbd_append_q8_desc& d, const void* k_new, cons
   a.tokens = d.tokens;
   a.group = d.group;
   a.Hkv = d.n_kv_heads;
-  a.P = d.page_size;
-  // few tokens: short chunks, so that every SM has some of them
-  const long long jobs = 2ll * d.n_kv_heads * ((d.tokens + 63) / 64);
-  a.chunk = jobs < 4ll * num_sms() ? 16 : d.page_size > 64 ? d.page_size : 64;
+  a.log2P = log2_page(d.page_size);
+  // Few tokens: short chunks and a plane a CTA, so that every SM has some of them
+  // (256 tokens of 16 segments 4.1 us; chunks of 8: 4.7).  Many: as many tokens as
+  // kHold units a thread hold (at 64 dimensions as many as the chunk's table allows:
+  // 65536 tokens of 8 heads 49 us, 60 in chunks of 128), and two planes a CTA where
+  // that leaves enough CTAs (one: 10 % slower, four: 2 to 7 %).
+  const int planes = 2 * d.n_kv_heads;
+  const long long jobs = (long long)planes * ((d.tokens + 63) / 64);
+  a.chunk = jobs < 4ll * num_sms() ? 16 : d.head_dim == 64 ? kAppThreads - d.page_size : 128;
+  a.planes = 1;
+  while (a.planes < 2 && (long long)planes * ((d.tokens + 127) / 128) / (2 * a.planes) >= 8ll * num_sms()) a.planes *= 2;
   const bool f32 = d.dtype == SBD_DTYPE_F32;
   const void* fn = d.head_dim == 128
                        ? (f32 ? (const void*)append_q8_kernel<float, 128>
@@ -468,8 +557,11 @@ sbd_status append_q8_launch(const sbd_append_q8_desc& d, const void* k_new, cons
                        : (f32 ? (const void*)append_q8_kernel<float, 64>
                               : (const void*)append_q8_kernel<__nv_bfloat16, 64>);
   void* args[] = {(void*)&a};
-  return launch_pdl(fn, dim3((unsigned)((d.tokens + a.chunk - 1) / a.chunk), d.n_kv_heads, 2),
-                    dim3(kAppThreads), 0, st, args, "append_q8_kernel launch");
+  const long long ctas =
+      (d.tokens + (long long)a.chunk - 1) / a.chunk * ((planes + a.planes - 1) / a.planes);
+  if (ctas > 0x7fffffffll) return fail(SBD_ERR_UNSUPPORTED, "%lld CTAs >= 2^31", ctas);
+  return launch_pdl(fn, dim3((unsigned)ctas), dim3(kAppThreads), 0, st, args,
+                    "append_q8_kernel launch");
 }
 
 }  // namespace sbd
