@@ -46,6 +46,7 @@ constexpr int kTile = 128;                   // keys of an MMA; a step is two ti
 constexpr int kRT = 16;                      // rows of a softmax thread
 constexpr int kControl = 3;                  // warps: pages and TMA, products S, products O
 constexpr int kMaxStages = 8;
+constexpr int kTables = 8 * 1024;            // shared memory outside the operands
 constexpr int kBlkKeys = 32;                 // block keys, padded
 constexpr int kMaxSplits = 16;
 constexpr float kPScale = 256.f;             // P = 2^8 p
@@ -199,15 +200,8 @@ __device__ __forceinline__ uint32_t mapa_shared(uint32_t addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ float2 ld_cluster_v2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 struct Args {
@@ -233,11 +227,9 @@ struct Shape {
   static constexpr int kNO = 2 * R;                    // columns of O, bytes of a key's row of P
   static constexpr int kOCol = 4 * kNS;                // S: two buffers of two tiles
   static constexpr int kTmemCols = kOCol + 2 * kNO <= 256 ? 256 : 512;
-  // Four softmax warps take 16 rows of a step; all the rows of a step are the parts'
-  // together, and with few rows two sets of parts take alternate steps.
+  // Four softmax warps take 16 rows of a step.
   static constexpr int kParts = R / kRT;
-  static constexpr int kGroups = R < 64 ? 2 : 1;
-  static constexpr int kSoftWarps = 4 * kParts * kGroups;
+  static constexpr int kSoftWarps = 4 * kParts;
   static constexpr int kThreads = 32 * (kControl + kSoftWarps);
   static constexpr int kKV = kTile * D;                // a K or V tile
   static constexpr int kQ = 2 * R * D;
@@ -250,13 +242,13 @@ struct Shape {
   static constexpr int kBlk = 2 * kBlkKeys * D;
   static constexpr int kBlkSub = kBlkKeys * 128;
   static constexpr int kFixed = 1024 + kQ + (kPInK ? 0 : 4 * kP) + kPBlk + 2 * kBlk;
-  static constexpr int kLeft = 227 * 1024 - 12 * 1024 - kFixed;    // 12 KB: barriers and tables
+  static constexpr int kLeft = 227 * 1024 - kTables - kFixed;
   static constexpr int kStages = kLeft / (2 * kKV) < kMaxStages ? kLeft / (2 * kKV) : kMaxStages;
   static constexpr int kSmem = kFixed + kStages * 2 * kKV;
   static constexpr int kPStride = D + 4;               // floats of a partial row
   static_assert(kStages >= 4, "two steps of two tiles");
   static_assert(kPBlk % 1024 == 0, "operands begin on 1 KB");
-  static_assert(R * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
+  static_assert((R + kMaxSplits) * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
   static_assert(kBlk + kTile * D <= 2 * kBlk + kStages * 2 * kKV, "reads past the block's keys stay inside");
 };
 
@@ -330,7 +322,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
   using C = Shape<D, R>;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
-  constexpr int kParts = C::kParts, kGroups = C::kGroups, kSoftWarps = C::kSoftWarps;
+  constexpr int kParts = C::kParts, kSoftWarps = C::kSoftWarps;
   static_assert(R == 16 || R == 32 || R == 64, "a key's row of P is one swizzle atom");
 
   extern __shared__ uint8_t smem_raw[];
@@ -344,11 +336,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
-  __shared__ __align__(16) float red_sh[kSoftWarps / 4][2][4][kRT];  // maxima of four warps, two steps
-  __shared__ __align__(16) float sum_sh[kSoftWarps][kRT];            // a warp's sums of probabilities
-  __shared__ __align__(16) float mq_sh[kSoftWarps][kRT];             // a warp's copy of the step's maxima, negated
-  __shared__ __align__(16) float f_sh[kSoftWarps][2][kRT];           // its rows' weights: of a step's product, of what was before
-  __shared__ float lsum_sh[kSoftWarps][kRT], mref_sh[kGroups][R], lse_sh[R];
+  __shared__ __align__(16) float red_sh[kParts][2][4][kRT];  // maxima of a part's warps, two steps
+  __shared__ __align__(16) float sum_sh[kSoftWarps][kRT];    // a warp's sums of probabilities
+  __shared__ __align__(16) float mq_sh[kSoftWarps][kRT];     // a warp's copy of the step's maxima, negated
+  __shared__ __align__(16) float f_sh[kSoftWarps][2][kRT];   // its rows' weights: of a step's product, of what was before
+  __shared__ float lse_sh[R + kMaxSplits];                   // of the rows merged here, a row's splits together
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_s = sbase, pblk_s = q_s + C::kQ, p_s = pblk_s + C::kPBlk;
@@ -368,19 +360,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 2);              // the product, and its issuer's view of the scales
-      mbar_init(&s_free[i], 4 * kParts);
+      mbar_init(&s_free[i], kSoftWarps);
       mbar_init(&o_full[i], 1);
-      mbar_init(&o_free[i], 4 * kParts);
+      mbar_init(&o_free[i], kSoftWarps);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&p_full[i], 4 * kParts);
+    for (int i = 0; i < 4; ++i) mbar_init(&p_full[i], kSoftWarps);
     mbar_init(&q_ready, kSoftWarps);
     mbar_init(&blk_ready, kSoftWarps);
     mbar_init(&tail_bar, 1);
     blk_bad = 0;
     fence_mbar_init();
   }
-  // Tensor memory is taken only after the previous grid is done, so that no CTA
-  // of it can be left waiting for it.
+  __syncthreads();
+  // What the previous grid may still write is read from here on.  There is no
+  // barrier of the block any more before the work begins: tensor memory, the table
+  // and the first copies, and the rows are fetched side by side.
   grid_dependency_wait();
   const int cap = a.max_pages << a.page_log2;
   if (a.order) {
@@ -388,7 +382,6 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     __syncthreads();
   }
   const int b = a.order ? b_pick : (int)blockIdx.z;
-  if (warp == 1) tc_alloc(&tmem_base_sh, C::kTmemCols);
   int len = a.lens[b];
   if (len < 0 || len > cap) {
     if (threadIdx.x == 0 && split == 0 && blockIdx.y == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
@@ -404,10 +397,6 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   const int n = (nc + 1) / 2 + (has_block ? 1 : 0);
   // keys of local cache tile j
   auto keys_of = [&](int j) { return max(0, min(kTile, j < nc ? len - (t_begin + j) * kTile : 0)); };
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_base_sh;
 
   if (warp == 0) {
     // ------------------------------------------------ pages and TMA
@@ -490,6 +479,12 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     // ------------------------------------------------ S = K Q^T
     // Ahead of the softmax by the second buffer.  The whole warp runs the loop
     // (descriptors stay in uniform registers) and one lane issues.
+    // Tensor memory is taken only after the previous grid is done, so that no CTA of
+    // it can be left waiting for it.  Its address reaches the other warps with the
+    // first scores.
+    tc_alloc(&tmem_base_sh, C::kTmemCols);
+    __syncwarp();
+    const uint32_t tmem = *(volatile uint32_t*)&tmem_base_sh;
     const bool leader = elect_one();
     bool ok = n > 0 && mbar_wait(&q_ready, 0, a.err);
     const uint32_t id_s = idesc_f8(kTile, kNS, false);
@@ -540,6 +535,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
+      const uint32_t tmem = *(volatile uint32_t*)&tmem_base_sh;
       const uint32_t o = tmem + C::kOCol + (uint32_t)((i & 1) * kNO);
       if (has_block && i == n - 1) {
         const uint64_t vd = desc<128>(bv_s, C::kBlkSub), pd = desc<kNO>(pblk_s);
@@ -565,8 +561,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     }
   } else {
     // ------------------------------------------------ softmax and accumulators
-    const int sw = warp - kControl, quad = warp & 3, grp = sw / (4 * kParts);
-    const int r0 = sw / 4 % kParts * kRT;              // its rows: r0 .. r0 + 15
+    const int sw = warp - kControl, quad = warp & 3, part = sw / 4;
+    const int r0 = part * kRT;                         // its rows: r0 .. r0 + 15
+    uint32_t tmem = 0;
     const int key = quad * 32 + lane;                  // of both tiles
     const int at = sw * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
@@ -671,7 +668,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free[i & 1]);
     };
-    for (int i = grp; i < n; i += kGroups) {
+    for (int i = 0; i < n; ++i) {
       const int buf = i & 1, phase = (i >> 1) & 1;
       const bool blk = has_block && i == n - 1;
       const int j0 = 2 * i, st0 = j0 % kStages, st1 = (j0 + 1) % kStages;
@@ -683,6 +680,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       float vw0 = 1.f, vw1 = 1.f, vref = 1.f;
       if (ok) {
         tc_fence_after();
+        tmem = *(volatile uint32_t*)&tmem_base_sh;
         if (has0) {
           // (the scales come with the stages, which stay until P is handed in)
           float kf0 = 0.f, kf1 = 0.f;
@@ -737,17 +735,17 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         if (has0) {
 #pragma unroll
           for (int r = 0; r < kRT; r += 4)
-            st_shared_v4_if(lane == 0, smem_u32(&red_sh[sw / 4][(i / kGroups) & 1][quad][r]),
+            st_shared_v4_if(lane == 0, smem_u32(&red_sh[part][i & 1][quad][r]),
                             redux_max_nan(max_nan(z0[r], z1[r])), redux_max_nan(max_nan(z0[r + 1], z1[r + 1])),
                             redux_max_nan(max_nan(z0[r + 2], z1[r + 2])),
                             redux_max_nan(max_nan(z0[r + 3], z1[r + 3])));
         } else {
-          red_sh[sw / 4][(i / kGroups) & 1][quad][own] = -INFINITY;
+          red_sh[part][i & 1][quad][own] = -INFINITY;
         }
       }
-      bar_sync(1 + sw / 4, 128);
+      bar_sync(1 + part, 128);
       if (!ok) continue;
-      const float(*x)[kRT] = red_sh[sw / 4][(i / kGroups) & 1];
+      const float(*x)[kRT] = red_sh[part][i & 1];
       const float my = max_nan(max_nan(x[0][own], x[1][own]), max_nan(x[2][own], x[3][own])) * c_own;   // c > 0
       mq_sh[sw][own] = my == -INFINITY ? 0.f : -my;
       __syncwarp();
@@ -803,7 +801,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (lane == 0) mbar_arrive(&p_full[i & 3]);
       // The step before's product, done by now.  (A warp is past it before it hands
       // in its next P but one, so no phase of p_full is ever two behind.)
-      if (i >= kGroups) add_product(i - kGroups);
+      if (i > 0) add_product(i - 1);
       const float m_new = max_nan(m_ref, my);
       const float keep = m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - m_new);
       const float g = my == -INFINITY ? 0.f : ex2_ftz(my - m_new);
@@ -817,129 +815,106 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       m_ref = m_new;
       __syncwarp();
     }
-    if (n > grp) add_product(n - 1 - (n - 1 - grp) % kGroups);
+    if (n > 0) add_product(n - 1);
     grid_dependents_launch();
     // ------------------------------------------------ epilogue
-    lsum_sh[sw][own] = l;
-    if (quad == 0) mref_sh[grp][r0 + own] = m_ref;
-    bar_sync(5, 32 * kSoftWarps);
-    {
-      const int r = r0 + own;
-      float m_run = mref_sh[0][r], sum = 0.f;
-      if constexpr (kGroups > 1) m_run = max_nan(m_run, mref_sh[1][r]);
+    sum_sh[sw][own] = l;
+    bar_sync(1 + part, 128);
+    const float sum = (sum_sh[4 * part][own] + sum_sh[4 * part + 1][own]) +
+                      (sum_sh[4 * part + 2][own] + sum_sh[4 * part + 3][own]);
+    f_sh[sw][0][own] = m_ref == -INFINITY ? 0.f : 1.f / sum;
+    __syncwarp();
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        const float m = mref_sh[g][r];
-        if (m == -INFINITY) continue;                  // no step
-        const float(*lw)[kRT] = lsum_sh + 4 * (g * kParts + r0 / kRT);
-        sum += ((lw[0][own] + lw[1][own]) + (lw[2][own] + lw[3][own])) * ex2_ftz(m - m_run);
-      }
-      __syncwarp();
-      f_sh[sw][0][own] = m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - m_run) / sum;
-      if (quad == 0 && grp == 0) lse_sh[r] = n > 0 && ok ? m_run + log2f(sum) : -INFINITY;
-      __syncwarp();
+    for (int r = 0; r < kRT; r += 4) {
+      const float4 f4 = *reinterpret_cast<const float4*>(&f_sh[sw][0][r]);
+      acc[r] *= f4.x, acc[r + 1] *= f4.y, acc[r + 2] *= f4.z, acc[r + 3] *= f4.w;
     }
-    // The normalised rows through shared memory (the ring is idle: every product
-    // has been waited for), then out 8 dimensions a thread.  M = 64 leaves 16
-    // dimensions in the first half of every quadrant's lanes.
+    // M = 64 leaves 16 dimensions in the first half of every quadrant's lanes
     const int d = D == 128 ? quad * 32 + lane : quad * 16 + (lane & 15);
-    float* part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw))) + d;
+    const bool has_d = D == 128 || lane < 16;
+    const int row = chunk * R + r0;                    // packed rows row .. row + 15
+    if (has_block && blk_bad && has_d) {
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      if (g == grp && (D == 128 || lane < 16)) {
-#pragma unroll
-        for (int r = 0; r < kRT; r += 4) {
-          const float4 f4 = *reinterpret_cast<const float4*>(&f_sh[sw][0][r]);
-          const float f[4] = {f4.x, f4.y, f4.z, f4.w};
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float* dst = part + (r0 + r + q) * C::kPStride;
-            *dst = g == 0 ? acc[r + q] * f[q] : fmaf(acc[r + q], f[q], *dst);
-          }
-        }
-      }
-      bar_sync(5, 32 * kSoftWarps);
-    }
-    part -= d;
-    if (has_block && blk_bad) {
+      for (int r = 0; r < kRT; ++r) {
 #pragma unroll 1
-      for (int e = at; e < R * D; e += 32 * kSoftWarps) {
-        const int r = e / D, dd = e % D;
-        float o = part[r * C::kPStride + dd];
-        for (int i = 0; i < vis_sh[r]; ++i) {
-          const float v = __bfloat162float(a.vb[(((size_t)b * a.k + i) * a.Hkv + hkv) * D + dd]);
-          if (!(fabsf(v) < INFINITY)) o += v;
+        for (int e = 0; e < vis_sh[r0 + r]; ++e) {
+          const float v = __bfloat162float(a.vb[(((size_t)b * a.k + e) * a.Hkv + hkv) * D + d]);
+          if (!(fabsf(v) < INFINITY)) acc[r] += v;
         }
-        part[r * C::kPStride + dd] = o;
       }
-      bar_sync(5, 32 * kSoftWarps);
     }
     if (a.splits == 1) {
-#pragma unroll 1
-      for (int e = at; e < R * (D / 8); e += 32 * kSoftWarps) {
-        const int r = e / (D / 8), c = e % (D / 8), row = chunk * R + r, i = row / a.G;
-        if (row >= a.M) break;
-        const float* src = part + r * C::kPStride + 8 * c;
-        const float4 x = *reinterpret_cast<const float4*>(src), y = *reinterpret_cast<const float4*>(src + 4);
-        *reinterpret_cast<uint4*>(a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + 8 * c) =
-            make_uint4(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w), pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+      int i = row / a.G, q = row - i * a.G;            // block position, query head of the group
+      __nv_bfloat16* dst = a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + q) * D + d;
+#pragma unroll
+      for (int r = 0; r < kRT; ++r) {
+        if (has_d && row + r < a.M) *dst = __float2bfloat16(acc[r]);
+        dst += D;
+        if (++q == a.G) q = 0, dst += (size_t)(a.Hq - a.G) * D;
+      }
+    } else {
+      // Row r is merged in CTA r mod splits of the cluster: its partial rows go into
+      // that one's ring, which is idle there once every CTA has come here.
+      const float lse = n > 0 && ok ? m_ref + log2f(sum) : -INFINITY;
+      cluster_sync_all();
+      if (quad == 0) {
+        const int to = (r0 + own) % a.splits, slot = (r0 + own) / a.splits;
+        st_cluster_f32(mapa_shared(smem_u32(&lse_sh[slot * a.splits + split]), to), lse);
+      }
+      int to = r0 % a.splits, slot = r0 / a.splits;
+#pragma unroll
+      for (int r = 0; r < kRT; ++r) {
+        if (has_d && row + r < a.M)
+          st_cluster_f32(mapa_shared(ring + 4u * ((slot * a.splits + split) * C::kPStride + d), to),
+                         n > 0 ? acc[r] : 0.f);
+        if (++to == a.splits) to = 0, ++slot;
       }
     }
   }
+  if (a.splits > 1 && warp < kControl) cluster_sync_all();
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tc_dealloc(tmem, C::kTmemCols);
+    tc_dealloc(*(volatile uint32_t*)&tmem_base_sh, C::kTmemCols);
   }
   if (a.splits == 1) return;
   // ------------------------------------------------ merge in the cluster
-  // The CTAs of a cluster are the splits of one (sequence, KV head, chunk), each
-  // holding its normalised rows and their log2-sum-exps in shared memory; CTA
-  // `split` merges rows split, split + splits, ..., a warp a row.  The second
-  // barrier keeps shared memory alive until every CTA has read it.
+  // The CTAs of a cluster are the splits of one (sequence, KV head, chunk); CTA
+  // `split` has all splits' normalised rows split, split + splits, ... and their
+  // log2-sum-exps in its own shared memory now, a warp a row.  (Rows read from the
+  // other CTAs, all splits of a row requested at once, took 3.5 us of one user's
+  // 15: the requests were 250 instructions that run once.)
   cluster_sync_all();
-  {
-    constexpr int kPer = D / 32;
-    const uint32_t lse_s = smem_u32(lse_sh);
+  constexpr int kPer = D / 32;
 #pragma unroll 1
-    for (int r = split + a.splits * warp; r < R && chunk * R + r < a.M;
-         r += a.splits * (C::kThreads / 32)) {
-      const float l = lane < a.splits ? ld_cluster_f32(mapa_shared(lse_s + 4u * r, lane)) : -INFINITY;
-      float2 v[kMaxSplits][kPer / 2];
+  for (int slot = warp; slot * a.splits + split < R; slot += C::kThreads / 32) {
+    const int row = chunk * R + slot * a.splits + split;
+    if (row >= a.M) break;
+    const float l = lane < a.splits ? lse_sh[slot * a.splits + lane] : -INFINITY;
+    const float mx = warp_max(l);
+    const float w = l == -INFINITY ? 0.f : exp2f(l - mx);
+    const float inv = 1.f / warp_sum(w);
+    const float* src = reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))) +
+                       slot * a.splits * C::kPStride + kPer * lane;
+    float o[kPer];
 #pragma unroll
-      for (int s = 0; s < kMaxSplits; ++s)
-        if (s < a.splits) {
-          const uint32_t src = mapa_shared(ring + 4u * (r * C::kPStride + kPer * lane), s);
+    for (int c = 0; c < kPer; ++c) o[c] = 0.f;
+#pragma unroll 2
+    for (int s = 0; s < a.splits; ++s) {
+      const float ws = __shfl_sync(0xffffffffu, w, s);
+      if (!(ws == 0.f)) {
 #pragma unroll
-          for (int c = 0; c < kPer / 2; ++c) v[s][c] = ld_cluster_v2(src + 8 * c);
-        }
-      const float mx = warp_max(l);
-      const float w = l == -INFINITY ? 0.f : exp2f(l - mx);
-      const float inv = 1.f / warp_sum(w);
-      float o[kPer];
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) o[c] = 0.f;
-#pragma unroll
-      for (int s = 0; s < kMaxSplits; ++s) {
-        const float ws = __shfl_sync(0xffffffffu, w, s);
-        if (s < a.splits && !(ws == 0.f)) {
-#pragma unroll
-          for (int c = 0; c < kPer / 2; ++c) {
-            o[2 * c] = fmaf(ws, v[s][c].x, o[2 * c]);
-            o[2 * c + 1] = fmaf(ws, v[s][c].y, o[2 * c + 1]);
-          }
-        }
+        for (int c = 0; c < kPer; ++c) o[c] = fmaf(ws, src[s * C::kPStride + c], o[c]);
       }
-      const int row = chunk * R + r, i = row / a.G;
-      __nv_bfloat16* dst =
-          a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + kPer * lane;
-#pragma unroll
-      for (int c = 0; c < kPer; c += 2)
-        *reinterpret_cast<__nv_bfloat162*>(dst + c) = __floats2bfloat162_rn(o[c] * inv, o[c + 1] * inv);
     }
+    const int i = row / a.G;
+    __nv_bfloat16* dst =
+        a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + kPer * lane;
+#pragma unroll
+    for (int c = 0; c < kPer; c += 2)
+      *reinterpret_cast<__nv_bfloat162*>(dst + c) = __floats2bfloat162_rn(o[c] * inv, o[c + 1] * inv);
   }
-  cluster_sync_all();
 }
 
 struct Kernel {

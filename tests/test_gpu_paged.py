@@ -303,6 +303,16 @@ def test_attention_splits(sbd, num_splits, dtype, D, k):
     _attend(sbd, _attention_case(rng, 2, k, 8, 2, D, 64, [1500, 31]), dtype, num_splits=num_splits)
 
 
+@pytest.mark.parametrize("B,k,Hq,H,D,page,hi", [
+    (200, 1, 2, 1, 128, 16, 700), (97, 3, 4, 2, 64, 32, 300), (45, 8, 16, 4, 128, 64, 900), (513, 2, 1, 1, 64, 16, 90),
+    (170, 1, 1, 1, 128, 128, 0), (30, 16, 16, 8, 64, 128, 400), (21, 32, 8, 2, 128, 64, 3000), (160, 5, 1, 1, 128, 64, 260)])
+def test_attention_of_more_jobs_than_sms(sbd, B, k, Hq, H, D, page, hi):
+    """Sequences of all lengths, empty ones among them, whose tiles the CTAs share out."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, hi + 1, B) * (rng.random(B) < 0.9)
+    _attend(sbd, _attention_case(rng, B, k, Hq, H, D, page, lens), n_causal=k // 2)
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 def test_attention_peaked_flat_and_scaled(sbd, dtype):
     rng = np.random.default_rng(9)
