@@ -24,8 +24,7 @@ sbd_status append_q8_launch(const sbd_append_q8_desc& d, const void* k_new, cons
 struct AttnQ8Plan {
   int B, k, Hq, Hkv, G, D, P, max_pages, n_pages, M, n_causal;
   int rows, chunks;   // packed rows of a CTA, and how many CTAs share a KV head's rows
-  int splits;         // key ranges of a (sequence, KV head, chunk)
-  bool cluster;       // they merge in a thread-block cluster
+  int splits;         // key ranges of a (sequence, KV head, chunk): a thread-block cluster
   float scale_log2;   // softmax scale * log2(e)
   bool bf16;
 };

@@ -1,5 +1,6 @@
 // Block attention over the paged 8-bit cache on the tcgen05 tensor cores, for
-// bf16 activations.
+// bf16 activations with up to 32 packed rows of a KV head (r = i*G + g: block
+// position i, query head g of the group); and the plan and launch of all of them.
 //
 // The codes are what the tensor cores read (kind::f8f6f4): no conversion of the
 // cache anywhere.  Activations carry 8 significant bits and a code 4, so every
@@ -11,14 +12,15 @@
 //                                     B = the rows' hi codes, then their lo codes
 //   O[dim, (hi|lo) row] += V^T P^T    A = V tile (MN-major), B = P (MN-major)
 //
-// so that N follows the rows of the call (R = 16, 32 or 64 packed rows of the KV
-// head's group a CTA, r = i*G + g) and a thread of the softmax owns one key: its
-// page's scales are scalars of the thread, masks a comparison, a row's maximum and
-// sum one redux a warp.
+// so that N follows the rows of the call (R = 16 or 32 a CTA) and a thread of the
+// softmax owns one key: its page's scales are scalars of the thread, masks a
+// comparison, a row's maximum and sum one redux a warp.  Above 32 rows those
+// reductions cost more than the tile's loads, and rows are on the lanes
+// (paged_attention_rows.cu): at 64 rows over 19 x 4096 keys, 128 dimensions, 45.7 us
+// instead of the 50.4 that this kernel took, at 128 rows over 16 x 8192 82 instead of 177.
 //
 // Tiles go in steps of two (256 keys): what a step costs by row and not by key --
-// redux, the row's scale and maximum from shared memory, the accumulators -- is all
-// on the path to shared memory that sets the pace from 32 rows on.
+// redux, the row's scale and maximum from shared memory, the accumulators.
 //
 // P.  Probabilities span more octaves than two codes: next to a key that takes all
 // the weight, a thousand weak ones would vanish.  So P is relative to the maximum
@@ -32,198 +34,34 @@
 // like the rows, two products for S; the values as they are against P in bf16
 // (kind::f16), since a row may see a single small value of a key.
 //
+// Bounds and figures (8 KV heads, 128 dimensions; floor: the cache's bytes at the
+// measured copy rate).  One query a request, 4 rows, 19 x 4096 keys: 31 us, 5.1 TB/s,
+// the ring's depth (a tile of K and V leaves it only after the step's product);
+// 4 x 32768 keys: 49 us, 5.5 TB/s.  Eight queries, 32 rows, 19 x 4096: 34 us, there the
+// softmax warps' instructions.  One request of 4096 keys, 16 splits: 9 us, of which
+// launch, lengths -> table -> copies, tensor memory and the merge are 6.
+//
 // Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
 // O; from 3 the softmax and the accumulators, four warps for 16 rows of a step.
 #include <math.h>
 
-#include "paged.cuh"
+#include "paged_tc.cuh"
 
 namespace {
 
 using namespace sbd_dev;
 
-constexpr int kTile = 128;                   // keys of an MMA; a step is two tiles
 constexpr int kRT = 16;                      // rows of a softmax thread
 constexpr int kControl = 3;                  // warps: pages and TMA, products S, products O
-constexpr int kMaxStages = 8;
 constexpr int kTables = 8 * 1024;            // shared memory outside the operands
-constexpr int kBlkKeys = 32;                 // block keys, padded
-constexpr int kMaxSplits = 16;
 constexpr float kPScale = 256.f;             // P = 2^8 p
 constexpr float kLoScale = 32.f;             // lo codes of P hold 2^5 of the rest
 
-// ------------------------------------------------------------ tcgen05 PTX
-__device__ __forceinline__ void tc_alloc(uint32_t* dst_smem, uint32_t ncols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                   smem_u32(dst_smem)),
-               "r"(ncols)
-               : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tc_dealloc(uint32_t taddr, uint32_t ncols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols)
-               : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() {
-  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_after() {
-  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ bool elect_one() {
-  uint32_t p;
-  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
-  return p != 0;
-}
-__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
-                                          uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void tc_mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
-                                            uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-          smem_u32(bar))
-      : "memory");
-}
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t (&r)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-                 "=r"(r[7])
-               : "r"(taddr));
-}
-__device__ __forceinline__ void tc_wait_ld() {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar,
-                                            int c0, int c1, int c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
-}
-// The maximum over a warp (NaN only where every lane has it).
-__device__ __forceinline__ float redux_max(float v) {
-  float r;
-  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-
-// The same, NaN where any lane has it; and of two.
-__device__ __forceinline__ float redux_max_nan(float v) {
-  float r;
-  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float max_nan(float x, float y) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
-  return r;
-}
-
-// Shared-memory operands of rows of `W` = 32, 64 or 128 bytes, swizzled over W:
-// 16-byte pieces of a row permuted by the row's place, the pattern repeating every
-// 8 rows (one 8 W-byte atom).
-template <int W>
-__device__ __forceinline__ uint32_t swz(uint32_t base, int row, int piece) {
-  constexpr int kMask = W / 16 - 1;
-  constexpr int kShift = W == 128 ? 0 : W == 64 ? 1 : 2;
-  return base + row * W + ((piece ^ ((row >> kShift) & kMask)) << 4);
-}
-// Descriptor of such an operand: 8-row groups 8 W apart; `next` bytes from one
-// atom to the next along a row (MN-major operands wider than an atom).
-template <int W>
-__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t next = 16) {
-  constexpr uint64_t kMode = W == 128 ? 2 : W == 64 ? 4 : 6;
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(next >> 4) << 16 |
-         (uint64_t)(8 * W >> 4) << 32 | (uint64_t)1 << 46 | kMode << 61;
-}
-// e4m3 A and B, fp32 D.
-__device__ __forceinline__ uint32_t idesc_f8(int M, int N, bool mn_major) {
-  return 1u << 4 | (mn_major ? 1u : 0u) << 15 | (mn_major ? 1u : 0u) << 16 |
-         (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24;
-}
-// bf16 A and B, both MN-major, fp32 D.
-__device__ __forceinline__ uint32_t idesc_bf16_mn(int M, int N) {
-  return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(N >> 3) << 17 |
-         (uint32_t)(M >> 4) << 24;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&v);
-}
-__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z),
-               "r"(v.w)
-               : "memory");
-}
-// The same without a branch (what it stores is the warp's, one lane does it).
-__device__ __forceinline__ void st_shared_v4_if(bool p, uint32_t addr, float x, float y, float z, float w) {
-  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t@q st.shared.v4.f32 [%0], {%1,%2,%3,%4};\n\t}"
-               ::"r"(addr), "f"(x), "f"(y), "f"(z), "f"(w), "r"((uint32_t)p)
-               : "memory");
-}
-__device__ __forceinline__ void bar_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-
-// ------------------------------------------------------------ clusters
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
-               "barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t mapa_shared(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
-}
-
-struct Args {
-  const __nv_bfloat16 *q, *kb, *vb;
-  const float *ks, *vs;
-  const int32_t *table, *lens;
-  __nv_bfloat16* out;
-  int* err;
-  int B, k, Hq, Hkv, G, M, max_pages, n_pages, n_causal, splits, chunks;
-  int page_log2;
-  int order;                 // blockIdx.z -> sequence by descending length
-  float scale_log2;
-};
-
 template <int D, int R>
 struct Shape {
-  // The rows' hi and lo codes side by side along N, or one after the other into the
-  // same columns of S.  An MMA of M = 128 takes 53 clocks up to N = 64 and 68 at N =
-  // 128, so the pair costs less side by side, but then the softmax reads two columns
-  // a row and adds them, and at R = 64 it sets the pace.
-  static constexpr bool kBeside = R < 64;
-  static constexpr int kNS = kBeside ? 2 * R : R;      // columns of a tile's S
+  // The rows' hi and lo codes lie side by side along N.  (An MMA of M = 128 takes 53
+  // clocks up to N = 64: one after the other into the same columns costs twice.)
+  static constexpr int kNS = 2 * R;                    // columns of a tile's S
   static constexpr int kNO = 2 * R;                    // columns of O, bytes of a key's row of P
   static constexpr int kOCol = 4 * kNS;                // S: two buffers of two tiles
   static constexpr int kTmemCols = kOCol + 2 * kNO <= 256 ? 256 : 512;
@@ -233,15 +71,14 @@ struct Shape {
   static constexpr int kThreads = 32 * (kControl + kSoftWarps);
   static constexpr int kKV = kTile * D;                // a K or V tile
   static constexpr int kQ = 2 * R * D;
-  // P of a tile takes the place of its K, which is dead by then, where it fits.
-  static constexpr int kP = kTile * kNO;
-  static constexpr bool kPInK = kP <= kKV;
+  // P of a tile takes the place of its K, which is dead by then.
+  static_assert(kTile * kNO <= kKV, "P fits there");
   static constexpr int kPBlk = kBlkKeys * kNO;         // the block's P
   // The block's keys (hi rows, then lo rows), or its values (bf16, 64 dimensions
   // a sub-tile).
   static constexpr int kBlk = 2 * kBlkKeys * D;
   static constexpr int kBlkSub = kBlkKeys * 128;
-  static constexpr int kFixed = 1024 + kQ + (kPInK ? 0 : 4 * kP) + kPBlk + 2 * kBlk;
+  static constexpr int kFixed = 1024 + kQ + kPBlk + 2 * kBlk;
   static constexpr int kLeft = 227 * 1024 - kTables - kFixed;
   static constexpr int kStages = kLeft / (2 * kKV) < kMaxStages ? kLeft / (2 * kKV) : kMaxStages;
   static constexpr int kSmem = kFixed + kStages * 2 * kKV;
@@ -252,68 +89,24 @@ struct Shape {
   static_assert(kBlk + kTile * D <= 2 * kBlk + kStages * 2 * kKV, "reads past the block's keys stay inside");
 };
 
-__device__ __forceinline__ float finite_size(float x) {
-  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-  return u < 0x7f800000u ? __uint_as_float(u) : 0.f;
-}
-// 16 consecutive bf16 values of a row; the D / 16 lanes of a row lie together.
-template <int D>
-struct Piece {
-  uint4 w[2];
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-    w[0] = reinterpret_cast<const uint4*>(p)[0];
-    w[1] = reinterpret_cast<const uint4*>(p)[1];
-  }
-  __device__ __forceinline__ void zero() { w[0] = w[1] = make_uint4(0, 0, 0, 0); }
-  // x = s (hi + lo) for the row's scale s, which it returns: the codes become
-  // piece `c` of rows hi_row and lo_row of the operand at `base`.  What is not
-  // finite becomes NaN.
-  __device__ __forceinline__ float store(uint32_t base, int hi_row, int lo_row, int c) const {
-    float x[16];
-    const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
-    float amax = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[2 * e] = __uint_as_float(u[e] << 16);
-      x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-      amax = fmaxf(amax, fmaxf(finite_size(x[2 * e]), finite_size(x[2 * e + 1])));
-    }
-#pragma unroll
-    for (int o = 1; o < D / 16; o *= 2) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const float s = scale_for(amax), inv = 1.f / s;
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float y[4], h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float v = x[4 * e + i];
-        y[i] = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? __int_as_float(0x7fffffff) : v * inv;
-      }
-      hi[e] = e4m3x4(y[0], y[1], y[2], y[3]);
-      e4m3x4_values(hi[e], h);
-      lo[e] = e4m3x4(y[0] - h[0], y[1] - h[1], y[2] - h[2], y[3] - h[3]);
-    }
-    st_shared_v4(swz<D>(base, hi_row, c), make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    st_shared_v4(swz<D>(base, lo_row, c), make_uint4(lo[0], lo[1], lo[2], lo[3]));
-    return s;
-  }
-};
-
 // Four probabilities as code pairs.  The fp16 pattern of p in [0, 1], shifted right
 // by 7, is the e4m3 pattern of 2^8 p (the exponents are 8 apart, and so are the
-// subnormal steps), so a code is a rounded shift: hi = p to 4 bits, lo = 2^5 (p - hi)
-// to 4 more (exact in fp16, with a sign).  Together they hold p to 2^-9, and to
-// 2^-23 of the tile's largest.
+// subnormal steps), so hi, p to 4 bits, is a rounded shift; lo = 2^5 (p - hi), exact in
+// fp16, to 4 more.  Together they hold p to 2^-9, and to 2^-23 of the step's largest.
 __device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, uint32_t* lo) {
   auto bits = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
   auto half2 = [](uint32_t x) { return *reinterpret_cast<const __half2*>(&x); };
-  const uint32_t a = bits(p01) + 0x00400040u, b = bits(p23) + 0x00400040u;
-  *hi = __byte_perm(a << 1, b << 1, 0x7531);
-  const __half2 up = __float2half2_rn(kLoScale);
-  const uint32_t c = bits(__hmul2(__hsub2(p01, half2(a & 0xff80ff80u)), up)) + 0x00400040u;
-  const uint32_t d = bits(__hmul2(__hsub2(p23, half2(b & 0xff80ff80u)), up)) + 0x00400040u;
-  *lo = __byte_perm(((c << 1) & 0x7fff7fffu) | (c & 0x80008000u), ((d << 1) & 0x7fff7fffu) | (d & 0x80008000u), 0x7531);
+  const uint32_t a = bits(p01), b = bits(p23);         // p <= 1: bits 14, 15 and 30, 31 are 0
+  *hi = __byte_perm(a + a + 0x00800080u, b + b + 0x00800080u, 0x7531);
+  const uint32_t na = ((a + 0x00400040u) & 0xff80ff80u) ^ 0x80008000u;   // -hi
+  const uint32_t nb = ((b + 0x00400040u) & 0xff80ff80u) ^ 0x80008000u;
+  const __half2 up = __float2half2_rn(kPScale * kLoScale);
+  const uint32_t c = bits(__hmul2(__hadd2(p01, half2(na)), up));
+  const uint32_t d = bits(__hmul2(__hadd2(p23, half2(nb)), up));
+  uint16_t x, y;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(x) : "r"(c));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(y) : "r"(d));
+  *lo = (uint32_t)x | (uint32_t)y << 16;
 }
 
 template <int D, int R>
@@ -323,7 +116,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   using C = Shape<D, R>;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
   constexpr int kParts = C::kParts, kSoftWarps = C::kSoftWarps;
-  static_assert(R == 16 || R == 32 || R == 64, "a key's row of P is one swizzle atom");
+  static_assert(R == 16 || R == 32, "a key's row of P is one swizzle atom");
 
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
@@ -331,8 +124,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
-  // a stage's page scales: of the keys; of the values over their step's largest; that
-  __shared__ float ks_sh[kMaxStages][8], vw_sh[kMaxStages][8], vref_sh[kMaxStages];
+  __shared__ PageScales pages;
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
@@ -343,13 +135,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ float lse_sh[R + kMaxSplits];                   // of the rows merged here, a row's splits together
 
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_s = sbase, pblk_s = q_s + C::kQ, p_s = pblk_s + C::kPBlk;
-  const uint32_t bk_s = p_s + (C::kPInK ? 0 : 4 * C::kP), bv_s = bk_s + C::kBlk;
+  const uint32_t q_s = sbase, pblk_s = q_s + C::kQ;
+  const uint32_t bk_s = pblk_s + C::kPBlk, bv_s = bk_s + C::kBlk;
   const uint32_t ring = bv_s + C::kBlk;
   auto k_tile = [&](int j) { return ring + (uint32_t)(j % kStages) * 2 * C::kKV; };
   auto v_tile = [&](int j) { return k_tile(j) + C::kKV; };
-  // P of local tile j
-  auto p_tile = [&](int j) { return C::kPInK ? k_tile(j) : p_s + (uint32_t)(j & 3) * C::kP; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
@@ -404,77 +194,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       tma_prefetch_desc(&tmap_k);
       tma_prefetch_desc(&tmap_v);
     }
-    const int P = 1 << a.page_log2, per_tile = kTile >> a.page_log2;
-    const int p_first = t_begin * per_tile;
-    const int p_end = (int)((min((t_begin + nc) * (long long)kTile, (long long)len) + P - 1) >> a.page_log2);
-    const int32_t* table = a.table + (size_t)b * a.max_pages;
-    // Pages come in windows of 32, one a lane: ids a window ahead, their scales a
-    // tile into the window before.  A page out of range lies past the tensor's
-    // end for the copy, which reads zeros there.
-    auto id_at = [&](int p) {
-      if (p >= p_end) return -1;
-      const int id = table[p];
-      if (id >= 0 && id < a.n_pages) return id;
-      record_error(a.err, SBD_DEVERR_PAGE);
-      return a.n_pages;
-    };
-    auto scale_at = [&](const float* s, int id) {
-      return id >= 0 && id < a.n_pages ? s[(size_t)id * a.Hkv + hkv] : 0.f;
-    };
-    int id = id_at(p_first + lane), id_next = id_at(p_first + 32 + lane);
-    float ks = scale_at(a.ks, id), vs = scale_at(a.vs, id), ks_next = 0.f, vs_next = 0.f;
-    const int per_window = 32 / per_tile;
-    int issued = 0;
-    for (int j = 0; j < nc; ++j) {
-      const int w = j % per_window;
-      if (w == 0 && j > 0) {
-        id = id_next, ks = ks_next, vs = vs_next;
-        id_next = id_at(p_first + (j / per_window + 1) * 32 + lane);
-      }
-      if (w == 1) ks_next = scale_at(a.ks, id_next), vs_next = scale_at(a.vs, id_next);
-      const int stage = j % kStages;
-      const bool freed = mbar_wait(&kv_empty[stage], ((j / kStages) & 1) ^ 1, a.err);
-      if (!__all_sync(0xffffffffu, freed)) break;
-      const int valid = keys_of(j), n_pg = (valid + P - 1) >> a.page_log2;
-      const int src = (w * per_tile + lane) & 31;      // lane i < n_pg: the tile's page i
-      const int pg = __shfl_sync(0xffffffffu, id, src);
-      // Values past the length may be anything (NaN); the products go on to the
-      // next multiple of 32 keys, so those become zeros once the copy is there.
-      const bool tail = (valid & 31) != 0;
-      uint64_t* bar = tail ? &tail_bar : &kv_full[stage];
-      // The copies first; the scales (whose loads may still be on their way) are in
-      // place before the barrier's one arrival.
-      if (lane < n_pg) {
-        const int row = pg < a.n_pages ? pg * a.Hkv + hkv : a.n_pages * a.Hkv;
-        tma_load_3d(k_tile(j) + lane * P * D, &tmap_k, bar, 0, 0, row);
-        tma_load_3d(v_tile(j) + lane * P * D, &tmap_v, bar, 0, 0, row);
-      }
-      issued = j + 1;
-      const float k_sc = __shfl_sync(0xffffffffu, ks, src);
-      const float v_sc = __shfl_sync(0xffffffffu, vs, src);
-      // the largest value scale of the step's pages (lanes without a page have 0)
-      const int pair = (w & ~1) * per_tile;
-      const float v_max = redux_max(lane >= pair && lane < pair + 2 * per_tile ? vs : 0.f);
-      if (lane < n_pg) {
-        ks_sh[stage][lane] = k_sc;
-        vw_sh[stage][lane] = v_max > 0.f ? v_sc / v_max : v_sc * 0.f;
-      }
-      if (lane == 0) vref_sh[stage] = v_max;
-      __syncwarp();
-      if (lane == 0) mbar_arrive_expect_tx(bar, 2 * n_pg * P * D);
-      if (tail) {
-        mbar_wait(&tail_bar, 0, a.err);
-        const int end = (valid + 31) & ~31;
-        for (int c = lane; c < (end - valid) * (D / 16); c += 32)
-          st_shared_v4(v_tile(j) + valid * D + 16 * c, make_uint4(0, 0, 0, 0));
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&kv_full[stage]);
-      }
-    }
-    // no copy is in flight when the CTA ends, whatever became of its consumers
-    for (int j = max(0, issued - kStages); j < issued; ++j)
-      mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
+    load_tiles<D, kStages, kStages, 2>(tmap_k, tmap_v, a, b, hkv, len, t_begin, nc, ring, pages, kv_full, kv_empty, &tail_bar);
   } else if (warp == 1) {
     // ------------------------------------------------ S = K Q^T
     // Ahead of the softmax by the second buffer.  The whole warp runs the loop
@@ -488,14 +208,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const bool leader = elect_one();
     bool ok = n > 0 && mbar_wait(&q_ready, 0, a.err);
     const uint32_t id_s = idesc_f8(kTile, kNS, false);
-    constexpr int kPasses = C::kBeside ? 1 : 2;        // hi codes, then lo codes
     const uint64_t qd = desc<D>(q_s);
     auto product = [&](uint32_t d, uint64_t kd, bool add) {
 #pragma unroll
-      for (int h = 0; h < kPasses; ++h)
-#pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk)
-          tc_mma_f8(d, kd + 2 * kk, qd + (h * R * D / 16 + 2 * kk), id_s, add || h > 0 || kk > 0);
+      for (int kk = 0; kk < D / 32; ++kk) tc_mma_f8(d, kd + 2 * kk, qd + 2 * kk, id_s, add || kk > 0);
     };
     for (int i = 0; i < n && ok; ++i) {
       const uint32_t d = tmem + (uint32_t)((i & 1) * 2 * kNS);
@@ -546,7 +262,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         }
       } else {
         for (int j = 2 * i; j < min(nc, 2 * i + 2); ++j) {
-          const uint64_t vd = desc<D>(v_tile(j)), pd = desc<kNO>(p_tile(j));
+          const uint64_t vd = desc<D>(v_tile(j)), pd = desc<kNO>(k_tile(j));
           const int steps = (keys_of(j) + 31) / 32;
           if (leader) {
 #pragma unroll
@@ -688,34 +404,22 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
             kf0 = bks_sh[key & (kBlkKeys - 1)];
           } else {
             const int pg = key >> a.page_log2;
-            kf0 = ks_sh[st0][pg], vw0 = vw_sh[st0][pg], vref = vref_sh[st0];
-            if (has1) kf1 = ks_sh[st1][pg], vw1 = vw_sh[st1][pg];
+            kf0 = pages.ks[st0][pg], vw0 = pages.vw[st0][pg], vref = pages.vref[st0];
+            if (has1) kf1 = pages.ks[st1][pg], vw1 = pages.vw[st1][pg];
           }
           // Both tiles' columns are read, also where the second has no keys.
           const uint32_t sa = tmem + lane_addr + (uint32_t)(buf * 2 * kNS + r0);
-          if constexpr (C::kBeside) {
-            uint32_t h[16], lo[16];
-            tc_ld16(sa, h);
-            tc_ld16(sa + R, lo);
-            tc_wait_ld();
+          uint32_t h[16], lo[16];
+          tc_ld16(sa, h);
+          tc_ld16(sa + R, lo);
+          tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < kRT; ++r) z0[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf0;
-            tc_ld16(sa + kNS, h);
-            tc_ld16(sa + kNS + R, lo);
-            tc_wait_ld();
+          for (int r = 0; r < kRT; ++r) z0[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf0;
+          tc_ld16(sa + kNS, h);
+          tc_ld16(sa + kNS + R, lo);
+          tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < kRT; ++r) z1[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf1;
-          } else {
-            uint32_t h0[16], h1[16];
-            tc_ld16(sa, h0);
-            tc_ld16(sa + kNS, h1);
-            tc_wait_ld();
-#pragma unroll
-            for (int r = 0; r < kRT; ++r) {
-              z0[r] = __uint_as_float(h0[r]) * kf0;
-              z1[r] = __uint_as_float(h1[r]) * kf1;
-            }
-          }
+          for (int r = 0; r < kRT; ++r) z1[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf1;
           if (blk) {
 #pragma unroll
             for (int r = 0; r < kRT; ++r) z0[r] = key < vis_sh[r0 + r] ? z0[r] : -INFINITY;
@@ -777,7 +481,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
             p_codes(__hmul2(__floats2half2_rn(p[0], p[1]), w0), __hmul2(__floats2half2_rn(p[2], p[3]), w0), &hi0[e], &lo0[e]);
             p_codes(__hmul2(__floats2half2_rn(q[0], q[1]), w1), __hmul2(__floats2half2_rn(q[2], q[3]), w1), &hi1[e], &lo1[e]);
           }
-          const uint32_t p0 = p_tile(j0), p1 = p_tile(j0 + 1);
+          const uint32_t p0 = k_tile(j0), p1 = k_tile(j0 + 1);
           st_shared_v4(swz<kNO>(p0, key, r0 / 16), make_uint4(hi0[0], hi0[1], hi0[2], hi0[3]));
           st_shared_v4(swz<kNO>(p0, key, (R + r0) / 16), make_uint4(lo0[0], lo0[1], lo0[2], lo0[3]));
           if (has1) {
@@ -808,7 +512,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       const uint32_t steps = __float_as_uint(sum_sh[sw][own]) - 32u * 0x3f800000u;
       l = fmaf(l, keep, has0 ? (float)steps * (1.f / (1 << 22)) * g : 0.f);
       __syncwarp();                                    // f of the step before is read
-      if (!has0) vref = blk ? 1.f : vref_sh[st0];
+      if (!has0) vref = blk ? 1.f : pages.vref[st0];
       f_sh[sw][0][own] = g * vref * (1.f / kPScale);
       f_sh[sw][1][own] = keep;
       moved = __any_sync(0xffffffffu, m_new != m_ref && m_ref != -INFINITY);
@@ -886,62 +590,36 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // other CTAs, all splits of a row requested at once, took 3.5 us of one user's
   // 15: the requests were 250 instructions that run once.)
   cluster_sync_all();
-  constexpr int kPer = D / 32;
-#pragma unroll 1
-  for (int slot = warp; slot * a.splits + split < R; slot += C::kThreads / 32) {
-    const int row = chunk * R + slot * a.splits + split;
-    if (row >= a.M) break;
-    const float l = lane < a.splits ? lse_sh[slot * a.splits + lane] : -INFINITY;
-    const float mx = warp_max(l);
-    const float w = l == -INFINITY ? 0.f : exp2f(l - mx);
-    const float inv = 1.f / warp_sum(w);
-    const float* src = reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))) +
-                       slot * a.splits * C::kPStride + kPer * lane;
-    float o[kPer];
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) o[c] = 0.f;
-#pragma unroll 2
-    for (int s = 0; s < a.splits; ++s) {
-      const float ws = __shfl_sync(0xffffffffu, w, s);
-      if (!(ws == 0.f)) {
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) o[c] = fmaf(ws, src[s * C::kPStride + c], o[c]);
-      }
-    }
-    const int i = row / a.G;
-    __nv_bfloat16* dst =
-        a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + kPer * lane;
-#pragma unroll
-    for (int c = 0; c < kPer; c += 2)
-      *reinterpret_cast<__nv_bfloat162*>(dst + c) = __floats2bfloat162_rn(o[c] * inv, o[c + 1] * inv);
-  }
+  merge_rows<D, R, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh, b, hkv,
+                                     chunk, split);
 }
 
-struct Kernel {
-  const void* fn;
-  size_t smem;
-  int threads;
-};
 template <int D, int R>
-Kernel instance() {
+TcKernel instance() {
   return {(const void*)paged_tc_kernel<D, R>, Shape<D, R>::kSmem, Shape<D, R>::kThreads};
 }
-template <int D>
-Kernel kernel_of(int R) {
-  return R == 16 ? instance<D, 16>() : R == 32 ? instance<D, 32>() : instance<D, 64>();
+TcKernel kernel_for(int D, int R) {
+  if (R == 128) return sbd::paged_rows_kernel_for(D);
+  if (D == 128) return R == 16 ? instance<128, 16>() : instance<128, 32>();
+  return R == 16 ? instance<64, 16>() : instance<64, 32>();
 }
-Kernel kernel_for(int D, int R) { return D == 128 ? kernel_of<128>(R) : kernel_of<64>(R); }
 
 }  // namespace
 
 namespace sbd {
 
 void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
-  p->rows = p->M <= 16 ? 16 : p->M <= 32 ? 32 : 64;
+  // Up to 32 rows keys are on the lanes, above them rows, 128 a CTA (less than 128 leaves
+  // lanes idle, and is faster all the same: see the head of this file).
+  p->rows = p->M <= 16 ? 16 : p->M <= 32 ? 32 : 128;
   p->chunks = (p->M + p->rows - 1) / p->rows;
-  const Kernel kern = kernel_for(p->D, p->rows);
+  const TcKernel kern = kernel_for(p->D, p->rows);
   const long long jobs = (long long)p->B * p->Hkv * p->chunks;
   const long long tiles = ((long long)p->max_pages * p->P + kTile - 1) / kTile + 1;
+  // Splits.  The host knows the capacity and not the lengths, so it splits while one wave
+  // holds all CTAs, and never into a second: 16 requests of 4096 keys on 128 CTAs take
+  // 29 us whole and 38 in halves, of 100 to 8000 keys 48 whole and 36 in halves, of 200
+  // to 600 keys in a cache for many more 10 and 18.
   int s = 1;
   if (num_splits > 0) {
     for (s = num_splits < kMaxSplits ? num_splits : kMaxSplits; s > 1; --s)
@@ -954,11 +632,10 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
       if (cluster_slots(kern.fn, kern.threads, kern.smem, s) >= jobs) break;
   }
   p->splits = s < 1 ? 1 : s;
-  p->cluster = p->splits > 1;
 }
 
 sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st) {
-  const Kernel kern = kernel_for(p.D, p.rows);
+  const TcKernel kern = kernel_for(p.D, p.rows);
   // Codes as bytes: (D, tokens of a page, page and head); a copy is a page.
   CUtensorMap tk, tv;
   const uint64_t dims[3] = {(uint64_t)p.D, (uint64_t)p.P, (uint64_t)p.n_pages * p.Hkv};

@@ -313,6 +313,51 @@ def test_attention_of_more_jobs_than_sms(sbd, B, k, Hq, H, D, page, hi):
     _attend(sbd, _attention_case(rng, B, k, Hq, H, D, page, lens), n_causal=k // 2)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("k,Hq,H,n_causal", [(9, 8, 2, 0), (16, 8, 1, 8), (16, 12, 2, 16), (32, 4, 1, 16), (25, 16, 2, 3), (32, 12, 1, 1)])
+def test_attention_of_many_rows(sbd, k, Hq, H, n_causal, D):
+    """33 to 384 packed rows of a KV head: rows on the lanes, 128 a CTA."""
+    rng = np.random.default_rng(k + Hq + D)
+    for page, lens, splits in ((16, [0, 5, 1000], 0), (128, [129, 2300], 1), (64, [640, 31, 0], 3)):
+        _attend(sbd, _attention_case(rng, len(lens), k, Hq, H, D, page, lens), n_causal=n_causal, num_splits=splits)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_many_rows_extremes(sbd, D):
+    rng = np.random.default_rng(D)
+    for spread, scale in ((30.0, 0.0), (0.01, 0.0), (2.0, 1e-6)):
+        _attend(sbd, _attention_case(rng, 2, 32, 4, 1, D, 64, [900, 333], spread=spread), scale=scale)
+    got = _attend(sbd, _attention_case(rng, 1, 32, 4, 1, D, 64, [6000], spread=1.0, sink=0.85))
+    assert np.abs(got).max() > 0
+    # block values that a causal row does not see, rows of NaN, and a NaN in the cache
+    case = _attention_case(rng, 2, 32, 4, 1, D, 32, [40, 300])
+    case[6][0, 20] = np.inf
+    case[0][1, 3] = np.nan
+    got = _attend(sbd, case, n_causal=32, check=False)
+    assert np.isfinite(got[0, :20]).all() and not np.isfinite(got[0, 20:]).any()
+    assert np.isnan(got[1, 3]).all() and np.isfinite(np.delete(got[1], 3, 0)).all()
+    case = _attention_case(rng, 2, 32, 4, 1, D, 32, [40, 300])
+    case[1][1][case[3][0, 0], :, 7] = 0x7F
+    got = _attend(sbd, case, check=False)
+    assert np.isnan(got[0]).all() and np.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("k,D", [(4, 64), (8, 128), (16, 128), (32, 64)])
+def test_attention_of_partial_tiles_after_nan_everywhere(sbd, k, D):
+    """A call before this one has left NaN all over shared memory: nothing of a
+    tile's places without a page may reach the result."""
+    import torch
+    rng = np.random.default_rng(k)
+    nan = [np.full((160, 8, 4, 128), np.nan), [np.full((322, 2, 16, 128), 0x7F, np.uint8)] * 2, [np.full((322, 2), np.nan, np.float32)] * 2,
+           np.arange(320, dtype=np.int32).reshape(160, 2), np.full(160, 32, np.int32), *[np.full((160, 8, 2, 128), np.nan)] * 2]
+    case = _attention_case(rng, 160, k, 4, 2, D, 16, rng.integers(1, 120, 160))
+    _attend(sbd, case)
+    for _ in range(3):
+        _attend(sbd, nan, "float32", check=False)
+        torch.cuda.synchronize()
+        _attend(sbd, case)
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 def test_attention_peaked_flat_and_scaled(sbd, dtype):
     rng = np.random.default_rng(9)
