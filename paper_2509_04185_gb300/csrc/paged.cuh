@@ -25,6 +25,7 @@ struct AttnQ8Plan {
   int B, k, Hq, Hkv, G, D, P, max_pages, n_pages, M, n_causal;
   int rows, chunks;   // packed rows of a CTA, and how many CTAs share a KV head's rows
   int splits;         // key ranges of a (sequence, KV head, chunk): a thread-block cluster
+  int ctas;           // tcgen05 kernel: that share an SM
   float scale_log2;   // softmax scale * log2(e)
   bool bf16;
 };

@@ -432,6 +432,7 @@ AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d) {
   p.rows = kern.rows;
   p.chunks = (p.M + kern.rows - 1) / kern.rows;
   p.splits = fma_splits(p, kern, d.num_splits);
+  p.ctas = 1;
   return p;
 }
 

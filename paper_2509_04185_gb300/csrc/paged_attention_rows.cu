@@ -145,6 +145,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
   __shared__ PageScales pages;
+  __shared__ __align__(16) int order_sh[kMaxOrder];
   __shared__ __align__(16) float bks_sh[kBlkKeys];
   __shared__ float c_sh[kRows];                        // a row's score scale, log2 units
   __shared__ float2 stat_sh[4][kRows];                 // a step's maximum and sum of a row
@@ -182,11 +183,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // What the previous grid may still write is read from here on.
   grid_dependency_wait();
   const int cap = a.max_pages << a.page_log2;
-  if (a.order) {
-    longest_first_pick(a.lens, a.B, cap, blockIdx.z, &b_pick);
-    __syncthreads();
-  }
-  const int b = a.order ? b_pick : (int)blockIdx.z;
+  const int b = a.order ? longest_first(a.lens, a.B, cap, blockIdx.z, order_sh, &b_pick) : (int)blockIdx.z;
   int len = a.lens[b];
   if (len < 0 || len > cap) {
     if (threadIdx.x == 0 && split == 0 && blockIdx.y == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);

@@ -57,14 +57,17 @@ constexpr int kTables = 8 * 1024;            // shared memory outside the operan
 constexpr float kPScale = 256.f;             // P = 2^8 p
 constexpr float kLoScale = 32.f;             // lo codes of P hold 2^5 of the rest
 
-template <int D, int R>
+template <int D, int R, int kCtas>
 struct Shape {
   // The rows' hi and lo codes lie side by side along N.  (An MMA of M = 128 takes 53
   // clocks up to N = 64: one after the other into the same columns costs twice.)
   static constexpr int kNS = 2 * R;                    // columns of a tile's S
   static constexpr int kNO = 2 * R;                    // columns of O, bytes of a key's row of P
-  static constexpr int kOCol = 4 * kNS;                // S: two buffers of two tiles
-  static constexpr int kTmemCols = kOCol + 2 * kNO <= 256 ? 256 : 512;
+  // Two buffers of S (of two tiles), or one for each of two CTAs that share an SM.
+  static constexpr int kSBufs = 2 / kCtas;
+  static constexpr int kOCol = kSBufs * 2 * kNS;
+  static constexpr int kTmemCols = kOCol + 2 * kNO <= 128 ? 128 : kOCol + 2 * kNO <= 256 ? 256 : 512;
+  static_assert(kCtas * kTmemCols <= 512, "tensor memory holds them");
   // Four softmax warps take 16 rows of a step.
   static constexpr int kParts = R / kRT;
   static constexpr int kSoftWarps = 4 * kParts;
@@ -79,11 +82,11 @@ struct Shape {
   static constexpr int kBlk = 2 * kBlkKeys * D;
   static constexpr int kBlkSub = kBlkKeys * 128;
   static constexpr int kFixed = 1024 + kQ + kPBlk + 2 * kBlk;
-  static constexpr int kLeft = 227 * 1024 - kTables - kFixed;
+  static constexpr int kLeft = (228 / kCtas - 1) * 1024 - kTables - kFixed;
   static constexpr int kStages = kLeft / (2 * kKV) < kMaxStages ? kLeft / (2 * kKV) : kMaxStages;
   static constexpr int kSmem = kFixed + kStages * 2 * kKV;
   static constexpr int kPStride = D + 4;               // floats of a partial row
-  static_assert(kStages >= 4, "two steps of two tiles");
+  static_assert(kStages >= 4 / kCtas, "two steps of two tiles");
   static_assert(kPBlk % 1024 == 0, "operands begin on 1 KB");
   static_assert((R + kMaxSplits) * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
   static_assert(kBlk + kTile * D <= 2 * kBlk + kStages * 2 * kKV, "reads past the block's keys stay inside");
@@ -109,11 +112,12 @@ __device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, 
   *lo = (uint32_t)x | (uint32_t)y << 16;
 }
 
-template <int D, int R>
-__global__ void __launch_bounds__(Shape<D, R>::kThreads, 1)
+template <int D, int R, int kCtas>
+__global__ void __launch_bounds__(Shape<D, R, kCtas>::kThreads, kCtas)
 paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
-  using C = Shape<D, R>;
+  using C = Shape<D, R, kCtas>;
+  constexpr int kSBufs = C::kSBufs;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
   constexpr int kParts = C::kParts, kSoftWarps = C::kSoftWarps;
   static_assert(R == 16 || R == 32, "a key's row of P is one swizzle atom");
@@ -125,6 +129,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
   __shared__ PageScales pages;
+  __shared__ __align__(16) int order_sh[kMaxOrder];
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
   __shared__ int vis_sh[R];                            // block keys that it sees
@@ -167,11 +172,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // and the first copies, and the rows are fetched side by side.
   grid_dependency_wait();
   const int cap = a.max_pages << a.page_log2;
-  if (a.order) {
-    longest_first_pick(a.lens, a.B, cap, blockIdx.z, &b_pick);
-    __syncthreads();
-  }
-  const int b = a.order ? b_pick : (int)blockIdx.z;
+  const int b = a.order ? longest_first(a.lens, a.B, cap, blockIdx.z, order_sh, &b_pick) : (int)blockIdx.z;
   int len = a.lens[b];
   if (len < 0 || len > cap) {
     if (threadIdx.x == 0 && split == 0 && blockIdx.y == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
@@ -214,8 +215,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       for (int kk = 0; kk < D / 32; ++kk) tc_mma_f8(d, kd + 2 * kk, qd + 2 * kk, id_s, add || kk > 0);
     };
     for (int i = 0; i < n && ok; ++i) {
-      const uint32_t d = tmem + (uint32_t)((i & 1) * 2 * kNS);
-      ok = mbar_wait(&s_free[i & 1], ((i >> 1) & 1) ^ 1, a.err);
+      const int buf = i % kSBufs;
+      const uint32_t d = tmem + (uint32_t)(buf * 2 * kNS);
+      ok = mbar_wait(&s_free[buf], (i / kSBufs & 1) ^ 1, a.err);
       if (has_block && i == n - 1) {
         ok = ok && mbar_wait(&blk_ready, 0, a.err);
         ok = __all_sync(0xffffffffu, ok);
@@ -235,8 +237,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         if (!ok) break;
       }
       if (leader) {
-        tc_commit(&s_full[i & 1]);
-        mbar_arrive(&s_full[i & 1]);
+        tc_commit(&s_full[buf]);
+        mbar_arrive(&s_full[buf]);
       }
       __syncwarp();
     }
@@ -385,7 +387,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (lane == 0) mbar_arrive(&o_free[i & 1]);
     };
     for (int i = 0; i < n; ++i) {
-      const int buf = i & 1, phase = (i >> 1) & 1;
+      const int buf = i % kSBufs, phase = i / kSBufs & 1;
       const bool blk = has_block && i == n - 1;
       const int j0 = 2 * i, st0 = j0 % kStages, st1 = (j0 + 1) % kStages;
       const int valid0 = blk ? a.k : keys_of(j0), valid1 = blk ? 0 : keys_of(j0 + 1);
@@ -594,14 +596,18 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                                      chunk, split);
 }
 
-template <int D, int R>
+template <int D, int R, int kCtas>
 TcKernel instance() {
-  return {(const void*)paged_tc_kernel<D, R>, Shape<D, R>::kSmem, Shape<D, R>::kThreads};
+  return {(const void*)paged_tc_kernel<D, R, kCtas>, Shape<D, R, kCtas>::kSmem, Shape<D, R, kCtas>::kThreads};
 }
-TcKernel kernel_for(int D, int R) {
+template <int D>
+TcKernel kernel_of(int R, int ctas) {
+  if (R == 32) return instance<D, 32, 1>();
+  return ctas == 1 ? instance<D, 16, 1>() : instance<D, 16, 2>();
+}
+TcKernel kernel_for(int D, int R, int ctas) {
   if (R == 128) return sbd::paged_rows_kernel_for(D);
-  if (D == 128) return R == 16 ? instance<128, 16>() : instance<128, 32>();
-  return R == 16 ? instance<64, 16>() : instance<64, 32>();
+  return D == 128 ? kernel_of<128>(R, ctas) : kernel_of<64>(R, ctas);
 }
 
 }  // namespace
@@ -613,29 +619,43 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
   // lanes idle, and is faster all the same: see the head of this file).
   p->rows = p->M <= 16 ? 16 : p->M <= 32 ? 32 : 128;
   p->chunks = (p->M + p->rows - 1) / p->rows;
-  const TcKernel kern = kernel_for(p->D, p->rows);
-  const long long jobs = (long long)p->B * p->Hkv * p->chunks;
+  const long long jobs = (long long)p->B * p->Hkv * p->chunks, sms = num_sms();
   const long long tiles = ((long long)p->max_pages * p->P + kTile - 1) / kTile + 1;
   // Splits.  The host knows the capacity and not the lengths, so it splits while one wave
   // holds all CTAs, and never into a second: 16 requests of 4096 keys on 128 CTAs take
   // 29 us whole and 38 in halves, of 100 to 8000 keys 48 whole and 36 in halves, of 200
   // to 600 keys in a cache for many more 10 and 18.
-  int s = 1;
-  if (num_splits > 0) {
-    for (s = num_splits < kMaxSplits ? num_splits : kMaxSplits; s > 1; --s)
-      if (cluster_slots(kern.fn, kern.threads, kern.smem, s) > 0) break;
-  } else if (jobs > 0) {
-    // one wave of CTAs, the clusters of all jobs at once
-    long long most = num_sms() / jobs;
-    if (most > tiles) most = tiles;
-    for (s = most < kMaxSplits ? (int)most : kMaxSplits; s > 1; --s)
-      if (cluster_slots(kern.fn, kern.threads, kern.smem, s) >= jobs) break;
+  const auto fill = [&](long long slots) {
+    const long long most = jobs > 0 ? slots / jobs : 1;
+    return (int)(most > kMaxSplits ? kMaxSplits : most > tiles ? tiles : most);
+  };
+  int s = num_splits > 0 ? num_splits : fill(sms);
+  // Up to 16 rows two CTAs may share an SM, with half of the ring each (32 rows would
+  // spill at their 80 registers).
+  // More CTAs than a wave: the start of one hides behind the other (64 requests, one query
+  // each, 500 keys: 35 -> 25 us).  At 128 dimensions the ring is short for that, so only with
+  // a capacity of 1024 keys, or from three waves on (64 requests of 0 .. 4000 keys 68 -> 60
+  // us, of 4000 118 -> 124; 26 of 0 .. 4000 29 -> 51).
+  p->ctas = 1;
+  if (p->rows == 16 && jobs * (s < 1 ? 1 : s) > sms && (p->D == 64 || tiles <= 9 || jobs > 3 * sms)) p->ctas = 2;
+  // At 64 dimensions also in one wave, where five tiles and more are left to a split (19
+  // requests of 4096 keys 28 -> 22 us, 4 of 32000 49 -> 43; 8 of 500 keys 9.1 -> 10.5).
+  if (p->rows == 16 && p->D == 64 && num_splits == 0 && fill(2 * sms) > s && tiles >= 5 * fill(2 * sms)) {
+    p->ctas = 2;
+    s = fill(2 * sms);
   }
+  if (s > kMaxSplits) s = kMaxSplits;
+  // (Asked for two CTAs an SM, the driver still answers for one.)
+  const TcKernel kern = kernel_for(p->D, p->rows, p->ctas), one = kernel_for(p->D, p->rows, 1);
+  for (; s > 1; --s)
+    if (cluster_slots(kern.fn, kern.threads, kern.smem, s) > 0 &&
+        p->ctas * cluster_slots(one.fn, one.threads, one.smem, s) >= (num_splits > 0 ? 1 : jobs))
+      break;
   p->splits = s < 1 ? 1 : s;
 }
 
 sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st) {
-  const TcKernel kern = kernel_for(p.D, p.rows);
+  const TcKernel kern = kernel_for(p.D, p.rows, p.ctas);
   // Codes as bytes: (D, tokens of a page, page and head); a copy is a page.
   CUtensorMap tk, tv;
   const uint64_t dims[3] = {(uint64_t)p.D, (uint64_t)p.P, (uint64_t)p.n_pages * p.Hkv};
@@ -672,7 +692,7 @@ sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStre
   a.page_log2 = log2_page(p.P);
   // more CTAs than one wave: the longest sequences first (the pick costs B^2
   // comparisons a CTA, hence the limit)
-  a.order = p.B > 1 && p.B <= 128 &&
+  a.order = p.B > 1 && p.B <= kMaxOrder &&
             (long long)p.B * p.Hkv * p.chunks * p.splits > num_sms();
   a.scale_log2 = p.scale_log2;
   s = allow_smem(kern.fn, kern.smem, "cudaFuncSetAttribute(paged_tc_kernel)");

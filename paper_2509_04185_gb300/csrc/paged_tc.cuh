@@ -11,6 +11,7 @@ constexpr int kTile = 128;                   // keys of an MMA; a step is two ti
 constexpr int kMaxStages = 8;
 constexpr int kBlkKeys = 32;                 // block keys, padded
 constexpr int kMaxSplits = 16;
+constexpr int kMaxOrder = 128;               // sequences that a launch sorts by length
 
 // ------------------------------------------------------------ tcgen05 PTX
 __device__ __forceinline__ void tc_alloc(uint32_t* dst_smem, uint32_t ncols) {
@@ -228,6 +229,28 @@ struct Piece {
     return s;
   }
 };
+
+// The sequence of rank z in descending length (ties by index), for launches of more than
+// one wave: the longest start first.  All threads come; B <= kMaxOrder, `sh` has room for
+// as many.  (Lengths compared from shared memory, four at a time: from global memory one
+// by one took a microsecond of a CTA's seven at 64 sequences.)
+__device__ __forceinline__ int longest_first(const int32_t* lens, int B, int cap, int z, int* sh, int* pick) {
+  const int t = threadIdx.x;
+  if (t < kMaxOrder) sh[t] = t < B ? min(max(lens[t], 0), cap) : -1;
+  __syncthreads();
+  if (t < B) {
+    const int mine = sh[t];
+    int rank = 0;
+    for (int j = 0; j < B; j += 4) {
+      const int4 x = *reinterpret_cast<const int4*>(sh + j);
+      rank += (x.x > mine || (x.x == mine && j < t)) + (x.y > mine || (x.y == mine && j + 1 < t)) +
+              (x.z > mine || (x.z == mine && j + 2 < t)) + (x.w > mine || (x.w == mine && j + 3 < t));
+    }
+    if (rank == z) *pick = t;
+  }
+  __syncthreads();
+  return *pick;
+}
 
 // One warp brings the tiles t_begin .. t_begin + nc - 1 of a sequence's cache into the
 // ring of kStages stages (a tile of K, then of V) and their pages' scales to kSlots
