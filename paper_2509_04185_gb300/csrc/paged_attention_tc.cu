@@ -12,7 +12,8 @@
 //                                     B = the rows' hi codes, then their lo codes
 //   O[dim, (hi|lo) row] += V^T P^T    A = V tile (MN-major), B = P (MN-major)
 //
-// so that N follows the rows of the call (R = 16 or 32 a CTA) and a thread of the
+// so that N follows the rows of the call (R = 16 or 32 a CTA, 8 of 16 computed on for up
+// to 8) and a thread of the
 // softmax owns one key: its page's scales are scalars of the thread, masks a
 // comparison, a row's maximum and sum one redux a warp.  Above 32 rows those
 // reductions cost more than the tile's loads, and rows are on the lanes
@@ -26,7 +27,7 @@
 // the weight, a thousand weak ones would vanish.  So P is relative to the maximum
 // of its own step (times the value scale over the step's largest, and 2^8), every
 // step's product starts at zero, and the softmax warps add the product of the step
-// before to fp32 accumulators in registers (16 rows, a dimension a thread), weighted
+// before to fp32 accumulators in registers (8 rows, a dimension a thread), weighted
 // 2^(m_step - m).  No accumulator in tensor memory is ever rescaled, and no warp
 // waits for a product that has just been asked for.
 //
@@ -35,14 +36,16 @@
 // (kind::f16), since a row may see a single small value of a key.
 //
 // Bounds and figures (8 KV heads, 128 dimensions; floor: the cache's bytes at the
-// measured copy rate).  One query a request, 4 rows, 19 x 4096 keys: 31 us, 5.1 TB/s,
-// the ring's depth (a tile of K and V leaves it only after the step's product);
-// 4 x 32768 keys: 49 us, 5.5 TB/s.  Eight queries, 32 rows, 19 x 4096: 34 us, there the
-// softmax warps' instructions.  One request of 4096 keys, 16 splits: 9 us, of which
-// launch, lengths -> table -> copies, tensor memory and the merge are 6.
+// measured copy rate).  One query a request, 4 rows: 4 x 32768 keys 45.5 us, 5.9 TB/s of
+// 6.8 on 128 of 152 SMs; 19 x 4096 keys 30 us, 5.3 TB/s, of which the start, before any
+// copy is under way, is 4.  Eight queries, 32 rows, 19 x 4096: 34 us, the softmax warps'
+// instructions.  One request of 4096 keys in 12 splits: 8 us, of which launch, lengths ->
+// table -> copies, tensor memory and the merge are 6.
 //
 // Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
-// O; from 3 the softmax and the accumulators, four warps for 16 rows of a step.
+// O; from 3 the softmax and the accumulators, four warps for 8 rows of a step: with 16
+// rows a warp's instructions were the longer part of a step (51 us instead of 45.5 for
+// 4 rows of 16, 31.1 instead of 30.2 for 16).
 #include <math.h>
 
 #include "paged_tc.cuh"
@@ -51,13 +54,13 @@ namespace {
 
 using namespace sbd_dev;
 
-constexpr int kRT = 16;                      // rows of a softmax thread
 constexpr int kControl = 3;                  // warps: pages and TMA, products S, products O
+constexpr int kRT = 8;                       // rows of a softmax thread
 constexpr int kTables = 8 * 1024;            // shared memory outside the operands
 constexpr float kPScale = 256.f;             // P = 2^8 p
 constexpr float kLoScale = 32.f;             // lo codes of P hold 2^5 of the rest
 
-template <int D, int R, int kCtas>
+template <int D, int R, int kUse, int kCtas>
 struct Shape {
   // The rows' hi and lo codes lie side by side along N.  (An MMA of M = 128 takes 53
   // clocks up to N = 64: one after the other into the same columns costs twice.)
@@ -68,8 +71,9 @@ struct Shape {
   static constexpr int kOCol = kSBufs * 2 * kNS;
   static constexpr int kTmemCols = kOCol + 2 * kNO <= 128 ? 128 : kOCol + 2 * kNO <= 256 ? 256 : 512;
   static_assert(kCtas * kTmemCols <= 512, "tensor memory holds them");
-  // Four softmax warps take 16 rows of a step.
-  static constexpr int kParts = R / kRT;
+  // Four softmax warps take 8 rows of a step, of the first kUse (what the others' columns
+  // hold reaches no column that is read).
+  static constexpr int kParts = kUse / kRT;
   static constexpr int kSoftWarps = 4 * kParts;
   static constexpr int kThreads = 32 * (kControl + kSoftWarps);
   static constexpr int kKV = kTile * D;                // a K or V tile
@@ -112,11 +116,15 @@ __device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, 
   *lo = (uint32_t)x | (uint32_t)y << 16;
 }
 
-template <int D, int R, int kCtas>
-__global__ void __launch_bounds__(Shape<D, R, kCtas>::kThreads, kCtas)
+__device__ __forceinline__ void st_shared_v2(uint32_t addr, const uint32_t (&x)[2]) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x[0]), "r"(x[1]) : "memory");
+}
+
+template <int D, int R, int kUse, int kCtas>
+__global__ void __launch_bounds__(Shape<D, R, kUse, kCtas>::kThreads, kCtas)
 paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
-  using C = Shape<D, R, kCtas>;
+  using C = Shape<D, R, kUse, kCtas>;
   constexpr int kSBufs = C::kSBufs;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
   constexpr int kParts = C::kParts, kSoftWarps = C::kSoftWarps;
@@ -280,7 +288,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   } else {
     // ------------------------------------------------ softmax and accumulators
     const int sw = warp - kControl, quad = warp & 3, part = sw / 4;
-    const int r0 = part * kRT;                         // its rows: r0 .. r0 + 15
+    const int r0 = part * kRT;                         // its rows: r0 .. r0 + kRT - 1
     uint32_t tmem = 0;
     const int key = quad * 32 + lane;                  // of both tiles
     const int at = sw * 32 + lane;
@@ -411,14 +419,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           }
           // Both tiles' columns are read, also where the second has no keys.
           const uint32_t sa = tmem + lane_addr + (uint32_t)(buf * 2 * kNS + r0);
-          uint32_t h[16], lo[16];
-          tc_ld16(sa, h);
-          tc_ld16(sa + R, lo);
+          uint32_t h[kRT], lo[kRT];
+          tc_ld8(sa, h);
+          tc_ld8(sa + R, lo);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < kRT; ++r) z0[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf0;
-          tc_ld16(sa + kNS, h);
-          tc_ld16(sa + kNS + R, lo);
+          tc_ld8(sa + kNS, h);
+          tc_ld8(sa + kNS + R, lo);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < kRT; ++r) z1[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf1;
@@ -475,20 +483,20 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         };
         if (!blk) {
           const __half2 w0 = __float2half2_rn(vw0), w1 = __float2half2_rn(vw1);
-          uint32_t hi0[4], lo0[4], hi1[4], lo1[4];
+          uint32_t hi0[kRT / 4], lo0[kRT / 4], hi1[kRT / 4], lo1[kRT / 4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < kRT / 4; ++e) {
             float p[4], q[4];
             probs(4 * e, p, q);
             p_codes(__hmul2(__floats2half2_rn(p[0], p[1]), w0), __hmul2(__floats2half2_rn(p[2], p[3]), w0), &hi0[e], &lo0[e]);
             p_codes(__hmul2(__floats2half2_rn(q[0], q[1]), w1), __hmul2(__floats2half2_rn(q[2], q[3]), w1), &hi1[e], &lo1[e]);
           }
-          const uint32_t p0 = k_tile(j0), p1 = k_tile(j0 + 1);
-          st_shared_v4(swz<kNO>(p0, key, r0 / 16), make_uint4(hi0[0], hi0[1], hi0[2], hi0[3]));
-          st_shared_v4(swz<kNO>(p0, key, (R + r0) / 16), make_uint4(lo0[0], lo0[1], lo0[2], lo0[3]));
+          const uint32_t p0 = k_tile(j0) + r0 % 16, p1 = k_tile(j0 + 1) + r0 % 16;
+          st_shared_v2(swz<kNO>(p0, key, r0 / 16), hi0);
+          st_shared_v2(swz<kNO>(p0, key, (R + r0) / 16), lo0);
           if (has1) {
-            st_shared_v4(swz<kNO>(p1, key, r0 / 16), make_uint4(hi1[0], hi1[1], hi1[2], hi1[3]));
-            st_shared_v4(swz<kNO>(p1, key, (R + r0) / 16), make_uint4(lo1[0], lo1[1], lo1[2], lo1[3]));
+            st_shared_v2(swz<kNO>(p1, key, r0 / 16), hi1);
+            st_shared_v2(swz<kNO>(p1, key, (R + r0) / 16), lo1);
           }
         } else {
 #pragma unroll
@@ -596,18 +604,20 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                                      chunk, split);
 }
 
-template <int D, int R, int kCtas>
+template <int D, int R, int kUse, int kCtas>
 TcKernel instance() {
-  return {(const void*)paged_tc_kernel<D, R, kCtas>, Shape<D, R, kCtas>::kSmem, Shape<D, R, kCtas>::kThreads};
+  using C = Shape<D, R, kUse, kCtas>;
+  return {(const void*)paged_tc_kernel<D, R, kUse, kCtas>, C::kSmem, C::kThreads};
 }
 template <int D>
-TcKernel kernel_of(int R, int ctas) {
-  if (R == 32) return instance<D, 32, 1>();
-  return ctas == 1 ? instance<D, 16, 1>() : instance<D, 16, 2>();
+TcKernel kernel_of(int M, int ctas) {
+  if (M > 16) return instance<D, 32, 32, 1>();
+  if (M > 8) return ctas == 1 ? instance<D, 16, 16, 1>() : instance<D, 16, 16, 2>();
+  return ctas == 1 ? instance<D, 16, 8, 1>() : instance<D, 16, 8, 2>();
 }
-TcKernel kernel_for(int D, int R, int ctas) {
-  if (R == 128) return sbd::paged_rows_kernel_for(D);
-  return D == 128 ? kernel_of<128>(R, ctas) : kernel_of<64>(R, ctas);
+TcKernel kernel_for(int D, int M, int ctas) {
+  if (M > 32) return sbd::paged_rows_kernel_for(D);
+  return D == 128 ? kernel_of<128>(M, ctas) : kernel_of<64>(M, ctas);
 }
 
 }  // namespace
@@ -633,7 +643,7 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
   // Up to 16 rows two CTAs may share an SM, with half of the ring each (32 rows would
   // spill at their 80 registers).
   // More CTAs than a wave: the start of one hides behind the other (64 requests, one query
-  // each, 500 keys: 35 -> 25 us).  At 128 dimensions the ring is short for that, so only with
+  // each, 500 keys: 33 -> 22 us).  At 128 dimensions the ring is short for that, so only with
   // a capacity of 1024 keys, or from three waves on (64 requests of 0 .. 4000 keys 68 -> 60
   // us, of 4000 118 -> 124; 26 of 0 .. 4000 29 -> 51).
   p->ctas = 1;
@@ -646,7 +656,7 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
   }
   if (s > kMaxSplits) s = kMaxSplits;
   // (Asked for two CTAs an SM, the driver still answers for one.)
-  const TcKernel kern = kernel_for(p->D, p->rows, p->ctas), one = kernel_for(p->D, p->rows, 1);
+  const TcKernel kern = kernel_for(p->D, p->M, p->ctas), one = kernel_for(p->D, p->M, 1);
   for (; s > 1; --s)
     if (cluster_slots(kern.fn, kern.threads, kern.smem, s) > 0 &&
         p->ctas * cluster_slots(one.fn, one.threads, one.smem, s) >= (num_splits > 0 ? 1 : jobs))
@@ -655,7 +665,7 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
 }
 
 sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st) {
-  const TcKernel kern = kernel_for(p.D, p.rows, p.ctas);
+  const TcKernel kern = kernel_for(p.D, p.M, p.ctas);
   // Codes as bytes: (D, tokens of a page, page and head); a copy is a page.
   CUtensorMap tk, tv;
   const uint64_t dims[3] = {(uint64_t)p.D, (uint64_t)p.P, (uint64_t)p.n_pages * p.Hkv};
