@@ -426,7 +426,15 @@ sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new
  *   cache_len [B] int32, 0 .. max_pages * P; what the cache holds past it (and
  *   pages it does not reach) is never used and may be NaN
  *
- * Products of codes and activations accumulate in fp32, scales apply in fp32.
+ * Products accumulate in fp32, scales, maxima and sums are fp32.  With bf16
+ * activations the tensor cores read the codes; a row of q and of k_blk enters as
+ * x = s (hi + lo), two e4m3 codes an element (8 bits of the row's largest; what is
+ * not finite becomes NaN), a probability as 8 bits (11 above 32 packed rows k G)
+ * relative to its own 256 (128) keys' largest.  Scales are positive; a value whose
+ * page's scale is below 2^-14 of the largest among the same 256 keys loses bits.
+ * With fp32 activations everything is fp32.
+ *
+ * No workspace: its size is 0 and the arguments are not looked at.
  * A length out of range is clamped and sets SBD_DEVERR_CACHE_LEN; a page id out
  * of range sets SBD_DEVERR_PAGE and its keys and values count as zeros.
  * Supported: 1 <= k <= 32, D in {64, 128}, Hq % Hkv == 0, max_pages * P + k <

@@ -37,11 +37,10 @@ struct AttnQ8Tensors {
   void* out;
 };
 AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d);
-size_t attn_q8_workspace_bytes(const AttnQ8Plan& p);
-// The tcgen05 kernel: its rows, chunks and splits, and its launch.
+// The tcgen05 kernels: their rows, chunks and splits, and the launch.
 void paged_tc_plan(AttnQ8Plan* p, int num_splits);
 sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st);
-sbd_status attn_q8_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, void* ws, cudaStream_t st);
+sbd_status attn_q8_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st);
 
 }  // namespace sbd
 

@@ -154,8 +154,8 @@ sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new
 }
 
 size_t sbd_block_attention_q8_workspace_size(const sbd_attn_q8_desc* desc) {
-  if (check_attn_q8_desc(desc) != SBD_OK || sbd::device_ready() != SBD_OK) return 0;
-  return sbd::attn_q8_workspace_bytes(sbd::attn_q8_plan(*desc));
+  check_attn_q8_desc(desc);
+  return 0;                                  // splits merge on the chip
 }
 
 sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
@@ -163,7 +163,7 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
                                   const float* k_scale, const float* v_scale,
                                   const int32_t* block_table, const int32_t* cache_len,
                                   const void* k_blk, const void* v_blk, void* out,
-                                  void* workspace, size_t workspace_bytes, void* stream) {
+                                  void*, size_t, void* stream) {
   sbd_status s = check_attn_q8_desc(desc);
   if (s != SBD_OK) return s;
   if (desc->batch == 0) return SBD_OK;
@@ -181,18 +181,9 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
   if (s != SBD_OK) return s;
   s = sbd::device_ready();
   if (s != SBD_OK) return s;
-  const sbd::AttnQ8Plan p = sbd::attn_q8_plan(*desc);
-  const size_t need = sbd::attn_q8_workspace_bytes(p);
-  if (need > 0) {
-    if (!workspace || workspace_bytes < need)
-      return fail(SBD_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
-                  workspace ? workspace_bytes : (size_t)0);
-    if (!aligned16(workspace))
-      return fail(SBD_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-  }
   const sbd::AttnQ8Tensors t{q,           k_cache,   v_cache, k_scale, v_scale,
                              block_table, cache_len, k_blk,   v_blk,   out};
-  return sbd::attn_q8_launch(p, t, workspace, (cudaStream_t)stream);
+  return sbd::attn_q8_launch(sbd::attn_q8_plan(*desc), t, (cudaStream_t)stream);
 }
 
 }  // extern "C"
