@@ -102,10 +102,6 @@ __device__ __forceinline__ uint32_t half2_of(uint32_t c, __half2 w) {
   const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&x), w);
   return *reinterpret_cast<const uint32_t*>(&y);
 }
-__device__ __forceinline__ void st_cluster_v4(uint32_t addr, float x, float y, float z, float w) {
-  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(x), "f"(y), "f"(z), "f"(w)
-               : "memory");
-}
 
 template <int D>
 struct Shape {
@@ -127,6 +123,7 @@ struct Shape {
   static constexpr int kSmem = kFixed + kStages * 2 * kKV;
   static constexpr int kPStride = D + 4;
   static_assert(kStages >= 2, "a tile ahead");
+  static_assert(kRows * kPStride * 4 <= kQ + 2 * kV16, "the partial rows fit the places of Q and V");
   static_assert((kRows + kMaxSplits) * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
 };
 
@@ -141,7 +138,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
   __shared__ __align__(8) uint64_t s_full[2], s_free[2], p_full[2], v_full[2], o_full[2], o_free[2];
-  __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
+  __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar, merge_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
   __shared__ PageScales pages;
@@ -158,8 +155,10 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
   auto k_tile = [&](int j) { return ring + (uint32_t)(j % kStages) * 2 * C::kKV; };
   auto v_tile = [&](int j) { return k_tile(j) + C::kKV; };
 
+  float* const local = reinterpret_cast<float*>(smem_raw + (q_s - smem_u32(smem_raw)));   // partial rows, at the end
+
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
+  const int split = blockIdx.x, hkv = whole_part(blockIdx.y, a.inv_chunks), chunk = blockIdx.y - hkv * a.chunks;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&kv_full[s], 1);
@@ -176,10 +175,15 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     mbar_init(&q_ready, kWorkWarps);
     mbar_init(&blk_ready, kWorkWarps);
     mbar_init(&tail_bar, 1);
+    mbar_init(&merge_bar, 1);
     blk_bad = 0;
     fence_mbar_init();
+    if (a.splits > 1) mbar_arrive_expect_tx(&merge_bar, merge_bytes<D>(min(kRows, a.M - chunk * kRows), split, a.splits));
   }
   __syncthreads();
+  // On their way to L2 while the previous grid ends: the lengths, the table's first
+  // pages, and the rows and the block's keys and values, which it may have written.
+  if (warp >= kControl && !a.order) prefetch_inputs<D, kRows, 32 * kWorkWarps>(a, threadIdx.x - 32 * kControl, blockIdx.z, hkv, chunk);
   // What the previous grid may still write is read from here on.
   grid_dependency_wait();
   const int cap = a.max_pages << a.page_log2;
@@ -190,8 +194,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     len = len < 0 ? 0 : cap;
   }
   const int n_tiles = (int)(((long long)len + kTile - 1) / kTile) + 1;
-  const int t_begin = (int)((long long)split * n_tiles / a.splits);
-  const int t_end = (int)((long long)(split + 1) * n_tiles / a.splits);
+  const int t_begin = (int)((uint32_t)split * n_tiles / a.splits);
+  const int t_end = (int)((uint32_t)(split + 1) * n_tiles / a.splits);
   const bool has_block = t_end == n_tiles && t_end > t_begin;
   // This CTA's cache tiles, a step each, and the block's keys as a last step.
   const int nc = t_end - t_begin - (has_block ? 1 : 0);
@@ -225,9 +229,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
         const uint32_t id = idesc_f8(kRows, kBlkKeys, false);
         const uint64_t kd = desc<D>(bk_s);
         if (leader) {                                  // the keys' hi codes, then their lo codes
-#pragma unroll
+#pragma unroll 1
           for (int h = 0; h < 4; ++h)
-#pragma unroll
+#pragma unroll 1
             for (int kk = 0; kk < D / 32; ++kk)
               tc_mma_f8(d, qd + ((h & 1) * kLo + 2 * kk), kd + ((h >> 1) * kBlkKeys * D / 16 + 2 * kk), id, h > 0 || kk > 0);
         }
@@ -284,55 +288,71 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const int r = quad * 32 + lane, row = chunk * kRows + r;   // lane of tensor memory, packed row
     const int at = sw * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
-    constexpr int kRowsTurn = 32 * kWorkWarps / (D / 16);
-    {
-      const int c = at % (D / 16);
+    // The chunk's rows become code pairs, then the block's keys; the block's values stay
+    // as they are.  All loads first, and one loop for rows and keys: its code comes
+    // from L2 once (a copy of its own for the keys took 2,700 clocks of one user's
+    // 25,000).  What lies behind the last row is left as it is: rows of the products
+    // that nothing reads.
+    constexpr int kTurn = 32 * kWorkWarps / (D / 16);  // rows of a turn
+    constexpr int kQTurns = kRows / kTurn;
+    static_assert(kQTurns * kTurn == kRows && kBlkKeys <= kTurn, "rows in whole turns, keys in one");
+    const int c = at % (D / 16), r0 = at / (D / 16);
+    const int q_turns = min(kQTurns, (a.M - chunk * kRows + kTurn - 1) / kTurn);
+    Piece<D> piece[kQTurns + 1], value;
+    const bool key_here = has_block && r0 < a.k;
+    const size_t key_off = (((size_t)b * a.k + r0) * a.Hkv + hkv) * D + 16 * c;
+#pragma unroll
+    for (int e = 0; e < kQTurns; ++e) {
+      const int x = chunk * kRows + r0 + e * kTurn, i = a.position(x);
+      piece[e].zero();
+      if (x < a.M) piece[e].load(a.q + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + x - i * a.G) * D + 16 * c);
+    }
+    piece[kQTurns].zero(), value.zero();
+    if (key_here) {
+      piece[kQTurns].load(a.kb + key_off);
+      value.load(a.vb + key_off);
+    }
 #pragma unroll 1
-      for (int e = at / (D / 16); e < kRows; e += kRowsTurn) {
-        const int x = chunk * kRows + e, i = x / a.G;
-        Piece<D> q;
-        q.zero();
-        if (x < a.M) q.load(a.q + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + x - i * a.G) * D + 16 * c);
-        const float s = q.store(q_s, e, kRows + e, c);
-        if (c == 0) c_sh[e] = s * a.scale_log2;
+    for (int e = 0; e <= kQTurns; ++e) {
+      const bool keys = e == kQTurns;
+      if (keys ? has_block && r0 < kBlkKeys : e < q_turns) {   // (whole warps)
+        const int to = keys ? r0 : r0 + e * kTurn;
+        const float s = piece[0].store(keys ? bk_s : q_s, to, to + (keys ? kBlkKeys : kRows), c);
+        if (c == 0) *(keys ? &bks_sh[to] : &c_sh[to]) = keys ? s : s * a.scale_log2;
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_ready);
-      bar_sync(5, 32 * kWorkWarps);                    // c of all rows
+#pragma unroll
+      for (int x = 0; x < kQTurns; ++x) piece[x] = piece[x + 1];
+      if (e == kQTurns - 1) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_ready);
+      }
     }
     if (has_block) {
-      const int c = at % (D / 16);
       bool bad = false;
+      // Values that are not finite stay out of the product (a row that does not
+      // see them would multiply them by 0) and are added at the end.
+      auto finite2 = [&](uint32_t w) {
+        const bool lo_bad = (w & 0x7f80u) == 0x7f80u, hi_bad = (w & 0x7f800000u) == 0x7f800000u;
+        bad |= lo_bad || hi_bad;
+        return (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
+      };
+      if (r0 < kBlkKeys) {
 #pragma unroll 1
-      for (int key = at / (D / 16); key < kBlkKeys; key += kRowsTurn) {
-        Piece<D> x, y;
-        x.zero(), y.zero();
-        if (key < a.k) {
-          const size_t off = (((size_t)b * a.k + key) * a.Hkv + hkv) * D + 16 * c;
-          x.load(a.kb + off);
-          y.load(a.vb + off);
+        for (int e = 0; e < 2; ++e) {                  // 8 dimensions each
+          const uint4 v = value.w[0];
+          st_shared_v4(swz<128>(bv_s + (2 * c + e) / 8 * C::kBlkSub, r0, (2 * c + e) % 8),
+                       make_uint4(finite2(v.x), finite2(v.y), finite2(v.z), finite2(v.w)));
+          value.w[0] = value.w[1];
         }
-        const float s = x.store(bk_s, key, kBlkKeys + key, c);
-        if (c == 0) bks_sh[key] = s;
-        // Values that are not finite stay out of the product (a row that does not
-        // see them would multiply them by 0) and are added at the end.
-        auto finite2 = [&](uint32_t w) {
-          const bool lo_bad = (w & 0x7f80u) == 0x7f80u, hi_bad = (w & 0x7f800000u) == 0x7f800000u;
-          bad |= lo_bad || hi_bad;
-          return (lo_bad ? 0u : w & 0xffffu) | (hi_bad ? 0u : w & 0xffff0000u);
-        };
-#pragma unroll
-        for (int e = 0; e < 2; ++e)                    // 8 dimensions each
-          st_shared_v4(swz<128>(bv_s + (2 * c + e) / 8 * C::kBlkSub, key, (2 * c + e) % 8),
-                       make_uint4(finite2(y.w[e].x), finite2(y.w[e].y), finite2(y.w[e].z), finite2(y.w[e].w)));
       }
       if (bad) blk_bad = 1;
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&blk_ready);
     }
-    const int vis = row / a.G < a.n_causal ? row / a.G + 1 : a.k;
+    bar_sync(5, 32 * kWorkWarps);                      // c of all rows
+    const int pos = a.position(row), vis = pos < a.n_causal ? pos + 1 : a.k;
     const bool rows_here = chunk * kRows + quad * 32 < a.M;   // whole warps without rows only keep step
     bool ok = true;
     if (sw < C::kSoftWarps) {
@@ -526,12 +546,13 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
         if (lane == 0) mbar_arrive(&o_free[i % kOBufs]);
       }
       grid_dependents_launch();
+      if (a.splits > 1) cluster_arrive();
       // ------------------------------------------------ epilogue
-      const float inv = m_ref == -INFINITY ? 0.f : 1.f / l;
+      const float inv = m_ref == -INFINITY ? 0.f : __fdividef(1.f, l);
 #pragma unroll
       for (int e = 0; e < kDims / 2; ++e) acc[e].x *= inv, acc[e].y *= inv;
       const bool mine = row < a.M;
-      const int i = row / a.G;
+      const int i = pos;
       if (has_block && blk_bad && mine) {
 #pragma unroll 1
         for (int e = 0; e < vis; ++e) {
@@ -554,24 +575,16 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
                            pack_bf16(acc[e + 2].x, acc[e + 2].y), pack_bf16(acc[e + 3].x, acc[e + 3].y));
         }
       } else {
-        // Row r is merged in CTA r mod splits of the cluster: its partial rows go into
-        // that one's ring, which is idle there once every CTA has come here.
-        cluster_sync_all();
-        if (mine) {
-          const int to = r % a.splits, slot = r / a.splits;
-          if (part == 0) {
-            const float lse = n > 0 && ok ? m_ref + log2f(l) : -INFINITY;
-            st_cluster_f32(mapa_shared(smem_u32(&lse_sh[slot * a.splits + split]), to), lse);
-          }
-          const uint32_t dst = mapa_shared(ring + 4u * ((slot * a.splits + split) * C::kPStride + part * kDims), to);
+        // The places of Q and V are idle, the ring may not be yet in other CTAs.
+        float* dst = local + r * C::kPStride + part * kDims;
 #pragma unroll
-          for (int e = 0; e < kDims / 2; e += 2)
-            st_cluster_v4(dst + 8 * e, acc[e].x, acc[e].y, acc[e + 1].x, acc[e + 1].y);
-        }
+        for (int e = 0; e < kDims / 2; e += 2)
+          *reinterpret_cast<float4*>(dst + 2 * e) = make_float4(acc[e].x, acc[e].y, acc[e + 1].x, acc[e + 1].y);
+        if (part == 0) c_sh[r] = n > 0 && ok ? m_ref + __log2f(l) : -INFINITY;
       }
     }
   }
-  if (a.splits > 1 && warp < kControl + C::kSoftWarps) cluster_sync_all();
+  if (a.splits > 1 && warp < kControl + C::kSoftWarps) cluster_arrive();
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -579,7 +592,22 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     tc_dealloc(*(volatile uint32_t*)&tmem_base_sh, 512);
   }
   if (a.splits == 1) return;
-  cluster_sync_all();
+  // Row r is merged in CTA r mod splits of the cluster: its partial rows go into that
+  // one's ring, which is idle there once every CTA has come here.  A warp a row (every
+  // lane a row of its own took 4,000 clocks: 16 bytes a packet).
+  cluster_wait();
+  const int rows = min(kRows, a.M - chunk * kRows);
+  const float inv_splits = __fdividef(1.f, (float)a.splits);
+#pragma unroll 1
+  for (int r = warp; r < rows; r += C::kThreads / 32) {
+    const int slot = whole_part(r, inv_splits), to = r - slot * a.splits, at = slot * a.splits + split;
+    const uint32_t bar = mapa_shared(smem_u32(&merge_bar), to);
+    if (lane < D / 4)
+      st_async(mapa_shared(ring + 4u * (at * C::kPStride + 4 * lane), to),
+               *reinterpret_cast<const float4*>(local + r * C::kPStride + 4 * lane), bar);
+    if (lane == 0) st_async(mapa_shared(smem_u32(&lse_sh[at]), to), c_sh[r], bar);
+  }
+  mbar_wait(&merge_bar, 0, a.err);
   merge_rows<D, kRows, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh,
                                      b, hkv, chunk, split);
 }

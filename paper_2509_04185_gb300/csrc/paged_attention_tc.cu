@@ -133,7 +133,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
   __shared__ __align__(8) uint64_t s_full[2], s_free[2], p_full[4], o_full[2], o_free[2];
-  __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar;
+  __shared__ __align__(8) uint64_t q_ready, blk_ready, tail_bar, merge_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int b_pick, blk_bad;
   __shared__ PageScales pages;
@@ -155,7 +155,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   auto v_tile = [&](int j) { return k_tile(j) + C::kKV; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
+  const int split = blockIdx.x, hkv = whole_part(blockIdx.y, a.inv_chunks), chunk = blockIdx.y - hkv * a.chunks;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&kv_full[s], 1);
@@ -171,8 +171,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     mbar_init(&q_ready, kSoftWarps);
     mbar_init(&blk_ready, kSoftWarps);
     mbar_init(&tail_bar, 1);
+    mbar_init(&merge_bar, 1);
     blk_bad = 0;
     fence_mbar_init();
+    if (a.splits > 1) mbar_arrive_expect_tx(&merge_bar, merge_bytes<D>(min(R, a.M - chunk * R), split, a.splits));
   }
   __syncthreads();
   // What the previous grid may still write is read from here on.  There is no
@@ -188,8 +190,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   }
   const int n_cache = (int)(((long long)len + kTile - 1) / kTile);
   const int n_tiles = n_cache + 1;
-  const int t_begin = (int)((long long)split * n_tiles / a.splits);
-  const int t_end = (int)((long long)(split + 1) * n_tiles / a.splits);
+  const int t_begin = (int)((uint32_t)split * n_tiles / a.splits);
+  const int t_end = (int)((uint32_t)(split + 1) * n_tiles / a.splits);
   const bool has_block = t_end == n_tiles && t_end > t_begin;
   // This CTA's cache tiles, two a step, and the block's keys as a last step.
   const int nc = t_end - t_begin - (has_block ? 1 : 0);
@@ -298,7 +300,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       const int c = at % (D / 16);
 #pragma unroll 1
       for (int r = at / (D / 16); r < R; r += kRowsTurn) {
-        const int row = chunk * R + r, i = row / a.G;
+        const int row = chunk * R + r, i = a.position(row);
         Piece<D> x;
         x.zero();
         if (row < a.M) x.load(a.q + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + 16 * c);
@@ -531,12 +533,13 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     }
     if (n > 0) add_product(n - 1);
     grid_dependents_launch();
+    if (a.splits > 1) cluster_arrive();
     // ------------------------------------------------ epilogue
     sum_sh[sw][own] = l;
     bar_sync(1 + part, 128);
     const float sum = (sum_sh[4 * part][own] + sum_sh[4 * part + 1][own]) +
                       (sum_sh[4 * part + 2][own] + sum_sh[4 * part + 3][own]);
-    f_sh[sw][0][own] = m_ref == -INFINITY ? 0.f : 1.f / sum;
+    f_sh[sw][0][own] = m_ref == -INFINITY ? 0.f : __fdividef(1.f, sum);
     __syncwarp();
 #pragma unroll
     for (int r = 0; r < kRT; r += 4) {
@@ -558,7 +561,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       }
     }
     if (a.splits == 1) {
-      int i = row / a.G, q = row - i * a.G;            // block position, query head of the group
+      int i = a.position(row), q = row - i * a.G;      // block position, query head of the group
       __nv_bfloat16* dst = a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + q) * D + d;
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {
@@ -569,23 +572,27 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     } else {
       // Row r is merged in CTA r mod splits of the cluster: its partial rows go into
       // that one's ring, which is idle there once every CTA has come here.
-      const float lse = n > 0 && ok ? m_ref + log2f(sum) : -INFINITY;
-      cluster_sync_all();
-      if (quad == 0) {
-        const int to = (r0 + own) % a.splits, slot = (r0 + own) / a.splits;
-        st_cluster_f32(mapa_shared(smem_u32(&lse_sh[slot * a.splits + split]), to), lse);
+      const float lse = n > 0 && ok ? m_ref + __log2f(sum) : -INFINITY;
+      const float inv_splits = __fdividef(1.f, (float)a.splits);
+      cluster_wait();
+      if (quad == 0 && lane < kRT && row + own < a.M) {
+        const int slot = whole_part(r0 + own, inv_splits), to = r0 + own - slot * a.splits;
+        st_async(mapa_shared(smem_u32(&lse_sh[slot * a.splits + split]), to), lse, mapa_shared(smem_u32(&merge_bar), to));
       }
-      int to = r0 % a.splits, slot = r0 / a.splits;
+      int slot = whole_part(r0, inv_splits), to = r0 - slot * a.splits;
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {
         if (has_d && row + r < a.M)
-          st_cluster_f32(mapa_shared(ring + 4u * ((slot * a.splits + split) * C::kPStride + d), to),
-                         n > 0 ? acc[r] : 0.f);
+          st_async(mapa_shared(ring + 4u * ((slot * a.splits + split) * C::kPStride + d), to), n > 0 ? acc[r] : 0.f,
+                   mapa_shared(smem_u32(&merge_bar), to));
         if (++to == a.splits) to = 0, ++slot;
       }
     }
   }
-  if (a.splits > 1 && warp < kControl) cluster_sync_all();
+  if (a.splits > 1 && warp < kControl) {
+    cluster_arrive();
+    cluster_wait();
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -599,7 +606,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // log2-sum-exps in its own shared memory now, a warp a row.  (Rows read from the
   // other CTAs, all splits of a row requested at once, took 3.5 us of one user's
   // 15: the requests were 250 instructions that run once.)
-  cluster_sync_all();
+  mbar_wait(&merge_bar, 0, a.err);
   merge_rows<D, R, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh, b, hkv,
                                      chunk, split);
 }
@@ -705,6 +712,8 @@ sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStre
   a.order = p.B > 1 && p.B <= kMaxOrder &&
             (long long)p.B * p.Hkv * p.chunks * p.splits > num_sms();
   a.scale_log2 = p.scale_log2;
+  a.inv_G = 1.f / (float)p.G;
+  a.inv_chunks = 1.f / (float)p.chunks;
   s = allow_smem(kern.fn, kern.smem, "cudaFuncSetAttribute(paged_tc_kernel)");
   if (s != SBD_OK) return s;
   void* args[] = {(void*)&tk, (void*)&tv, (void*)&a};

@@ -152,18 +152,34 @@ __device__ __forceinline__ void bar_sync(int id, int threads) {
 }
 
 // ------------------------------------------------------------ clusters
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
-               "barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+// (Every thread of the cluster comes to both, the wait as late as it can.)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t mapa_shared(uint32_t addr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+// Stores into a CTA of the cluster that count towards the bytes its barrier waits for.
+__device__ __forceinline__ void st_async(uint32_t addr, float v, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(addr), "f"(v), "r"(bar)
+               : "memory");
 }
+__device__ __forceinline__ void st_async(uint32_t addr, float4 v, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr),
+               "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(bar)
+               : "memory");
+}
+// Bytes that come to CTA `split` for the merge of `rows` rows of D floats and a sum.
+template <int D>
+__device__ __forceinline__ uint32_t merge_bytes(int rows, int split, int splits) {
+  return split < rows ? (uint32_t)((rows - split + splits - 1) / splits * splits * (4 * D + 4)) : 0u;
+}
+
+// floor(x / d) for 0 <= x < 2^20 and inv = 1 / d to a few units in the last place: x + 1/2
+// is half a unit of 1 / d away from where the quotient steps.  (A division of integers is
+// 30 instructions, and what runs once waits for L2 to bring its code: 300 clocks for 8.)
+__device__ __forceinline__ int whole_part(int x, float inv) { return __float2int_rz(((float)x + 0.5f) * inv); }
 
 struct Args {
   const __nv_bfloat16 *q, *kb, *vb;
@@ -175,6 +191,9 @@ struct Args {
   int page_log2;
   int order;                 // blockIdx.z -> sequence by descending length
   float scale_log2;
+  float inv_G, inv_chunks;   // 1 / G, 1 / chunks
+  // The block position of packed row x.
+  __device__ __forceinline__ int position(int x) const { return whole_part(x, inv_G); }
 };
 
 // A tile's page scales: of the keys; of the values over the largest of their step; that.
@@ -334,6 +353,27 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& tmap_k, const CUte
     mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
 }
 
+// Asks for what a CTA reads whatever the lengths are, by kThreads threads.
+template <int D, int kRows, int kThreads>
+__device__ __forceinline__ void prefetch_inputs(const Args& a, int thread, int b, int hkv, int chunk) {
+  constexpr int kLines = D * 2 / 128;                  // of a row
+  const int rows = min(kRows, a.M - chunk * kRows);
+#pragma unroll 1
+  for (int i = thread; i < (rows + a.k) * kLines + 2; i += kThreads) {
+    const int x = i / kLines, at = i % kLines * 64;
+    if (x < rows) {
+      const int r = chunk * kRows + x, p = a.position(r);
+      prefetch_l2(a.q + (((size_t)b * a.k + p) * a.Hq + hkv * a.G + r - p * a.G) * D + at);
+    } else if (x < rows + a.k) {
+      const size_t off = (((size_t)b * a.k + x - rows) * a.Hkv + hkv) * D + at;
+      prefetch_l2(a.kb + off);
+      prefetch_l2(a.vb + off);
+    } else {
+      prefetch_l2(i - (rows + a.k) * kLines == 0 ? (const void*)(a.lens + b) : (const void*)(a.table + (size_t)b * a.max_pages));
+    }
+  }
+}
+
 // The CTAs of a cluster are the splits of one (sequence, KV head, chunk); CTA `split`
 // has all splits' normalised rows split, split + splits, ... (`rows`, kPStride floats
 // each) and their log2-sum-exps in its shared memory.  A warp a row.
@@ -348,9 +388,9 @@ __device__ __forceinline__ void merge_rows(const Args& a, const float* rows, con
     const int row = chunk * R + slot * a.splits + split;
     if (row >= a.M) break;
     const float l = lane < a.splits ? lse[slot * a.splits + lane] : -INFINITY;
-    const float mx = warp_max(l);
-    const float w = l == -INFINITY ? 0.f : exp2f(l - mx);
-    const float inv = 1.f / warp_sum(w);
+    const float mx = redux_max(l);
+    const float w = l == -INFINITY ? 0.f : ex2_ftz(l - mx);
+    const float inv = __fdividef(1.f, warp_sum(w));
     const float* src = rows + slot * a.splits * kPStride + kPer * lane;
     float o[kPer];
 #pragma unroll
@@ -363,7 +403,7 @@ __device__ __forceinline__ void merge_rows(const Args& a, const float* rows, con
         for (int c = 0; c < kPer; ++c) o[c] = fmaf(ws, src[s * kPStride + c], o[c]);
       }
     }
-    const int i = row / a.G;
+    const int i = a.position(row);
     __nv_bfloat16* dst =
         a.out + (((size_t)b * a.k + i) * a.Hq + hkv * a.G + row - i * a.G) * D + kPer * lane;
 #pragma unroll
