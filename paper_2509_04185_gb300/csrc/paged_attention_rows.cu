@@ -21,11 +21,14 @@
 // 10 the softmax, two groups of four that take the tiles in turn; 11 to 18 the conversion
 // of V and the accumulators, two warps to a quadrant of 32 rows.
 //
-// Bounds and figures.  16 requests of 8192 keys, 128 rows and dimensions: 82 us, 2,300
+// Bounds and figures.  16 requests of 8192 keys, 128 rows and dimensions: 80 us, 2,300
 // clocks for a tile of 128 rows and keys, where memory would allow 41 us and the products
 // 37 (16 a tile, 68 clocks each).  What sets the pace is a chain from tile to tile: the
 // product O, the accumulators' warps that read and add it (tensor memory has no place for
 // a second O beside two S and two P at 128 dimensions) and convert the next V meanwhile.
+// 19 x 4096 keys, 64 rows: 43.5 us, the same chain (24 us of bytes).  One request of 4096
+// keys, 64 rows, 12 splits of three tiles: 11.5 us, of which 2 are the launch, 2.5 the
+// way to the first scores (lengths -> table -> copies), 3 the merge of the splits.
 // Registers matter more than instructions: shared memory leaves no L1, so a spill is a trip
 // to L2; 150 bytes of them in the cold path of cut tiles cost 25 us.
 #include <math.h>
@@ -181,9 +184,6 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     if (a.splits > 1) mbar_arrive_expect_tx(&merge_bar, merge_bytes<D>(min(kRows, a.M - chunk * kRows), split, a.splits));
   }
   __syncthreads();
-  // On their way to L2 while the previous grid ends: the lengths, the table's first
-  // pages, and the rows and the block's keys and values, which it may have written.
-  if (warp >= kControl && !a.order) prefetch_inputs<D, kRows, 32 * kWorkWarps>(a, threadIdx.x - 32 * kControl, blockIdx.z, hkv, chunk);
   // What the previous grid may still write is read from here on.
   grid_dependency_wait();
   const int cap = a.max_pages << a.page_log2;

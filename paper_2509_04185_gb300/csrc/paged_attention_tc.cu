@@ -13,12 +13,11 @@
 //   O[dim, (hi|lo) row] += V^T P^T    A = V tile (MN-major), B = P (MN-major)
 //
 // so that N follows the rows of the call (R = 16 or 32 a CTA, 8 of 16 computed on for up
-// to 8) and a thread of the
-// softmax owns one key: its page's scales are scalars of the thread, masks a
+// to 8) and a thread of the softmax owns one key: its page's scales are scalars of the thread, masks a
 // comparison, a row's maximum and sum one redux a warp.  Above 32 rows those
 // reductions cost more than the tile's loads, and rows are on the lanes
-// (paged_attention_rows.cu): at 64 rows over 19 x 4096 keys, 128 dimensions, 45.7 us
-// instead of the 50.4 that this kernel took, at 128 rows over 16 x 8192 82 instead of 177.
+// (paged_attention_rows.cu): at 64 rows over 19 x 4096 keys, 128 dimensions, 43.5 us
+// instead of the 50.4 that this kernel took, at 128 rows over 16 x 8192 80 instead of 177.
 //
 // Tiles go in steps of two (256 keys): what a step costs by row and not by key --
 // redux, the row's scale and maximum from shared memory, the accumulators.
@@ -39,8 +38,8 @@
 // measured copy rate).  One query a request, 4 rows: 4 x 32768 keys 45.5 us, 5.9 TB/s of
 // 6.8 on 128 of 152 SMs; 19 x 4096 keys 30 us, 5.3 TB/s, of which the start, before any
 // copy is under way, is 4.  Eight queries, 32 rows, 19 x 4096: 34 us, the softmax warps'
-// instructions.  One request of 4096 keys in 12 splits: 8 us, of which launch, lengths ->
-// table -> copies, tensor memory and the merge are 6.
+// instructions.  One request of 4096 keys in 12 splits: 7.2 us, of which launch, lengths ->
+// table -> copies, tensor memory and the merge are 5.
 //
 // Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
 // O; from 3 the softmax and the accumulators, four warps for 8 rows of a step: with 16
@@ -603,9 +602,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // ------------------------------------------------ merge in the cluster
   // The CTAs of a cluster are the splits of one (sequence, KV head, chunk); CTA
   // `split` has all splits' normalised rows split, split + splits, ... and their
-  // log2-sum-exps in its own shared memory now, a warp a row.  (Rows read from the
-  // other CTAs, all splits of a row requested at once, took 3.5 us of one user's
-  // 15: the requests were 250 instructions that run once.)
+  // log2-sum-exps in its own shared memory once as many bytes have come as they make, a
+  // warp a row.  (Rows read from the other CTAs, all splits of a row requested at once,
+  // took 3.5 us of one user's 15: the requests were 250 instructions that run once.
+  // Pushed between two barriers of the cluster they took 0.5 us longer.)
   mbar_wait(&merge_bar, 0, a.err);
   merge_rows<D, R, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh, b, hkv,
                                      chunk, split);

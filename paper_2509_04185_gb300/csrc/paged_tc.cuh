@@ -353,27 +353,6 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& tmap_k, const CUte
     mbar_wait(&kv_full[j % kStages], (j / kStages) & 1, a.err);
 }
 
-// Asks for what a CTA reads whatever the lengths are, by kThreads threads.
-template <int D, int kRows, int kThreads>
-__device__ __forceinline__ void prefetch_inputs(const Args& a, int thread, int b, int hkv, int chunk) {
-  constexpr int kLines = D * 2 / 128;                  // of a row
-  const int rows = min(kRows, a.M - chunk * kRows);
-#pragma unroll 1
-  for (int i = thread; i < (rows + a.k) * kLines + 2; i += kThreads) {
-    const int x = i / kLines, at = i % kLines * 64;
-    if (x < rows) {
-      const int r = chunk * kRows + x, p = a.position(r);
-      prefetch_l2(a.q + (((size_t)b * a.k + p) * a.Hq + hkv * a.G + r - p * a.G) * D + at);
-    } else if (x < rows + a.k) {
-      const size_t off = (((size_t)b * a.k + x - rows) * a.Hkv + hkv) * D + at;
-      prefetch_l2(a.kb + off);
-      prefetch_l2(a.vb + off);
-    } else {
-      prefetch_l2(i - (rows + a.k) * kLines == 0 ? (const void*)(a.lens + b) : (const void*)(a.table + (size_t)b * a.max_pages));
-    }
-  }
-}
-
 // The CTAs of a cluster are the splits of one (sequence, KV head, chunk); CTA `split`
 // has all splits' normalised rows split, split + splits, ... (`rows`, kPStride floats
 // each) and their log2-sum-exps in its shared memory.  A warp a row.
