@@ -28,8 +28,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 // It serves fp32 activations, whose tolerance the tensor cores' types do not meet.
 // Bound: latency while the ranges are short (one request of 128 keys, 2 KV heads of 64
 // dimensions, 4 rows: 5.2 us, a launch and the chain lengths -> page -> keys -> merge);
-// then shared memory, two reads for 16 FMAs: 8 requests of 2000 keys, 8 KV heads of 128
-// dimensions, 32 rows: 91 us, 23 of 80 TFLOP/s.
+// then shared memory, every warp reading the tile for its few rows: 8 requests of 2000
+// keys, 8 KV heads of 128 dimensions, 32 rows: 82 us, 26 of 80 TFLOP/s; 4 rows: 39 us.
+// (Divisions by the page size and stores that met in a bank took a quarter more.)
 constexpr int kKeys = 64;                    // keys per tile
 constexpr int kGranule = 16;                 // key ranges are multiples of this
 
@@ -46,6 +47,13 @@ __device__ __forceinline__ float ld_rank(const float* p, int rank) {
   return v;
 }
 
+// Words n, n + 1, ... of four.
+__device__ __forceinline__ uint4 rotated(uint4 v, int n) {
+  if (n & 1) v = make_uint4(v.y, v.z, v.w, v.x);
+  if (n & 2) v = make_uint4(v.z, v.w, v.x, v.y);
+  return v;
+}
+
 struct Args {
   const float* q;
   const uint8_t *kc, *vc;
@@ -54,7 +62,7 @@ struct Args {
   const float *kb, *vb;
   float* out;
   int* err;
-  int k, Hq, Hkv, G, M, P, max_pages, n_pages, n_causal, splits, chunks;
+  int k, Hq, Hkv, G, M, log2P, max_pages, n_pages, n_causal, splits, chunks;
   float scale_log2;
 };
 
@@ -71,7 +79,7 @@ constexpr size_t fma_smem_bytes() {
 }
 
 template <int D, int RW, int W>
-__global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args a) {
+__global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const Args a) {
   constexpr int kThreads = 32 * W;
   constexpr int kRowsCta = W * RW;
   constexpr int kKS = k_stride<D>();
@@ -94,7 +102,7 @@ __global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args a) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
   const int b = blockIdx.z;
-  const int cap = a.max_pages * a.P;
+  const int cap = a.max_pages << a.log2P;
   int len = a.lens[b];
   if (len < 0 || len > cap) {
     if (tid == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
@@ -114,13 +122,13 @@ __global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args a) {
       kf[e] = vf[e] = make_uint4(0, 0, 0, 0);
       ksf[e] = vsf[e] = 0.f;
       if (u < u_end && u < len) {
-        const int page = table[u / a.P];
+        const int page = table[u >> a.log2P];
         if (page < 0 || page >= a.n_pages) {
           record_error(a.err, SBD_DEVERR_PAGE);
           continue;
         }
         const size_t ph = (size_t)page * a.Hkv + hkv;
-        const size_t at = (ph * a.P + u % a.P) * D + 16 * c;
+        const size_t at = ((ph << a.log2P) + (u & ((1 << a.log2P) - 1))) * D + 16 * c;
         kf[e] = *reinterpret_cast<const uint4*>(a.kc + at);
         vf[e] = *reinterpret_cast<const uint4*>(a.vc + at);
         ksf[e] = a.ks[ph];
@@ -145,15 +153,19 @@ __global__ void __launch_bounds__(32 * W, 2) paged_fma_kernel(const Args a) {
         if (c == 0) sc_s[j] = 1.f;
         continue;
       }
-      const uint32_t kw[4] = {kf[e].x, kf[e].y, kf[e].z, kf[e].w};
-      const uint32_t vw[4] = {vf[e].x, vf[e].y, vf[e].z, vf[e].w};
+      // The words of a piece go in an order that differs between lanes, so that eight of
+      // them store to eight places of 128 bytes.
+      const int turn = (c >> 1) & 3;
+      const uint4 kw = rotated(kf[e], turn), vw = rotated(vf[e], turn);
+      const uint32_t kx[4] = {kw.x, kw.y, kw.z, kw.w}, vx[4] = {vw.x, vw.y, vw.z, vw.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float x[4], y[4];
-        e4m3x4_values(kw[i], x);
-        e4m3x4_values(vw[i], y);
-        *reinterpret_cast<float4*>(kd + 4 * i) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4*>(vd + 4 * i) =
+        e4m3x4_values(kx[i], x);
+        e4m3x4_values(vx[i], y);
+        const int to = 4 * ((i + turn) & 3);
+        *reinterpret_cast<float4*>(kd + to) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(vd + to) =
             make_float4(y[0] * vsf[e], y[1] * vsf[e], y[2] * vsf[e], y[3] * vsf[e]);
       }
       if (c == 0) sc_s[j] = ksf[e];
@@ -361,15 +373,15 @@ Kernel fma_kernel_of(int M) {
 }
 Kernel fma_kernel_for(int D, int M) { return D == 128 ? fma_kernel_of<128>(M) : fma_kernel_of<64>(M); }
 
-// Key ranges per (sequence, KV head, row chunk): as many as two CTAs per SM
-// allow, one range per kGranule keys at most, in a cluster size whose clusters
+// Key ranges per (sequence, KV head, row chunk): as many as three CTAs per SM (of four
+// warps, two of eight) allow, one range per kGranule keys at most, in a cluster size whose clusters
 // the device holds all at once.
 int fma_splits(const sbd::AttnQ8Plan& p, const Kernel& kern, int asked) {
   const long long jobs = (long long)p.B * p.Hkv * p.chunks;
   const long long by_keys = ((long long)p.max_pages * p.P + p.k + kGranule - 1) / kGranule;
   if (jobs <= 0) return 1;
   for (int s : {16, 12, 10, 8, 6, 5, 4, 3, 2}) {
-    if (asked > 0 ? s > asked : s > by_keys || s * jobs > 2ll * sbd::num_sms()) continue;
+    if (asked > 0 ? s > asked : s > by_keys || s * jobs > (kern.threads == 128 ? 3ll : 2ll) * sbd::num_sms()) continue;
     if (sbd::cluster_slots(kern.fn, kern.threads, kern.smem, s) >= (asked > 0 ? 1 : jobs)) return s;
   }
   return 1;
@@ -394,7 +406,7 @@ sbd_status fma_launch(const sbd::AttnQ8Plan& p, const sbd::AttnQ8Tensors& t, cud
   a.Hkv = p.Hkv;
   a.G = p.G;
   a.M = p.M;
-  a.P = p.P;
+  a.log2P = sbd::log2_page(p.P);
   a.max_pages = p.max_pages;
   a.n_pages = p.n_pages;
   a.n_causal = p.n_causal;
