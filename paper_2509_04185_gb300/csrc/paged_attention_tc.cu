@@ -41,10 +41,10 @@
 // instructions.  One request of 4096 keys in 12 splits: 7.2 us, of which launch, lengths ->
 // table -> copies, tensor memory and the merge are 5.
 //
-// Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products
-// O; from 3 the softmax and the accumulators, four warps for 8 rows of a step: with 16
-// rows a warp's instructions were the longer part of a step (51 us instead of 45.5 for
-// 4 rows of 16, 31.1 instead of 30.2 for 16).
+// Warp roles: 0 pages and TMA, 1 tensor memory and the products S, 2 the products O (1
+// too, where two CTAs of 32 rows share an SM); then the softmax and the accumulators, four
+// warps for 8 rows of a step: with 16 rows a warp's instructions were the longer part of
+// a step (51 us instead of 45.5 for 4 rows of 16, 31.1 instead of 30.2 for 16).
 #include <math.h>
 
 #include "paged_tc.cuh"
@@ -53,8 +53,6 @@ namespace {
 
 using namespace sbd_dev;
 
-constexpr int kControl = 3;                  // warps: pages and TMA, products S, products O
-constexpr int kRT = 8;                       // rows of a softmax thread
 constexpr int kTables = 8 * 1024;            // shared memory outside the operands
 constexpr float kPScale = 256.f;             // P = 2^8 p
 constexpr float kLoScale = 32.f;             // lo codes of P hold 2^5 of the rest
@@ -71,7 +69,11 @@ struct Shape {
   static constexpr int kTmemCols = kOCol + 2 * kNO <= 128 ? 128 : kOCol + 2 * kNO <= 256 ? 256 : 512;
   static_assert(kCtas * kTmemCols <= 512, "tensor memory holds them");
   // Four softmax warps take 8 rows of a step, of the first kUse (what the others' columns
-  // hold reaches no column that is read).
+  // hold reaches no column that is read); 16 where two CTAs of 32 rows share an SM, with
+  // one warp less for the products: five warps a scheduler leave 96 registers each.
+  static constexpr bool kFew = R == 32 && kCtas == 2;
+  static constexpr int kRT = kFew ? 16 : 8;
+  static constexpr int kControl = kFew ? 2 : 3;        // warps: pages and TMA, products S, products O
   static constexpr int kParts = kUse / kRT;
   static constexpr int kSoftWarps = 4 * kParts;
   static constexpr int kThreads = 32 * (kControl + kSoftWarps);
@@ -115,8 +117,14 @@ __device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, 
   *lo = (uint32_t)x | (uint32_t)y << 16;
 }
 
-__device__ __forceinline__ void st_shared_v2(uint32_t addr, const uint32_t (&x)[2]) {
+__device__ __forceinline__ void tc_ld(uint32_t taddr, uint32_t (&r)[8]) { tc_ld8(taddr, r); }
+__device__ __forceinline__ void tc_ld(uint32_t taddr, uint32_t (&r)[16]) { tc_ld16(taddr, r); }
+// The codes of 8 rows, or of 16.
+__device__ __forceinline__ void st_codes(uint32_t addr, const uint32_t (&x)[2]) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x[0]), "r"(x[1]) : "memory");
+}
+__device__ __forceinline__ void st_codes(uint32_t addr, const uint32_t (&x)[4]) {
+  st_shared_v4(addr, make_uint4(x[0], x[1], x[2], x[3]));
 }
 
 template <int D, int R, int kUse, int kCtas>
@@ -124,7 +132,7 @@ __global__ void __launch_bounds__(Shape<D, R, kUse, kCtas>::kThreads, kCtas)
 paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
   using C = Shape<D, R, kUse, kCtas>;
-  constexpr int kSBufs = C::kSBufs;
+  constexpr int kSBufs = C::kSBufs, kRT = C::kRT, kControl = C::kControl;
   constexpr int kStages = C::kStages, kNS = C::kNS, kNO = C::kNO;
   constexpr int kParts = C::kParts, kSoftWarps = C::kSoftWarps;
   static_assert(R == 16 || R == 32, "a key's row of P is one swizzle atom");
@@ -198,6 +206,39 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // keys of local cache tile j
   auto keys_of = [&](int j) { return max(0, min(kTile, j < nc ? len - (t_begin + j) * kTile : 0)); };
 
+  // O = V^T P^T of step i, from uniform code of one warp.
+  auto output = [&](int i, bool leader) {
+    const uint32_t id_pv = idesc_f8(D, kNO, true);
+    bool ok = mbar_wait(&o_free[i & 1], ((i >> 1) & 1) ^ 1, a.err) &&
+         mbar_wait(&p_full[i & 3], (i >> 2) & 1, a.err);
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return false;
+    tc_fence_after();
+    const uint32_t o = *(volatile uint32_t*)&tmem_base_sh + C::kOCol + (uint32_t)((i & 1) * kNO);
+    if (has_block && i == n - 1) {
+      const uint64_t vd = desc<128>(bv_s, C::kBlkSub), pd = desc<kNO>(pblk_s);
+      if (leader) {
+#pragma unroll
+        for (int kk = 0; kk < kBlkKeys / 16; ++kk)
+          tc_mma_bf16(o, vd + kk * 128, pd + kk * kNO, idesc_bf16_mn(D, R), kk > 0);
+      }
+    } else {
+      for (int j = 2 * i; j < min(nc, 2 * i + 2); ++j) {
+        const uint64_t vd = desc<D>(v_tile(j)), pd = desc<kNO>(k_tile(j));
+        const int steps = (keys_of(j) + 31) / 32;
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < kTile / 32; ++kk)
+            if (kk < steps) tc_mma_f8(o, vd + kk * 2 * D, pd + kk * 2 * kNO, id_pv, (j & 1) || kk > 0);
+          tc_commit(&kv_empty[j % kStages]);
+        }
+      }
+    }
+    if (leader) tc_commit(&o_full[i & 1]);
+    __syncwarp();
+    return true;
+  };
+
   if (warp == 0) {
     // ------------------------------------------------ pages and TMA
     if (lane == 0) {
@@ -207,7 +248,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     load_tiles<D, kStages, kStages, 2>(tmap_k, tmap_v, a, b, hkv, len, t_begin, nc, ring, pages, kv_full, kv_empty, &tail_bar);
   } else if (warp == 1) {
     // ------------------------------------------------ S = K Q^T
-    // Ahead of the softmax by the second buffer.  The whole warp runs the loop
+    // Ahead of the softmax by the second buffer (with one, after the step's product O,
+    // whose tiles leave the ring for the next ones).  The whole warp runs the loop
     // (descriptors stay in uniform registers) and one lane issues.
     // Tensor memory is taken only after the previous grid is done, so that no CTA of
     // it can be left waiting for it.  Its address reaches the other warps with the
@@ -216,21 +258,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     __syncwarp();
     const uint32_t tmem = *(volatile uint32_t*)&tmem_base_sh;
     const bool leader = elect_one();
-    bool ok = n > 0 && mbar_wait(&q_ready, 0, a.err);
+    const bool ready = n > 0 && mbar_wait(&q_ready, 0, a.err);
     const uint32_t id_s = idesc_f8(kTile, kNS, false);
     const uint64_t qd = desc<D>(q_s);
     auto product = [&](uint32_t d, uint64_t kd, bool add) {
 #pragma unroll
       for (int kk = 0; kk < D / 32; ++kk) tc_mma_f8(d, kd + 2 * kk, qd + 2 * kk, id_s, add || kk > 0);
     };
-    for (int i = 0; i < n && ok; ++i) {
+    auto scores = [&](int i) {
       const int buf = i % kSBufs;
       const uint32_t d = tmem + (uint32_t)(buf * 2 * kNS);
-      ok = mbar_wait(&s_free[buf], (i / kSBufs & 1) ^ 1, a.err);
+      bool ok = mbar_wait(&s_free[buf], (i / kSBufs & 1) ^ 1, a.err);
       if (has_block && i == n - 1) {
         ok = ok && mbar_wait(&blk_ready, 0, a.err);
         ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
+        if (!ok) return false;
         tc_fence_after();
         if (leader) {                                  // the keys' hi codes, then their lo codes
           product(d, desc<D>(bk_s), false);
@@ -243,49 +285,26 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           tc_fence_after();
           if (leader && ok) product(d + (uint32_t)((j & 1) * kNS), desc<D>(k_tile(j)), false);
         }
-        if (!ok) break;
+        if (!ok) return false;
       }
       if (leader) {
         tc_commit(&s_full[buf]);
         mbar_arrive(&s_full[buf]);
       }
       __syncwarp();
+      return true;
+    };
+    if (ready) {
+      for (int i = 0; i <= n; ++i) {
+        if (C::kFew && i > 0 && !output(i - 1, leader)) break;
+        if (i == n || !scores(i)) break;
+      }
     }
-  } else if (warp == 2) {
+  } else if (!C::kFew && warp == 2) {
     // ------------------------------------------------ O = V^T P^T
     const bool leader = elect_one();
-    bool ok = true;
-    const uint32_t id_pv = idesc_f8(D, kNO, true);
-    for (int i = 0; i < n && ok; ++i) {
-      ok = mbar_wait(&o_free[i & 1], ((i >> 1) & 1) ^ 1, a.err) &&
-           mbar_wait(&p_full[i & 3], (i >> 2) & 1, a.err);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t tmem = *(volatile uint32_t*)&tmem_base_sh;
-      const uint32_t o = tmem + C::kOCol + (uint32_t)((i & 1) * kNO);
-      if (has_block && i == n - 1) {
-        const uint64_t vd = desc<128>(bv_s, C::kBlkSub), pd = desc<kNO>(pblk_s);
-        if (leader) {
-#pragma unroll
-          for (int kk = 0; kk < kBlkKeys / 16; ++kk)
-            tc_mma_bf16(o, vd + kk * 128, pd + kk * kNO, idesc_bf16_mn(D, R), kk > 0);
-        }
-      } else {
-        for (int j = 2 * i; j < min(nc, 2 * i + 2); ++j) {
-          const uint64_t vd = desc<D>(v_tile(j)), pd = desc<kNO>(k_tile(j));
-          const int steps = (keys_of(j) + 31) / 32;
-          if (leader) {
-#pragma unroll
-            for (int kk = 0; kk < kTile / 32; ++kk)
-              if (kk < steps) tc_mma_f8(o, vd + kk * 2 * D, pd + kk * 2 * kNO, id_pv, (j & 1) || kk > 0);
-            tc_commit(&kv_empty[j % kStages]);
-          }
-        }
-      }
-      if (leader) tc_commit(&o_full[i & 1]);
-      __syncwarp();
-    }
+    for (int i = 0; i < n; ++i)
+      if (!output(i, leader)) break;
   } else {
     // ------------------------------------------------ softmax and accumulators
     const int sw = warp - kControl, quad = warp & 3, part = sw / 4;
@@ -421,13 +440,13 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           // Both tiles' columns are read, also where the second has no keys.
           const uint32_t sa = tmem + lane_addr + (uint32_t)(buf * 2 * kNS + r0);
           uint32_t h[kRT], lo[kRT];
-          tc_ld8(sa, h);
-          tc_ld8(sa + R, lo);
+          tc_ld(sa, h);
+          tc_ld(sa + R, lo);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < kRT; ++r) z0[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf0;
-          tc_ld8(sa + kNS, h);
-          tc_ld8(sa + kNS + R, lo);
+          tc_ld(sa + kNS, h);
+          tc_ld(sa + kNS + R, lo);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < kRT; ++r) z1[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf1;
@@ -493,11 +512,11 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
             p_codes(__hmul2(__floats2half2_rn(q[0], q[1]), w1), __hmul2(__floats2half2_rn(q[2], q[3]), w1), &hi1[e], &lo1[e]);
           }
           const uint32_t p0 = k_tile(j0) + r0 % 16, p1 = k_tile(j0 + 1) + r0 % 16;
-          st_shared_v2(swz<kNO>(p0, key, r0 / 16), hi0);
-          st_shared_v2(swz<kNO>(p0, key, (R + r0) / 16), lo0);
+          st_codes(swz<kNO>(p0, key, r0 / 16), hi0);
+          st_codes(swz<kNO>(p0, key, (R + r0) / 16), lo0);
           if (has1) {
-            st_shared_v2(swz<kNO>(p1, key, r0 / 16), hi1);
-            st_shared_v2(swz<kNO>(p1, key, (R + r0) / 16), lo1);
+            st_codes(swz<kNO>(p1, key, r0 / 16), hi1);
+            st_codes(swz<kNO>(p1, key, (R + r0) / 16), lo1);
           }
         } else {
 #pragma unroll
@@ -618,7 +637,7 @@ TcKernel instance() {
 }
 template <int D>
 TcKernel kernel_of(int M, int ctas) {
-  if (M > 16) return instance<D, 32, 32, 1>();
+  if (M > 16) return ctas == 1 ? instance<D, 32, 32, 1>() : instance<D, 32, 32, 2>();
   if (M > 8) return ctas == 1 ? instance<D, 16, 16, 1>() : instance<D, 16, 16, 2>();
   return ctas == 1 ? instance<D, 16, 8, 1>() : instance<D, 16, 8, 2>();
 }
@@ -647,15 +666,17 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
     return (int)(most > kMaxSplits ? kMaxSplits : most > tiles ? tiles : most);
   };
   int s = num_splits > 0 ? num_splits : fill(sms);
-  // Up to 16 rows two CTAs may share an SM, with half of the ring each (32 rows would
-  // spill at their 80 registers).
-  // More CTAs than a wave: the start of one hides behind the other (64 requests, one query
-  // each, 500 keys: 33 -> 22 us).  At 128 dimensions the ring is short for that, so only with
-  // a capacity of 1024 keys, or from three waves on (64 requests of 0 .. 4000 keys 68 -> 60
-  // us, of 4000 118 -> 124; 26 of 0 .. 4000 29 -> 51).
+  // Up to 32 rows two CTAs may share an SM, with half of the ring each.  More CTAs than
+  // a wave: the start of one hides behind the other (64 requests, one query each, 500
+  // keys: 33 -> 21 us; eight queries, 40 -> 31).  At 128 dimensions the ring is short for
+  // that, so only with a capacity of 1024 keys, or up to 16 rows from three waves on (64
+  // requests of 0 .. 4000 keys 68 -> 60 us, of 4000 118 -> 124, 32 rows 73 -> 84; 26 of 0 ..
+  // 4000 29 -> 51); at 64 dimensions always (32 rows: 64 requests of 4000 keys 126 -> 115
+  // us, 32 of 1000 26 -> 21, of 0 .. 2000 25 -> 27).
   p->ctas = 1;
-  if (p->rows == 16 && jobs * (s < 1 ? 1 : s) > sms && (p->D == 64 || tiles <= 9 || jobs > 3 * sms)) p->ctas = 2;
-  // At 64 dimensions also in one wave, where five tiles and more are left to a split (19
+  if (p->rows <= 32 && jobs * (s < 1 ? 1 : s) > sms && (p->D == 64 || tiles <= 9 || (p->rows == 16 && jobs > 3 * sms)))
+    p->ctas = 2;
+  // At 64 dimensions up to 16 rows also in one wave, where five tiles and more are left to a split (19
   // requests of 4096 keys 28 -> 22 us, 4 of 32000 49 -> 43; 8 of 500 keys 9.1 -> 10.5).
   if (p->rows == 16 && p->D == 64 && num_splits == 0 && fill(2 * sms) > s && tiles >= 5 * fill(2 * sms)) {
     p->ctas = 2;
