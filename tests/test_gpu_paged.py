@@ -444,3 +444,67 @@ def test_on_another_stream(sbd):
         got = _attend(sbd, case, check=False)
     st.synchronize()
     assert (got == ref).all()
+
+
+@pytest.mark.parametrize("B,k,D", [(1, 32, 64), (1, 16, 128), (40, 8, 64), (40, 2, 128), (160, 2, 64)])
+def test_attention_refusals_in_every_kernel(sbd, B, k, D):
+    """Pages out of range count as zeros, lengths out of range are clamped, in
+    splits, in more CTAs than a wave, with rows and with keys on the lanes."""
+    rng = np.random.default_rng(B + k)
+    case = list(_attention_case(rng, B, k, 16, 4, D, 32, [300] * B, extra_cols=0))
+    full = _attend(sbd, tuple(case), check=True)
+    bad = [x.copy() if isinstance(x, np.ndarray) else x for x in case]
+    bad[3][0, 2] = 10 ** 6
+    bad[3][B - 1, 5] = -7
+    got = _attend(sbd, tuple(bad), check=False)
+    assert np.isfinite(got).all() and sbd.sbd_device_error() == sbd.SBD_DEVERR_PAGE
+    assert (got[1:B - 1] == full[1:B - 1]).all()
+    ref = [x.copy() if isinstance(x, np.ndarray) else x for x in case]
+    ref[1] = [c.copy() for c in case[1]]
+    for w in range(2):                               # those pages as zeros
+        ref[1][w][case[3][0, 2]] = 0
+        ref[1][w][case[3][B - 1, 5]] = 0
+    assert np.abs(got - _attend(sbd, tuple(ref))).max() <= 2e-2
+    long = list(case)
+    long[4] = np.array([10 ** 6] + [300] * (B - 2) + [-3] * (B > 1), np.int32)
+    got = _attend(sbd, tuple(long), check=False)
+    assert sbd.sbd_device_error() == sbd.SBD_DEVERR_CACHE_LEN
+    assert (got[1:B - 1] == full[1:B - 1]).all()
+
+
+def test_a_turn_in_a_cuda_graph(sbd):
+    """Tables, append and attention of a step, captured and replayed."""
+    import torch
+    rng = np.random.default_rng(21)
+    B, H, D, P, n_pages = 5, 2, 128, 64, 40
+    lens, grow = np.array([0, 63, 64, 200, 5], np.int32), np.array([1, 16, 7, 16, 0], np.int32)
+    table, spare = _table(rng, lens, P, n_pages, 8)
+    free = np.zeros(n_pages, np.int32)
+    free[:len(spare)] = spare
+    state = dict(len=_i32(lens), target=_i32(lens + grow), table=_i32(table), free=_i32(free), n_free=_i32([len(spare)]))
+    codes = [torch.zeros(n_pages, H, P, D, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.ones(n_pages, H, device="cuda") for _ in range(2)]
+    new = torch.randn(int(grow.sum()), 2 * H, D, device="cuda").bfloat16()
+    outs = sbd.block_tables_outputs(state["len"], state["table"], int(grow.sum()))
+    blocks = [[torch.randn(B, k, h, D, device="cuda").bfloat16() for h in (4 * H, H, H)] for k in (1, 8, 32)]
+    results = [torch.empty_like(q) for q, _, _ in blocks]
+
+    def turn():
+        sbd.sbd_block_tables(*state.values(), P, outputs=outs)
+        sbd.sbd_cache_append_q8(new[:, :H], new[:, H:], outs[3], *codes, *scales)
+        for (q, kb, vb), out in zip(blocks, results):
+            sbd.sbd_block_attention_q8(q, *codes, *scales, outs[0], outs[1], kb, vb, out)
+
+    turn()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in results] + [c.view(torch.uint8).clone() for c in codes]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        turn()
+    for x in results + [c.view(torch.uint8) for c in codes]:
+        x.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, ref in zip(results + [c.view(torch.uint8) for c in codes], want):
+        assert torch.equal(got, ref)
+    assert sbd.sbd_device_error() == 0
