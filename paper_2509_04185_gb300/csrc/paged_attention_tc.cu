@@ -119,12 +119,8 @@ __device__ __forceinline__ void p_codes(__half2 p01, __half2 p23, uint32_t* hi, 
 
 __device__ __forceinline__ void tc_ld(uint32_t taddr, uint32_t (&r)[8]) { tc_ld8(taddr, r); }
 __device__ __forceinline__ void tc_ld(uint32_t taddr, uint32_t (&r)[16]) { tc_ld16(taddr, r); }
-// The codes of 8 rows, or of 16.
-__device__ __forceinline__ void st_codes(uint32_t addr, const uint32_t (&x)[2]) {
+__device__ __forceinline__ void st_shared_v2(uint32_t addr, const uint32_t (&x)[2]) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x[0]), "r"(x[1]) : "memory");
-}
-__device__ __forceinline__ void st_codes(uint32_t addr, const uint32_t (&x)[4]) {
-  st_shared_v4(addr, make_uint4(x[0], x[1], x[2], x[3]));
 }
 
 template <int D, int R, int kUse, int kCtas>
@@ -503,20 +499,23 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         };
         if (!blk) {
           const __half2 w0 = __float2half2_rn(vw0), w1 = __float2half2_rn(vw1);
-          uint32_t hi0[kRT / 4], lo0[kRT / 4], hi1[kRT / 4], lo1[kRT / 4];
-#pragma unroll
-          for (int e = 0; e < kRT / 4; ++e) {
-            float p[4], q[4];
-            probs(4 * e, p, q);
-            p_codes(__hmul2(__floats2half2_rn(p[0], p[1]), w0), __hmul2(__floats2half2_rn(p[2], p[3]), w0), &hi0[e], &lo0[e]);
-            p_codes(__hmul2(__floats2half2_rn(q[0], q[1]), w1), __hmul2(__floats2half2_rn(q[2], q[3]), w1), &hi1[e], &lo1[e]);
-          }
           const uint32_t p0 = k_tile(j0) + r0 % 16, p1 = k_tile(j0 + 1) + r0 % 16;
-          st_codes(swz<kNO>(p0, key, r0 / 16), hi0);
-          st_codes(swz<kNO>(p0, key, (R + r0) / 16), lo0);
-          if (has1) {
-            st_codes(swz<kNO>(p1, key, r0 / 16), hi1);
-            st_codes(swz<kNO>(p1, key, (R + r0) / 16), lo1);
+#pragma unroll
+          for (int g = 0; g < kRT; g += 8) {           // 8 rows, half a piece
+            uint32_t hi0[2], lo0[2], hi1[2], lo1[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float p[4], q[4];
+              probs(g + 4 * e, p, q);
+              p_codes(__hmul2(__floats2half2_rn(p[0], p[1]), w0), __hmul2(__floats2half2_rn(p[2], p[3]), w0), &hi0[e], &lo0[e]);
+              p_codes(__hmul2(__floats2half2_rn(q[0], q[1]), w1), __hmul2(__floats2half2_rn(q[2], q[3]), w1), &hi1[e], &lo1[e]);
+            }
+            st_shared_v2(swz<kNO>(p0, key, r0 / 16) + g, hi0);
+            st_shared_v2(swz<kNO>(p0, key, (R + r0) / 16) + g, lo0);
+            if (has1) {
+              st_shared_v2(swz<kNO>(p1, key, r0 / 16) + g, hi1);
+              st_shared_v2(swz<kNO>(p1, key, (R + r0) / 16) + g, lo1);
+            }
           }
         } else {
 #pragma unroll
