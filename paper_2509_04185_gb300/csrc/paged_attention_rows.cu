@@ -607,9 +607,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
                *reinterpret_cast<const float4*>(local + r * C::kPStride + 4 * lane), bar);
     if (lane == 0) st_async(mapa_shared(smem_u32(&lse_sh[at]), to), c_sh[r], bar);
   }
-  mbar_wait(&merge_bar, 0, a.err);
-  merge_rows<D, kRows, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh,
-                                     b, hkv, chunk, split);
+  merge_in_cluster<D, kRows, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh,
+                                           b, hkv, chunk, split, &merge_bar);
 }
 
 }  // namespace

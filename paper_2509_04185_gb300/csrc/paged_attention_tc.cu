@@ -624,9 +624,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   // warp a row.  (Rows read from the other CTAs, all splits of a row requested at once,
   // took 3.5 us of one user's 15: the requests were 250 instructions that run once.
   // Pushed between two barriers of the cluster they took 0.5 us longer.)
-  mbar_wait(&merge_bar, 0, a.err);
-  merge_rows<D, R, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh, b, hkv,
-                                     chunk, split);
+  merge_in_cluster<D, R, C::kThreads / 32>(a, reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw))), lse_sh, b,
+                                           hkv, chunk, split, &merge_bar);
 }
 
 template <int D, int R, int kUse, int kCtas>

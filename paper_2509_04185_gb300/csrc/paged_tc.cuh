@@ -391,6 +391,23 @@ __device__ __forceinline__ void merge_rows(const Args& a, const float* rows, con
   }
 }
 
+// The end of a CTA of such a cluster, after its own pushes; every thread comes.  A CTA
+// whose rows do not come in time writes none.  No CTA ends before all of the cluster have
+// pushed: the barrier's arrival goes before the merge, its wait behind it.  Pushes issued
+// may still be on their way then, and the one whose wait gave up has not seen them arrive:
+// it waits again.
+template <int D, int R, int kWarps>
+__device__ __forceinline__ void merge_in_cluster(const Args& a, const float* rows, const float* lse, int b, int hkv, int chunk,
+                                                 int split, uint64_t* merge_bar) {
+  __syncwarp();
+  cluster_arrive();
+  const bool come = __all_sync(0xffffffffu, mbar_wait(merge_bar, 0, a.err));
+  if (come) merge_rows<D, R, kWarps>(a, rows, lse, b, hkv, chunk, split);
+  __syncwarp();
+  cluster_wait();
+  if (!come) mbar_wait(merge_bar, 0, a.err);
+}
+
 struct TcKernel {
   const void* fn;
   size_t smem;
