@@ -213,6 +213,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     // ------------------------------------------------ S = Q K^T
     tc_alloc(&tmem_base_sh, 512);
     __syncwarp();
+    if (n == 0) grid_dependents_launch();              // (nothing else here tells of the allocation)
     const uint32_t tmem = *(volatile uint32_t*)&tmem_base_sh;
     const bool leader = elect_one();
     bool ok = n > 0 && mbar_wait(&q_ready, 0, a.err);
@@ -545,7 +546,10 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
         __syncwarp();
         if (lane == 0) mbar_arrive(&o_free[i % kOBufs]);
       }
-      grid_dependents_launch();
+      // A kernel that takes tensor memory before it waits for this grid may follow, and what
+      // it holds it keeps until this grid is done: it starts only where this CTA has its own,
+      // as the products show (a CTA without any leaves it to warp 1, one that gave up to its end).
+      if (n > 0 && ok) grid_dependents_launch();
       if (a.splits > 1) cluster_arrive();
       // ------------------------------------------------ epilogue
       const float inv = m_ref == -INFINITY ? 0.f : __fdividef(1.f, l);

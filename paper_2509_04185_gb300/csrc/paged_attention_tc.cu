@@ -252,6 +252,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     // first scores.
     tc_alloc(&tmem_base_sh, C::kTmemCols);
     __syncwarp();
+    if (n == 0) grid_dependents_launch();              // (nothing else here tells of the allocation)
     const uint32_t tmem = *(volatile uint32_t*)&tmem_base_sh;
     const bool leader = elect_one();
     const bool ready = n > 0 && mbar_wait(&q_ready, 0, a.err);
@@ -549,7 +550,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       __syncwarp();
     }
     if (n > 0) add_product(n - 1);
-    grid_dependents_launch();
+    // A kernel that takes tensor memory before it waits for this grid may follow, and what
+    // it holds it keeps until this grid is done: it starts only where this CTA has its own,
+    // as the products show (a CTA without any leaves it to warp 1, one that gave up to its end).
+    if (n > 0 && ok) grid_dependents_launch();
     if (a.splits > 1) cluster_arrive();
     // ------------------------------------------------ epilogue
     sum_sh[sw][own] = l;

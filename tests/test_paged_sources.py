@@ -41,3 +41,12 @@ def test_no_cta_of_a_cluster_ends_before_all_have_pushed():
         assert not re.search(r"\bmerge_rows\b|mbar_wait\(&merge_bar", body)
         # the only early end is that of a CTA without a cluster
         assert re.findall(r"[^;{}]*\breturn;", body[body.index("tc_dealloc"):]) == ["\n  if (a.splits == 1) return;"]
+
+
+def test_dependents_start_only_where_tensor_memory_is_taken():
+    """The kernel that follows may take tensor memory before it waits for this grid."""
+    for name, kernel in (("paged_attention_tc.cu", "paged_tc_kernel"), ("paged_attention_rows.cu", "paged_rows_kernel")):
+        body = _body(_code(name), kernel)
+        conditions = [x.strip() for x in re.findall(r"([^;{}]*)grid_dependents_launch\(\);", body)]
+        assert conditions == ["if (n == 0)", "if (n > 0 && ok)"]
+        _in_order(body, "tc_alloc(", "if (n == 0) grid_dependents_launch();")
