@@ -8,6 +8,7 @@
 // rows r = i*G + g (block position i, query head g of the KV head's group).
 #include <math.h>
 
+#include "key_ranges.h"
 #include "paged.cuh"
 
 namespace {
@@ -103,22 +104,25 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
   const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
   const int b = blockIdx.z;
   const int cap = a.max_pages << a.log2P;
-  int len = a.lens[b];
-  if (len < 0 || len > cap) {
+  int cached = a.lens[b];
+  if (cached < 0 || cached > cap) {
     if (tid == 0) record_error(a.err, SBD_DEVERR_CACHE_LEN);
-    len = len < 0 ? 0 : cap;
+    cached = cached < 0 ? 0 : cap;
   }
-  const int total = len + a.k;
-  const int range = ((total + a.splits - 1) / a.splits + kGranule - 1) / kGranule * kGranule;
-  const int u_begin = min(total, split * range), u_end = min(total, u_begin + range);
+  // Places of keys are unsigned: the length may be 2^31 - 1 less the block, and a tile
+  // reaches past it.
+  const uint32_t len = cached;
+  const sbd::KeyRange keys = sbd::key_range(len + a.k, a.splits, split, kGranule);
+  const uint32_t u_begin = keys.begin, u_end = keys.end;
   const int32_t* table = a.table + (size_t)b * a.max_pages;
 
   uint4 kf[kFetch], vf[kFetch];
   float ksf[kFetch], vsf[kFetch];
-  auto fetch = [&](int t0) {
+  auto fetch = [&](uint32_t t0) {
 #pragma unroll
     for (int e = 0; e < kFetch; ++e) {
-      const int u = t0 + (tid + e * kThreads) / kC16, c = (tid + e * kThreads) % kC16;
+      const uint32_t u = t0 + (tid + e * kThreads) / kC16;
+      const int c = (tid + e * kThreads) % kC16;
       kf[e] = vf[e] = make_uint4(0, 0, 0, 0);
       ksf[e] = vsf[e] = 0.f;
       if (u < u_end && u < len) {
@@ -137,10 +141,11 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
     }
   };
   // rows past u_end are zeros (PV takes 4 keys at a time)
-  auto commit = [&](int t0) {
+  auto commit = [&](uint32_t t0) {
 #pragma unroll
     for (int e = 0; e < kFetch; ++e) {
-      const int j = (tid + e * kThreads) / kC16, c = (tid + e * kThreads) % kC16, u = t0 + j;
+      const int j = (tid + e * kThreads) / kC16, c = (tid + e * kThreads) % kC16;
+      const uint32_t u = t0 + j;
       float* kd = k_s + j * kKS + 16 * c;
       float* vd = v_s + j * D + 16 * c;
       if (u >= len && u < u_end) {
@@ -184,7 +189,7 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
   }
 
   // this warp's rows: local rows RW*warp .. + RW - 1; keys u < vis[r] are seen
-  int vis[RW], vis_min = u_end;
+  uint32_t vis[RW], vis_min = u_end;
 #pragma unroll
   for (int r = 0; r < RW; ++r) {
     const int i = (chunk * kRowsCta + RW * warp + r) / a.G;
@@ -203,8 +208,8 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
   const float* qw = q_s + RW * warp * D;
   float* pw = p_s + RW * warp * kKeys;
 
-  for (int t0 = u_begin; t0 < u_end; t0 += kKeys) {
-    const int n = min(kKeys, u_end - t0);
+  for (uint32_t t0 = u_begin; t0 < u_end; t0 += kKeys) {
+    const int n = min((uint32_t)kKeys, u_end - t0);
     commit(t0);
     __syncthreads();
     if (t0 + kKeys < u_end) fetch(t0 + kKeys);
@@ -261,7 +266,7 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
     }
     __syncwarp();
     // ---- O += P V, 4 keys at a time, as far as every row of the warp sees them
-    const int n_all = t0 + n <= vis_min ? n : max(0, vis_min - t0) & ~3;
+    const int n_all = t0 + n <= vis_min ? n : t0 < vis_min ? (int)(vis_min - t0) & ~3 : 0;
 #pragma unroll 2
     for (int j = 0; j < n_all; j += 4) {
       float v[4][kPer];

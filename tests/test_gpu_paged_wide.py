@@ -1,0 +1,35 @@
+"""The paged cache's calls at the far end of what they accept: 32-bit places that the
+next step would leave."""
+import numpy as np
+import pytest
+
+from test_gpu_paged import _i32, sbd  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,k,P,clamped", [("float32", 15, 16, False), ("bfloat16", 15, 16, True), ("float32", 1, 128, True)])
+def test_attention_over_the_longest_table(sbd, dtype, k, P, clamped):  # noqa: F811
+    """A request of as many keys as a block table has places for, 2^31 - 1 with the
+    block's (or one whose length is clamped to that).  All of its pages are one and the
+    same but the last, whose keys outweigh the others by e^128: the result is the mean
+    of the last page's values."""
+    import torch
+    D, cols = 64, (1 << 31) // P - 1
+    table = torch.zeros(1, cols, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    kc = torch.zeros(2, 1, P, D, device="cuda")
+    kc[1] = 1.0
+    vc = torch.full((2, 1, P, D), 7.0, device="cuda")
+    want = torch.arange(D, device="cuda") % 8 + 0.5
+    vc[1, 0] = torch.arange(D, device="cuda") % 8 + (torch.arange(P, device="cuda") % 2)[:, None]
+    one = torch.ones(2, 1, device="cuda")
+    dt = getattr(torch, dtype)
+    q = torch.full((1, k, 1, D), 16.0, device="cuda", dtype=dt)
+    block = torch.zeros(1, k, 1, D, device="cuda", dtype=dt)
+    f8 = torch.float8_e4m3fn
+    length = (1 << 31) - 1 if clamped else cols * P
+    out = sbd.sbd_block_attention_q8(q, kc.to(f8), vc.to(f8), one, one, table, _i32([length]), block, block - 3)
+    assert sbd.sbd_device_error() == (sbd.SBD_DEVERR_CACHE_LEN if clamped else 0)
+    # the weights of the last page are equal, their sum and the products exact in either type
+    assert (out.float() - want).abs().max().item() <= 1e-5
