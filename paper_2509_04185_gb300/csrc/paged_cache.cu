@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
     const int held = pages(len_s[b]);
     if (p < held) return a.table[(size_t)b * a.max_pages + p];
     const int i = need_at[b] + p - held;
-    return i < n_back ? released(i) : a.free_pages[n_free + n_back - 1 - i];
+    return i < n_back ? released(i) : a.free_pages[n_free - 1 - (i - n_back)];
   };
 
   const int gwarp = blockIdx.x * kTabWarps + warp, gwarps = gridDim.x * kTabWarps;
@@ -203,8 +203,8 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
   }
   // released pages go on top of the stack, the first one topmost, so that a
   // later call of the same growth gets the same pages back in the same order
-  for (int i = blockIdx.x * kTabThreads + tid; i < n_back; i += gridDim.x * kTabThreads) {
-    const int page = released(i);
+  for (uint32_t i = blockIdx.x * kTabThreads + tid; i < (uint32_t)n_back; i += gridDim.x * kTabThreads) {
+    const int page = released((int)i);
     const long long j = (long long)n_free + n_back - 1 - i;
     if (page < 0 || page >= a.n_pages || j >= a.n_pages) bad_page = true;
     if (j < a.n_pages) a.free_pages[j] = page;

@@ -33,3 +33,19 @@ def test_attention_over_the_longest_table(sbd, dtype, k, P, clamped):  # noqa: F
     assert sbd.sbd_device_error() == (sbd.SBD_DEVERR_CACHE_LEN if clamped else 0)
     # the weights of the last page are equal, their sum and the products exact in either type
     assert (out.float() - want).abs().max().item() <= 1e-5
+
+
+def test_tables_that_give_back_nearly_all_places(sbd):  # noqa: F811
+    """4096 requests of 524287 pages each end at once: 2^31 - 4096 pages, more than the
+    stack has room for, which is told; what fits is on it in order."""
+    import torch
+    B, cols, n_pages = 4096, (1 << 19) - 1, 1024
+    table = torch.zeros(B, cols, dtype=torch.int32, device="cuda")
+    table[-1, -n_pages:] = torch.arange(n_pages, dtype=torch.int32, device="cuda")
+    lens = torch.full((B,), 16 * cols, dtype=torch.int32, device="cuda")
+    free = torch.full((n_pages,), -5, dtype=torch.int32, device="cuda")
+    out = sbd.sbd_block_tables(lens, torch.zeros_like(lens), table, free, _i32([0]), 16, 0)
+    assert sbd.sbd_device_error() == sbd.SBD_DEVERR_PAGE
+    assert out[0].max().item() == -1 and out[0].min().item() == -1 and (out[1] == 0).all()
+    assert out[4].item() == n_pages
+    assert (free == torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device="cuda")).all()
