@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8
     const T* src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)(is_v ? plane - a.Hkv : plane) * D;
     const long long stride = is_v ? a.v_token_stride : a.k_token_stride;
     for (int i = threadIdx.x; i < a.chunk * kLines; i += kAppThreads)
-      if (t0 + i / kLines < a.tokens)
+      if ((uint32_t)t0 + i / kLines < (uint32_t)a.tokens)      // (may pass 2^31)
         prefetch_l2(src + (t0 + i / kLines) * stride + i % kLines * (128 / (int)sizeof(T)));
   };
   fetch_ahead(set);
@@ -344,9 +344,9 @@ __global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8
   // ---- the segments that begin in this chunk; chunk + P <= kAppThreads tokens
   // are looked at, as far as the last of them can reach
   {
-    const int t = t0 + tid;
-    const int s = t < a.tokens ? a.slot_map[t] : -1;
-    const int prev = t > 0 && t < a.tokens ? a.slot_map[t - 1] : -1;
+    const bool here = tid < a.tokens - t0;
+    const int s = here ? a.slot_map[t0 + tid] : -1;
+    const int prev = here && t0 + tid > 0 ? a.slot_map[t0 + tid - 1] : -1;
     const bool valid = s >= 0 && s < a.n_slots;
     if (s >= a.n_slots && set == 0) record_error(a.err, SBD_DEVERR_PAGE);
     const bool join = valid && prev >= 0 && prev + 1 == s && (s & last) != 0;
@@ -549,10 +549,10 @@ sbd_status append_q8_launch(const sbd_append_q8_desc& d, const void* k_new, cons
   // 65536 tokens of 8 heads 49 us, 60 in chunks of 128), and two planes a CTA where
   // that leaves enough CTAs (one: 10 % slower, four: 2 to 7 %).
   const int planes = 2 * d.n_kv_heads;
-  const long long jobs = (long long)planes * ((d.tokens + 63) / 64);
+  const long long jobs = planes * ((d.tokens + 63ll) / 64);
   a.chunk = jobs < 4ll * num_sms() ? 16 : d.head_dim == 64 ? kAppThreads - d.page_size : 128;
   a.planes = 1;
-  while (a.planes < 2 && (long long)planes * ((d.tokens + 127) / 128) / (2 * a.planes) >= 8ll * num_sms()) a.planes *= 2;
+  while (a.planes < 2 && planes * ((d.tokens + 127ll) / 128) / (2 * a.planes) >= 8ll * num_sms()) a.planes *= 2;
   const bool f32 = d.dtype == SBD_DTYPE_F32;
   const void* fn = d.head_dim == 128
                        ? (f32 ? (const void*)append_q8_kernel<float, 128>

@@ -35,6 +35,24 @@ def test_attention_over_the_longest_table(sbd, dtype, k, P, clamped):  # noqa: F
     assert (out.float() - want).abs().max().item() <= 1e-5
 
 
+def test_append_of_as_many_tokens_as_there_are_places(sbd):  # noqa: F811
+    """2^31 - 1 tokens (one row of memory, a stride of 0) of which the last three are stored."""
+    import torch
+    T = (1 << 31) - 1
+    slots = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    slots[-3:] = torch.arange(16, 19, dtype=torch.int32, device="cuda")
+    row = torch.arange(64, device="cuda").bfloat16().view(1, 1, 64)
+    codes = [torch.zeros(2, 1, 16, 64, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.zeros(2, 1, device="cuda") for _ in range(2)]
+    sbd.sbd_cache_append_q8(row.expand(T, 1, 64), (-row).expand(T, 1, 64), slots, *codes, *scales)
+    assert sbd.sbd_device_error() == 0
+    want = (row.float() * 4).to(torch.float8_e4m3fn).float().view(64) / 4       # 63 <= 448 / 4, > 448 / 8
+    for c, s, sign in zip(codes, scales, (1, -1)):
+        assert s.tolist() == [[0.0], [0.25]]
+        v = c.float() * 0.25
+        assert (v[1, 0, :3] == sign * want).all() and (v[1, 0, 3:] == 0).all() and (v[0] == 0).all()
+
+
 def test_tables_that_give_back_nearly_all_places(sbd):  # noqa: F811
     """4096 requests of 524287 pages each end at once: 2^31 - 4096 pages, more than the
     stack has room for, which is told; what fits is on it in order."""
