@@ -359,7 +359,9 @@ sbd_status sbd_select(int32_t rule, int32_t batch, int32_t block_k, const float*
  * or its tokens end past max_new; it keeps what it has.  Nothing of block_table
  * is overwritten, so a step in flight may still read it; block_table_out must
  * be other memory.  A length out of range is clamped, its request left as it is,
- * and SBD_DEVERR_CACHE_LEN set; a page id or an n_free out of range sets
+ * and SBD_DEVERR_CACHE_LEN set.  An n_free out of range is clamped, and a page id
+ * out of range, kept, granted or released, becomes -1 in block_table_out or on
+ * the stack (it counts as a page there) and the slots of its tokens -1; both set
  * SBD_DEVERR_PAGE.  No workspace.
  * Supported: 1 <= B <= 4096, B * max_pages < 2^31, max_new >= 0.
  * ---------------------------------------------------------------------- */

@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
   int* need_at = fresh_at + a.B;             // [B] pages they need
   int* back_at = need_at + a.B;              // [B] pages they release
   int* len_s = back_at + a.B;                // [B]
-  int* after_s = len_s + a.B;                // [B] length after the call
+  int* after_s = len_s + a.B;                // [B] length after the call; ~ of it where one was out of range
   __shared__ Sums warp_sum_sh[kTabWarps];
   __shared__ int used_sh[kTabWarps];
   grid_dependency_wait();
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
   int used = 0;
   for (int b = b0; b < b1; ++b) {
     int l, t;
-    request(b, &l, &t);
+    const bool bad = request(b, &l, &t);
     const int fresh = max(t - l, 0), need = max(pages(t) - pages(l), 0);
     const bool served = (need == 0 || (long long)at.need + need <= avail) &&
                         (fresh == 0 || at.fresh + fresh <= a.max_new);
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
     need_at[b] = at.need;
     back_at[b] = at.back;
     len_s[b] = l;
-    after_s[b] = served ? t : l;
+    after_s[b] = bad ? ~l : served ? t : l;
     if (served) used += need;
     if (blockIdx.x == 0) {
       a.len_out[b] = served ? t : l;
@@ -155,12 +155,21 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
     const int b = last_not_above(back_at, a.B, i);
     return a.table[(size_t)b * a.max_pages + pages(after_s[b]) + (i - back_at[b])];
   };
-  // the page at column p of request b after the call
+  // the page at column p of request b after the call; -1 where it is none of the cache's,
+  // which is told unless the request is left as it is
   auto page_at = [&](int b, int p) {
     const int held = pages(len_s[b]);
-    if (p < held) return a.table[(size_t)b * a.max_pages + p];
-    const int i = need_at[b] + p - held;
-    return i < n_back ? released(i) : a.free_pages[n_free - 1 - (i - n_back)];
+    int page;
+    if (p < held) {
+      page = a.table[(size_t)b * a.max_pages + p];
+    } else {
+      const int i = need_at[b] + p - held;
+      page = i < n_back ? released(i) : a.free_pages[n_free - 1 - (i - n_back)];
+    }
+    if ((uint32_t)page < (uint32_t)a.n_pages) return page;
+    if (after_s[b] < 0) return page;
+    bad_page = true;
+    return -1;
   };
 
   const int gwarp = blockIdx.x * kTabWarps + warp, gwarps = gridDim.x * kTabWarps;
@@ -168,7 +177,7 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
   const int units = a.B * chunks;                  // <= B max_pages < 2^31
   for (int u = gwarp; u < units; u += gwarps) {
     const int b = u / chunks, c0 = (u - b * chunks) * kTabCols;
-    const int keeps = pages(after_s[b]);
+    const int after = after_s[b], keeps = pages(after < 0 ? ~after : after);
 #pragma unroll
     for (int e = 0; e < kTabCols / 32; ++e) {
       const int p = c0 + 32 * e + lane;
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
       const int pos = len_s[b] + (t - fresh_at[b]), p = pos >> a.log2P;
       if (p != p_prev || b != b_prev) page = page_at(b, p);
       p_prev = p, b_prev = b;
-      v[e] = (page << a.log2P) + (pos & last);
+      v[e] = page < 0 ? -1 : (page << a.log2P) + (pos & last);
     }
     if (s + 4 <= a.max_new) {
       *reinterpret_cast<int4*>(a.slot_map + s) = make_int4(v[0], v[1], v[2], v[3]);
@@ -204,10 +213,10 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
   // released pages go on top of the stack, the first one topmost, so that a
   // later call of the same growth gets the same pages back in the same order
   for (uint32_t i = blockIdx.x * kTabThreads + tid; i < (uint32_t)n_back; i += gridDim.x * kTabThreads) {
-    const int page = released((int)i);
+    int page = released((int)i);
     const long long j = (long long)n_free + n_back - 1 - i;
-    if (page < 0 || page >= a.n_pages || j >= a.n_pages) bad_page = true;
-    if (j < a.n_pages) a.free_pages[j] = page;
+    if ((uint32_t)page >= (uint32_t)a.n_pages) bad_page = true, page = -1;
+    if (j < a.n_pages) a.free_pages[j] = page; else bad_page = true;
   }
   if (bad_page) record_error(a.err, SBD_DEVERR_PAGE);
   if (bad_len) record_error(a.err, SBD_DEVERR_CACHE_LEN);
