@@ -13,11 +13,14 @@ namespace sbd {
 
 class LaunchCache {
  public:
-  // Entries of one device: about 60 for the bf16 attention (4 kernels x cluster
+  // Cluster shapes of one device: 60 for the bf16 attention (4 kernels x cluster
   // sizes 2 to 16), 54 for the fp32 attention (6 x 9), 70 for sbd_linear (10
-  // sizes of shared memory x 7), 6 CTA-pair kernels and one a kernel for its
-  // shared memory.
-  static constexpr int kEntries = 512;
+  // sizes of shared memory x 7), 6 CTA-pair kernels; over the paged cache 210
+  // for bf16 (14 x 15) and 54 for fp32: about 460.
+  static constexpr int kEntries = 1024;
+  // Kernels with a limit of their own on shared memory: about 50 in the library.
+  // They have their own places, so that no number of shapes takes one.
+  static constexpr int kKernels = 256;
 
   // query(): clusters the device holds at once, or < 0 when it could not be
   // asked; that is returned as 0 and not kept, so that the next call asks again.
@@ -26,7 +29,7 @@ class LaunchCache {
     {
       std::lock_guard<std::mutex> lock(mu_);
       const Entry* e = slot(fn, threads, smem, cluster_x);
-      if (e && e->fn) return (int)e->value;
+      if (e && e->fn) return e->value;
     }
     const int n = query();
     if (n < 0) return 0;
@@ -42,10 +45,10 @@ class LaunchCache {
   template <class Set>
   int allow_smem(const void* fn, size_t smem, Set set) {
     std::lock_guard<std::mutex> lock(mu_);
-    Entry* e = slot(fn, 0, 0, 0);
-    const size_t most = e && e->fn && (size_t)e->value > smem ? (size_t)e->value : smem;
+    Limit* e = limit(fn);
+    const size_t most = e && e->fn && e->smem > smem ? e->smem : smem;
     const int st = set(most);
-    if (st == 0 && e) *e = Entry{fn, 0, 0, 0, (long long)most};
+    if (st == 0 && e) *e = Limit{fn, most};
     return st;
   }
 
@@ -54,7 +57,11 @@ class LaunchCache {
     const void* fn;      // nullptr: free
     size_t smem;
     int threads, cluster_x;
-    long long value;
+    int value;
+  };
+  struct Limit {
+    const void* fn;      // nullptr: free
+    size_t smem;
   };
 
   // The entry of this key, or the free one it would take; nullptr when full.
@@ -69,8 +76,19 @@ class LaunchCache {
     return nullptr;
   }
 
+  // The same of a kernel's limit.
+  Limit* limit(const void* fn) {
+    const uint64_t h = ((uint64_t)(uintptr_t)fn >> 4) * 1000003u;
+    for (int i = 0; i < kKernels; ++i) {
+      Limit& e = limits_[(h + (uint64_t)i) % kKernels];
+      if (!e.fn || e.fn == fn) return &e;
+    }
+    return nullptr;
+  }
+
   std::mutex mu_;
   Entry entries_[kEntries] = {};
+  Limit limits_[kKernels] = {};
 };
 
 }  // namespace sbd
