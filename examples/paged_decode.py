@@ -8,7 +8,8 @@ pages back to the next one.  A block is
     sbd_block_tables            pages and slots for the tokens that enter the cache
     sbd_linear                  the fused projection of the rows
     sbd_block_attention_q8      the previous block's rows (causal, first iteration
-                                only) and the block's, over the cache
+                                only) and the block's, over the cache; a request just
+                                taken in has no previous block, and is in a call apart
     sbd_cache_append_q8         the previous block's keys and values, straight from
                                 the fused projection
     sbd_head_entropy_sample, sbd_eb_select
@@ -59,7 +60,8 @@ class PagedDecoder:
         self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device="cuda")
         self.length = ints(requests)                # tokens in the cache
         self.alive = torch.zeros(requests, dtype=torch.bool, device="cuda")
-        self.last = None                            # the block that is not in the cache yet [B, k]
+        # The block of each request that is not in the cache yet; a row of masks: there is none.
+        self.last = torch.full((requests, k), MASK, dtype=torch.int32, device="cuda")
         self.forwards = 0
 
     def _resize(self, target, max_new):
@@ -76,9 +78,12 @@ class PagedDecoder:
         return x, y.view(len(x), q + 2 * kv, d)
 
     def admit(self, prompts):
-        """Takes in {request: prompt [n] int32}: its keys and values enter the cache."""
+        """Takes in {request: prompt [n] int32}: its keys and values enter the cache.  A place
+        whose request has ended has no block waiting, unless the caller writes one to `last`."""
         target = self.length.clone()
         for b, p in prompts.items():
+            if bool(self.alive[b]):
+                raise ValueError(f"request {b} is still running")
             target[b] = len(p)
         order = sorted(prompts)
         tokens = torch.cat([prompts[b] for b in order]).cuda()
@@ -96,42 +101,67 @@ class PagedDecoder:
         for b in requests:
             target[b] = 0
             self.alive[b] = False
+            self.last[b] = MASK
         self._resize(target, 0)
+
+    def _rows(self, at, rows, n_causal):
+        """Hidden rows, keys, values and attention of rows [b, n] of the requests `at`, of
+        which the first n_causal are the block before."""
+        q, kv, d = self.heads
+        b, n = rows.shape
+        length = self.length[at].contiguous()
+        x, qkv = self._project(rows.reshape(-1), (length[:, None] + torch.arange(n, device="cuda")).reshape(-1))
+        qkv = qkv.view(b, n, q + 2 * kv, d)
+        keys, values = qkv[:, :, q:q + kv], qkv[:, :, q + kv:]
+        out = sbd.sbd_block_attention_q8(
+            qkv[:, :, :q].contiguous(), *self.cache, *self.scale, self.table[at].contiguous(), length,
+            keys.contiguous(), values.contiguous(), n_causal=n_causal)
+        return x.view(b, n, -1), keys, values, out
+
+    def _store_block(self, at, pending, keys, values):
+        """The previous block's keys and values, of the requests `at` that had one, enter the
+        cache.  A request that finds no page ends here."""
+        runs = self.alive & pending
+        target = self.length + self.k * runs.int()
+        _, slots = self._resize(target, self.B * self.k)
+        live = runs[at]
+        if not bool(live.all()):
+            keys, values = keys[live], values[live]
+        sbd.sbd_cache_append_q8(keys, values, slots, *self.cache, *self.scale)
+        self.alive &= self.length == target
 
     def decode_block(self):
         """The next k tokens of every request [B, k] int32 (of ended ones too: their rows mean nothing)."""
-        B, k, (q, kv, d) = self.B, self.k, self.heads
+        B, k, (q, _, d) = self.B, self.k, self.heads
         tokens = torch.full((B, k), MASK, dtype=torch.int32, device="cuda")
         masked = torch.ones((B, k), dtype=torch.uint8, device="cuda")
-        previous = self.last
+        everyone = slice(None)
+        pending = (self.last != MASK).all(1)
+        some, every = bool(pending.any()), bool(pending.all())
         while True:
-            rows = tokens if previous is None else torch.cat([previous, tokens], 1)
-            n = rows.shape[1]
-            x, qkv = self._project(rows.reshape(-1), (self.length[:, None] + torch.arange(n, device="cuda")).reshape(-1))
-            qkv = qkv.view(B, n, q + 2 * kv, d)
-            keys, values = qkv[:, :, q:q + kv], qkv[:, :, q + kv:]
-            out = sbd.sbd_block_attention_q8(
-                qkv[:, :, :q].contiguous(), *self.cache, *self.scale, self.table, self.length,
-                keys.contiguous(), values.contiguous(), n_causal=n - k)
-            if previous is not None:
-                # The previous block enters the cache; a request that finds no page ends here.
-                target = self.length + k * self.alive.int()
-                _, slots = self._resize(target, B * k)
-                if bool(self.alive.all()):
-                    sbd.sbd_cache_append_q8(keys[:, :k], values[:, :k], slots, *self.cache, *self.scale)
-                else:
-                    live = self.alive.nonzero()[:, 0]
-                    sbd.sbd_cache_append_q8(keys[live, :k], values[live, :k], slots, *self.cache, *self.scale)
-                self.alive &= self.length == target
-                previous = None
-            flat = out[:, n - k:].reshape(B * k, q * d)
-            y = torch.cat([sbd.sbd_linear(flat[i:i + 512], self.w_out) for i in range(0, len(flat), 512)])
-            h = x.view(B, n, -1)[:, n - k:] + y.view(B, k, -1)
+            if some:                                # the first time: who has a block waiting, and who has none
+                at = everyone if every else pending.nonzero()[:, 0]
+                hidden, keys, values, out = self._rows(at, torch.cat([self.last, tokens], 1)[at], k)
+                parts = [(at, hidden[:, k:], out[:, k:])]
+                if not every:
+                    rest = (~pending).nonzero()[:, 0]
+                    hidden, _, _, out = self._rows(rest, tokens[rest], 0)
+                    parts.append((rest, hidden, out))
+                self._store_block(at, pending, keys[:, :k], values[:, :k])
+                some = False
+            else:
+                hidden, _, _, out = self._rows(everyone, tokens, 0)
+                parts = [(everyone, hidden, out)]
+            h = torch.empty((B, k, self.embed.shape[1]), dtype=torch.bfloat16, device="cuda")
+            for at, hidden, out in parts:
+                flat = out.reshape(-1, q * d)
+                y = torch.cat([sbd.sbd_linear(flat[i:i + 512], self.w_out) for i in range(0, len(flat), 512)])
+                h[at] = hidden + y.view(hidden.shape)
             entropy, token = sbd.sbd_head_entropy_sample(h, self.w_head, masked, None, 0.0)
             sbd.sbd_eb_select(entropy, token, self.gamma, masked, tokens)
             self.forwards += 1
             if not bool(masked.any()):
-                self.last = tokens
+                self.last = torch.where(self.alive[:, None], tokens, MASK)
                 return tokens
 
 
