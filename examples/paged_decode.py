@@ -128,7 +128,9 @@ class PagedDecoder:
         if not bool(live.all()):
             keys, values = keys[live], values[live]
         sbd.sbd_cache_append_q8(keys, values, slots, *self.cache, *self.scale)
-        self.alive &= self.length == target
+        refused = (self.length != target).nonzero()[:, 0].tolist()
+        if refused:
+            self.finish(refused)
 
     def decode_block(self):
         """The next k tokens of every request [B, k] int32 (of ended ones too: their rows mean nothing)."""
