@@ -249,3 +249,54 @@ def test_the_same_call_answers_the_same_bits(sbd, dtype, B, k, Hq, H, D, page, h
         for c, x in zip(calls, first):
             differ += (run(c) != x).sum()
     assert differ.item() == 0 and sbd.sbd_device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("k,Hq,D,num_splits", [(1, 2, 128, 0), (4, 8, 64, 0), (8, 8, 128, 3), (8, 8, 64, 1), (16, 12, 128, 0), (32, 8, 64, 2)])
+def test_attention_keeps_nan_where_it_belongs(sbd, dtype, k, Hq, D, num_splits):  # noqa: F811
+    """NaN and infinities in a row of q, a cached key, a cached value, a block key and a
+    block value: whoever does not see them answers the same bits as without them."""
+    rng = np.random.default_rng(k)
+    case = tp._attention_case(rng, 3, k, Hq, 2, D, 32, [300, 40, 129])
+    copy = lambda: [x.copy() if isinstance(x, np.ndarray) else [y.copy() for y in x] for x in case]  # noqa: E731
+    run = lambda c: tp._attend(sbd, tuple(c), dtype, n_causal=k - 1, num_splits=num_splits, check=False)  # noqa: E731
+    want = run(case)
+    assert np.isfinite(want).all()
+    g = Hq // 2
+
+    def others(got, b, i, heads):                   # all but rows i (a slice) of these heads of request b
+        seen = np.ones(got.shape[:3], bool)
+        seen[b, i, heads] = False
+        return (got[seen] == want[seen]).all()
+
+    for bad in (np.nan, np.inf):
+        c = copy()
+        c[0][1, k // 2, g, 5] = bad                 # q: one row
+        got = run(c)
+        assert np.isnan(got[1, k // 2, g]).all() and others(got, 1, k // 2, g)
+    every, second = slice(None), slice(g, None)     # the second KV head's
+    c = copy()
+    c[1][0][case[3][0, 3], 1, 17, 3] = 0x7F         # a cached key: every row of its request and head
+    got = run(c)
+    assert np.isnan(got[0, :, second]).all() and others(got, 0, every, second)
+    c = copy()
+    c[1][1][case[3][0, 9], 1, 11, 3] = 0xFF         # a cached value (the last token): one dimension
+    got = run(c)
+    assert np.isnan(got[0, :, second, 3]).all() and others(got, 0, every, second)
+    rest = np.arange(D) != 3
+    assert (got[0, :, second][..., rest] == want[0, :, second][..., rest]).all()
+    for bad in (np.nan, np.inf):
+        last = slice(k - 1, None)
+        c = copy()
+        c[5][2, k - 1, 1, 4] = bad                  # the last block key: only the last row sees it
+        got = run(c)
+        assert others(got, 2, last, second) and (bad == np.inf or np.isnan(got[2, k - 1, second]).all())
+        c = copy()
+        c[6][2, k - 1, 1, 4] = bad                  # its value
+        got = run(c)
+        assert others(got, 2, last, second) and not np.isfinite(got[2, k - 1, second, 4]).any()
+    # slots past the length
+    c = copy()
+    c[1][0][case[3][2, 4], :, 1:] = 0x7F
+    c[1][1][case[3][2, 4], :, 1:] = 0xFF
+    assert (run(c) == want).all() and sbd.sbd_device_error() == 0
