@@ -284,6 +284,11 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
       }
       __syncwarp();
     }
+    // A kernel that takes tensor memory before it waits for this grid may follow, and what it
+    // holds it keeps until this grid is done: it starts only where this CTA has its own, as
+    // the products show (a CTA without any leaves it to warp 1, one that gave up to its end).
+    // (The accumulators' warps have no register to spare for the condition.)
+    if (n > 0 && ok) grid_dependents_launch();
   } else {
     const int sw = warp - kControl, quad = warp & 3;
     const int r = quad * 32 + lane, row = chunk * kRows + r;   // lane of tensor memory, packed row
@@ -546,10 +551,6 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
         __syncwarp();
         if (lane == 0) mbar_arrive(&o_free[i % kOBufs]);
       }
-      // A kernel that takes tensor memory before it waits for this grid may follow, and what
-      // it holds it keeps until this grid is done: it starts only where this CTA has its own,
-      // as the products show (a CTA without any leaves it to warp 1, one that gave up to its end).
-      if (n > 0 && ok) grid_dependents_launch();
       if (a.splits > 1) cluster_arrive();
       // ------------------------------------------------ epilogue
       const float inv = m_ref == -INFINITY ? 0.f : __fdividef(1.f, l);
