@@ -432,8 +432,10 @@ sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new
  * activations the tensor cores read the codes; a row of q and of k_blk enters as
  * x = s (hi + lo), two e4m3 codes an element (8 bits of the row's largest; what is
  * not finite becomes NaN), a probability as 8 bits (11 above 32 packed rows k G)
- * relative to its own 256 (128) keys' largest.  Scales are positive; a value whose
- * page's scale is below 2^-14 of the largest among the same 256 keys loses bits.
+ * relative to its own 256 (128) keys' largest.  Scales are positive.  A value scale
+ * enters as fp16, relative to the largest among the same 256 (128) keys: exact for
+ * powers of two (the append's) down to 2^-14 of it, below that bits are lost; one
+ * that is no power of two costs two roundings of 2^-11.  Key scales stay fp32.
  * With fp32 activations everything is fp32.
  *
  * No workspace: its size is 0 and the arguments are not looked at.

@@ -21,12 +21,14 @@
 // 10 the softmax, two groups of four that take the tiles in turn; 11 to 18 the conversion
 // of V and the accumulators, two warps to a quadrant of 32 rows.
 //
-// Bounds and figures.  16 requests of 8192 keys, 128 rows and dimensions: 80 us, 2,300
+// Bounds and figures.  16 requests of 8192 keys, 128 rows and dimensions: 81 us, 2,300
 // clocks for a tile of 128 rows and keys, where memory would allow 41 us and the products
 // 37 (16 a tile, 68 clocks each).  What sets the pace is a chain from tile to tile: the
-// product O, the accumulators' warps that read and add it (tensor memory has no place for
-// a second O beside two S and two P at 128 dimensions) and convert the next V meanwhile.
-// 19 x 4096 keys, 64 rows: 43.5 us, the same chain (24 us of bytes).  One request of 4096
+// product O, the accumulators' warps that read and add it and convert the next V
+// meanwhile.  At 128 dimensions there is one O: two S, two P in columns of their own and
+// two O would be 640 columns of 512.  (P over the S it came from would leave room for a
+// second; not built.)
+// 19 x 4096 keys, 64 rows: 45 us, the same chain (24 us of bytes).  One request of 4096
 // keys, 64 rows, 12 splits of three tiles: 11.5 us, of which 2 are the launch, 2.5 the
 // way to the first scores (lengths -> table -> copies), 3 the merge of the splits.
 // Registers matter more than instructions: shared memory leaves no L1, so a spill is a trip

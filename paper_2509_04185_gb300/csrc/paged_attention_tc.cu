@@ -16,8 +16,8 @@
 // to 8) and a thread of the softmax owns one key: its page's scales are scalars of the thread, masks a
 // comparison, a row's maximum and sum one redux a warp.  Above 32 rows those
 // reductions cost more than the tile's loads, and rows are on the lanes
-// (paged_attention_rows.cu): at 64 rows over 19 x 4096 keys, 128 dimensions, 43.5 us
-// instead of the 50.4 that this kernel took, at 128 rows over 16 x 8192 80 instead of 177.
+// (paged_attention_rows.cu): at 64 rows over 19 x 4096 keys, 128 dimensions, 45 us
+// instead of the 50.4 that this kernel took, at 128 rows over 16 x 8192 81 instead of 177.
 //
 // Tiles go in steps of two (256 keys): what a step costs by row and not by key --
 // redux, the row's scale and maximum from shared memory, the accumulators.
@@ -70,7 +70,8 @@ struct Shape {
   static_assert(kCtas * kTmemCols <= 512, "tensor memory holds them");
   // Four softmax warps take 8 rows of a step, of the first kUse (what the others' columns
   // hold reaches no column that is read); 16 where two CTAs of 32 rows share an SM, with
-  // one warp less for the products: five warps a scheduler leave 96 registers each.
+  // one warp less for the products: five warps a scheduler leave 96 registers each (and
+  // a dozen more are spilled, 64 bytes at 64 dimensions, 52 at 128).
   static constexpr bool kFew = R == 32 && kCtas == 2;
   static constexpr int kRT = kFew ? 16 : 8;
   static constexpr int kControl = kFew ? 2 : 3;        // warps: pages and TMA, products S, products O
@@ -361,7 +362,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
       __syncwarp();
       if (lane == 0) mbar_arrive(&blk_ready);
     }
-    // A lane keeps the statistics of one row (two lanes a row) over its warp's keys:
+    // A lane keeps the statistics of one row (32 / kRT lanes a row) over its warp's keys:
     // the running maximum (the same in the four warps of a part) and the sum of
     // probabilities against it.  A thread also keeps the accumulators of its warp's
     // rows for one dimension, against the same maximum.
@@ -570,7 +571,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     // M = 64 leaves 16 dimensions in the first half of every quadrant's lanes
     const int d = D == 128 ? quad * 32 + lane : quad * 16 + (lane & 15);
     const bool has_d = D == 128 || lane < 16;
-    const int row = chunk * R + r0;                    // packed rows row .. row + 15
+    const int row = chunk * R + r0;                    // packed rows row .. row + kRT - 1
     if (has_block && blk_bad && has_d) {
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {

@@ -23,8 +23,9 @@ using namespace sbd_dev;
 // are few) and then share the outputs out.
 // Bound: latency, the chain lengths -> sums -> page -> store.  32 requests gain 8
 // tokens: 3.7 us, a launch and that chain; 256 requests gain a million, 4.2 MB of
-// slots and 0.6 MB of table: 8.6 us (10.2 with half as many CTAs, which go round
-// twice).
+// slots and 0.6 MB of table: 8.6 us, much of it the sums that every one of 1,216 CTAs
+// forms and a search of up to eight steps for four tokens (10.2 with half as many
+// CTAs, which go round twice).
 constexpr int kTabThreads = 256;
 constexpr int kTabWarps = kTabThreads / 32;
 constexpr int kTabCols = 128;                // columns of a table row per warp and turn
@@ -231,8 +232,9 @@ __global__ void __launch_bounds__(kTabThreads) block_tables_kernel(const TablesA
 //   code  = e4m3(x / s), round to nearest even; infinities saturate, NaN stays;
 // and where s > s_old the codes the page holds already become e4m3(c s_old / s):
 // s_old / s is a power of two, so only codes that leave the normal range round.
-// That is why scales are powers of two: a page filled over many calls loses
-// nothing each time its scale grows, and x / s is exact.
+// That is why scales are powers of two: x / s is exact, and a page filled over many
+// calls loses nothing when its scale grows, but for codes that fall below 2^-6, the
+// normal range, and are rounded there to a multiple of 2^-9 s once more.
 //
 // A CTA finds the segments that begin in its chunk of tokens and works on them for
 // some planes (K or V of a head); its 8 warps form as many teams as there are
