@@ -461,6 +461,162 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
                                   const void* k_blk, const void* v_blk, void* out,
                                   void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * A turn of drafted decoding over the paged 8-bit cache.
+ *
+ * Drafted tokens (from the k marginals of a block forward, or from another
+ * model) are checked against the model's own next-token distribution in one
+ * forward.  A request's rows form a tree of n nodes: node 0 is the last token
+ * that was kept, not in the cache yet, and node i > 0 a drafted token that
+ * follows node parent[b, i] < i.  A node with a negative parent begins a tree of
+ * its own: padding, which no walk from node 0 reaches.  A chain is parent = i - 1.
+ *
+ *   sbd_qk_norm_rope           the nodes' fused projection becomes normed and
+ *                              rotated queries and keys, and values
+ *   sbd_tree_attention_q8      a node sees the cache, itself and its ancestors
+ *   sbd_verify_tree            which nodes are accepted, and the token after them
+ *   sbd_block_tables           pages for the accepted nodes: target_len =
+ *                              cache_len + count
+ *   sbd_cache_append_path_q8   their keys and values enter the cache
+ *
+ * A parent that is not below its node, a drafted token outside [0, vocab) or a
+ * path entry outside [0, n) sets SBD_DEVERR_TREE; the node then begins a tree of
+ * its own, the token is passed over, the entry is not stored.
+ * ---------------------------------------------------------------------- */
+
+/* ------------------------------------------------------------------------
+ * Queries and keys normed by head and rotated by position, values copied:
+ *   y = w * x / sqrt(mean_d x_d^2 + eps)      (w NULL: y = x)
+ *   pair j < R / 2 of y turns by the angle a = positions[t] * inv_freq[j]:
+ *     (y1 cos a - y2 sin a, y2 cos a + y1 sin a)
+ * where pair j is (j, j + R / 2), or (2 j, 2 j + 1) where desc->interleaved; what
+ * lies past the first R = rotary_dim dimensions is not turned.  One rounding at the
+ * end.  Angles are exact to 2^-31 of a turn for |position * inv_freq| < 2^21 turns
+ * (the product is kept in fixed point, whole turns dropped), so any position does.
+ *
+ *   q [T, Hq, D], k, v [T, Hkv, D]   desc->dtype; token t lies (t / group) *
+ *                                    group_stride + (t % group) * token_stride
+ *                                    elements behind the first (heads contiguous)
+ *   positions [T] int32              NULL iff rotary_dim == 0
+ *   inv_freq [R / 2] fp32            finite; NULL iff rotary_dim == 0
+ *   q_weight, k_weight [D]           desc->dtype; NULL: not normed
+ *   q_out [T, Hq, D], k_out, v_out [T, Hkv, D]   contiguous, other memory than the
+ *                                    inputs; v and v_out may be NULL (both)
+ * Supported: D in {64, 128}, R a multiple of 16, 0 <= R <= D, eps >= 0 and
+ * finite, strides that are multiples of 16 bytes, group >= 1.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t tokens;       /* T */
+  int32_t group;        /* tokens of a group; T where there is one stride only */
+  int32_t n_q_heads;    /* Hq */
+  int32_t n_kv_heads;   /* Hkv */
+  int32_t head_dim;     /* D */
+  int32_t rotary_dim;   /* R */
+  int32_t interleaved;  /* pairs are neighbours */
+  int32_t dtype;        /* sbd_dtype */
+  float eps;
+  int64_t q_group_stride, q_token_stride; /* elements */
+  int64_t k_group_stride, k_token_stride;
+  int64_t v_group_stride, v_token_stride;
+} sbd_norm_rope_desc;
+
+sbd_status sbd_qk_norm_rope(const sbd_norm_rope_desc* desc, const void* q, const void* k,
+                            const void* v, const int32_t* positions, const float* inv_freq,
+                            const void* q_weight, const void* k_weight, void* q_out, void* k_out,
+                            void* v_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * sbd_block_attention_q8 for a tree: block row i sees the cached keys and, of
+ * the block keys, its own and its ancestors'.  desc->block_k is the number of
+ * nodes, 1 .. 64, and desc->n_causal must be 0.
+ *   parent [B, n] int32 (device)
+ * Everything else, the workspace (none) and the errors are those of
+ * sbd_block_attention_q8.
+ * ---------------------------------------------------------------------- */
+size_t sbd_tree_attention_q8_workspace_size(const sbd_attn_q8_desc* desc);
+sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, const void* k_cache,
+                                 const void* v_cache, const float* k_scale, const float* v_scale,
+                                 const int32_t* block_table, const int32_t* cache_len,
+                                 const void* k_blk, const void* v_blk, const int32_t* parent,
+                                 void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Verification of drafted tokens, from given random numbers.  Per request, with
+ * p_i = softmax(target_logits[b, i] / tau) and q_i = softmax(draft_logits[b, i] / tau):
+ *
+ *   node = 0; r = p_0
+ *   for every child c of node, in index order, with its token x = token[b, c]:
+ *     accept c iff uniform[b, c] * q_node(x) < r(x):  node = c, r = p_c, go on there;
+ *     else r = max(r - q_node, 0), normalised (r stays where nothing is left)
+ *   where no child is accepted, or there is none: the last token is
+ *     argmax_v (ln r(v) + gumbel[b, v]), lowest v on ties
+ *
+ * The tokens that come out are distributed as p if a node's children were drawn from
+ * q_node one by one, uniform is uniform on [0, 1) and gumbel is standard Gumbel noise
+ * (sbd_gumbel_philox).  draft_logits NULL: a drafted token was not drawn but given, q is
+ * 1 there and 0 elsewhere.  tau = 0: p is 1 at the largest logit (lowest index of equal
+ * ones); draft_logits, uniform and gumbel are not read.  A logit that is NaN counts
+ * as -inf, one that is +inf as the largest finite number.  Where no logit of a row is
+ * above -inf nothing is accepted there, and the last token is 0.
+ *
+ *   target_logits, draft_logits [B, n, V]   desc->dtype; draft row i: what i's children
+ *                                           were drawn from (read where it has some)
+ *   parent, token [B, n] int32              token[b, 0] is not read
+ *   uniform [B, n] fp32, gumbel [B, V] fp32 NULL iff tau == 0
+ *   path [B, n] int32 out      accepted nodes from node 0 on, then -1
+ *   out_tokens [B, n] int32 out  the tokens of path[1], ..., then the last token, then -1
+ *   logprob [B, n] fp32 out    ln p of each of them (at temperature 1 where tau = 0), then 0
+ *   count [B] int32 out        nodes on the path = tokens that come out, 1 .. n
+ *
+ * Logits, exponentials and sums in fp32.  No workspace: its size is 0.  The rows of nodes
+ * that the walk does not come to are not read.
+ * Supported: 1 <= n <= 64, V >= 1, B <= 65535, tau = 0 or 2^-20 <= tau <= 2^20.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch;   /* B */
+  int32_t nodes;   /* n */
+  int32_t vocab;   /* V */
+  int32_t dtype;   /* sbd_dtype of the logits */
+} sbd_verify_desc;
+
+size_t sbd_verify_tree_workspace_size(const sbd_verify_desc* desc);
+sbd_status sbd_verify_tree(const sbd_verify_desc* desc, const void* target_logits,
+                           const void* draft_logits, const int32_t* parent, const int32_t* token,
+                           const float* uniform, const float* gumbel, float tau, int32_t* path,
+                           int32_t* out_tokens, float* logprob, int32_t* count, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The keys and values of accepted nodes into their slots: sbd_cache_append_q8 for
+ * nodes that do not lie one behind the other.  Request b gains new_start[b + 1] -
+ * new_start[b] tokens (n at most), its j-th in slot slot_map[new_start[b] + j] with the
+ * keys and values of node path[b, j].
+ *
+ *   k_new, v_new [B, n, Hkv, D]   desc->dtype; node i of request b lies b *
+ *                                 batch_stride + i * node_stride elements behind the
+ *                                 first (heads contiguous)
+ *   path [B, n] int32, new_start [B + 1] int32, slot_map [max_new] int32
+ *                                 as sbd_verify_tree and sbd_block_tables give them
+ *
+ * Segments, scales, codes and errors are those of sbd_cache_append_q8; a slot that is
+ * negative or past max_new is not stored.  Requests do not share the pages they append to.
+ * Supported: 1 <= n <= 64, B <= 65535, strides that are multiples of 16 bytes.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch, nodes;   /* B, n */
+  int32_t n_kv_heads, head_dim, page_size, n_pages;
+  int32_t max_new;        /* entries of slot_map */
+  int32_t dtype;          /* sbd_dtype of k_new and v_new */
+  int64_t k_batch_stride, k_node_stride; /* elements */
+  int64_t v_batch_stride, v_node_stride;
+} sbd_append_path_desc;
+
+sbd_status sbd_cache_append_path_q8(const sbd_append_path_desc* desc, const void* k_new,
+                                    const void* v_new, const int32_t* path,
+                                    const int32_t* new_start, const int32_t* slot_map,
+                                    void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                                    void* stream);
+
 /* Status name ("SBD_OK", ...). Never NULL. */
 const char* sbd_status_string(sbd_status status);
 
@@ -476,6 +632,7 @@ sbd_status sbd_device_error(int32_t* code);
 #define SBD_DEVERR_TIMEOUT 2     /* a bounded wait inside a kernel gave up  */
 #define SBD_DEVERR_ROWS 4        /* more masked rows than the head supports */
 #define SBD_DEVERR_PAGE 8        /* a page id, slot or free-page count was out of range */
+#define SBD_DEVERR_TREE 16       /* a node's parent, drafted token or path entry was out of range */
 
 /* Library version, major * 10000 + minor * 100 + patch. */
 int32_t sbd_version(void);

@@ -20,6 +20,15 @@ A serving batch may keep its KV cache in 8-bit pages instead:
     sbd_cache_append_q8(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_scale)
     sbd_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table,
                            cache_len, k_blk, v_blk)
+
+Drafted tokens are checked against the model in one forward over that cache:
+
+    sbd_qk_norm_rope(q, k, v, positions, inv_freq, q_weight, k_weight)
+    sbd_tree_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table,
+                          cache_len, k_blk, v_blk, parent)
+    sbd_verify_tree(target_logits, draft_logits, parent, token, uniform, gumbel, tau)
+    sbd_cache_append_path_q8(k_new, v_new, path, new_start, slot_map, k_cache,
+                             v_cache, k_scale, v_scale)
 """
 from __future__ import annotations
 
@@ -40,6 +49,7 @@ SBD_DEVERR_CACHE_LEN = 1
 SBD_DEVERR_TIMEOUT = 2
 SBD_DEVERR_ROWS = 4
 SBD_DEVERR_PAGE = 8
+SBD_DEVERR_TREE = 16
 SBD_HEAD_NOALLOC_MAX_SCRATCH = 8 << 20
 SBD_SELECT_EB_ENTROPY = 0
 SBD_SELECT_EB_CONFIDENCE = 1
@@ -65,6 +75,12 @@ EXPORTS = (
     "sbd_cache_append_q8",
     "sbd_block_attention_q8_workspace_size",
     "sbd_block_attention_q8",
+    "sbd_qk_norm_rope",
+    "sbd_tree_attention_q8_workspace_size",
+    "sbd_tree_attention_q8",
+    "sbd_verify_tree_workspace_size",
+    "sbd_verify_tree",
+    "sbd_cache_append_path_q8",
     "sbd_status_string",
     "sbd_last_error",
     "sbd_device_error",
@@ -113,6 +129,31 @@ class AttnQ8Desc(ctypes.Structure):
                 ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("n_causal", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("num_splits", ctypes.c_int32)]
+
+
+class NormRopeDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float),
+                ("q_group_stride", ctypes.c_int64), ("q_token_stride", ctypes.c_int64),
+                ("k_group_stride", ctypes.c_int64), ("k_token_stride", ctypes.c_int64),
+                ("v_group_stride", ctypes.c_int64), ("v_token_stride", ctypes.c_int64)]
+
+
+class VerifyDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("nodes", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class AppendPathDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("nodes", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("k_batch_stride", ctypes.c_int64), ("k_node_stride", ctypes.c_int64),
+                ("v_batch_stride", ctypes.c_int64), ("v_node_stride", ctypes.c_int64)]
 
 
 class SbdError(RuntimeError):
@@ -167,6 +208,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sbd_block_attention_q8_workspace_size.restype = sz
     lib.sbd_block_attention_q8.argtypes = [ctypes.POINTER(AttnQ8Desc)] + [vp] * 11 + [sz, vp]
     lib.sbd_block_attention_q8.restype = ctypes.c_int
+    lib.sbd_qk_norm_rope.argtypes = [ctypes.POINTER(NormRopeDesc)] + [vp] * 11
+    lib.sbd_qk_norm_rope.restype = ctypes.c_int
+    lib.sbd_tree_attention_q8_workspace_size.argtypes = [ctypes.POINTER(AttnQ8Desc)]
+    lib.sbd_tree_attention_q8_workspace_size.restype = sz
+    lib.sbd_tree_attention_q8.argtypes = [ctypes.POINTER(AttnQ8Desc)] + [vp] * 12 + [sz, vp]
+    lib.sbd_tree_attention_q8.restype = ctypes.c_int
+    lib.sbd_verify_tree_workspace_size.argtypes = [ctypes.POINTER(VerifyDesc)]
+    lib.sbd_verify_tree_workspace_size.restype = sz
+    lib.sbd_verify_tree.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 6 + [f32] + [vp] * 5 + [sz, vp]
+    lib.sbd_verify_tree.restype = ctypes.c_int
+    lib.sbd_cache_append_path_q8.argtypes = [ctypes.POINTER(AppendPathDesc)] + [vp] * 10
+    lib.sbd_cache_append_path_q8.restype = ctypes.c_int
     lib.sbd_status_string.argtypes = [ctypes.c_int]
     lib.sbd_status_string.restype = ctypes.c_char_p
     lib.sbd_last_error.argtypes = []
@@ -489,6 +542,14 @@ def _need_shape(shape, **tensors):
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
+def _need_here(**tensors):
+    """The kernels run on the current device: that is where the tensors have to be."""
+    here = _torch().cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.device.index != here:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+
+
 def block_tables_outputs(cache_len, block_table, max_new: int):
     """Outputs for sbd_block_tables: (block_table [B, max_pages], length [B],
     new_start [B + 1], slot_map [max_new], n_free [1]), all int32."""
@@ -592,7 +653,8 @@ def sbd_cache_append_q8(k_new, v_new, slot_map, k_cache, v_cache, k_scale, v_sca
 
 
 def _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk, v_blk, out,
-                  n_causal, scale, num_splits, workspace, stream):
+                  n_causal, scale, num_splits, workspace, stream, parent=None):
+    """Arguments of sbd_block_attention_q8; of sbd_tree_attention_q8 where there are parents."""
     torch = _torch()
     n_pages, H, P, D = _cache_desc(k_cache, v_cache, k_scale, v_scale)
     _need_cuda(q=q, block_table=block_table, cache_len=cache_len, k_blk=k_blk, v_blk=v_blk, out=out,
@@ -609,12 +671,23 @@ def _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len,
         raise ValueError("block_table must be [B, max_pages]")
     d = AttnQ8Desc(B, k, Hq, H, D, P, block_table.shape[1], n_pages, _dtype_code(q), int(n_causal),
                    float(scale), int(num_splits))
-    ws = _workspace(lib.sbd_block_attention_q8_workspace_size(ctypes.byref(d)), q.device, workspace)
+    tree = ()
+    if parent is not None:
+        _need_cuda(parent=parent)
+        _need_type(torch.int32, parent=parent)
+        _need_shape((B, k), parent=parent)
+        _need_here(q=q, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale,
+                   block_table=block_table, cache_len=cache_len, k_blk=k_blk, v_blk=v_blk,
+                   parent=parent, out=out)
+        tree = (_ptr(parent),)
+    size = lib.sbd_block_attention_q8_workspace_size if parent is None else \
+        lib.sbd_tree_attention_q8_workspace_size
+    ws = _workspace(size(ctypes.byref(d)), q.device, workspace)
     args = (ctypes.byref(d), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
-            _ptr(block_table), _ptr(cache_len), _ptr(k_blk), _ptr(v_blk), _ptr(out), _ptr(ws),
-            _nbytes(ws), _stream(stream))
+            _ptr(block_table), _ptr(cache_len), _ptr(k_blk), _ptr(v_blk), *tree, _ptr(out),
+            _ptr(ws), _nbytes(ws), _stream(stream))
     return args, (d, q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk, v_blk,
-                  out, ws)
+                  parent, out, ws)
 
 
 def sbd_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
@@ -631,6 +704,170 @@ def sbd_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table, c
                             v_blk, out, n_causal, scale, num_splits, workspace, stream)
     _check(lib.sbd_block_attention_q8(*args))
     return out
+
+
+# ------------------------------------------------------------------ drafted decoding
+
+def _norm_rope_args(q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out, eps,
+                    interleaved, stream):
+    torch = _torch()
+    T, group, qg, qt = _token_strides("q", q)
+    _, _, kg, kt = _token_strides("k", k)
+    vg = vt = 0
+    if v is not None:
+        _, _, vg, vt = _token_strides("v", v)
+        _need_shape(k.shape, v=v)
+    Hq, D = q.shape[-2:]
+    H = k.shape[-2]
+    _need_shape((*q.shape[:-2], H, D), k=k)
+    _need_type(q.dtype, k=k, v=v, q_weight=q_weight, k_weight=k_weight, q_out=q_out, k_out=k_out,
+               v_out=v_out)
+    _need_cuda(positions=positions, inv_freq=inv_freq, q_weight=q_weight, k_weight=k_weight,
+               q_out=q_out, k_out=k_out, v_out=v_out)
+    _need_here(q=q, k=k, v=v, positions=positions, inv_freq=inv_freq, q_weight=q_weight,
+               k_weight=k_weight, q_out=q_out, k_out=k_out, v_out=v_out)
+    R = 0
+    if inv_freq is not None:
+        _need_type(torch.float32, inv_freq=inv_freq)
+        if inv_freq.dim() != 1:
+            raise ValueError("inv_freq has one dimension")
+        R = 2 * inv_freq.shape[0]
+    if R > 0:
+        if positions is None:
+            raise ValueError("inv_freq needs positions")
+        _need_type(torch.int32, positions=positions)
+        if positions.numel() != T:
+            raise ValueError(f"positions has {positions.numel()} entries, expected {T}")
+    _need_shape((D,), q_weight=q_weight, k_weight=k_weight)
+    _need_shape(q.shape, q_out=q_out)
+    _need_shape(k.shape, k_out=k_out, v_out=v_out)
+    d = NormRopeDesc(T, group, Hq, H, D, R, int(bool(interleaved)), _dtype_code(q), float(eps),
+                     qg, qt, kg, kt, vg, vt)
+    tensors = (q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out)
+    return (ctypes.byref(d), *(_ptr(t) for t in tensors), _stream(stream)), (d, tensors)
+
+
+def sbd_qk_norm_rope(q, k, v, positions, inv_freq, q_weight=None, k_weight=None, q_out=None,
+                     k_out=None, v_out=None, *, eps: float = 1e-6, interleaved: bool = False,
+                     stream=None):
+    """Norms of queries and keys by head, and their rotation by position, from a fused
+    projection: q [T, Hq, D] or [B, n, Hq, D], k and v [.., Hkv, D], bf16 or fp32, the heads
+    of a token contiguous and tokens any multiple of 16 bytes apart; positions int32, one
+    for each token; inv_freq [R / 2] fp32 (None: no rotation); q_weight, k_weight [D] (None:
+    no norm).  Pairs are (j, j + R / 2), or neighbours.  v (may be None) is copied.  Returns
+    contiguous (q, k, v)."""
+    torch = _torch()
+    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+    q_out = new(q) if q_out is None else q_out
+    k_out = new(k) if k_out is None else k_out
+    v_out = new(v) if v_out is None and v is not None else v_out
+    args, _ = _norm_rope_args(q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out,
+                              eps, interleaved, stream)
+    _check(lib.sbd_qk_norm_rope(*args))
+    return q_out, k_out, v_out
+
+
+def sbd_tree_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                          v_blk, parent, out=None, *, scale: float = 0.0, num_splits: int = 0,
+                          workspace=None, stream=None):
+    """sbd_block_attention_q8 for a tree of n <= 64 nodes: block row i sees the cache, itself
+    and its ancestors.  parent [B, n] int32, parent[b, i] < i; negative: a root.  Returns out
+    [B, n, Hq, D]."""
+    if out is None:
+        out = _torch().empty_like(q)
+    if parent is None:
+        raise ValueError("parent is needed")
+    args, _ = _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                            v_blk, out, 0, scale, num_splits, workspace, stream, parent)
+    _check(lib.sbd_tree_attention_q8(*args))
+    return out
+
+
+def _verify_args(target_logits, draft_logits, parent, token, uniform, gumbel, tau, path, out_tokens,
+                 logprob, count, workspace, stream):
+    torch = _torch()
+    tensors = dict(target_logits=target_logits, draft_logits=draft_logits, parent=parent,
+                   token=token, uniform=uniform, gumbel=gumbel, path=path, out_tokens=out_tokens,
+                   logprob=logprob, count=count)
+    _need_cuda(**tensors, workspace=workspace)
+    _need_here(**tensors)
+    if target_logits.dim() != 3:
+        raise ValueError("target_logits must be [B, n, V]")
+    B, n, V = target_logits.shape
+    _need_type(target_logits.dtype, draft_logits=draft_logits)
+    _need_type(torch.int32, parent=parent, token=token, path=path, out_tokens=out_tokens, count=count)
+    _need_type(torch.float32, uniform=uniform, gumbel=gumbel, logprob=logprob)
+    _need_shape((B, n, V), draft_logits=draft_logits)
+    _need_shape((B, n), parent=parent, token=token, uniform=uniform, path=path,
+                out_tokens=out_tokens, logprob=logprob)
+    _need_shape((B, V), gumbel=gumbel)
+    _need_shape((B,), count=count)
+    d = VerifyDesc(B, n, V, _dtype_code(target_logits))
+    ws = _workspace(lib.sbd_verify_tree_workspace_size(ctypes.byref(d)), target_logits.device,
+                    workspace)
+    args = (ctypes.byref(d), _ptr(target_logits), _ptr(draft_logits), _ptr(parent), _ptr(token),
+            _ptr(uniform), _ptr(gumbel), float(tau), _ptr(path), _ptr(out_tokens), _ptr(logprob),
+            _ptr(count), _ptr(ws), _nbytes(ws), _stream(stream))
+    return args, (d, tensors, ws)
+
+
+def sbd_verify_tree(target_logits, draft_logits, parent, token, uniform, gumbel, tau: float,
+                    path=None, out_tokens=None, logprob=None, count=None, *, workspace=None,
+                    stream=None):
+    """Walks down a tree of drafted tokens from node 0, accepting them by the target's
+    probabilities: target_logits [B, n, V] bf16 or fp32, draft_logits alike or None (the
+    drafted tokens were given, not drawn), parent and token [B, n] int32, uniform [B, n] fp32
+    and gumbel [B, V] fp32 (None where tau == 0: greedy).  Returns (path [B, n] int32: the
+    accepted nodes from node 0 on, then -1; out_tokens [B, n] int32: their tokens and the one
+    that follows; logprob [B, n] fp32; count [B] int32: how many)."""
+    torch = _torch()
+    new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=target_logits.device)  # noqa: E731
+    B, n = target_logits.shape[:2]
+    path = new(torch.int32, B, n) if path is None else path
+    out_tokens = new(torch.int32, B, n) if out_tokens is None else out_tokens
+    logprob = new(torch.float32, B, n) if logprob is None else logprob
+    count = new(torch.int32, B) if count is None else count
+    args, _ = _verify_args(target_logits, draft_logits, parent, token, uniform, gumbel, tau, path,
+                           out_tokens, logprob, count, workspace, stream)
+    _check(lib.sbd_verify_tree(*args))
+    return path, out_tokens, logprob, count
+
+
+def _append_path_args(k_new, v_new, path, new_start, slot_map, k_cache, v_cache, k_scale, v_scale,
+                      stream):
+    torch = _torch()
+    n_pages, H, P, D = _cache_desc(k_cache, v_cache, k_scale, v_scale)
+    if k_new.dim() != 4:
+        raise ValueError("k_new must be [B, n, Hkv, D]")
+    _, _, kb, kn = _token_strides("k_new", k_new)
+    _, _, vb, vn = _token_strides("v_new", v_new)
+    _need_shape(k_new.shape, v_new=v_new)
+    _need_type(k_new.dtype, v_new=v_new)
+    B, n = k_new.shape[:2]
+    if tuple(k_new.shape[-2:]) != (H, D):
+        raise ValueError(f"k_new has heads {tuple(k_new.shape[-2:])}, the cache {(H, D)}")
+    _need_cuda(path=path, new_start=new_start, slot_map=slot_map)
+    _need_type(torch.int32, path=path, new_start=new_start, slot_map=slot_map)
+    _need_here(k_new=k_new, v_new=v_new, path=path, new_start=new_start, slot_map=slot_map,
+               k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale)
+    _need_shape((B, n), path=path)
+    _need_shape((B + 1,), new_start=new_start)
+    if slot_map.dim() != 1:
+        raise ValueError("slot_map has one dimension")
+    d = AppendPathDesc(B, n, H, D, P, n_pages, slot_map.shape[0], _dtype_code(k_new), kb, kn, vb, vn)
+    tensors = (k_new, v_new, path, new_start, slot_map, k_cache, v_cache, k_scale, v_scale)
+    return (ctypes.byref(d), *(_ptr(t) for t in tensors), _stream(stream)), (d, tensors)
+
+
+def sbd_cache_append_path_q8(k_new, v_new, path, new_start, slot_map, k_cache, v_cache, k_scale,
+                             v_scale, *, stream=None):
+    """Quantises the keys and values of accepted nodes into their slots of a paged cache:
+    k_new, v_new [B, n, Hkv, D], bf16 or fp32, the heads of a node contiguous; path [B, n]
+    of sbd_verify_tree, new_start [B + 1] and slot_map of sbd_block_tables, all int32.
+    k_cache, v_cache, k_scale and v_scale are updated in place."""
+    args, _ = _append_path_args(k_new, v_new, path, new_start, slot_map, k_cache, v_cache, k_scale,
+                                v_scale, stream)
+    _check(lib.sbd_cache_append_path_q8(*args))
 
 
 class Prepared:
@@ -734,6 +971,41 @@ def prepare_block_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_tabl
     args, keep = _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
                                v_blk, out, n_causal, scale, num_splits, workspace, stream)
     return Prepared(lib.sbd_block_attention_q8, args, keep)
+
+
+def prepare_qk_norm_rope(q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out, *,
+                         eps: float = 1e-6, interleaved: bool = False, stream=None) -> Prepared:
+    """sbd_qk_norm_rope bound to fixed tensors (see Prepared)."""
+    args, keep = _norm_rope_args(q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out,
+                                 v_out, eps, interleaved, stream)
+    return Prepared(lib.sbd_qk_norm_rope, args, keep)
+
+
+def prepare_tree_attention_q8(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                              v_blk, parent, out, workspace=None, *, scale: float = 0.0,
+                              num_splits: int = 0, stream=None) -> Prepared:
+    """sbd_tree_attention_q8 bound to fixed tensors (see Prepared)."""
+    if parent is None:
+        raise ValueError("parent is needed")
+    args, keep = _attn_q8_args(q, k_cache, v_cache, k_scale, v_scale, block_table, cache_len, k_blk,
+                               v_blk, out, 0, scale, num_splits, workspace, stream, parent)
+    return Prepared(lib.sbd_tree_attention_q8, args, keep)
+
+
+def prepare_verify_tree(target_logits, draft_logits, parent, token, uniform, gumbel, tau: float, path,
+                        out_tokens, logprob, count, workspace=None, *, stream=None) -> Prepared:
+    """sbd_verify_tree bound to fixed tensors (see Prepared)."""
+    args, keep = _verify_args(target_logits, draft_logits, parent, token, uniform, gumbel, tau, path,
+                              out_tokens, logprob, count, workspace, stream)
+    return Prepared(lib.sbd_verify_tree, args, keep)
+
+
+def prepare_cache_append_path_q8(k_new, v_new, path, new_start, slot_map, k_cache, v_cache, k_scale,
+                                 v_scale, *, stream=None) -> Prepared:
+    """sbd_cache_append_path_q8 bound to fixed tensors (see Prepared)."""
+    args, keep = _append_path_args(k_new, v_new, path, new_start, slot_map, k_cache, v_cache, k_scale,
+                                   v_scale, stream)
+    return Prepared(lib.sbd_cache_append_path_q8, args, keep)
 
 
 def sbd_device_error() -> int:

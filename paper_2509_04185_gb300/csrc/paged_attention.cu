@@ -67,6 +67,7 @@ struct Args {
   int* err;
   int k, Hq, Hkv, G, M, log2P, max_pages, n_pages, n_causal, splits, chunks;
   float scale_log2;
+  const int32_t* parent;     // of a tree
 };
 
 template <int D>
@@ -81,7 +82,8 @@ constexpr size_t fma_smem_bytes() {
                           + kKeys);                                 // key scales
 }
 
-template <int D, int RW, int W>
+// kTree: block rows see themselves and their ancestors.
+template <int D, int RW, int W, bool kTree>
 __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const Args a) {
   constexpr int kThreads = 32 * W;
   constexpr int kRowsCta = W * RW;
@@ -91,6 +93,7 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
   constexpr int kC16 = D / 16;                 // 16-byte pieces of a row of codes
   constexpr int kFetch = kKeys * kC16 / kThreads;
   static_assert(kFetch * kThreads == kKeys * kC16, "a tile is a whole number of turns");
+  __shared__ BlockViews views;                 // of a tree: the block keys that a node sees
   extern __shared__ __align__(16) float sm[];
   float* q_s = sm;                             // [kRowsCta][D]
   float* k_s = q_s + kRowsCta * D;             // [kKeys][kKS]
@@ -190,14 +193,28 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
     *reinterpret_cast<float4*>(q_s + rl * D + 4 * c) = v;
   }
 
-  // this warp's rows: local rows RW*warp .. + RW - 1; keys u < vis[r] are seen
+  // This warp's rows: local rows RW*warp .. + RW - 1; keys u < vis[r] are seen, of a tree's
+  // block keys those among them that views has for the row's node.
   uint32_t vis[RW], vis_min = u_end;
+  int node[RW];
+  if (kTree && u_end > len) {                  // (the range has block keys)
+    if (warp == 0) {
+      Parents parents;
+      parents.load(a.parent + (size_t)b * a.k, a.k);
+      block_views(views, parents, a.err);
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int r = 0; r < RW; ++r) {
     const int i = (chunk * kRowsCta + RW * warp + r) / a.G;
-    vis[r] = min(u_end, len + (i < a.n_causal ? i + 1 : a.k));
-    vis_min = min(vis_min, vis[r]);
+    node[r] = min(i, a.k - 1);                 // (of rows past the last: anything)
+    vis[r] = min(u_end, len + (kTree ? node[r] + 1 : i < a.n_causal ? i + 1 : a.k));
+    vis_min = min(vis_min, kTree ? min(len, u_end) : vis[r]);
   }
+  auto sees = [&](int r, uint32_t u) {
+    return u < vis[r] && (!kTree || u < len || (views.seen[node[r]] >> (u - len) & 1));
+  };
   float m[RW], l[RW];                          // l: this lane's share of the row sum
   float o[RW][kPer];
 #pragma unroll
@@ -248,8 +265,8 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
       const float f0 = sc_s[lane] * a.scale_log2, f1 = sc_s[lane + 32] * a.scale_log2;
 #pragma unroll
       for (int r = 0; r < RW; ++r) {
-        s[r][0] = t0 + lane < vis[r] ? acc[r][0] * f0 : -INFINITY;
-        s[r][1] = two && t0 + lane + 32 < vis[r] ? acc[r][1] * f1 : -INFINITY;
+        s[r][0] = sees(r, t0 + lane) ? acc[r][0] * f0 : -INFINITY;
+        s[r][1] = two && sees(r, t0 + lane + 32) ? acc[r][1] * f1 : -INFINITY;
       }
     }
     // ---- softmax of the tile
@@ -294,7 +311,7 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
         }
       }
     }
-    // The rest, block keys that some causal row must not see: their values are
+    // The rest, block keys that some row must not see: their values are
     // left out there, not multiplied by 0 (they may be infinite or NaN).
 #pragma unroll 1
     for (int j = n_all; j < n; ++j) {
@@ -303,7 +320,7 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
       for (int c = 0; c < kPer; ++c) v[c] = v_s[j * D + kPer * lane + c];
 #pragma unroll
       for (int r = 0; r < RW; ++r) {
-        if (t0 + j >= vis[r]) continue;
+        if (!sees(r, t0 + j)) continue;
         const float p = pw[r * kKeys + j];
 #pragma unroll
         for (int c = 0; c < kPer; ++c) o[r][c] = fmaf(p, v[c], o[r][c]);
@@ -372,13 +389,16 @@ struct Kernel {
   int rows;          // packed rows per CTA
   int threads;
 };
-template <int D>
+template <int D, bool kTree>
 Kernel fma_kernel_of(int M) {
-  if (M <= 8) return {(const void*)paged_fma_kernel<D, 2, 4>, fma_smem_bytes<D, 2, 4>(), 8, 128};
-  if (M <= 16) return {(const void*)paged_fma_kernel<D, 4, 4>, fma_smem_bytes<D, 4, 4>(), 16, 128};
-  return {(const void*)paged_fma_kernel<D, 4, 8>, fma_smem_bytes<D, 4, 8>(), 32, 256};
+  if (M <= 8) return {(const void*)paged_fma_kernel<D, 2, 4, kTree>, fma_smem_bytes<D, 2, 4>(), 8, 128};
+  if (M <= 16) return {(const void*)paged_fma_kernel<D, 4, 4, kTree>, fma_smem_bytes<D, 4, 4>(), 16, 128};
+  return {(const void*)paged_fma_kernel<D, 4, 8, kTree>, fma_smem_bytes<D, 4, 8>(), 32, 256};
 }
-Kernel fma_kernel_for(int D, int M) { return D == 128 ? fma_kernel_of<128>(M) : fma_kernel_of<64>(M); }
+Kernel fma_kernel_for(const sbd::AttnQ8Plan& p) {
+  if (p.tree) return p.D == 128 ? fma_kernel_of<128, true>(p.M) : fma_kernel_of<64, true>(p.M);
+  return p.D == 128 ? fma_kernel_of<128, false>(p.M) : fma_kernel_of<64, false>(p.M);
+}
 
 // Key ranges per (sequence, KV head, row chunk): as many as three CTAs per SM (of four
 // warps, two of eight) allow, one range per kGranule keys at most, in a cluster size whose clusters
@@ -395,7 +415,7 @@ int fma_splits(const sbd::AttnQ8Plan& p, const Kernel& kern, int asked) {
 }
 
 sbd_status fma_launch(const sbd::AttnQ8Plan& p, const sbd::AttnQ8Tensors& t, cudaStream_t st) {
-  const Kernel kern = fma_kernel_for(p.D, p.M);
+  const Kernel kern = fma_kernel_for(p);
   Args a;
   a.q = (const float*)t.q;
   a.kc = (const uint8_t*)t.k_cache;
@@ -404,6 +424,7 @@ sbd_status fma_launch(const sbd::AttnQ8Plan& p, const sbd::AttnQ8Tensors& t, cud
   a.vs = t.v_scale;
   a.table = t.table;
   a.lens = t.lens;
+  a.parent = t.parent;
   a.kb = (const float*)t.kb;
   a.vb = (const float*)t.vb;
   a.out = (float*)t.out;
@@ -431,7 +452,7 @@ sbd_status fma_launch(const sbd::AttnQ8Plan& p, const sbd::AttnQ8Tensors& t, cud
 
 namespace sbd {
 
-AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d) {
+AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d, bool tree) {
   AttnQ8Plan p;
   p.B = d.batch;
   p.k = d.block_k;
@@ -445,13 +466,14 @@ AttnQ8Plan attn_q8_plan(const sbd_attn_q8_desc& d) {
   p.M = p.G * p.k;
   p.n_causal = d.n_causal;
   p.bf16 = d.dtype == SBD_DTYPE_BF16;
+  p.tree = tree;
   const float scale = d.scale != 0.f ? d.scale : 1.0f / sqrtf((float)d.head_dim);
   p.scale_log2 = scale * kLog2e;
   if (p.bf16) {
     paged_tc_plan(&p, d.num_splits);
     return p;
   }
-  const Kernel kern = fma_kernel_for(p.D, p.M);
+  const Kernel kern = fma_kernel_for(p);
   p.rows = kern.rows;
   p.chunks = (p.M + kern.rows - 1) / kern.rows;
   p.splits = fma_splits(p, kern, d.num_splits);

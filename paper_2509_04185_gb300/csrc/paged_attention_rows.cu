@@ -108,7 +108,8 @@ __device__ __forceinline__ uint32_t half2_of(uint32_t c, __half2 w) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-template <int D>
+// kBlkKeys: block keys, padded.
+template <int D, int kBlkKeys>
 struct Shape {
   static constexpr int kSoftWarps = 8, kAccWarps = 8, kWorkWarps = kSoftWarps + kAccWarps;
   static constexpr int kDims = D / 2;                  // of an accumulators' thread
@@ -125,18 +126,21 @@ struct Shape {
   static constexpr int kLeft = 227 * 1024 - kTables - kFixed;
   // (a tile's scales are read until two tiles behind the last one that left the ring)
   static constexpr int kStages = kLeft / (2 * kKV) < kSlots - 2 ? kLeft / (2 * kKV) : kSlots - 2;
-  static constexpr int kSmem = kFixed + kStages * 2 * kKV;
   static constexpr int kPStride = D + 4;
+  // The ring is where partial rows are merged, too.
+  static constexpr int kMerge = (kRows + kMaxSplits) * kPStride * 4;
+  static constexpr int kRing = kStages * 2 * kKV > kMerge ? kStages * 2 * kKV : kMerge;
+  static constexpr int kSmem = kFixed + kRing;
   static_assert(kStages >= 2, "a tile ahead");
   static_assert(kRows * kPStride * 4 <= kQ + 2 * kV16, "the partial rows fit the places of Q and V");
-  static_assert((kRows + kMaxSplits) * kPStride * 4 <= kStages * 2 * kKV, "the partial rows fit the ring");
+  static_assert(kSmem <= 227 * 1024 - kTables, "shared memory holds them");
 };
 
-template <int D>
-__global__ void __launch_bounds__(Shape<D>::kThreads, 1)
+template <int D, int kBlkKeys, bool kTree>
+__global__ void __launch_bounds__(Shape<D, kBlkKeys>::kThreads, 1)
 paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
                   const __grid_constant__ CUtensorMap tmap_v, const Args a) {
-  using C = Shape<D>;
+  using C = Shape<D, kBlkKeys>;
   constexpr int kStages = C::kStages, kDims = C::kDims, kOBufs = C::kOBufs;
   constexpr int kWorkWarps = C::kWorkWarps;
 
@@ -150,6 +154,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(16) int order_sh[kMaxOrder];
   __shared__ __align__(16) float bks_sh[kBlkKeys];
   __shared__ float c_sh[kRows];                        // a row's score scale, log2 units
+  __shared__ BlockViews views;                         // of a tree: the block keys that a node sees
   __shared__ float2 stat_sh[4][kRows];                 // a step's maximum and sum of a row
   __shared__ float lse_sh[kRows + kMaxSplits];         // of the rows merged here, a row's splits together
 
@@ -306,6 +311,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
     static_assert(kQTurns * kTurn == kRows && kBlkKeys <= kTurn, "rows in whole turns, keys in one");
     const int c = at % (D / 16), r0 = at / (D / 16);
     const int q_turns = min(kQTurns, (a.M - chunk * kRows + kTurn - 1) / kTurn);
+    const bool look = kTree && has_block && sw == 0;
+    Parents parents;
+    if (look) parents.load(a.parent + (size_t)b * a.k, a.k);
     Piece<D> piece[kQTurns + 1], value;
     const bool key_here = has_block && r0 < a.k;
     const size_t key_off = (((size_t)b * a.k + r0) * a.Hkv + hkv) * D + 16 * c;
@@ -359,8 +367,9 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
       __syncwarp();
       if (lane == 0) mbar_arrive(&blk_ready);
     }
-    bar_sync(5, 32 * kWorkWarps);                      // c of all rows
-    const int pos = a.position(row), vis = pos < a.n_causal ? pos + 1 : a.k;
+    if (look) block_views(views, parents, a.err);
+    bar_sync(5, 32 * kWorkWarps);                      // c of all rows, the views
+    const int pos = a.position(row), vis = kTree || pos >= a.n_causal ? a.k : pos + 1;
     const bool rows_here = chunk * kRows + quad * 32 < a.M;   // whole warps without rows only keep step
     bool ok = true;
     if (sw < C::kSoftWarps) {
@@ -389,10 +398,12 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
           tc_ld16(sa + 16 * c, x);
           tc_wait_ld();
           const int seen = (blk ? vis : valid) - 16 * c;
+          // (of rows past the last: anything)
+          const uint32_t above = kTree && blk ? (uint32_t)(views.seen[min(pos, a.k - 1)] >> 16 * c) : ~0u;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float y = blk ? __uint_as_float(x[e]) * bks_sh[(16 * c + e) & (kBlkKeys - 1)] : __uint_as_float(x[e]);
-            z[e] = e < seen ? y : -INFINITY;
+            z[e] = e < seen && (!kTree || above >> e & 1) ? y : -INFINITY;
           }
         };
         auto top = [](const float (&z)[16]) {          // NaN propagates
@@ -563,6 +574,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
       if (has_block && blk_bad && mine) {
 #pragma unroll 1
         for (int e = 0; e < vis; ++e) {
+          if (kTree && !(views.seen[i] >> e & 1)) continue;
           const __nv_bfloat16* v = a.vb + (((size_t)b * a.k + e) * a.Hkv + hkv) * D + part * kDims;
 #pragma unroll
           for (int d = 0; d < kDims / 2; ++d) {
@@ -622,9 +634,15 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
 
 namespace sbd {
 
-sbd_dev::TcKernel paged_rows_kernel_for(int D) {
-  if (D == 128) return {(const void*)paged_rows_kernel<128>, Shape<128>::kSmem, Shape<128>::kThreads};
-  return {(const void*)paged_rows_kernel<64>, Shape<64>::kSmem, Shape<64>::kThreads};
+template <int D, int kBlk, bool kTree>
+static sbd_dev::TcKernel rows_instance() {
+  using C = Shape<D, kBlk>;
+  return {(const void*)paged_rows_kernel<D, kBlk, kTree>, C::kSmem, C::kThreads};
+}
+sbd_dev::TcKernel paged_rows_kernel_for(int D, int k, bool tree) {
+  if (k > 32) return D == 128 ? rows_instance<128, 64, true>() : rows_instance<64, 64, true>();
+  if (tree) return D == 128 ? rows_instance<128, 32, true>() : rows_instance<64, 32, true>();
+  return D == 128 ? rows_instance<128, 32, false>() : rows_instance<64, 32, false>();
 }
 
 }  // namespace sbd

@@ -124,7 +124,9 @@ __device__ __forceinline__ void st_shared_v2(uint32_t addr, const uint32_t (&x)[
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x[0]), "r"(x[1]) : "memory");
 }
 
-template <int D, int R, int kUse, int kCtas>
+// kTree: block rows see themselves and their ancestors (an instance of its own: the masks
+// cost a block's attention 0.1 to 1 us).
+template <int D, int R, int kUse, int kCtas, bool kTree>
 __global__ void __launch_bounds__(Shape<D, R, kUse, kCtas>::kThreads, kCtas)
 paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                 const __grid_constant__ CUtensorMap tmap_v, const Args a) {
@@ -144,7 +146,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
   __shared__ __align__(16) int order_sh[kMaxOrder];
   __shared__ float bks_sh[kBlkKeys];
   __shared__ __align__(16) float c_sh[R];              // a row's score scale, log2 units
-  __shared__ int vis_sh[R];                            // block keys that it sees
+  __shared__ int vis_sh[R];                            // block keys that it sees; of a tree: its node
+  __shared__ BlockViews views;                         // of a tree: the block keys that a node sees
   __shared__ __align__(16) float red_sh[kParts][2][4][kRT];  // maxima of a part's warps, two steps
   __shared__ __align__(16) float sum_sh[kSoftWarps][kRT];    // a warp's sums of probabilities
   __shared__ __align__(16) float mq_sh[kSoftWarps][kRT];     // a warp's copy of the step's maxima, negated
@@ -313,6 +316,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     constexpr int kRowsTurn = 32 * kSoftWarps / (D / 16);
     {
+      const bool look = kTree && has_block && sw == 0;
+      Parents parents;
+      if (look) parents.load(a.parent + (size_t)b * a.k, a.k);
       const int c = at % (D / 16);
 #pragma unroll 1
       for (int r = at / (D / 16); r < R; r += kRowsTurn) {
@@ -323,13 +329,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
         const float s = x.store(q_s, r, R + r, c);
         if (c == 0) {
           c_sh[r] = fmaxf(s * a.scale_log2, 1.17549435e-38f);   // > 0: masked scores stay -inf
-          vis_sh[r] = i < a.n_causal ? i + 1 : a.k;
+          vis_sh[r] = kTree ? min(i, a.k - 1) : i < a.n_causal ? i + 1 : a.k;
         }
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_ready);
-      bar_sync(5, 32 * kSoftWarps);                    // c and vis of all rows
+      if (look) block_views(views, parents, a.err);
+      bar_sync(5, 32 * kSoftWarps);                    // c and vis of all rows, the views
     }
     if (has_block) {
       const int c = at % (D / 16);
@@ -450,7 +457,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
           for (int r = 0; r < kRT; ++r) z1[r] = (__uint_as_float(h[r]) + __uint_as_float(lo[r])) * kf1;
           if (blk) {
 #pragma unroll
-            for (int r = 0; r < kRT; ++r) z0[r] = key < vis_sh[r0 + r] ? z0[r] : -INFINITY;
+            for (int r = 0; r < kRT; ++r) {            // (32 keys at most: quad is 0)
+              const bool sees = kTree ? (uint32_t)views.seen[vis_sh[r0 + r]] >> lane & 1 : key < vis_sh[r0 + r];
+              z0[r] = sees ? z0[r] : -INFINITY;
+            }
           } else if (valid0 < quad * 32 + 32) {
 #pragma unroll
             for (int r = 0; r < kRT; ++r) z0[r] = key < valid0 ? z0[r] : -INFINITY;
@@ -576,7 +586,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {
 #pragma unroll 1
-        for (int e = 0; e < vis_sh[r0 + r]; ++e) {
+        for (int e = 0; e < (kTree ? a.k : vis_sh[r0 + r]); ++e) {
+          if (kTree && !((uint32_t)views.seen[vis_sh[r0 + r]] >> e & 1)) continue;
           const float v = __bfloat162float(a.vb[(((size_t)b * a.k + e) * a.Hkv + hkv) * D + d]);
           if (!(fabsf(v) < INFINITY)) acc[r] += v;
         }
@@ -633,20 +644,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k,
                                            hkv, chunk, split, &merge_bar);
 }
 
-template <int D, int R, int kUse, int kCtas>
+template <int D, int R, int kUse, int kCtas, bool kTree>
 TcKernel instance() {
   using C = Shape<D, R, kUse, kCtas>;
-  return {(const void*)paged_tc_kernel<D, R, kUse, kCtas>, C::kSmem, C::kThreads};
+  return {(const void*)paged_tc_kernel<D, R, kUse, kCtas, kTree>, C::kSmem, C::kThreads};
 }
-template <int D>
+template <int D, bool kTree>
 TcKernel kernel_of(int M, int ctas) {
-  if (M > 16) return ctas == 1 ? instance<D, 32, 32, 1>() : instance<D, 32, 32, 2>();
-  if (M > 8) return ctas == 1 ? instance<D, 16, 16, 1>() : instance<D, 16, 16, 2>();
-  return ctas == 1 ? instance<D, 16, 8, 1>() : instance<D, 16, 8, 2>();
+  if (M > 16) return ctas == 1 ? instance<D, 32, 32, 1, kTree>() : instance<D, 32, 32, 2, kTree>();
+  if (M > 8) return ctas == 1 ? instance<D, 16, 16, 1, kTree>() : instance<D, 16, 16, 2, kTree>();
+  return ctas == 1 ? instance<D, 16, 8, 1, kTree>() : instance<D, 16, 8, 2, kTree>();
 }
-TcKernel kernel_for(int D, int M, int ctas) {
-  if (M > 32) return sbd::paged_rows_kernel_for(D);
-  return D == 128 ? kernel_of<128>(M, ctas) : kernel_of<64>(M, ctas);
+TcKernel kernel_for(const sbd::AttnQ8Plan& p, int ctas) {
+  if (p.M > 32) return sbd::paged_rows_kernel_for(p.D, p.k, p.tree);
+  if (p.tree) return p.D == 128 ? kernel_of<128, true>(p.M, ctas) : kernel_of<64, true>(p.M, ctas);
+  return p.D == 128 ? kernel_of<128, false>(p.M, ctas) : kernel_of<64, false>(p.M, ctas);
 }
 
 }  // namespace
@@ -687,7 +699,7 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
   }
   if (s > kMaxSplits) s = kMaxSplits;
   // (Asked for two CTAs an SM, the driver still answers for one.)
-  const TcKernel kern = kernel_for(p->D, p->M, p->ctas), one = kernel_for(p->D, p->M, 1);
+  const TcKernel kern = kernel_for(*p, p->ctas), one = kernel_for(*p, 1);
   for (; s > 1; --s)
     if (cluster_slots(kern.fn, kern.threads, kern.smem, s) > 0 &&
         p->ctas * cluster_slots(one.fn, one.threads, one.smem, s) >= (num_splits > 0 ? 1 : jobs))
@@ -696,7 +708,7 @@ void paged_tc_plan(AttnQ8Plan* p, int num_splits) {
 }
 
 sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStream_t st) {
-  const TcKernel kern = kernel_for(p.D, p.M, p.ctas);
+  const TcKernel kern = kernel_for(p, p.ctas);
   // Codes as bytes: (D, tokens of a page, page and head); a copy is a page.
   CUtensorMap tk, tv;
   const uint64_t dims[3] = {(uint64_t)p.D, (uint64_t)p.P, (uint64_t)p.n_pages * p.Hkv};
@@ -717,6 +729,7 @@ sbd_status paged_tc_launch(const AttnQ8Plan& p, const AttnQ8Tensors& t, cudaStre
   a.vs = t.v_scale;
   a.table = t.table;
   a.lens = t.lens;
+  a.parent = t.parent;
   a.out = (__nv_bfloat16*)t.out;
   a.err = device_error_word();
   a.B = p.B;

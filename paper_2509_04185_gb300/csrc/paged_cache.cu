@@ -503,9 +503,156 @@ __global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8
   grid_dependents_launch();
 }
 
+// ------------------------------------------------------ append of a path
+// The append for a tree's accepted nodes, which lie anywhere among a request's nodes: a
+// CTA has one plane of one request, at most 64 tokens, and takes its segments (formulas
+// above) one after the other, since each of them is a page's worth at most.
+// Bound: latency; the chain new_start -> slots and path -> rows and old scale -> codes,
+// then the earlier codes where the page's scale grew.
+constexpr int kPathThreads = 128;
+constexpr int kPathHold = 8;                 // units of 8 elements a thread keeps
+
+struct PathArgs {
+  const void *k_new, *v_new;
+  const int32_t *path, *new_start, *slot_map;
+  uint8_t *k_cache, *v_cache;
+  float *k_scale, *v_scale;
+  int* err;
+  long long k_batch_stride, k_node_stride, v_batch_stride, v_node_stride;   // elements
+  long long n_slots;
+  int nodes, max_new, Hkv, log2P;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kPathThreads) append_path_q8_kernel(const PathArgs a) {
+  constexpr int kUnits = D / 8;              // units of a row
+  constexpr int kWarps = kPathThreads / 32;
+  constexpr int kStep = kPathThreads / kUnits;         // tokens of a turn
+  __shared__ int slot_sh[kMaxNodes], node_sh[kMaxNodes];
+  __shared__ float max_sh[kWarps];
+  grid_dependency_wait();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool is_v = (int)blockIdx.x >= a.Hkv;
+  const int h = is_v ? blockIdx.x - a.Hkv : blockIdx.x, b = blockIdx.y;
+  const int last = (1 << a.log2P) - 1;
+  const long long from = a.new_start[b];
+  const int m = (int)max(0ll, min((long long)a.nodes, a.new_start[b + 1] - from));
+  if (tid < m) {
+    const long long at = from + tid;
+    int slot = at >= 0 && at < a.max_new ? a.slot_map[at] : -1;
+    const int node = a.path[(size_t)b * a.nodes + tid];
+    if (slot >= a.n_slots) {
+      if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_PAGE);
+      slot = -1;
+    }
+    if (slot >= 0 && (uint32_t)node >= (uint32_t)a.nodes) {
+      if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_TREE);
+      slot = -1;
+    }
+    slot_sh[tid] = max(slot, -1);
+    node_sh[tid] = node;
+  }
+  __syncthreads();
+  const T* src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)h * D +
+                 b * (is_v ? a.v_batch_stride : a.k_batch_stride) + tid % kUnits * 8;
+  const long long stride = is_v ? a.v_node_stride : a.k_node_stride;
+  uint8_t* cache = is_v ? a.v_cache : a.k_cache;
+  float* scales = is_v ? a.v_scale : a.k_scale;
+  for (int j0 = 0, j1; j0 < m; j0 = j1) {
+    const int slot = slot_sh[j0];
+    j1 = j0 + 1;
+    if (slot < 0) continue;
+    while (j1 < m && slot_sh[j1] == slot + (j1 - j0) && (slot_sh[j1] & last) != 0) ++j1;
+    const int off = slot & last;
+    const long long ph = (long long)(slot >> a.log2P) * a.Hkv + h;
+    const float s_old = off > 0 ? scales[ph] : 0.f;
+    Eight<T> hold[kPathHold];
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPathHold; ++e) {
+      const int j = j0 + tid / kUnits + e * kStep;
+      if (j < j1) hold[e].load(src + node_sh[j] * stride);
+    }
+#pragma unroll
+    for (int e = 0; e < kPathHold; ++e)
+      if (j0 + tid / kUnits + e * kStep < j1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_size(hold[e].get(i)));
+      }
+    amax = warp_max(amax);
+    if (lane == 0) max_sh[warp] = amax;
+    __syncthreads();                         // (every thread has the old scale, too)
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) amax = fmaxf(amax, max_sh[w]);
+    const float s = fmaxf(s_old, scale_for(amax));
+    if (tid == 0) scales[ph] = s;
+    uint8_t* dst = cache + (ph << a.log2P) * D;
+    // s is a power of two unless a caller's own scale is kept: then the products are exact
+    const bool exact = (__float_as_uint(s) & 0x007fffffu) == 0;
+    const float inv = 1.f / s;
+#pragma unroll
+    for (int e = 0; e < kPathHold; ++e) {
+      const int j = j0 + tid / kUnits + e * kStep;
+      if (j >= j1) continue;
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = exact ? hold[e].get(i) * inv : hold[e].get(i) / s;
+      *reinterpret_cast<uint2*>(dst + (off + j - j0) * D + tid % kUnits * 8) =
+          make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
+    }
+    if (off > 0 && s != s_old) {             // the page's earlier codes move to the new scale
+      const float f = s_old / s;
+#pragma unroll 4
+      for (int u = tid; u < off * D / 16; u += kPathThreads) {
+        uint4 c = *reinterpret_cast<const uint4*>(dst + 16 * u);
+        c.x = e4m3x4_times(c.x, f), c.y = e4m3x4_times(c.y, f);
+        c.z = e4m3x4_times(c.z, f), c.w = e4m3x4_times(c.w, f);
+        *reinterpret_cast<uint4*>(dst + 16 * u) = c;
+      }
+    }
+    __syncthreads();                         // the maxima are read; the page is as the next segment finds it
+  }
+  grid_dependents_launch();
+}
+
 }  // namespace
 
 namespace sbd {
+
+sbd_status append_path_launch(const sbd_append_path_desc& d, const void* k_new, const void* v_new,
+                              const int32_t* path, const int32_t* new_start,
+                              const int32_t* slot_map, void* k_cache, void* v_cache, float* k_scale,
+                              float* v_scale, cudaStream_t st) {
+  PathArgs a;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.path = path;
+  a.new_start = new_start;
+  a.slot_map = slot_map;
+  a.k_cache = (uint8_t*)k_cache;
+  a.v_cache = (uint8_t*)v_cache;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.err = device_error_word();
+  a.k_batch_stride = d.k_batch_stride;
+  a.k_node_stride = d.k_node_stride;
+  a.v_batch_stride = d.v_batch_stride;
+  a.v_node_stride = d.v_node_stride;
+  a.n_slots = (long long)d.n_pages * d.page_size;
+  a.nodes = d.nodes;
+  a.max_new = d.max_new;
+  a.Hkv = d.n_kv_heads;
+  a.log2P = log2_page(d.page_size);
+  const bool f32 = d.dtype == SBD_DTYPE_F32;
+  const void* fn = d.head_dim == 128
+                       ? (f32 ? (const void*)append_path_q8_kernel<float, 128>
+                              : (const void*)append_path_q8_kernel<__nv_bfloat16, 128>)
+                       : (f32 ? (const void*)append_path_q8_kernel<float, 64>
+                              : (const void*)append_path_q8_kernel<__nv_bfloat16, 64>);
+  void* args[] = {(void*)&a};
+  return launch_pdl(fn, dim3(2 * d.n_kv_heads, d.batch), dim3(kPathThreads), 0, st, args,
+                    "append_path_q8_kernel launch");
+}
 
 size_t tables_smem_bytes(int B) { return (size_t)5 * B * sizeof(int); }
 

@@ -9,7 +9,7 @@ namespace sbd_dev {
 
 constexpr int kTile = 128;                   // keys of an MMA; a step is two tiles
 constexpr int kMaxStages = 8;
-constexpr int kBlkKeys = 32;                 // block keys, padded
+constexpr int kBlkKeys = 32;                 // block keys, padded (of trees: 64, rows on the lanes)
 constexpr int kMaxSplits = 16;
 constexpr int kMaxOrder = 128;               // sequences that a launch sorts by length
 
@@ -192,6 +192,7 @@ struct Args {
   int order;                 // blockIdx.z -> sequence by descending length
   float scale_log2;
   float inv_G, inv_chunks;   // 1 / G, 1 / chunks
+  const int32_t* parent;     // of a tree
   // The block position of packed row x.
   __device__ __forceinline__ int position(int x) const { return whole_part(x, inv_G); }
 };
@@ -418,7 +419,7 @@ struct TcKernel {
 
 namespace sbd {
 
-// The kernel with rows on the lanes, 128 packed rows a CTA.
-sbd_dev::TcKernel paged_rows_kernel_for(int D);
+// The kernel with rows on the lanes, 128 packed rows a CTA, for k block keys.
+sbd_dev::TcKernel paged_rows_kernel_for(int D, int k, bool tree);
 
 }  // namespace sbd

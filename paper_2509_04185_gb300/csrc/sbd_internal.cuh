@@ -16,6 +16,28 @@ namespace sbd {
 sbd_status fail(sbd_status st, const char* fmt, ...);
 sbd_status cuda_fail(cudaError_t e, const char* what);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+struct Named {
+  const void* p;
+  const char* name;
+};
+template <int N>
+sbd_status check_pointers(const Named (&ptrs)[N]) {
+  for (const Named& x : ptrs) {
+    if (!x.p) return fail(SBD_ERR_INVALID_ARG, "%s is NULL", x.name);
+    if (!aligned16(x.p)) return fail(SBD_ERR_INVALID_ARG, "%s is not 16-byte aligned", x.name);
+  }
+  return SBD_OK;
+}
+// Strides in elements of dtype, for rows that are read 16 bytes at a time.
+template <int N>
+sbd_status check_strides(const int64_t (&strides)[N], int dtype) {
+  const int unit = dtype == SBD_DTYPE_F32 ? 4 : 8;
+  for (int64_t x : strides)
+    if (x < 0 || x % unit != 0)
+      return fail(SBD_ERR_UNSUPPORTED, "stride of %lld elements is not a multiple of 16 bytes",
+                  (long long)x);
+  return SBD_OK;
+}
 // Queries the current device once (SM count, error-word address) and
 // fails with the reason recorded when that is impossible; every entry point
 // that launches calls it before num_sms() / device_error_word().
@@ -91,6 +113,25 @@ sbd_status gumbel_fill_launch(int n_rows, const int32_t* row_ids, int V, uint64_
 sbd_status select_launch(int rule, int B, int k, const float* entropy, const float* confidence,
                          const int32_t* token, float threshold, uint8_t* masked,
                          int32_t* block_tokens, int32_t* n_unmasked, cudaStream_t st);
+
+struct NormRopeTensors {
+  const void *q, *k, *v;
+  const int32_t* positions;
+  const float* inv_freq;
+  const void *q_weight, *k_weight;
+  void *q_out, *k_out, *v_out;
+};
+sbd_status norm_rope_launch(const sbd_norm_rope_desc& d, const NormRopeTensors& t, cudaStream_t st);
+
+struct VerifyTensors {
+  const void *target, *draft;
+  const int32_t *parent, *token;
+  const float *uniform, *gumbel;
+  int32_t *path, *out_tokens;
+  float* logprob;
+  int32_t* count;
+};
+sbd_status verify_launch(const sbd_verify_desc& d, const VerifyTensors& t, float tau, cudaStream_t st);
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

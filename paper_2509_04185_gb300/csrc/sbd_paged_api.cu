@@ -4,25 +4,13 @@
 
 #include "paged.cuh"
 
-using sbd::aligned16;
+using sbd::check_pointers;
 using sbd::fail;
+using sbd::Named;
 
 namespace {
 
 constexpr long long kMax32 = 0x7fffffffll;
-
-struct Named {
-  const void* p;
-  const char* name;
-};
-template <int N>
-sbd_status check_pointers(const Named (&ptrs)[N]) {
-  for (const Named& x : ptrs) {
-    if (!x.p) return fail(SBD_ERR_INVALID_ARG, "%s is NULL", x.name);
-    if (!aligned16(x.p)) return fail(SBD_ERR_INVALID_ARG, "%s is not 16-byte aligned", x.name);
-  }
-  return SBD_OK;
-}
 
 sbd_status check_pool(int page_size, int n_pages) {
   if (page_size < 1 || n_pages < 1)
@@ -49,7 +37,7 @@ sbd_status check_heads(int n_kv_heads, int n_pages, int head_dim, int dtype) {
   return SBD_OK;
 }
 
-sbd_status check_attn_q8_desc(const sbd_attn_q8_desc* d) {
+sbd_status check_attn_q8_desc(const sbd_attn_q8_desc* d, int max_block) {
   if (!d) return fail(SBD_ERR_INVALID_ARG, "desc is NULL");
   if (d->batch < 0 || d->block_k < 1 || d->n_q_heads < 1 || d->max_pages < 1)
     return fail(SBD_ERR_INVALID_ARG, "bad sizes: batch=%d block_k=%d n_q_heads=%d max_pages=%d",
@@ -67,7 +55,7 @@ sbd_status check_attn_q8_desc(const sbd_attn_q8_desc* d) {
   if (d->n_causal < 0 || d->n_causal > d->block_k)
     return fail(SBD_ERR_INVALID_ARG, "n_causal %d outside [0, block_k = %d]", d->n_causal,
                 d->block_k);
-  if (d->block_k > 32) return fail(SBD_ERR_UNSUPPORTED, "block_k %d > 32", d->block_k);
+  if (d->block_k > max_block) return fail(SBD_ERR_UNSUPPORTED, "block_k %d > %d", d->block_k, max_block);
   if (d->batch > 65535) return fail(SBD_ERR_UNSUPPORTED, "batch %d > 65535", d->batch);
   if ((long long)d->max_pages * d->page_size + d->block_k > kMax32)
     return fail(SBD_ERR_UNSUPPORTED, "max_pages * page_size + block_k = %lld >= 2^31",
@@ -134,13 +122,10 @@ sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new
   if (s != SBD_OK) return s;
   s = check_pool(desc->page_size, desc->n_pages);
   if (s != SBD_OK) return s;
-  const int unit = desc->dtype == SBD_DTYPE_F32 ? 4 : 8;      // elements of 16 bytes
   const int64_t strides[] = {desc->k_group_stride, desc->k_token_stride, desc->v_group_stride,
                              desc->v_token_stride};
-  for (int64_t x : strides)
-    if (x < 0 || x % unit != 0)
-      return fail(SBD_ERR_UNSUPPORTED, "stride of %lld elements is not a multiple of 16 bytes",
-                  (long long)x);
+  s = sbd::check_strides(strides, desc->dtype);
+  if (s != SBD_OK) return s;
   if (desc->tokens == 0) return SBD_OK;
   const Named ptrs[] = {{k_new, "k_new"},     {v_new, "v_new"},     {slot_map, "slot_map"},
                         {k_cache, "k_cache"}, {v_cache, "v_cache"}, {k_scale, "k_scale"},
@@ -154,7 +139,7 @@ sbd_status sbd_cache_append_q8(const sbd_append_q8_desc* desc, const void* k_new
 }
 
 size_t sbd_block_attention_q8_workspace_size(const sbd_attn_q8_desc* desc) {
-  check_attn_q8_desc(desc);
+  check_attn_q8_desc(desc, 32);
   return 0;                                  // splits merge on the chip
 }
 
@@ -164,7 +149,7 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
                                   const int32_t* block_table, const int32_t* cache_len,
                                   const void* k_blk, const void* v_blk, void* out,
                                   void*, size_t, void* stream) {
-  sbd_status s = check_attn_q8_desc(desc);
+  sbd_status s = check_attn_q8_desc(desc, 32);
   if (s != SBD_OK) return s;
   if (desc->batch == 0) return SBD_OK;
   const Named ptrs[] = {{q, "q"},
@@ -181,9 +166,76 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
   if (s != SBD_OK) return s;
   s = sbd::device_ready();
   if (s != SBD_OK) return s;
-  const sbd::AttnQ8Tensors t{q,           k_cache,   v_cache, k_scale, v_scale,
-                             block_table, cache_len, k_blk,   v_blk,   out};
-  return sbd::attn_q8_launch(sbd::attn_q8_plan(*desc), t, (cudaStream_t)stream);
+  const sbd::AttnQ8Tensors t{q,         k_cache, v_cache, k_scale, v_scale, block_table,
+                             cache_len, k_blk,   v_blk,   nullptr, out};
+  return sbd::attn_q8_launch(sbd::attn_q8_plan(*desc, false), t, (cudaStream_t)stream);
+}
+
+size_t sbd_tree_attention_q8_workspace_size(const sbd_attn_q8_desc* desc) {
+  check_attn_q8_desc(desc, sbd_dev::kMaxNodes);
+  return 0;
+}
+
+sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, const void* k_cache,
+                                 const void* v_cache, const float* k_scale, const float* v_scale,
+                                 const int32_t* block_table, const int32_t* cache_len,
+                                 const void* k_blk, const void* v_blk, const int32_t* parent,
+                                 void* out, void*, size_t, void* stream) {
+  sbd_status s = check_attn_q8_desc(desc, sbd_dev::kMaxNodes);
+  if (s != SBD_OK) return s;
+  if (desc->n_causal != 0)
+    return fail(SBD_ERR_INVALID_ARG, "n_causal %d: a tree's rows see what parent says", desc->n_causal);
+  if (desc->batch == 0) return SBD_OK;
+  const Named ptrs[] = {{q, "q"},
+                        {k_cache, "k_cache"},
+                        {v_cache, "v_cache"},
+                        {k_scale, "k_scale"},
+                        {v_scale, "v_scale"},
+                        {block_table, "block_table"},
+                        {cache_len, "cache_len"},
+                        {k_blk, "k_blk"},
+                        {v_blk, "v_blk"},
+                        {parent, "parent"},
+                        {out, "out"}};
+  s = check_pointers(ptrs);
+  if (s != SBD_OK) return s;
+  s = sbd::device_ready();
+  if (s != SBD_OK) return s;
+  const sbd::AttnQ8Tensors t{q,         k_cache, v_cache, k_scale, v_scale, block_table,
+                             cache_len, k_blk,   v_blk,   parent,  out};
+  return sbd::attn_q8_launch(sbd::attn_q8_plan(*desc, true), t, (cudaStream_t)stream);
+}
+
+sbd_status sbd_cache_append_path_q8(const sbd_append_path_desc* desc, const void* k_new,
+                                    const void* v_new, const int32_t* path,
+                                    const int32_t* new_start, const int32_t* slot_map,
+                                    void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                                    void* stream) {
+  if (!desc) return fail(SBD_ERR_INVALID_ARG, "desc is NULL");
+  if (desc->batch < 0 || desc->nodes < 1 || desc->max_new < 0)
+    return fail(SBD_ERR_INVALID_ARG, "bad sizes: batch=%d nodes=%d max_new=%d", desc->batch,
+                desc->nodes, desc->max_new);
+  sbd_status s = check_heads(desc->n_kv_heads, desc->n_pages, desc->head_dim, desc->dtype);
+  if (s != SBD_OK) return s;
+  s = check_pool(desc->page_size, desc->n_pages);
+  if (s != SBD_OK) return s;
+  if (desc->nodes > sbd_dev::kMaxNodes)
+    return fail(SBD_ERR_UNSUPPORTED, "nodes %d > %d", desc->nodes, sbd_dev::kMaxNodes);
+  if (desc->batch > 65535) return fail(SBD_ERR_UNSUPPORTED, "batch %d > 65535", desc->batch);
+  const int64_t strides[] = {desc->k_batch_stride, desc->k_node_stride, desc->v_batch_stride,
+                             desc->v_node_stride};
+  s = sbd::check_strides(strides, desc->dtype);
+  if (s != SBD_OK) return s;
+  if (desc->batch == 0 || desc->max_new == 0) return SBD_OK;
+  const Named ptrs[] = {{k_new, "k_new"},         {v_new, "v_new"},       {path, "path"},
+                        {new_start, "new_start"}, {slot_map, "slot_map"}, {k_cache, "k_cache"},
+                        {v_cache, "v_cache"},     {k_scale, "k_scale"},   {v_scale, "v_scale"}};
+  s = check_pointers(ptrs);
+  if (s != SBD_OK) return s;
+  s = sbd::device_ready();
+  if (s != SBD_OK) return s;
+  return sbd::append_path_launch(*desc, k_new, v_new, path, new_start, slot_map, k_cache, v_cache,
+                                 k_scale, v_scale, (cudaStream_t)stream);
 }
 
 }  // extern "C"
