@@ -555,9 +555,10 @@ sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, co
  * q_node one by one, uniform is uniform on [0, 1) and gumbel is standard Gumbel noise
  * (sbd_gumbel_philox).  draft_logits NULL: a drafted token was not drawn but given, q is
  * 1 there and 0 elsewhere.  tau = 0: p is 1 at the largest logit (lowest index of equal
- * ones); draft_logits, uniform and gumbel are not read.  A logit that is NaN counts
- * as -inf, one that is +inf as the largest finite number.  Where no logit of a row is
- * above -inf nothing is accepted there, and the last token is 0.
+ * ones; NaN is below all); draft_logits, uniform and gumbel are not read.  In a
+ * softmax a logit counts as -2^23 tau at least and 2^23 tau at most, NaN as the least: what
+ * is masked with -inf or a type's lowest value never comes out beside an ordinary logit,
+ * and in a row of nothing else all count alike.
  *
  *   target_logits, draft_logits [B, n, V]   desc->dtype; draft row i: what i's children
  *                                           were drawn from (read where it has some)

@@ -74,12 +74,11 @@ def tree_attention(q, kc, vc, ks, vs, table, lens, kb, vb, parent, scale=None):
 def _softmax(z, tau):
     """p, ln p (not ln of p: apart from a logit of 3e38 a sum of exponentials would vanish), and the logits."""
     z = np.asarray(z, np.float64)
-    z = np.where(np.isnan(z), -np.inf, np.minimum(z, 3.4028234663852886e38))
-    m = z.max()
-    if m == -np.inf:
-        return np.zeros_like(z), np.full_like(z, -np.inf), z
-    e = np.exp((z - m) / tau)
-    return e / e.sum(), (z - m) / tau - math.log(e.sum()), z
+    z = np.where(np.isnan(z), -np.inf, z)
+    y = np.clip(z, -2.0 ** 23 * tau, 2.0 ** 23 * tau)
+    m = y.max()
+    e = np.exp((y - m) / tau)
+    return e / e.sum(), (y - m) / tau - math.log(e.sum()), z
 
 
 def verify(target, draft, parent, token, uniform, gumbel, tau):
@@ -99,7 +98,7 @@ def verify(target, draft, parent, token, uniform, gumbel, tau):
         children = [c for c in range(1, n) if parent[c] == node and parent[c] < c and 0 <= token[c] < V]
         if tau == 0:
             best = int(np.argmax(z))
-            hit = [c for c in children if token[c] == best and z.max() > -math.inf]
+            hit = [c for c in children if token[c] == best]
             say(best)
             if not hit:
                 return path, tokens, logprob, margin

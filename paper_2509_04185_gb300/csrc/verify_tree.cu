@@ -1,7 +1,9 @@
 // Verification of drafted tokens: the walk down a tree of nodes that accepts tokens by
 // the target's probabilities and given random numbers (include/sbd.h has the rule).
 //
-// What a row of logits is needed for is its maximum m, its sum S = sum exp((z - m) / tau),
+// Probabilities are powers of two over a sum, p(v) = 2^(z_v c - M) / S with c = log2(e) / tau
+// and the whole number M = ceil(max z c): parts of a row that took different M are brought
+// together by exact factors, and z c - M is rounded once.  What a row is needed for is M, S,
 // the values at a few drafted tokens, and, where the walk ends, one argmax over
 //   ln r(v) + gumbel(v),   r = what is left of p after the rejected children:
 //   r_0 = p,  r_(k+1)(v) = max(r_k(v) - q(v), 0) / Z_k   (draft with probabilities)
@@ -9,10 +11,9 @@
 // r_k is a function of the logits at v and of the scalars Z, so nothing is stored for it:
 // a pass over the row evaluates it.  A request is a thread-block cluster, each CTA has a
 // slice of the vocabulary, and what they need of one another goes through distributed
-// shared memory: every CTA leaves its share of a sum in all of them, adds up in rank order,
-// and so comes to the same numbers and decisions as the others.  Only rows that the walk
-// comes to are read.
-#include <float.h>
+// shared memory: every warp leaves its share of a sum in all CTAs, each of which adds up in
+// the same order, and so comes to the same numbers and decisions as the others.  Only rows
+// that the walk comes to are read.
 #include <math.h>
 
 #include "sbd_internal.cuh"
@@ -25,6 +26,7 @@ constexpr int kMaxNodes = 64;
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
+constexpr float kLimit = 8388608.f;          // logits over tau stay within 2^23
 
 enum Mode { kGreedy, kGiven, kDrawn };       // tau = 0; drafts without, with probabilities
 
@@ -38,73 +40,75 @@ struct Args {
   int* err;
   long long total;           // elements of target
   int n, V, splits;
-  float inv_tau, scale;      // 1 / tau and log2(e) / tau (1 and log2(e) where tau = 0)
+  float scale, limit;        // log2(e) / tau and 2^23 tau (tau 1 where it is 0)
 };
 
-// What is kept of a part of a row.
-struct Sum {
-  float m, s;                // largest logit, sum of 2^((z - m) scale)
-};
-struct Best {
-  float score, z;
-  int v;
-};
-
-__device__ __forceinline__ Sum merge(Sum a, Sum b, float scale) {
-  Sum r;
-  r.m = fmaxf(a.m, b.m);
-  r.s = (a.s > 0.f ? a.s * exp2f((a.m - r.m) * scale) : 0.f) + (b.s > 0.f ? b.s * exp2f((b.m - r.m) * scale) : 0.f);
+__device__ __forceinline__ float redux_max(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-__device__ __forceinline__ Best better(Best a, Best b) {
-  return b.score > a.score || (b.score == a.score && b.v < a.v) ? b : a;
-}
-
-// NaN counts as -inf, +inf as the largest number.
-__device__ __forceinline__ float tame(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
-
-__device__ __forceinline__ float value(const __nv_bfloat16* p) { return tame(__bfloat162float(*p)); }
-__device__ __forceinline__ float value(const float* p) { return tame(*p); }
+// 2^x for the whole numbers x <= 0 that references differ by (0 from -126 on).
+__device__ __forceinline__ float pow2_diff(float x) { return ex2_ftz(x); }
 
 // The logits of a row in words of 16 bytes from the aligned place at or before its
-// beginning; word w has elements kPer w - shift ... of the row, outside of it -inf.
+// beginning; word w has elements kPer w - shift ... of the row.
 template <typename T>
 struct Row {
   static constexpr int kPer = 16 / sizeof(T);
+  static constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf
   const T* base;             // aligned
   const T* end;              // of the tensor
-  int shift, V;
+  int shift, V, words;
   __device__ __forceinline__ Row(const T* tensor, long long total, long long first, int V_) : end(tensor + total), V(V_) {
     shift = (int)(first % kPer);
     base = tensor + (first - shift);
+    words = (int)(((long long)V + shift + kPer - 1) / kPer);
   }
-  __device__ __forceinline__ int words() const { return (V + shift + kPer - 1) / kPer; }
-  __device__ __forceinline__ void load(int w, float (&z)[kPer]) const {
+  // Word w; what lies outside of the row -inf.
+  __device__ __forceinline__ uint4 load(int w) const {
     const T* p = base + (long long)w * kPer;
+    uint32_t u[4] = {kNone, kNone, kNone, kNone};
     if (p + kPer <= end) {
       const uint4 x = *reinterpret_cast<const uint4*>(p);
-      const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w;
+    } else {                                 // the tensor's last word
+      for (int e = 0; e < kPer && p + e < end; ++e) {
         if constexpr (sizeof(T) == 2) {
-          z[2 * e] = tame(__uint_as_float(u[e] << 16));
-          z[2 * e + 1] = tame(__uint_as_float(u[e] & 0xffff0000u));
+          const uint32_t x = *reinterpret_cast<const uint16_t*>(p + e);
+          u[e / 2] = e % 2 ? (u[e / 2] & 0xffffu) | x << 16 : (u[e / 2] & 0xffff0000u) | x;
         } else {
-          z[e] = tame(__uint_as_float(u[e]));
+          u[e] = __float_as_uint(p[e]);
         }
       }
-    } else {                                 // the tensor's last word
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) z[e] = p + e < end ? value(p + e) : -INFINITY;
     }
-    const int v = w * kPer - shift;
+    const long long v = (long long)w * kPer - shift;
     if (v < 0 || v + kPer > V) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e)
-        if (v + e < 0 || v + e >= V) z[e] = -INFINITY;
+      for (int e = 0; e < kPer; ++e) {
+        if (v + e >= 0 && v + e < V) continue;
+        if constexpr (sizeof(T) == 2) u[e / 2] = e % 2 ? (u[e / 2] & 0xffffu) | 0xff800000u : (u[e / 2] & 0xffff0000u) | 0xff80u;
+        else u[e] = kNone;
+      }
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  static __device__ __forceinline__ uint4 none() { return make_uint4(kNone, kNone, kNone, kNone); }
+  static __device__ __forceinline__ void get(const uint4& x, float (&z)[kPer]) {
+    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 2) {
+        z[2 * e] = __uint_as_float(u[e] << 16);
+        z[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+      } else {
+        z[e] = __uint_as_float(u[e]);
+      }
     }
   }
 };
+__device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float value(const float* p) { return *p; }
 
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, int rank) {
   uint32_t r;
@@ -119,136 +123,193 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Reductions over the cluster of four floats a thread; every thread of all CTAs gets the
-// same result.  `warp_sh` is the CTA's own, `all_sh` has every rank's share, in two
-// buffers taken in turn: a CTA that writes into one of them again has passed the barrier
-// of the other, before which everyone had read the first.
+// Four floats of every warp of the cluster, brought to all of its CTAs, in two buffers
+// taken in turn: a CTA that writes into one of them again has passed the barrier of the
+// other, before which everyone had read the first.
 struct Exchange {
-  float4 warp_sh[kWarps];
-  float4 all_sh[2][kMaxCluster];
+  float4 all[2][kMaxCluster * kWarps];
 };
-template <typename F>
-__device__ __forceinline__ float4 reduce(Exchange& x, int& turn, int splits, float4 mine, F&& join) {
+// `mine` is the warp's; returns where the splits * kWarps of them lie.
+__device__ __forceinline__ const float4* exchange(Exchange& x, int& turn, int splits, float4 mine) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    mine = join(mine, make_float4(__shfl_xor_sync(0xffffffffu, mine.x, o), __shfl_xor_sync(0xffffffffu, mine.y, o),
-                                  __shfl_xor_sync(0xffffffffu, mine.z, o), __shfl_xor_sync(0xffffffffu, mine.w, o)));
-  if (lane == 0) x.warp_sh[warp] = mine;
-  __syncthreads();
-  float4 r = x.warp_sh[0];
-#pragma unroll 1
-  for (int w = 1; w < kWarps; ++w) r = join(r, x.warp_sh[w]);
-  if (splits == 1) {
-    __syncthreads();                         // read before they are written again
-    return r;
-  }
-  uint32_t rank;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   turn ^= 1;
-  if (threadIdx.x < splits) st_cluster(mapa(smem_u32(&x.all_sh[turn][rank]), threadIdx.x), r);
-  cluster_sync();
-  r = x.all_sh[turn][0];
-  for (int i = 1; i < splits; ++i) r = join(r, x.all_sh[turn][i]);
-  return r;
+  if (splits == 1) {
+    if (lane == 0) x.all[turn][warp] = mine;
+    __syncthreads();
+  } else {
+    uint32_t rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    if (lane < splits) st_cluster(mapa(smem_u32(&x.all[turn][rank * kWarps + warp]), lane), mine);
+    cluster_sync();
+  }
+  return x.all[turn];
+}
+
+// M and S of a part of a row.
+struct Stat {
+  float M, S;
+};
+__device__ __forceinline__ Stat warp_stat(Stat a) {
+  const float M = redux_max(a.M);
+  return {M, warp_sum(a.S * pow2_diff(a.M - M))};
+}
+__device__ __forceinline__ Stat join(Stat a, float M, float S) {
+  const float top = fmaxf(a.M, M);
+  return {top, a.S * pow2_diff(a.M - top) + S * pow2_diff(M - top)};
+}
+struct Best {
+  float score, z;
+  int v;
+};
+__device__ __forceinline__ Best better(Best a, Best b) {
+  return b.score > a.score || (b.score == a.score && b.v < a.v) ? b : a;
+}
+__device__ __forceinline__ Best warp_best(Best a) {
+  const float top = redux_max(a.score);      // (not NaN: a NaN is never better)
+  const int v = __reduce_min_sync(0xffffffffu, a.score == top ? a.v : 0x7fffffff);
+  const uint32_t who = __ballot_sync(0xffffffffu, a.score == top && a.v == v);
+  return {top, __shfl_sync(0xffffffffu, a.z, __ffs(who) - 1), v};
 }
 
 template <typename T, Mode kMode>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const Args a) {
-  constexpr int kPer = Row<T>::kPer;
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
+  using R = Row<T>;
+  constexpr int kPer = R::kPer;
+  constexpr int kHold = kMode == kDrawn ? 2 : 4;       // words of a row that a thread has in flight
   __shared__ Exchange ex;
-  __shared__ int parent_sh[kMaxNodes], token_sh[kMaxNodes];
+  __shared__ unsigned long long child_sh[kMaxNodes];   // of a node, a bit each
+  __shared__ int token_sh[kMaxNodes];
   __shared__ float uniform_sh[kMaxNodes];
   __shared__ float z_sh[kMaxNodes], q_sh[kMaxNodes];   // logits at a child's token: the target's, the draft's
   __shared__ int rejected_sh[kMaxNodes];               // tokens
   __shared__ float left_sh[kMaxNodes];                 // 1 / Z
   if (a.splits > 1) cluster_sync();          // every CTA is there before one writes into another
   grid_dependency_wait();
-  const int split = blockIdx.x, b = blockIdx.y, n = a.n, V = a.V;
+  const int split = blockIdx.x, b = blockIdx.y, n = a.n, V = a.V, tid = threadIdx.x, lane = tid & 31;
   const T* target = (const T*)a.target;
   const T* draft = (const T*)a.draft;
-  if (threadIdx.x < n) {
-    const int i = threadIdx.x;
-    const size_t at = (size_t)b * n + i;
-    int p = a.parent[at];
-    bool bad = p >= i;
-    if (bad) p = -1;
-    if (i > 0 && p >= 0) {
-      const int x = a.token[at];
-      token_sh[i] = x;
-      if (x < 0 || x >= V) bad = true, p = -1;         // passed over
-      if (kMode != kGreedy) uniform_sh[i] = a.uniform[at];
+  const size_t out = (size_t)b * n;
+  if (tid < kMaxNodes) child_sh[tid] = 0;
+  __syncthreads();
+  if (tid < n) {
+    int p = a.parent[out + tid];
+    bool bad = p >= tid;
+    if (!bad && tid > 0 && p >= 0) {
+      const int x = a.token[out + tid];
+      token_sh[tid] = x;
+      bad = x < 0 || x >= V;                 // passed over
+      if (kMode != kGreedy) uniform_sh[tid] = a.uniform[out + tid];
+      if (!bad) atomicOr(&child_sh[p], 1ull << tid);
     }
     if (bad && split == 0) record_error(a.err, SBD_DEVERR_TREE);
-    parent_sh[i] = i == 0 ? -1 : p;
-  }
-  __syncthreads();
-  int turn = 0, node = 0, count = 1;
-  const bool writer = split == 0 && threadIdx.x == 0;
-  const size_t out = (size_t)b * n;
-  if (split == 0 && threadIdx.x < n) {
-    a.path[out + threadIdx.x] = threadIdx.x == 0 ? 0 : -1;
-    a.out_tokens[out + threadIdx.x] = -1;
-    a.logprob[out + threadIdx.x] = 0.f;
-  }
-  __syncthreads();                           // (written before single places of them are)
-  while (true) {
-    // ---- the row's largest logit and its sum (and the draft's, where it is asked for)
-    bool inner = false;
-    for (int c = node + 1; c < n; ++c) inner |= parent_sh[c] == node;
-    const Row<T> row(target, a.total, ((long long)b * n + node) * V, V);
-    const Row<T> row_q(draft, a.total, ((long long)b * n + node) * V, V);
-    const int words = row.words();
-    const int w0 = (int)((long long)split * words / a.splits), w1 = (int)((long long)(split + 1) * words / a.splits);
-    __syncthreads();                         // the level before is done with z_sh and q_sh
-    if (threadIdx.x < n && parent_sh[threadIdx.x] == node) {
-      const long long at = ((long long)b * n + node) * V + token_sh[threadIdx.x];
-      z_sh[threadIdx.x] = value(target + at);
-      if (kMode == kDrawn) q_sh[threadIdx.x] = value(draft + at);
+    if (split == 0) {
+      a.path[out + tid] = tid == 0 ? 0 : -1;
+      a.out_tokens[out + tid] = -1;
+      a.logprob[out + tid] = 0.f;
     }
-    Sum st{-INFINITY, 0.f}, sq{-INFINITY, 0.f};
-    Best best{-INFINITY, -INFINITY, 0x7fffffff};
-    auto take = [&](Sum& s, const float (&z)[kPer]) {
-      float m = s.m;
+  }
+  __syncthreads();                           // (the outputs, before single places of them are written)
+  int turn = 0, node = 0, count = 1;
+  const bool writer = split == 0 && tid == 0;
+  const float c2 = a.scale;
+  auto tame = [&](float z) { return fminf(fmaxf(z, -a.limit), a.limit); };   // NaN: the least
+  while (true) {
+    const unsigned long long children = child_sh[node];
+    const bool use_q = kMode == kDrawn && children != 0;
+    const long long first = ((long long)b * n + node) * V;
+    const R row(target, a.total, first, V);
+    const R row_q(draft, a.total, first, V);
+    const int w0 = (int)((long long)split * row.words / a.splits), w1 = (int)((long long)(split + 1) * row.words / a.splits);
+    if (tid < kMaxNodes && children >> tid & 1) {      // (read behind the next exchange)
+      z_sh[tid] = tame(value(target + first + token_sh[tid]));
+      if (kMode == kDrawn) q_sh[tid] = tame(value(draft + first + token_sh[tid]));
+    }
+    // ---- M and S of the row (and of the draft's, where it is asked for)
+    Stat st{-2.f * kLimit, 0.f}, sq = st;
+    Best best{-INFINITY, 0.f, 0x7fffffff};
+    auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
+      float m = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) m = fmaxf(m, z[e]);
-      if (m == -INFINITY) return;
-      float sum = s.s > 0.f ? s.s * exp2f((s.m - m) * a.scale) : 0.f;
+      for (int h = 0; h < kHold; ++h) {
+        float z[kPer];
+        R::get(x[h], z);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) sum += ex2_ftz((z[e] - m) * a.scale);
-      s.m = m, s.s = sum;
+        for (int e = 0; e < kPer; ++e) m = fmaxf(m, z[e]);
+      }
+      const float M = fmaxf(s.M, ceilf(tame(m) * c2));
+      float sum = 0.f;
+#pragma unroll
+      for (int h = 0; h < kHold; ++h) {
+        float z[kPer];
+        R::get(x[h], z);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sum += ex2_ftz(fmaf(tame(z[e]), c2, -M));
+      }
+      s.S = s.S * pow2_diff(s.M - M) + sum;
+      s.M = M;
     };
-    for (int w = w0 + threadIdx.x; w < w1; w += kThreads) {
-      float z[kPer];
-      row.load(w, z);
-      take(st, z);
+    for (int w = w0 + tid; w < w1; w += kHold * kThreads) {
+      uint4 x[kHold], y[kHold];
+#pragma unroll
+      for (int h = 0; h < kHold; ++h) {
+        const bool here = w + h * kThreads < w1;
+        x[h] = here ? row.load(w + h * kThreads) : R::none();
+        if (use_q) y[h] = here ? row_q.load(w + h * kThreads) : R::none();
+      }
+      take(st, x);
+      if (use_q) take(sq, y);
       if (kMode == kGreedy) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const int v = w * kPer - row.shift + e;
-          if (v >= 0 && v < V) best = better(best, Best{z[e], z[e], v});
+        for (int h = 0; h < kHold; ++h) {
+          float z[kPer];
+          R::get(x[h], z);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) {
+            const int v = (w + h * kThreads) * kPer - row.shift + e;
+            if (w + h * kThreads < w1 && v >= 0 && v < V) best = better(best, Best{fmaxf(z[e], -INFINITY), 0.f, v});
+          }
         }
       }
-      if (kMode == kDrawn && inner) {
-        float q[kPer];
-        row_q.load(w, q);
-        take(sq, q);
-      }
     }
-    const float scale = a.scale;
-    const float4 sums = reduce(ex, turn, a.splits, make_float4(st.m, st.s, sq.m, sq.s), [scale](float4 x, float4 y) {
-      const Sum t = merge(Sum{x.x, x.y}, Sum{y.x, y.y}, scale), q = merge(Sum{x.z, x.w}, Sum{y.z, y.w}, scale);
-      return make_float4(t.m, t.s, q.m, q.s);
-    });
-    const float m_t = sums.x == -INFINITY ? 0.f : sums.x, inv_t = sums.y > 0.f ? 1.f / sums.y : 0.f;
-    const float m_q = sums.z == -INFINITY ? 0.f : sums.z, inv_q = sums.w > 0.f ? 1.f / sums.w : 0.f;
-    const float log_s = logf(sums.y);
-    auto join_best = [](float4 x, float4 y) {
-      const Best r = better(Best{x.x, x.y, __float_as_int(x.z)}, Best{y.x, y.y, __float_as_int(y.z)});
-      return make_float4(r.score, r.z, __int_as_float(r.v), 0.f);
-    };
-    auto prob = [&](float z) { return ex2_ftz((z - m_t) * scale) * inv_t; };
-    auto prob_q = [&](float z) { return ex2_ftz((z - m_q) * scale) * inv_q; };
+    st = warp_stat(st);
+    float4 mine = make_float4(st.M, st.S, 0.f, 0.f);
+    if (kMode == kDrawn) {
+      sq = warp_stat(sq);
+      mine.z = sq.M, mine.w = sq.S;
+    }
+    if (kMode == kGreedy) {
+      best = warp_best(best);
+      mine.z = best.score, mine.w = __int_as_float(best.v);
+    }
+    const int parts = a.splits * kWarps;
+    {
+      const float4* all = exchange(ex, turn, a.splits, mine);
+      st = sq = Stat{-2.f * kLimit, 0.f};
+      best = Best{-INFINITY, 0.f, 0x7fffffff};
+      for (int i = lane; i < parts; i += 32) {
+        const float4 x = all[i];
+        st = join(st, x.x, x.y);
+        if (kMode == kDrawn) sq = join(sq, x.z, x.w);
+        if (kMode == kGreedy) best = better(best, Best{x.z, 0.f, __float_as_int(x.w)});
+      }
+      st = warp_stat(st);
+      if (kMode == kDrawn) sq = warp_stat(sq);
+      if (kMode == kGreedy) best = warp_best(best);
+    }
+    // What was read beyond the row counts for nothing, unless everything is as low as that.
+    const float low = ex2_ftz(fmaf(-a.limit, c2, -st.M)), low_q = ex2_ftz(fmaf(-a.limit, c2, -sq.M));
+    if (low > 0.f || (use_q && low_q > 0.f)) {
+      long long slots = 0;
+      for (int i = 0; i < a.splits; ++i) {
+        const int words = (int)((long long)(i + 1) * row.words / a.splits) - (int)((long long)i * row.words / a.splits);
+        slots += (long long)(words / (kHold * kThreads)) * kThreads + min(words % (kHold * kThreads), kThreads);
+      }
+      const float beyond = (float)(slots * (kHold * kPer) - V);
+      st.S -= beyond * low, sq.S -= beyond * low_q;
+    }
+    const float inv_s = 1.f / st.S, inv_q = 1.f / sq.S;
+    auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
+    auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
     // What is left of p(v) and of the draft's q(v) after the first k rejections.
     auto left = [&](float r, float q, int v, int k) {
       for (int i = 0; i < k; ++i) {
@@ -267,33 +328,34 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const Args a) {
     int k = 0;                               // rejections whose remainder is known
     bool pending = false;                    // one more, of which nothing is known yet
     if (kMode == kGreedy) {
-      const float4 r = reduce(ex, turn, a.splits, make_float4(best.score, best.z, __int_as_float(best.v), 0.f), join_best);
-      said = __float_as_int(r.z), said_z = r.y;
-      for (int c = node + 1; c < n && next < 0; ++c)
-        if (parent_sh[c] == node && token_sh[c] == said && r.x > -INFINITY) next = c;
+      said = best.v == 0x7fffffff ? 0 : best.v, said_z = tame(best.score);   // (nothing but NaN: 0)
+      for (unsigned long long c = children; c && next < 0; c &= c - 1)
+        if (token_sh[__ffsll(c) - 1] == said) next = __ffsll(c) - 1;
     } else {
-      for (int c = node + 1; c < n && next < 0; ++c) {
-        if (parent_sh[c] != node) continue;
+      for (unsigned long long todo = children; todo && next < 0; todo &= todo - 1) {
+        const int c = __ffsll(todo) - 1;
         if (pending) {
           // the remainder's sum, to go on with the next child
           float sum = 0.f;
-          for (int w = w0 + threadIdx.x; w < w1; w += kThreads) {
+          for (int w = w0 + tid; w < w1; w += kThreads) {
             float z[kPer], q[kPer];
-            row.load(w, z);
-            if (kMode == kDrawn) row_q.load(w, q);
+            R::get(row.load(w), z);
+            if (kMode == kDrawn) R::get(row_q.load(w), q);
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
               const int v = w * kPer - row.shift + e;
-              const float x = kMode == kDrawn ? prob_q(q[e]) : 0.f;
-              sum += rest(left(prob(z[e]), x, v, k), x, v, k);
+              if (v < 0 || v >= V) continue;
+              const float x = kMode == kDrawn ? prob_q(tame(q[e])) : 0.f;
+              sum += rest(left(prob(tame(z[e])), x, v, k), x, v, k);
             }
           }
-          const float total = reduce(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f), [](float4 x, float4 y) {
-                                return make_float4(x.x + y.x, 0.f, 0.f, 0.f);
-                              }).x;
+          sum = warp_sum(sum);
+          const float4* all = exchange(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f));
+          float total = 0.f;
+          for (int i = lane; i < parts; i += 32) total += all[i].x;
+          total = warp_sum(total);
           if (total > 0.f) {
-            __syncthreads();
-            if (threadIdx.x == 0) left_sh[k] = 1.f / total;
+            if (tid == 0) left_sh[k] = 1.f / total;
             __syncthreads();
             ++k;
           }
@@ -305,58 +367,66 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const Args a) {
         if (uniform_sh[c] * q < r) {
           next = c, said = x, said_z = z_sh[c];
         } else {
-          __syncthreads();
-          if (threadIdx.x == 0) rejected_sh[k] = x;
+          __syncthreads();                   // (what was here is read)
+          if (tid == 0) rejected_sh[k] = x;
           __syncthreads();
           pending = true;
         }
       }
     }
+    const float log_s = logf(st.S);
+    auto log_p = [&](float z) { return fmaf(fmaf(z, c2, -st.M), 0.69314718f, -log_s); };
     if (next >= 0) {
       if (writer) {
         a.path[out + count] = next;
         a.out_tokens[out + count - 1] = said;
-        a.logprob[out + count - 1] = (said_z - m_t) * a.inv_tau - log_s;
+        a.logprob[out + count - 1] = log_p(said_z);
       }
       ++count;
       node = next;
+      __syncthreads();                       // z_sh, q_sh and the rejections are read
       continue;
     }
     // ---- the last token
     if (kMode != kGreedy) {
       // of what the last rejection leaves; where that is nothing, of what was before it
-      Best after{-INFINITY, -INFINITY, 0x7fffffff}, before = after;
       const float* g = a.gumbel + (size_t)b * V;
-      for (int w = w0 + threadIdx.x; w < w1; w += kThreads) {
-        float z[kPer], q[kPer];
-        row.load(w, z);
-        if (kMode == kDrawn && (k > 0 || pending)) row_q.load(w, q);
+      for (bool after = pending;; after = false) {
+        best = Best{-INFINITY, 0.f, 0x7fffffff};
+        for (int w = w0 + tid; w < w1; w += kThreads) {
+          float z[kPer], q[kPer];
+          R::get(row.load(w), z);
+          if (kMode == kDrawn && (k > 0 || after)) R::get(row_q.load(w), q);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const int v = w * kPer - row.shift + e;
-          if (v < 0 || v >= V) continue;
-          const float noise = g[v];
-          if (k == 0 && !pending) {
-            before = better(before, Best{(z[e] - m_t) * a.inv_tau + noise, z[e], v});
-            continue;
+          for (int e = 0; e < kPer; ++e) {
+            const int v = w * kPer - row.shift + e;
+            if (v < 0 || v >= V) continue;
+            const float y = tame(z[e]);
+            float score;
+            if (k == 0 && !after) {
+              score = fmaf(fmaf(y, c2, -st.M), 0.69314718f, g[v]);
+            } else {
+              const float x = kMode == kDrawn ? prob_q(tame(q[e])) : 0.f;
+              float r = left(prob(y), x, v, k);
+              if (after) r = rest(r, x, v, k);
+              score = __logf(r) + g[v];
+            }
+            best = better(best, Best{score, y, v});
           }
-          const float x = kMode == kDrawn ? prob_q(q[e]) : 0.f;
-          const float r = left(prob(z[e]), x, v, k);
-          before = better(before, Best{logf(r) + noise, z[e], v});
-          if (pending) after = better(after, Best{logf(rest(r, x, v, k)) + noise, z[e], v});
         }
+        best = warp_best(best);
+        const float4* all = exchange(ex, turn, a.splits, make_float4(best.score, best.z, __int_as_float(best.v), 0.f));
+        best = Best{-INFINITY, 0.f, 0x7fffffff};
+        for (int i = lane; i < parts; i += 32) best = better(best, Best{all[i].x, all[i].y, __float_as_int(all[i].z)});
+        best = warp_best(best);
+        if (!after || best.score > -INFINITY) break;
       }
-      float4 r = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-      if (pending)
-        r = reduce(ex, turn, a.splits, make_float4(after.score, after.z, __int_as_float(after.v), 0.f), join_best);
-      if (!(r.x > -INFINITY))
-        r = reduce(ex, turn, a.splits, make_float4(before.score, before.z, __int_as_float(before.v), 0.f), join_best);
-      said = __float_as_int(r.z), said_z = r.y;
+      said = best.v, said_z = best.z;
+      if (said == 0x7fffffff) said = 0, said_z = tame(value(target + first));   // (no number among the scores)
     }
-    if (said == 0x7fffffff) said = 0, said_z = -INFINITY;   // (no number among the scores)
     if (writer) {
       a.out_tokens[out + count - 1] = said;
-      a.logprob[out + count - 1] = sums.y > 0.f ? (said_z - m_t) * a.inv_tau - log_s : -INFINITY;
+      a.logprob[out + count - 1] = log_p(said_z);
       a.count[b] = count;
     }
     break;
@@ -391,8 +461,9 @@ sbd_status verify_launch(const sbd_verify_desc& d, const VerifyTensors& t, float
   a.total = (long long)d.batch * d.nodes * d.vocab;
   a.n = d.nodes;
   a.V = d.vocab;
-  a.inv_tau = tau == 0.f ? 1.f : 1.f / tau;
-  a.scale = a.inv_tau * 1.4426950408889634f;
+  const float t1 = tau == 0.f ? 1.f : tau;
+  a.scale = 1.4426950408889634f / t1;
+  a.limit = kLimit * t1;
   const void* fn = d.dtype == SBD_DTYPE_F32 ? kernel_of<float>(mode) : kernel_of<__nv_bfloat16>(mode);
   // As many CTAs a request as one wave holds, 2048 logits each at least.
   int s = 1;

@@ -76,11 +76,12 @@ def test_verification_by_hand():
     # greedy: 0 -> child 2 (token 2) -> no child with token 0
     path, tokens, logprob, _ = do.verify(z, None, [-1, 0, 0, 2], [9, 1, 2, 1], None, None, 0)
     assert path == [0, 2] and tokens == [2, 0] and max(map(abs, logprob)) < 1e-12
-    # ties go to the lowest index, a row of nothing accepts nothing
+    # ties go to the lowest index, in a row of nothing all are alike
     assert do.verify(np.zeros((1, 4)), None, [-1], [0], None, None, 0)[1] == [0]
     none = np.full((2, 3), -np.inf)
-    assert do.verify(none, None, [-1, 0], [0, 0], [0, 0], np.zeros(3), 1.0)[:2] == ([0], [0])
-    assert do.verify(none, None, [-1, 0], [0, 0], None, None, 0)[:2] == ([0], [0])
+    assert do.verify(none, None, [-1, 0], [0, 1], [0, 0.4], np.zeros(3), 1.0)[:2] == ([0], [0])
+    assert do.verify(none, None, [-1, 0], [0, 1], [0, 0.3], np.zeros(3), 1.0)[:2] == ([0, 1], [1, 0])
+    assert do.verify(none, None, [-1, 0], [0, 0], None, None, 0)[:2] == ([0, 1], [0, 0])
     # equal distributions: accepted below 1, and where a token is refused all the same, p stays
     z = np.log([[0.25, 0.75], [0.5, 0.5]])
     assert do.verify(z, z, [-1, 0], [0, 0], [0, 0.999999], np.array([9.0, 0.0]), 1.0)[0] == [0, 1]
