@@ -23,7 +23,7 @@ namespace {
 using namespace sbd_dev;
 
 constexpr int kMaxNodes = 64;
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr float kLimit = 8388608.f;          // logits over tau stay within 2^23
@@ -38,7 +38,6 @@ struct Args {
   float* logprob;
   int32_t* count;
   int* err;
-  long long total;           // elements of target
   int n, V, splits;
   float scale, limit;        // log2(e) / tau and 2^23 tau (tau 1 where it is 0)
 };
@@ -51,48 +50,28 @@ __device__ __forceinline__ float redux_max(float v) {
 // 2^x for the whole numbers x <= 0 that references differ by (0 from -126 on).
 __device__ __forceinline__ float pow2_diff(float x) { return ex2_ftz(x); }
 
-// The logits of a row in words of 16 bytes from the aligned place at or before its
-// beginning; word w has elements kPer w - shift ... of the row.
+// The logits of a row: whole words of 16 bytes between the aligned places c0 and c1 (word w
+// has elements kPer w - shift ...), and up to 2 kPer - 2 edges, one by one.
 template <typename T>
 struct Row {
   static constexpr int kPer = 16 / sizeof(T);
   static constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf
   const T* base;             // aligned
-  const T* end;              // of the tensor
-  int shift, V, words;
-  __device__ __forceinline__ Row(const T* tensor, long long total, long long first, int V_) : end(tensor + total), V(V_) {
+  int shift, c0, c1, head, edges;
+  __device__ __forceinline__ Row(const T* tensor, long long first, int V) {
     shift = (int)(first % kPer);
     base = tensor + (first - shift);
-    words = (int)(((long long)V + shift + kPer - 1) / kPer);
+    c0 = shift ? 1 : 0;
+    c1 = max(c0, (int)(((long long)V + shift) / kPer));
+    head = shift ? min(V, kPer - shift) : 0;
+    edges = head + max(0, (int)(V - ((long long)c1 * kPer - shift)));
   }
-  // Word w; what lies outside of the row -inf.
   __device__ __forceinline__ uint4 load(int w) const {
-    const T* p = base + (long long)w * kPer;
-    uint32_t u[4] = {kNone, kNone, kNone, kNone};
-    if (p + kPer <= end) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p);
-      u[0] = x.x, u[1] = x.y, u[2] = x.z, u[3] = x.w;
-    } else {                                 // the tensor's last word
-      for (int e = 0; e < kPer && p + e < end; ++e) {
-        if constexpr (sizeof(T) == 2) {
-          const uint32_t x = *reinterpret_cast<const uint16_t*>(p + e);
-          u[e / 2] = e % 2 ? (u[e / 2] & 0xffffu) | x << 16 : (u[e / 2] & 0xffff0000u) | x;
-        } else {
-          u[e] = __float_as_uint(p[e]);
-        }
-      }
-    }
-    const long long v = (long long)w * kPer - shift;
-    if (v < 0 || v + kPer > V) {
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        if (v + e >= 0 && v + e < V) continue;
-        if constexpr (sizeof(T) == 2) u[e / 2] = e % 2 ? (u[e / 2] & 0xffffu) | 0xff800000u : (u[e / 2] & 0xffff0000u) | 0xff80u;
-        else u[e] = kNone;
-      }
-    }
-    return make_uint4(u[0], u[1], u[2], u[3]);
+    return *reinterpret_cast<const uint4*>(base + (long long)w * kPer);
   }
+  __device__ __forceinline__ int element(int w) const { return w * kPer - shift; }
+  // Edge i < edges.
+  __device__ __forceinline__ int edge(int i) const { return i < head ? i : c1 * kPer - shift + (i - head); }
   static __device__ __forceinline__ uint4 none() { return make_uint4(kNone, kNone, kNone, kNone); }
   static __device__ __forceinline__ void get(const uint4& x, float (&z)[kPer]) {
     const uint32_t u[4] = {x.x, x.y, x.z, x.w};
@@ -107,6 +86,47 @@ struct Row {
     }
   }
 };
+// The largest element of words (NaN left out).
+template <int N>
+__device__ __forceinline__ float largest(const uint4 (&x)[N], const __nv_bfloat16*) {
+  auto two = [](uint32_t u) { return *reinterpret_cast<const __nv_bfloat162*>(&u); };
+  __nv_bfloat162 m = __float2bfloat162_rn(-INFINITY);
+#pragma unroll
+  for (int h = 0; h < N; ++h)
+    m = __hmax2(__hmax2(m, __hmax2(two(x[h].x), two(x[h].y))), __hmax2(two(x[h].z), two(x[h].w)));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+template <int N>
+__device__ __forceinline__ float largest(const uint4 (&x)[N], const float*) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int h = 0; h < N; ++h)
+    m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(x[h].x), __uint_as_float(x[h].y))),
+              fmaxf(__uint_as_float(x[h].z), __uint_as_float(x[h].w)));
+  return m;
+}
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 __device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float value(const float* p) { return *p; }
 
@@ -172,7 +192,7 @@ __device__ __forceinline__ Best warp_best(Best a) {
 }
 
 template <typename T, Mode kMode>
-__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const Args a) {
   using R = Row<T>;
   constexpr int kPer = R::kPer;
   constexpr int kHold = kMode == kDrawn ? 2 : 4;       // words of a row that a thread has in flight
@@ -217,59 +237,86 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
     const unsigned long long children = child_sh[node];
     const bool use_q = kMode == kDrawn && children != 0;
     const long long first = ((long long)b * n + node) * V;
-    const R row(target, a.total, first, V);
-    const R row_q(draft, a.total, first, V);
-    const int w0 = (int)((long long)split * row.words / a.splits), w1 = (int)((long long)(split + 1) * row.words / a.splits);
+    const R row(target, first, V), row_q(draft, first, V);       // (alike but for the base)
+    const int w0 = row.c0 + (int)((long long)split * (row.c1 - row.c0) / a.splits);
+    const int w1 = row.c0 + (int)((long long)(split + 1) * (row.c1 - row.c0) / a.splits);
+    const int edge = split == 0 && tid < row.edges ? row.edge(tid) : -1;   // this thread's
+    const T* target_row = target + first;
+    const T* draft_row = draft + first;
     if (tid < kMaxNodes && children >> tid & 1) {      // (read behind the next exchange)
-      z_sh[tid] = tame(value(target + first + token_sh[tid]));
-      if (kMode == kDrawn) q_sh[tid] = tame(value(draft + first + token_sh[tid]));
+      z_sh[tid] = tame(value(target_row + token_sh[tid]));
+      if (kMode == kDrawn) q_sh[tid] = tame(value(draft_row + token_sh[tid]));
     }
     // ---- M and S of the row (and of the draft's, where it is asked for)
     Stat st{-2.f * kLimit, 0.f}, sq = st;
     Best best{-INFINITY, 0.f, 0x7fffffff};
+    // As they are: what is not ordinary (NaN, beyond the limit) shows in the sum or in M, and
+    // the thread's share is taken again, slowly.
     auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
-      float m = -INFINITY;
+      const float M = fmaxf(s.M, ceilf(tame(largest(x, (const T*)nullptr)) * c2));
+      float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
       for (int h = 0; h < kHold; ++h) {
         float z[kPer];
         R::get(x[h], z);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) m = fmaxf(m, z[e]);
+        for (int e = 0; e < kPer; e += 2) {
+          const float2 y = fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-M, -M));
+          sum = add2(sum, make_float2(ex2_ftz(y.x), ex2_ftz(y.y)));
+        }
       }
-      const float M = fmaxf(s.M, ceilf(tame(m) * c2));
-      float sum = 0.f;
-#pragma unroll
-      for (int h = 0; h < kHold; ++h) {
-        float z[kPer];
-        R::get(x[h], z);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) sum += ex2_ftz(fmaf(tame(z[e]), c2, -M));
-      }
-      s.S = s.S * pow2_diff(s.M - M) + sum;
+      s.S = fmaf(s.S, pow2_diff(s.M - M), sum.x + sum.y);
       s.M = M;
+    };
+    auto take_one = [&](Stat& s, float z) {
+      const float M = fmaxf(s.M, ceilf(tame(z) * c2));
+      s.S = fmaf(s.S, pow2_diff(s.M - M), ex2_ftz(fmaf(tame(z), c2, -M)));
+      s.M = M;
+    };
+    auto again = [&](Stat& s, const R& r, const T* elements) {
+      if (s.S < INFINITY && s.M >= 256.f - a.limit * c2) return;
+      s = Stat{-2.f * kLimit, 0.f};
+#pragma unroll 1
+      for (int w = w0 + tid; w < w1; w += kThreads)
+#pragma unroll 1
+        for (int e = 0; e < kPer; ++e) take_one(s, value(elements + r.element(w) + e));
     };
     for (int w = w0 + tid; w < w1; w += kHold * kThreads) {
       uint4 x[kHold], y[kHold];
 #pragma unroll
       for (int h = 0; h < kHold; ++h) {
         const bool here = w + h * kThreads < w1;
-        x[h] = here ? row.load(w + h * kThreads) : R::none();
-        if (use_q) y[h] = here ? row_q.load(w + h * kThreads) : R::none();
+        x[h] = R::none();
+        if (here) x[h] = row.load(w + h * kThreads);
+        if (use_q) {
+          y[h] = R::none();
+          if (here) y[h] = row_q.load(w + h * kThreads);
+        }
       }
       take(st, x);
       if (use_q) take(sq, y);
       if (kMode == kGreedy) {
+        const float top = largest(x, (const T*)nullptr);
+        if (top > best.score || best.v == 0x7fffffff) {  // (later ones have higher indices, and are not better if equal)
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) {
-          float z[kPer];
-          R::get(x[h], z);
+          for (int h = 0; h < kHold; ++h) {
+            float z[kPer];
+            R::get(x[h], z);
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) {
-            const int v = (w + h * kThreads) * kPer - row.shift + e;
-            if (w + h * kThreads < w1 && v >= 0 && v < V) best = better(best, Best{fmaxf(z[e], -INFINITY), 0.f, v});
+            for (int e = 0; e < kPer; ++e)
+              if (w + h * kThreads < w1)
+                best = better(best, Best{fmaxf(z[e], -INFINITY), 0.f, row.element(w + h * kThreads) + e});
           }
         }
       }
+    }
+    again(st, row, target_row);
+    if (use_q) again(sq, row_q, draft_row);
+    if (edge >= 0) {
+      const float z = value(target_row + edge);
+      take_one(st, z);
+      if (use_q) take_one(sq, value(draft_row + edge));
+      if (kMode == kGreedy) best = better(best, Best{fmaxf(z, -INFINITY), 0.f, edge});
     }
     st = warp_stat(st);
     float4 mine = make_float4(st.M, st.S, 0.f, 0.f);
@@ -296,32 +343,81 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
       if (kMode == kDrawn) sq = warp_stat(sq);
       if (kMode == kGreedy) best = warp_best(best);
     }
-    // What was read beyond the row counts for nothing, unless everything is as low as that.
-    const float low = ex2_ftz(fmaf(-a.limit, c2, -st.M)), low_q = ex2_ftz(fmaf(-a.limit, c2, -sq.M));
-    if (low > 0.f || (use_q && low_q > 0.f)) {
-      long long slots = 0;
-      for (int i = 0; i < a.splits; ++i) {
-        const int words = (int)((long long)(i + 1) * row.words / a.splits) - (int)((long long)i * row.words / a.splits);
-        slots += (long long)(words / (kHold * kThreads)) * kThreads + min(words % (kHold * kThreads), kThreads);
-      }
-      const float beyond = (float)(slots * (kHold * kPer) - V);
-      st.S -= beyond * low, sq.S -= beyond * low_q;
-    }
     const float inv_s = 1.f / st.S, inv_q = 1.f / sq.S;
     auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
     auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
-    // What is left of p(v) and of the draft's q(v) after the first k rejections.
-    auto left = [&](float r, float q, int v, int k) {
-      for (int i = 0; i < k; ++i) {
-        if (kMode == kDrawn) r = fmaxf(r - q, 0.f);
-        else if (v == rejected_sh[i]) r = 0.f;
-        r *= left_sh[i];
+    // A row whose logits are within the limit needs no taming of single ones but NaN.
+    const bool tamed = (st.M >= 256.f - a.limit * c2 && st.M < a.limit * c2 - 1.f) &&
+                       (!use_q || (sq.M >= 256.f - a.limit * c2 && sq.M < a.limit * c2 - 1.f));
+    // What is left of p at elements v, v + 1, ... after the first k rejections (and one more,
+    // `after`), not normalised by the last ones' sum.
+    auto remainder = [&](float (&z)[kPer], float (&q)[kPer], int v, int k, bool after, float (&r)[kPer]) {
+      if (!tamed) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) z[e] = tame(z[e]), q[e] = kMode == kDrawn ? tame(q[e]) : 0.f;
       }
-      return r;
+#pragma unroll
+      for (int e = 0; e < kPer; e += 2) {
+        float2 x = fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-st.M, -st.M));
+        x = mul2(make_float2(ex2_ftz(x.x), ex2_ftz(x.y)), make_float2(inv_s, inv_s));
+        r[e] = x.x, r[e + 1] = x.y;
+        if (kMode == kDrawn) {
+          x = fma2(make_float2(q[e], q[e + 1]), make_float2(c2, c2), make_float2(-sq.M, -sq.M));
+          x = mul2(make_float2(ex2_ftz(x.x), ex2_ftz(x.y)), make_float2(inv_q, inv_q));
+          q[e] = fmaxf(x.x, 0.f), q[e + 1] = fmaxf(x.y, 0.f);      // (NaN: 0)
+        }
+      }
+      if (kMode == kDrawn) {
+#pragma unroll 1
+        for (int i = 0; i < k; ++i) {
+          const float f = left_sh[i];
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) r[e] = fmaxf(r[e] - q[e], 0.f) * f;
+        }
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) r[e] = fmaxf(after ? r[e] - q[e] : r[e], 0.f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) r[e] = fmaxf(r[e], 0.f);
+#pragma unroll 1
+        for (int i = 0; i < k + after; ++i) {
+          const uint32_t at = (uint32_t)(rejected_sh[i] - v);
+          if (at < kPer) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) r[e] = e == (int)at ? 0.f : r[e];
+          }
+        }
+      }
     };
-    // One rejection more, not normalised.
-    auto rest = [&](float r, float q, int v, int k) {
-      return kMode == kDrawn ? fmaxf(r - q, 0.f) : v == rejected_sh[k] ? 0.f : r;
+    // The words of this CTA's slice, two in flight, as f(words of both rows, first element),
+    // and this thread's edge as f(values, element).
+    auto each = [&](bool with_q, auto&& f, auto&& f_edge) {
+#pragma unroll 1
+      for (int w = w0 + tid; w < w1; w += 2 * kThreads) {
+        uint4 x[2], y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (w + h * kThreads >= w1) continue;
+          x[h] = row.load(w + h * kThreads);
+          if (with_q) y[h] = row_q.load(w + h * kThreads);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (w + h * kThreads >= w1) continue;
+          float z[kPer], q[kPer];
+          R::get(x[h], z);
+          if (with_q) R::get(y[h], q);
+          f(z, q, row.element(w + h * kThreads));
+        }
+      }
+      if (edge >= 0) {                         // the other places -inf
+        float z[kPer], q[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) z[e] = q[e] = -INFINITY;
+        z[0] = value(target_row + edge);
+        if (with_q) q[0] = value(draft_row + edge);
+        f_edge(z, q, edge);
+      }
     };
     int next = -1, said = -1;
     float said_z = 0.f;
@@ -337,18 +433,18 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
         if (pending) {
           // the remainder's sum, to go on with the next child
           float sum = 0.f;
-          for (int w = w0 + tid; w < w1; w += kThreads) {
-            float z[kPer], q[kPer];
-            R::get(row.load(w), z);
-            if (kMode == kDrawn) R::get(row_q.load(w), q);
+          each(kMode == kDrawn,
+               [&](float (&z)[kPer], float (&q)[kPer], int v) {
+                 float r[kPer];
+                 remainder(z, q, v, k, true, r);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-              const int v = w * kPer - row.shift + e;
-              if (v < 0 || v >= V) continue;
-              const float x = kMode == kDrawn ? prob_q(tame(q[e])) : 0.f;
-              sum += rest(left(prob(tame(z[e])), x, v, k), x, v, k);
-            }
-          }
+                 for (int e = 0; e < kPer; ++e) sum += r[e];
+               },
+               [&](float (&z)[kPer], float (&q)[kPer], int v) {
+                 float r[kPer];
+                 remainder(z, q, v, k, true, r);
+                 sum += r[0];
+               });
           sum = warp_sum(sum);
           const float4* all = exchange(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f));
           float total = 0.f;
@@ -361,9 +457,15 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
           }
           pending = false;
         }
+        // r(x): step by step with a draft's probabilities; without, p(x) over what is left of it
         const int x = token_sh[c];
         const float q = kMode == kDrawn ? prob_q(q_sh[c]) : 1.f;
-        const float r = left(prob(z_sh[c]), q, x, k);
+        float r = prob(z_sh[c]);
+        for (int i = 0; i < k; ++i) {
+          if (kMode == kDrawn) r = fmaxf(r - q, 0.f) * left_sh[i];
+          else if (x == rejected_sh[i]) r = 0.f;
+        }
+        if (kMode == kGiven && k > 0) r *= left_sh[k - 1];
         if (uniform_sh[c] * q < r) {
           next = c, said = x, said_z = z_sh[c];
         } else {
@@ -391,29 +493,56 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Args a) {
     if (kMode != kGreedy) {
       // of what the last rejection leaves; where that is nothing, of what was before it
       const float* g = a.gumbel + (size_t)b * V;
+      // (the noise of a word is as many aligned words of four where the row is)
+      const bool aligned = ((long long)b * V - row.shift) % 4 == 0;
       for (bool after = pending;; after = false) {
         best = Best{-INFINITY, 0.f, 0x7fffffff};
-        for (int w = w0 + tid; w < w1; w += kThreads) {
-          float z[kPer], q[kPer];
-          R::get(row.load(w), z);
-          if (kMode == kDrawn && (k > 0 || after)) R::get(row_q.load(w), q);
+        const bool untouched = k == 0 && !after;
+        auto scores = [&](float (&z)[kPer], float (&q)[kPer], int v, const float (&noise)[kPer], int places) {
+          float s[kPer], y[kPer], top = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) {
-            const int v = w * kPer - row.shift + e;
-            if (v < 0 || v >= V) continue;
-            const float y = tame(z[e]);
-            float score;
-            if (k == 0 && !after) {
-              score = fmaf(fmaf(y, c2, -st.M), 0.69314718f, g[v]);
-            } else {
-              const float x = kMode == kDrawn ? prob_q(tame(q[e])) : 0.f;
-              float r = left(prob(y), x, v, k);
-              if (after) r = rest(r, x, v, k);
-              score = __logf(r) + g[v];
-            }
-            best = better(best, Best{score, y, v});
+          for (int e = 0; e < kPer; ++e) y[e] = z[e];
+          if (untouched) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) s[e] = fmaf(fmaf(tame(z[e]), c2, -st.M), 0.69314718f, noise[e]);
+          } else {
+            float r[kPer];
+            remainder(z, q, v, k, after, r);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) s[e] = __logf(r[e]) + noise[e];
           }
-        }
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) top = e < places ? fmaxf(top, s[e]) : top;
+          if (top > best.score || (best.v == 0x7fffffff && top >= best.score)) {   // (later words have higher indices)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+              if (e < places) best = better(best, Best{s[e], tame(y[e]), v + e});
+          }
+        };
+        each(kMode == kDrawn && !untouched,
+             [&](float (&z)[kPer], float (&q)[kPer], int v) {
+               float noise[kPer];
+               if (aligned) {
+#pragma unroll
+                 for (int e = 0; e < kPer; e += 4) {
+                   const float4 x = *reinterpret_cast<const float4*>(g + v + e);
+                   noise[e] = x.x, noise[e + 1] = x.y, noise[e + 2] = x.z, noise[e + 3] = x.w;
+                 }
+               } else {
+#pragma unroll
+                 for (int e = 0; e < kPer; ++e) noise[e] = g[v + e];
+               }
+               scores(z, q, v, noise, kPer);
+             },
+             [&](float (&z)[kPer], float (&q)[kPer], int v) {
+               float noise[kPer];
+#pragma unroll
+               for (int e = 0; e < kPer; ++e) noise[e] = g[v];
+               Best words = best;
+               best = Best{-INFINITY, 0.f, 0x7fffffff};
+               scores(z, q, v, noise, 1);
+               best = better(words, best);
+             });
         best = warp_best(best);
         const float4* all = exchange(ex, turn, a.splits, make_float4(best.score, best.z, __int_as_float(best.v), 0.f));
         best = Best{-INFINITY, 0.f, 0x7fffffff};
@@ -458,7 +587,6 @@ sbd_status verify_launch(const sbd_verify_desc& d, const VerifyTensors& t, float
   a.logprob = t.logprob;
   a.count = t.count;
   a.err = device_error_word();
-  a.total = (long long)d.batch * d.nodes * d.vocab;
   a.n = d.nodes;
   a.V = d.vocab;
   const float t1 = tau == 0.f ? 1.f : tau;
@@ -467,7 +595,7 @@ sbd_status verify_launch(const sbd_verify_desc& d, const VerifyTensors& t, float
   const void* fn = d.dtype == SBD_DTYPE_F32 ? kernel_of<float>(mode) : kernel_of<__nv_bfloat16>(mode);
   // As many CTAs a request as one wave holds, 2048 logits each at least.
   int s = 1;
-  while (s < kMaxCluster && 2ll * s * d.batch <= 2ll * num_sms() && d.vocab / (2 * s) >= 2048) s *= 2;
+  while (s < kMaxCluster && 2ll * s * d.batch <= (1024ll / kThreads) * num_sms() && d.vocab / (2 * s) >= 2048) s *= 2;
   while (s > 1 && cluster_slots(fn, kThreads, 0, s) < 1) s /= 2;
   a.splits = s;
   void* args[] = {(void*)&a};
