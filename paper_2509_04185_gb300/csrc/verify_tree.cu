@@ -23,8 +23,6 @@ namespace {
 using namespace sbd_dev;
 
 constexpr int kMaxNodes = 64;
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr float kLimit = 8388608.f;          // logits over tau stay within 2^23
 
@@ -39,6 +37,8 @@ struct Args {
   int32_t* count;
   int* err;
   int n, V, splits;
+  int slice;                 // words of a CTA
+  int ahead;                 // rows are fetched ahead
   float scale, limit;        // log2(e) / tau and 2^23 tau (tau 1 where it is 0)
 };
 
@@ -59,12 +59,12 @@ struct Row {
   const T* base;             // aligned
   int shift, c0, c1, head, edges;
   __device__ __forceinline__ Row(const T* tensor, long long first, int V) {
-    shift = (int)(first % kPer);
+    shift = (int)first & (kPer - 1);
     base = tensor + (first - shift);
     c0 = shift ? 1 : 0;
-    c1 = max(c0, (int)(((long long)V + shift) / kPer));
+    c1 = max(c0, (int)(((uint32_t)V + shift) / kPer));
     head = shift ? min(V, kPer - shift) : 0;
-    edges = head + max(0, (int)(V - ((long long)c1 * kPer - shift)));
+    edges = max(head, V - c1 * kPer + shift + head);
   }
   __device__ __forceinline__ uint4 load(int w) const {
     return *reinterpret_cast<const uint4*>(base + (long long)w * kPer);
@@ -143,26 +143,30 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Four floats of every warp of the cluster, brought to all of its CTAs, in two buffers
-// taken in turn: a CTA that writes into one of them again has passed the barrier of the
-// other, before which everyone had read the first.
+// Reductions of four floats over the cluster; every warp of it has the same result.  `join`
+// reduces over a warp (all lanes have its result); a warp's goes to the CTA, the CTA's to all
+// of the cluster.  The buffers are taken in turn: a CTA that writes into one of them again
+// has passed the barrier of the other, before which everyone had read the first.
+template <int kWarps>
 struct Exchange {
-  float4 all[2][kMaxCluster * kWarps];
+  float4 warps[2][kWarps];
+  float4 ranks[2][kMaxCluster];
 };
-// `mine` is the warp's; returns where the splits * kWarps of them lie.
-__device__ __forceinline__ const float4* exchange(Exchange& x, int& turn, int splits, float4 mine) {
+template <int kWarps, typename F>
+__device__ __forceinline__ float4 reduce(Exchange<kWarps>& x, int& turn, int splits, float4 mine, float4 none, F&& join) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   turn ^= 1;
-  if (splits == 1) {
-    if (lane == 0) x.all[turn][warp] = mine;
-    __syncthreads();
-  } else {
-    uint32_t rank;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    if (lane < splits) st_cluster(mapa(smem_u32(&x.all[turn][rank * kWarps + warp]), lane), mine);
-    cluster_sync();
-  }
-  return x.all[turn];
+  mine = join(mine);
+  if (lane == 0) x.warps[turn][warp] = mine;
+  __syncthreads();
+  if (splits == 1 || warp == 0) mine = join(lane < kWarps ? x.warps[turn][lane] : none);
+  if (splits == 1) return mine;
+  uint32_t rank;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  if (warp == 0 && lane < splits) st_cluster(mapa(smem_u32(&x.ranks[turn][rank]), lane), mine);
+  __syncwarp();
+  cluster_sync();
+  return join(lane < splits ? x.ranks[turn][lane] : none);
 }
 
 // M and S of a part of a row.
@@ -172,10 +176,6 @@ struct Stat {
 __device__ __forceinline__ Stat warp_stat(Stat a) {
   const float M = redux_max(a.M);
   return {M, warp_sum(a.S * pow2_diff(a.M - M))};
-}
-__device__ __forceinline__ Stat join(Stat a, float M, float S) {
-  const float top = fmaxf(a.M, M);
-  return {top, a.S * pow2_diff(a.M - top) + S * pow2_diff(M - top)};
 }
 struct Best {
   float score, z;
@@ -191,16 +191,20 @@ __device__ __forceinline__ Best warp_best(Best a) {
   return {top, __shfl_sync(0xffffffffu, a.z, __ffs(who) - 1), v};
 }
 
-template <typename T, Mode kMode>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const Args a) {
+template <typename T, Mode kMode, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kernel(const Args a) {
+  constexpr int kWarps = kThreads / 32;
   using R = Row<T>;
   constexpr int kPer = R::kPer;
   constexpr int kHold = kMode == kDrawn ? 2 : 4;       // words of a row that a thread has in flight
-  __shared__ Exchange ex;
+  __shared__ Exchange<kWarps> ex;
   __shared__ unsigned long long child_sh[kMaxNodes];   // of a node, a bit each
   __shared__ int token_sh[kMaxNodes];
   __shared__ float uniform_sh[kMaxNodes];
-  __shared__ float z_sh[kMaxNodes], q_sh[kMaxNodes];   // logits at a child's token: the target's, the draft's
+  __shared__ float z_sh[2][kMaxNodes], q_sh[2][kMaxNodes];   // logits at a child's token (target's, draft's), levels in turn
+  __shared__ int path_sh[kMaxNodes], said_sh[kMaxNodes];     // the walk, told at its end: nodes, tokens,
+  __shared__ float said_z_sh[kMaxNodes];                     // their logits, and their rows' M and S
+  __shared__ Stat said_st_sh[kMaxNodes];
   __shared__ int rejected_sh[kMaxNodes];               // tokens
   __shared__ float left_sh[kMaxNodes];                 // 1 / Z
   if (a.splits > 1) cluster_sync();          // every CTA is there before one writes into another
@@ -222,15 +226,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
       if (!bad) atomicOr(&child_sh[p], 1ull << tid);
     }
     if (bad && split == 0) record_error(a.err, SBD_DEVERR_TREE);
-    if (split == 0) {
-      a.path[out + tid] = tid == 0 ? 0 : -1;
-      a.out_tokens[out + tid] = -1;
-      a.logprob[out + tid] = 0.f;
-    }
   }
-  __syncthreads();                           // (the outputs, before single places of them are written)
+  __syncthreads();
   int turn = 0, node = 0, count = 1;
-  const bool writer = split == 0 && tid == 0;
+  // The walk's noise on its way to L2 (and below, a row ahead).
+  if (kMode != kGreedy) {
+    const float* g = a.gumbel + (size_t)b * V;
+    const int part = (V + a.splits - 1) / a.splits, v1 = min(V, (split + 1) * part);
+    for (int v = split * part + tid * 32; v < v1; v += kThreads * 32) prefetch_l2(g + v);
+  }
   const float c2 = a.scale;
   auto tame = [&](float z) { return fminf(fmaxf(z, -a.limit), a.limit); };   // NaN: the least
   while (true) {
@@ -238,14 +242,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
     const bool use_q = kMode == kDrawn && children != 0;
     const long long first = ((long long)b * n + node) * V;
     const R row(target, first, V), row_q(draft, first, V);       // (alike but for the base)
-    const int w0 = row.c0 + (int)((long long)split * (row.c1 - row.c0) / a.splits);
-    const int w1 = row.c0 + (int)((long long)(split + 1) * (row.c1 - row.c0) / a.splits);
+    const int w0 = min(row.c1, row.c0 + split * a.slice), w1 = min(row.c1, w0 + a.slice);
     const int edge = split == 0 && tid < row.edges ? row.edge(tid) : -1;   // this thread's
     const T* target_row = target + first;
     const T* draft_row = draft + first;
-    if (tid < kMaxNodes && children >> tid & 1) {      // (read behind the next exchange)
-      z_sh[tid] = tame(value(target_row + token_sh[tid]));
-      if (kMode == kDrawn) q_sh[tid] = tame(value(draft_row + token_sh[tid]));
+    const bool is_child = tid < kMaxNodes && children >> tid & 1;
+    float child_z = 0.f, child_q = 0.f;      // (stored once the row's loads are under way, too)
+    if (is_child) {
+      child_z = value(target_row + token_sh[tid]);
+      if (kMode == kDrawn) child_q = value(draft_row + token_sh[tid]);
     }
     // ---- M and S of the row (and of the draft's, where it is asked for)
     Stat st{-2.f * kLimit, 0.f}, sq = st;
@@ -310,6 +315,18 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
         }
       }
     }
+    // The first child's rows on their way to L2: the walk is likely to go there.
+    if (a.ahead && children) {
+      const int c = __ffsll(children) - 1;
+      const long long there = (long long)(c - node) * V;
+      const bool its_q = kMode == kDrawn && child_sh[c] != 0;
+      for (int w = w0 + tid * 8; w < w1; w += kThreads * 8) {          // a line each
+        prefetch_l2(row.base + there + (long long)w * kPer);
+        if (its_q) prefetch_l2(row_q.base + there + (long long)w * kPer);
+      }
+    }
+    const int level = count & 1;
+    if (is_child) z_sh[level][tid] = tame(child_z), q_sh[level][tid] = tame(child_q);   // (read behind the next exchange)
     again(st, row, target_row);
     if (use_q) again(sq, row_q, draft_row);
     if (edge >= 0) {
@@ -318,32 +335,23 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
       if (use_q) take_one(sq, value(draft_row + edge));
       if (kMode == kGreedy) best = better(best, Best{fmaxf(z, -INFINITY), 0.f, edge});
     }
-    st = warp_stat(st);
-    float4 mine = make_float4(st.M, st.S, 0.f, 0.f);
-    if (kMode == kDrawn) {
-      sq = warp_stat(sq);
-      mine.z = sq.M, mine.w = sq.S;
-    }
-    if (kMode == kGreedy) {
-      best = warp_best(best);
-      mine.z = best.score, mine.w = __int_as_float(best.v);
-    }
-    const int parts = a.splits * kWarps;
-    {
-      const float4* all = exchange(ex, turn, a.splits, mine);
-      st = sq = Stat{-2.f * kLimit, 0.f};
-      best = Best{-INFINITY, 0.f, 0x7fffffff};
-      for (int i = lane; i < parts; i += 32) {
-        const float4 x = all[i];
-        st = join(st, x.x, x.y);
-        if (kMode == kDrawn) sq = join(sq, x.z, x.w);
-        if (kMode == kGreedy) best = better(best, Best{x.z, 0.f, __float_as_int(x.w)});
-      }
-      st = warp_stat(st);
-      if (kMode == kDrawn) sq = warp_stat(sq);
-      if (kMode == kGreedy) best = warp_best(best);
-    }
-    const float inv_s = 1.f / st.S, inv_q = 1.f / sq.S;
+    float4 mine = make_float4(st.M, st.S, sq.M, sq.S);
+    if (kMode == kGreedy) mine.z = best.score, mine.w = __int_as_float(best.v);
+    mine = reduce(ex, turn, a.splits, mine,
+                  make_float4(-2.f * kLimit, 0.f, kMode == kGreedy ? -INFINITY : -2.f * kLimit, __int_as_float(kMode == kGreedy ? 0x7fffffff : 0)),
+                  [](float4 x) {
+                    const Stat t = warp_stat(Stat{x.x, x.y});
+                    if (kMode == kGreedy) {
+                      const Best r = warp_best(Best{x.z, 0.f, __float_as_int(x.w)});
+                      return make_float4(t.M, t.S, r.score, __int_as_float(r.v));
+                    }
+                    if (kMode == kGiven) return make_float4(t.M, t.S, 0.f, 0.f);
+                    const Stat q = warp_stat(Stat{x.z, x.w});
+                    return make_float4(t.M, t.S, q.M, q.S);
+                  });
+    st = Stat{mine.x, mine.y}, sq = Stat{mine.z, mine.w};
+    if (kMode == kGreedy) best = Best{mine.z, 0.f, __float_as_int(mine.w)};
+    const float inv_s = __fdividef(1.f, st.S), inv_q = __fdividef(1.f, sq.S);   // (S is in 1/2 .. 2^31)
     auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
     auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
     // A row whose logits are within the limit needs no taming of single ones but NaN.
@@ -445,11 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
                  remainder(z, q, v, k, true, r);
                  sum += r[0];
                });
-          sum = warp_sum(sum);
-          const float4* all = exchange(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f));
-          float total = 0.f;
-          for (int i = lane; i < parts; i += 32) total += all[i].x;
-          total = warp_sum(total);
+          const float total = reduce(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f),
+                                     [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); }).x;
           if (total > 0.f) {
             if (tid == 0) left_sh[k] = 1.f / total;
             __syncthreads();
@@ -459,15 +464,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
         }
         // r(x): step by step with a draft's probabilities; without, p(x) over what is left of it
         const int x = token_sh[c];
-        const float q = kMode == kDrawn ? prob_q(q_sh[c]) : 1.f;
-        float r = prob(z_sh[c]);
+        const float q = kMode == kDrawn ? prob_q(q_sh[level][c]) : 1.f;
+        float r = prob(z_sh[level][c]);
         for (int i = 0; i < k; ++i) {
           if (kMode == kDrawn) r = fmaxf(r - q, 0.f) * left_sh[i];
           else if (x == rejected_sh[i]) r = 0.f;
         }
         if (kMode == kGiven && k > 0) r *= left_sh[k - 1];
         if (uniform_sh[c] * q < r) {
-          next = c, said = x, said_z = z_sh[c];
+          next = c, said = x, said_z = z_sh[level][c];
         } else {
           __syncthreads();                   // (what was here is read)
           if (tid == 0) rejected_sh[k] = x;
@@ -476,17 +481,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
         }
       }
     }
-    const float log_s = logf(st.S);
-    auto log_p = [&](float z) { return fmaf(fmaf(z, c2, -st.M), 0.69314718f, -log_s); };
     if (next >= 0) {
-      if (writer) {
-        a.path[out + count] = next;
-        a.out_tokens[out + count - 1] = said;
-        a.logprob[out + count - 1] = log_p(said_z);
-      }
+      if (tid == 0) path_sh[count] = next, said_sh[count - 1] = said, said_z_sh[count - 1] = said_z, said_st_sh[count - 1] = st;
       ++count;
       node = next;
-      __syncthreads();                       // z_sh, q_sh and the rejections are read
       continue;
     }
     // ---- the last token
@@ -543,30 +541,41 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) verify_kernel(const
                scores(z, q, v, noise, 1);
                best = better(words, best);
              });
-        best = warp_best(best);
-        const float4* all = exchange(ex, turn, a.splits, make_float4(best.score, best.z, __int_as_float(best.v), 0.f));
-        best = Best{-INFINITY, 0.f, 0x7fffffff};
-        for (int i = lane; i < parts; i += 32) best = better(best, Best{all[i].x, all[i].y, __float_as_int(all[i].z)});
-        best = warp_best(best);
+        const float4 r = reduce(ex, turn, a.splits, make_float4(best.score, best.z, __int_as_float(best.v), 0.f),
+                                make_float4(-INFINITY, 0.f, __int_as_float(0x7fffffff), 0.f), [](float4 x) {
+                                  const Best y = warp_best(Best{x.x, x.y, __float_as_int(x.z)});
+                                  return make_float4(y.score, y.z, __int_as_float(y.v), 0.f);
+                                });
+        best = Best{r.x, r.y, __float_as_int(r.z)};
         if (!after || best.score > -INFINITY) break;
       }
       said = best.v, said_z = best.z;
       if (said == 0x7fffffff) said = 0, said_z = tame(value(target + first));   // (no number among the scores)
     }
-    if (writer) {
-      a.out_tokens[out + count - 1] = said;
-      a.logprob[out + count - 1] = log_p(said_z);
-      a.count[b] = count;
-    }
+    if (tid == 0) said_sh[count - 1] = said, said_z_sh[count - 1] = said_z, said_st_sh[count - 1] = st;
     break;
   }
   grid_dependents_launch();
+  if (split != 0) return;
+  __syncthreads();
+  if (tid < n) {
+    const bool on = tid < count;
+    a.path[out + tid] = !on ? -1 : tid == 0 ? 0 : path_sh[tid];
+    a.out_tokens[out + tid] = on ? said_sh[tid] : -1;
+    a.logprob[out + tid] = on ? fmaf(fmaf(said_z_sh[tid], c2, -said_st_sh[tid].M), 0.69314718f, -logf(said_st_sh[tid].S)) : 0.f;
+    if (tid == 0) a.count[b] = count;
+  }
 }
 
-template <typename T>
+template <typename T, int kThreads>
 const void* kernel_of(Mode m) {
-  return m == kGreedy ? (const void*)verify_kernel<T, kGreedy>
-                      : m == kGiven ? (const void*)verify_kernel<T, kGiven> : (const void*)verify_kernel<T, kDrawn>;
+  return m == kGreedy  ? (const void*)verify_kernel<T, kGreedy, kThreads>
+         : m == kGiven ? (const void*)verify_kernel<T, kGiven, kThreads>
+                       : (const void*)verify_kernel<T, kDrawn, kThreads>;
+}
+template <int kThreads>
+const void* kernel_for(int dtype, Mode m) {
+  return dtype == SBD_DTYPE_F32 ? kernel_of<float, kThreads>(m) : kernel_of<__nv_bfloat16, kThreads>(m);
 }
 
 }  // namespace
@@ -592,14 +601,20 @@ sbd_status verify_launch(const sbd_verify_desc& d, const VerifyTensors& t, float
   const float t1 = tau == 0.f ? 1.f : tau;
   a.scale = 1.4426950408889634f / t1;
   a.limit = kLimit * t1;
-  const void* fn = d.dtype == SBD_DTYPE_F32 ? kernel_of<float>(mode) : kernel_of<__nv_bfloat16>(mode);
-  // As many CTAs a request as one wave holds, 2048 logits each at least.
+  // As many CTAs a request as the SMs hold at once, 2048 logits each at least: of 256
+  // threads, or of 512 where the largest cluster leaves SMs without work.
+  const long long slots = 4ll * num_sms();
   int s = 1;
-  while (s < kMaxCluster && 2ll * s * d.batch <= (1024ll / kThreads) * num_sms() && d.vocab / (2 * s) >= 2048) s *= 2;
-  while (s > 1 && cluster_slots(fn, kThreads, 0, s) < 1) s /= 2;
+  while (s < kMaxCluster && 2ll * s * d.batch <= slots && d.vocab / (2 * s) >= 2048) s *= 2;
+  const int threads = s * d.batch <= num_sms() ? 512 : 256;
+  const void* fn = threads == 512 ? kernel_for<512>(d.dtype, mode) : kernel_for<256>(d.dtype, mode);
+  while (s > 1 && cluster_slots(fn, threads, 0, s) < 1) s /= 2;
   a.splits = s;
+  const int per = d.dtype == SBD_DTYPE_F32 ? 4 : 8;
+  a.ahead = s * d.batch <= 2 * num_sms();
+  a.slice = (int)(((long long)d.vocab + per - 1) / per + s - 1) / s;
   void* args[] = {(void*)&a};
-  return launch_pdl(fn, dim3(s, d.batch), dim3(kThreads), 0, st, args, "verify_kernel launch", s);
+  return launch_pdl(fn, dim3(s, d.batch), dim3(threads), 0, st, args, "verify_kernel launch", s);
 }
 
 }  // namespace sbd
