@@ -120,13 +120,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
-      "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
 __device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float value(const float* p) { return *p; }
 
@@ -196,7 +189,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
   constexpr int kWarps = kThreads / 32;
   using R = Row<T>;
   constexpr int kPer = R::kPer;
-  constexpr int kHold = kMode == kDrawn ? 2 : 4;       // words of a row that a thread has in flight
+  // Both rows of a level at once where a thread has few words of them, one after the other
+  // (and fewer registers and references) where it has many.
+  constexpr bool kBoth = kMode == kDrawn && kThreads == 512;
+  constexpr int kHold = kBoth ? 2 : 4;                 // words of a row that a thread has in flight
   __shared__ Exchange<kWarps> ex;
   __shared__ unsigned long long child_sh[kMaxNodes];   // of a node, a bit each
   __shared__ int token_sh[kMaxNodes];
@@ -293,13 +289,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         const bool here = w + h * kThreads < w1;
         x[h] = R::none();
         if (here) x[h] = row.load(w + h * kThreads);
-        if (use_q) {
+        if (kBoth && use_q) {
           y[h] = R::none();
           if (here) y[h] = row_q.load(w + h * kThreads);
         }
       }
       take(st, x);
-      if (use_q) take(sq, y);
+      if (kBoth && use_q) take(sq, y);
       if (kMode == kGreedy) {
         const float top = largest(x, (const T*)nullptr);
         if (top > best.score || best.v == 0x7fffffff) {  // (later ones have higher indices, and are not better if equal)
@@ -313,6 +309,17 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
                 best = better(best, Best{fmaxf(z[e], -INFINITY), 0.f, row.element(w + h * kThreads) + e});
           }
         }
+      }
+    }
+    if (!kBoth && use_q) {
+      for (int w = w0 + tid; w < w1; w += kHold * kThreads) {
+        uint4 y[kHold];
+#pragma unroll
+        for (int h = 0; h < kHold; ++h) {
+          y[h] = R::none();
+          if (w + h * kThreads < w1) y[h] = row_q.load(w + h * kThreads);
+        }
+        take(sq, y);
       }
     }
     // The first child's rows on their way to L2: the walk is likely to go there.
@@ -358,7 +365,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
     const bool tamed = (st.M >= 256.f - a.limit * c2 && st.M < a.limit * c2 - 1.f) &&
                        (!use_q || (sq.M >= 256.f - a.limit * c2 && sq.M < a.limit * c2 - 1.f));
     // What is left of p at elements v, v + 1, ... after the first k rejections (and one more,
-    // `after`), not normalised by the last ones' sum.
+    // `after`), times S and not normalised by the last ones' sum.
+    const float q_of_p = inv_q * st.S;
     auto remainder = [&](float (&z)[kPer], float (&q)[kPer], int v, int k, bool after, float (&r)[kPer]) {
       if (!tamed) {
 #pragma unroll
@@ -367,12 +375,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
 #pragma unroll
       for (int e = 0; e < kPer; e += 2) {
         float2 x = fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-st.M, -st.M));
-        x = mul2(make_float2(ex2_ftz(x.x), ex2_ftz(x.y)), make_float2(inv_s, inv_s));
-        r[e] = x.x, r[e + 1] = x.y;
+        r[e] = ex2_ftz(x.x), r[e + 1] = ex2_ftz(x.y);
         if (kMode == kDrawn) {
           x = fma2(make_float2(q[e], q[e + 1]), make_float2(c2, c2), make_float2(-sq.M, -sq.M));
-          x = mul2(make_float2(ex2_ftz(x.x), ex2_ftz(x.y)), make_float2(inv_q, inv_q));
-          q[e] = fmaxf(x.x, 0.f), q[e + 1] = fmaxf(x.y, 0.f);      // (NaN: 0)
+          q[e] = fmaxf(ex2_ftz(x.x), 0.f), q[e + 1] = fmaxf(ex2_ftz(x.y), 0.f);      // (NaN: 0)
         }
       }
       if (kMode == kDrawn) {
@@ -380,10 +386,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         for (int i = 0; i < k; ++i) {
           const float f = left_sh[i];
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) r[e] = fmaxf(r[e] - q[e], 0.f) * f;
+          for (int e = 0; e < kPer; ++e) r[e] = fmaxf(fmaf(-q_of_p, q[e], r[e]), 0.f) * f;
         }
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) r[e] = fmaxf(after ? r[e] - q[e] : r[e], 0.f);
+        for (int e = 0; e < kPer; ++e) r[e] = fmaxf(after ? fmaf(-q_of_p, q[e], r[e]) : r[e], 0.f);
       } else {
 #pragma unroll
         for (int e = 0; e < kPer; ++e) r[e] = fmaxf(r[e], 0.f);
@@ -454,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
                  sum += r[0];
                });
           const float total = reduce(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f),
-                                     [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); }).x;
+                                     [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); }).x * inv_s;
           if (total > 0.f) {
             if (tid == 0) left_sh[k] = 1.f / total;
             __syncthreads();
