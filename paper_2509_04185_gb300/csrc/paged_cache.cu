@@ -505,12 +505,12 @@ __global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8
 
 // ------------------------------------------------------ append of a path
 // The append for a tree's accepted nodes, which lie anywhere among a request's nodes: a
-// CTA has one plane of one request, at most 64 tokens, and takes its segments (formulas
-// above) one after the other, since each of them is a page's worth at most.
-// Bound: latency; the chain new_start -> slots and path -> rows and old scale -> codes,
-// then the earlier codes where the page's scale grew.
+// CTA has one plane of one request, at most 64 tokens, all of them in its registers at once.
+// Tokens have their maxima from shuffles and segments theirs from atomics in shared memory,
+// so that however many segments there are it is one chain: the starts and the path -> the
+// rows, the slots -> old scales -> codes, then earlier codes where a page's scale grew.
+// Bound: latency.
 constexpr int kPathThreads = 128;
-constexpr int kPathHold = 8;                 // units of 8 elements a thread keeps
 
 struct PathArgs {
   const void *k_new, *v_new;
@@ -526,91 +526,129 @@ struct PathArgs {
 template <typename T, int D>
 __global__ void __launch_bounds__(kPathThreads) append_path_q8_kernel(const PathArgs a) {
   constexpr int kUnits = D / 8;              // units of a row
-  constexpr int kWarps = kPathThreads / 32;
   constexpr int kStep = kPathThreads / kUnits;         // tokens of a turn
-  __shared__ int slot_sh[kMaxNodes], node_sh[kMaxNodes];
-  __shared__ float max_sh[kWarps];
+  constexpr int kHold = kMaxNodes / kStep;             // units a thread has
+  __shared__ int slot_sh[kMaxNodes];
+  __shared__ int node_sh[kMaxNodes];
+  __shared__ int begin_sh[kMaxNodes];        // of a token's segment, -1: not stored
+  __shared__ uint32_t joins_sh[2], moved_sh[2];        // tokens that go on with a segment; segments whose page's scale grew
+  __shared__ int max_sh[kMaxNodes];          // a segment's max |x| (its bits), at its beginning
+  __shared__ float scale_sh[kMaxNodes][2];   // a segment's scale before and after
   grid_dependency_wait();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x;
   const bool is_v = (int)blockIdx.x >= a.Hkv;
   const int h = is_v ? blockIdx.x - a.Hkv : blockIdx.x, b = blockIdx.y;
   const int last = (1 << a.log2P) - 1;
+  const int node = tid < a.nodes ? a.path[(size_t)b * a.nodes + tid] : -1;
   const long long from = a.new_start[b];
   const int m = (int)max(0ll, min((long long)a.nodes, a.new_start[b + 1] - from));
-  if (tid < m) {
-    const long long at = from + tid;
-    int slot = at >= 0 && at < a.max_new ? a.slot_map[at] : -1;
-    const int node = a.path[(size_t)b * a.nodes + tid];
-    if (slot >= a.n_slots) {
-      if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_PAGE);
-      slot = -1;
-    }
-    if (slot >= 0 && (uint32_t)node >= (uint32_t)a.nodes) {
-      if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_TREE);
-      slot = -1;
-    }
-    slot_sh[tid] = max(slot, -1);
-    node_sh[tid] = node;
-  }
+  uint8_t* cache = is_v ? a.v_cache : a.k_cache;
+  float* scales = is_v ? a.v_scale : a.k_scale;
+  const bool in_tree = (uint32_t)node < (uint32_t)a.nodes;
+  if (tid < kMaxNodes) node_sh[tid] = tid < m && in_tree ? node : -1;
   __syncthreads();
   const T* src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)h * D +
                  b * (is_v ? a.v_batch_stride : a.k_batch_stride) + tid % kUnits * 8;
   const long long stride = is_v ? a.v_node_stride : a.k_node_stride;
-  uint8_t* cache = is_v ? a.v_cache : a.k_cache;
-  float* scales = is_v ? a.v_scale : a.k_scale;
-  for (int j0 = 0, j1; j0 < m; j0 = j1) {
-    const int slot = slot_sh[j0];
-    j1 = j0 + 1;
-    if (slot < 0) continue;
-    while (j1 < m && slot_sh[j1] == slot + (j1 - j0) && (slot_sh[j1] & last) != 0) ++j1;
-    const int off = slot & last;
-    const long long ph = (long long)(slot >> a.log2P) * a.Hkv + h;
-    const float s_old = off > 0 ? scales[ph] : 0.f;
-    Eight<T> hold[kPathHold];
-    float amax = 0.f;
+  const int mine = tid / kUnits;             // its tokens: mine, mine + kStep, ...
+  Eight<T> hold[kHold];
 #pragma unroll
-    for (int e = 0; e < kPathHold; ++e) {
-      const int j = j0 + tid / kUnits + e * kStep;
-      if (j < j1) hold[e].load(src + node_sh[j] * stride);
+  for (int e = 0; e < kHold; ++e) {
+    const int at = node_sh[mine + e * kStep];
+    if (at >= 0) hold[e].load(src + at * stride);
+  }
+  if (tid < kMaxNodes) {
+    const long long at = from + tid;
+    int slot = tid < m && at >= 0 && at < a.max_new ? a.slot_map[at] : -1;
+    if (slot >= a.n_slots) {
+      if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_PAGE);
+      slot = -1;
+    }
+    if (slot >= 0 && !in_tree) {
+      if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_TREE);
+      slot = -1;
+    }
+    slot_sh[tid] = max(slot, -1);
+    max_sh[tid] = 0;
+  }
+  __syncthreads();
+  if (tid < kMaxNodes) {
+    const int slot = slot_sh[tid], before = tid > 0 ? slot_sh[tid - 1] : -1;
+    const uint32_t joins = __ballot_sync(0xffffffffu, slot >= 0 && before >= 0 && before + 1 == slot && (slot & last) != 0);
+    if (tid % 32 == 0) joins_sh[tid / 32] = joins;
+  }
+  __syncthreads();
+  int begin = -1;
+  if (tid < kMaxNodes) {
+    const uint64_t joins = joins_sh[0] | (uint64_t)joins_sh[1] << 32;
+    begin = 63 - __clzll(~joins & ((2ull << tid) - 1));          // (token 0 never joins)
+    if (slot_sh[tid] < 0) begin = -1;
+    begin_sh[tid] = begin;
+    if (begin == tid)
+      scale_sh[tid][0] = (slot_sh[tid] & last) ? scales[(long long)(slot_sh[tid] >> a.log2P) * a.Hkv + h] : 0.f;
+  }
+  float size[kHold];
+#pragma unroll
+  for (int e = 0; e < kHold; ++e) {
+    size[e] = 0.f;
+    if (node_sh[mine + e * kStep] >= 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) size[e] = fmaxf(size[e], finite_size(hold[e].get(i)));
     }
 #pragma unroll
-    for (int e = 0; e < kPathHold; ++e)
-      if (j0 + tid / kUnits + e * kStep < j1) {
+    for (int o = 1; o < kUnits; o *= 2) size[e] = fmaxf(size[e], __shfl_xor_sync(0xffffffffu, size[e], o));
+  }
+  __syncthreads();
+  if (tid % kUnits == 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_size(hold[e].get(i)));
-      }
-    amax = warp_max(amax);
-    if (lane == 0) max_sh[warp] = amax;
-    __syncthreads();                         // (every thread has the old scale, too)
+    for (int e = 0; e < kHold; ++e) {
+      const int j0 = begin_sh[mine + e * kStep];
+      if (j0 >= 0) atomicMax(&max_sh[j0], __float_as_int(size[e]));
+    }
+  }
+  __syncthreads();
+  if (tid < kMaxNodes) {
+    bool moved = false;
+    if (begin == tid) {
+      const float s = fmaxf(scale_sh[tid][0], scale_for(__int_as_float(max_sh[tid])));
+      scale_sh[tid][1] = s;
+      scales[(long long)(slot_sh[tid] >> a.log2P) * a.Hkv + h] = s;
+      moved = (slot_sh[tid] & last) && s != scale_sh[tid][0];
+    }
+    const uint32_t all = __ballot_sync(0xffffffffu, moved);
+    if (tid % 32 == 0) moved_sh[tid / 32] = all;
+  }
+  __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) amax = fmaxf(amax, max_sh[w]);
-    const float s = fmaxf(s_old, scale_for(amax));
-    if (tid == 0) scales[ph] = s;
-    uint8_t* dst = cache + (ph << a.log2P) * D;
+  for (int e = 0; e < kHold; ++e) {
+    const int j = mine + e * kStep, j0 = begin_sh[j];
+    if (j0 < 0) continue;
+    const float s = scale_sh[j0][1];
     // s is a power of two unless a caller's own scale is kept: then the products are exact
     const bool exact = (__float_as_uint(s) & 0x007fffffu) == 0;
     const float inv = 1.f / s;
+    float x[8];
 #pragma unroll
-    for (int e = 0; e < kPathHold; ++e) {
-      const int j = j0 + tid / kUnits + e * kStep;
-      if (j >= j1) continue;
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = exact ? hold[e].get(i) * inv : hold[e].get(i) / s;
-      *reinterpret_cast<uint2*>(dst + (off + j - j0) * D + tid % kUnits * 8) =
-          make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
-    }
-    if (off > 0 && s != s_old) {             // the page's earlier codes move to the new scale
-      const float f = s_old / s;
+    for (int i = 0; i < 8; ++i) x[i] = exact ? hold[e].get(i) * inv : hold[e].get(i) / s;
+    const int slot = slot_sh[j];
+    uint8_t* dst = cache + ((((long long)(slot >> a.log2P) * a.Hkv + h) << a.log2P) + (slot & last)) * D;
+    *reinterpret_cast<uint2*>(dst + tid % kUnits * 8) =
+        make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
+  }
+  // Pages' earlier codes move to the new scale; the segment of a page that began before
+  // is the first one, unless slots were passed over.
+#pragma unroll 1
+  for (uint64_t todo = moved_sh[0] | (uint64_t)moved_sh[1] << 32; todo; todo &= todo - 1) {
+    const int j = __ffsll(todo) - 1, off = slot_sh[j] & last;
+    const float f = scale_sh[j][0] / scale_sh[j][1];
+    uint8_t* dst = cache + (((long long)(slot_sh[j] >> a.log2P) * a.Hkv + h) << a.log2P) * D;
 #pragma unroll 4
-      for (int u = tid; u < off * D / 16; u += kPathThreads) {
-        uint4 c = *reinterpret_cast<const uint4*>(dst + 16 * u);
-        c.x = e4m3x4_times(c.x, f), c.y = e4m3x4_times(c.y, f);
-        c.z = e4m3x4_times(c.z, f), c.w = e4m3x4_times(c.w, f);
-        *reinterpret_cast<uint4*>(dst + 16 * u) = c;
-      }
+    for (int u = tid; u < off * D / 16; u += kPathThreads) {
+      uint4 c = *reinterpret_cast<const uint4*>(dst + 16 * u);
+      c.x = e4m3x4_times(c.x, f), c.y = e4m3x4_times(c.y, f);
+      c.z = e4m3x4_times(c.z, f), c.w = e4m3x4_times(c.w, f);
+      *reinterpret_cast<uint4*>(dst + 16 * u) = c;
     }
-    __syncthreads();                         // the maxima are read; the page is as the next segment finds it
   }
   grid_dependents_launch();
 }

@@ -485,10 +485,11 @@ def test_append_path_special_values_and_refusals(sbd):  # noqa: F811
         (p[b:b + 1, :1] if where is path else s[start[b]:start[b] + 1])[...] = value
         _append(sbd, x, p, start, s, codes, scale, 16, "bfloat16")
         assert sbd.sbd_device_error() == code
-    # starts out of range, or more tokens than nodes: what does not lie in the map is not stored
-    for shift in (-5, 10 ** 6, 2 ** 31 - 200):
-        _append(sbd, x, path, start + shift if shift > 0 else np.maximum(start + shift, -3), slots, codes, scale, 16, "bfloat16")
-    assert sbd.sbd_device_error() in (0, sbd.SBD_DEVERR_TREE)
+    # starts out of range, or that go down: nothing lies in the map, nothing is stored
+    for shift in (-10 ** 6, 10 ** 6, 2 ** 31 - 200):
+        _append(sbd, x, path, start + shift, slots, codes, scale, 16, "bfloat16")
+    _append(sbd, x, path, start[::-1].copy(), slots, codes, scale, 16, "bfloat16")
+    assert sbd.sbd_device_error() == 0
 
 
 def test_append_path_is_append(sbd):  # noqa: F811
