@@ -50,6 +50,18 @@ __device__ __forceinline__ float ld_rank(const float* p, int rank) {
   return v;
 }
 
+// The same of N consecutive floats.
+template <int N>
+__device__ __forceinline__ void ld_rank(const float* p, int rank, float (&v)[N]) {
+  static_assert(N == 2 || N == 4, "a load");
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  if constexpr (N == 4)
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(a) : "memory");
+  else
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(a) : "memory");
+}
+
 // Words n, n + 1, ... of four.
 __device__ __forceinline__ uint4 rotated(uint4 v, int n) {
   if (n & 1) v = make_uint4(v.y, v.z, v.w, v.x);
@@ -108,6 +120,8 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int split = blockIdx.x, hkv = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks;
   const int b = blockIdx.z;
+  Parents parents;
+  if (kTree && warp == 0) parents.load(a.parent + (size_t)b * a.k, a.k);
   const int cap = a.max_pages << a.log2P;
   int cached = a.lens[b];
   if (cached < 0 || cached > cap) {
@@ -198,11 +212,7 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
   uint32_t vis[RW], vis_min = u_end;
   int node[RW];
   if (kTree && u_end > len) {                  // (the range has block keys)
-    if (warp == 0) {
-      Parents parents;
-      parents.load(a.parent + (size_t)b * a.k, a.k);
-      block_views(views, parents, a.err);
-    }
+    if (warp == 0) block_views(views, parents, a.err);
     __syncthreads();
   }
 #pragma unroll
@@ -313,17 +323,24 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
     }
     // The rest, block keys that some row must not see: their values are
     // left out there, not multiplied by 0 (they may be infinite or NaN).
+    if (n_all < n) {
+      uint64_t seen[RW];                       // of the tile's keys, a bit each
+      const int ahead = (int)min(len - min(len, t0), 63u);   // cached ones
+#pragma unroll
+      for (int r = 0; r < RW; ++r)
+        if (kTree) seen[r] = t0 > len ? views.seen[node[r]] >> (t0 - len) : views.seen[node[r]] << ahead | ((1ull << ahead) - 1);
 #pragma unroll 1
-    for (int j = n_all; j < n; ++j) {
-      float v[kPer];
+      for (int j = n_all; j < n; ++j) {
+        float v[kPer];
 #pragma unroll
-      for (int c = 0; c < kPer; ++c) v[c] = v_s[j * D + kPer * lane + c];
+        for (int c = 0; c < kPer; ++c) v[c] = v_s[j * D + kPer * lane + c];
 #pragma unroll
-      for (int r = 0; r < RW; ++r) {
-        if (!sees(r, t0 + j)) continue;
-        const float p = pw[r * kKeys + j];
+        for (int r = 0; r < RW; ++r) {
+          if (kTree ? !(seen[r] >> j & 1) : t0 + j >= vis[r]) continue;
+          const float p = pw[r * kKeys + j];
 #pragma unroll
-        for (int c = 0; c < kPer; ++c) o[r][c] = fmaf(p, v[c], o[r][c]);
+          for (int c = 0; c < kPer; ++c) o[r][c] = fmaf(p, v[c], o[r][c]);
+        }
       }
     }
     __syncthreads();                           // the tile is consumed
@@ -369,12 +386,20 @@ __global__ void __launch_bounds__(32 * W, W == 4 ? 3 : 2) paged_fma_kernel(const
     float acc[kPer];
 #pragma unroll
     for (int c = 0; c < kPer; ++c) acc[c] = 0.f;
-#pragma unroll 4
-    for (int e = 0; e < a.splits; ++e) {
-      const float we = __shfl_sync(0xffffffffu, w, e);
+#pragma unroll 1
+    for (int e0 = 0; e0 < a.splits; e0 += 8) {  // (eight of the others' rows on their way at once)
+      float x[8][kPer];
 #pragma unroll
-      for (int c = 0; c < kPer; ++c)
-        acc[c] = fmaf(we, ld_rank(o_s + rl * D + kPer * lane + c, e), acc[c]);
+      for (int e = 0; e < 8; ++e)
+        if (e0 + e < a.splits) ld_rank(o_s + rl * D + kPer * lane, e0 + e, x[e]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float we = __shfl_sync(0xffffffffu, w, (e0 + e) & 31);
+        if (e0 + e < a.splits) {
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) acc[c] = fmaf(we, x[e][c], acc[c]);
+        }
+      }
     }
     store_row(rl, acc, lsum);
   }
