@@ -16,6 +16,8 @@
 // that the walk comes to are read.
 #include <math.h>
 
+#include <type_traits>
+
 #include "sbd_internal.cuh"
 
 namespace {
@@ -46,6 +48,12 @@ __device__ __forceinline__ float redux_max(float v) {
   float r;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
+}
+// log2 x (below 2^-126: -inf); within 2^-22, absolutely near 1.
+__device__ __forceinline__ float lg2_ftz(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 // 2^x for the whole numbers x <= 0 that references differ by (0 from -126 on).
 __device__ __forceinline__ float pow2_diff(float x) { return ex2_ftz(x); }
@@ -170,18 +178,22 @@ __device__ __forceinline__ Stat warp_stat(Stat a) {
   const float M = redux_max(a.M);
   return {M, warp_sum(a.S * pow2_diff(a.M - M))};
 }
+// The best score and where it is: the first element of its word, or an edge.  (Which element
+// of the word is looked up once, in the best one: told apart in every word it was 16 of 36
+// instructions an element.)
 struct Best {
-  float score, z;
+  float score;
   int v;
 };
-__device__ __forceinline__ Best better(Best a, Best b) {
+__device__ __forceinline__ void offer(Best& b, float score, int v) {   // (in ascending order, not NaN)
+  if (!(score <= b.score)) b.score = score, b.v = v;
+}
+__device__ __forceinline__ Best better(Best a, Best b) {   // (b may have nothing: NaN)
   return b.score > a.score || (b.score == a.score && b.v < a.v) ? b : a;
 }
 __device__ __forceinline__ Best warp_best(Best a) {
   const float top = redux_max(a.score);      // (not NaN: a NaN is never better)
-  const int v = __reduce_min_sync(0xffffffffu, a.score == top ? a.v : 0x7fffffff);
-  const uint32_t who = __ballot_sync(0xffffffffu, a.score == top && a.v == v);
-  return {top, __shfl_sync(0xffffffffu, a.z, __ffs(who) - 1), v};
+  return {top, (int)__reduce_min_sync(0xffffffffu, a.score == top ? a.v : 0x7fffffff)};
 }
 
 template <typename T, Mode kMode, int kThreads>
@@ -250,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
     }
     // ---- M and S of the row (and of the draft's, where it is asked for)
     Stat st{-2.f * kLimit, 0.f}, sq = st;
-    Best best{-INFINITY, 0.f, 0x7fffffff};
+    Best best{NAN, 0x7fffffff};
     // As they are: what is not ordinary (NaN, beyond the limit) shows in the sum or in M, and
     // the thread's share is taken again, slowly.
     auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
@@ -297,17 +309,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
       take(st, x);
       if (kBoth && use_q) take(sq, y);
       if (kMode == kGreedy) {
-        const float top = largest(x, (const T*)nullptr);
-        if (top > best.score || best.v == 0x7fffffff) {  // (later ones have higher indices, and are not better if equal)
 #pragma unroll
-          for (int h = 0; h < kHold; ++h) {
-            float z[kPer];
-            R::get(x[h], z);
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-              if (w + h * kThreads < w1)
-                best = better(best, Best{fmaxf(z[e], -INFINITY), 0.f, row.element(w + h * kThreads) + e});
-          }
+        for (int h = 0; h < kHold; ++h) {
+          const uint4 one[1] = {x[h]};
+          if (w + h * kThreads < w1) offer(best, largest(one, (const T*)nullptr), row.element(w + h * kThreads));
         }
       }
     }
@@ -340,7 +345,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
       const float z = value(target_row + edge);
       take_one(st, z);
       if (use_q) take_one(sq, value(draft_row + edge));
-      if (kMode == kGreedy) best = better(best, Best{fmaxf(z, -INFINITY), 0.f, edge});
+      if (kMode == kGreedy) best = better(Best{fmaxf(z, -INFINITY), edge}, best);
+    }
+    if (kMode == kGreedy) {
+      if (best.v == 0x7fffffff) best.score = -INFINITY;
+      const int v = best.v;
+      if (best.score == redux_max(best.score) && v >= row.element(w0) && v < row.element(w1)) {
+        for (int e = kPer - 1; e >= 0; --e)
+          if (fmaxf(value(target_row + v + e), -INFINITY) == best.score) best.v = v + e;
+      }
     }
     float4 mine = make_float4(st.M, st.S, sq.M, sq.S);
     if (kMode == kGreedy) mine.z = best.score, mine.w = __int_as_float(best.v);
@@ -349,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
                   [](float4 x) {
                     const Stat t = warp_stat(Stat{x.x, x.y});
                     if (kMode == kGreedy) {
-                      const Best r = warp_best(Best{x.z, 0.f, __float_as_int(x.w)});
+                      const Best r = warp_best(Best{x.z, __float_as_int(x.w)});
                       return make_float4(t.M, t.S, r.score, __int_as_float(r.v));
                     }
                     if (kMode == kGiven) return make_float4(t.M, t.S, 0.f, 0.f);
@@ -357,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
                     return make_float4(t.M, t.S, q.M, q.S);
                   });
     st = Stat{mine.x, mine.y}, sq = Stat{mine.z, mine.w};
-    if (kMode == kGreedy) best = Best{mine.z, 0.f, __float_as_int(mine.w)};
+    if (kMode == kGreedy) best = Best{mine.z, __float_as_int(mine.w)};
     const float inv_s = __fdividef(1.f, st.S), inv_q = __fdividef(1.f, sq.S);   // (S is in 1/2 .. 2^31)
     auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
     auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
@@ -403,17 +416,32 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         }
       }
     };
-    // The words of this CTA's slice, two in flight, as f(words of both rows, first element),
-    // and this thread's edge as f(values, element).
-    auto each = [&](bool with_q, auto&& f, auto&& f_edge) {
+    // The words of this CTA's slice, two in flight with all that belongs to them, as f(values
+    // of both rows, noise, first element, places), and this thread's edge alike.
+    auto each = [&](bool with_q, auto noisy, const float* g, auto&& f) {
+      constexpr bool kNoisy = decltype(noisy)::value;
+      // (the noise of a word is as many aligned words of four where the row is)
+      const bool aligned = kNoisy && ((long long)b * V - row.shift) % 4 == 0;
 #pragma unroll 1
       for (int w = w0 + tid; w < w1; w += 2 * kThreads) {
         uint4 x[2], y[2];
+        float noise[2][kPer];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (w + h * kThreads >= w1) continue;
           x[h] = row.load(w + h * kThreads);
           if (with_q) y[h] = row_q.load(w + h * kThreads);
+          const float* at = g + row.element(w + h * kThreads);
+          if (kNoisy && aligned) {
+#pragma unroll
+            for (int e = 0; e < kPer; e += 4) {
+              const float4 n4 = *reinterpret_cast<const float4*>(at + e);
+              noise[h][e] = n4.x, noise[h][e + 1] = n4.y, noise[h][e + 2] = n4.z, noise[h][e + 3] = n4.w;
+            }
+          } else if (kNoisy) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) noise[h][e] = at[e];
+          }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -421,16 +449,17 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
           float z[kPer], q[kPer];
           R::get(x[h], z);
           if (with_q) R::get(y[h], q);
-          f(z, q, row.element(w + h * kThreads));
+          f(z, q, noise[h], row.element(w + h * kThreads), kPer);
         }
       }
-      if (edge >= 0) {                         // the other places -inf
-        float z[kPer], q[kPer];
+      if (edge >= 0) {                         // (the other places -inf)
+        float z[kPer], q[kPer], noise[kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) z[e] = q[e] = -INFINITY;
+        for (int e = 0; e < kPer; ++e) z[e] = q[e] = noise[e] = -INFINITY;
         z[0] = value(target_row + edge);
         if (with_q) q[0] = value(draft_row + edge);
-        f_edge(z, q, edge);
+        if (kNoisy) noise[0] = g[edge];
+        f(z, q, noise, edge, 1);
       }
     };
     int next = -1, said = -1;
@@ -447,18 +476,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         if (pending) {
           // the remainder's sum, to go on with the next child
           float sum = 0.f;
-          each(kMode == kDrawn,
-               [&](float (&z)[kPer], float (&q)[kPer], int v) {
-                 float r[kPer];
-                 remainder(z, q, v, k, true, r);
+          each(kMode == kDrawn, std::false_type(), nullptr, [&](float (&z)[kPer], float (&q)[kPer], float (&)[kPer], int v, int places) {
+            float r[kPer];
+            remainder(z, q, v, k, true, r);
 #pragma unroll
-                 for (int e = 0; e < kPer; ++e) sum += r[e];
-               },
-               [&](float (&z)[kPer], float (&q)[kPer], int v) {
-                 float r[kPer];
-                 remainder(z, q, v, k, true, r);
-                 sum += r[0];
-               });
+            for (int e = 0; e < kPer; ++e) sum += e < places ? r[e] : 0.f;
+          });
           const float total = reduce(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f),
                                      [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); }).x * inv_s;
           if (total > 0.f) {
@@ -497,68 +520,63 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
     if (kMode != kGreedy) {
       // of what the last rejection leaves; where that is nothing, of what was before it
       const float* g = a.gumbel + (size_t)b * V;
-      // (the noise of a word is as many aligned words of four where the row is)
-      const bool aligned = ((long long)b * V - row.shift) % 4 == 0;
-      for (bool after = pending;; after = false) {
-        best = Best{-INFINITY, 0.f, 0x7fffffff};
-        const bool untouched = k == 0 && !after;
-        auto scores = [&](float (&z)[kPer], float (&q)[kPer], int v, const float (&noise)[kPer], int places) {
-          float s[kPer], y[kPer], top = -INFINITY;
+      bool after = pending;
+      auto evaluate = [&](float (&z)[kPer], float (&q)[kPer], float (&score)[kPer], int v) {
+        if (k == 0 && !after) {
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) y[e] = z[e];
-          if (untouched) {
+          for (int e = 0; e < kPer; ++e) score[e] = fmaf(fmaf(tame(z[e]), c2, -st.M), 0.69314718f, score[e]);
+        } else {
+          float r[kPer];
+          remainder(z, q, v, k, after, r);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) s[e] = fmaf(fmaf(tame(z[e]), c2, -st.M), 0.69314718f, noise[e]);
-          } else {
-            float r[kPer];
-            remainder(z, q, v, k, after, r);
+          for (int e = 0; e < kPer; ++e) score[e] = fmaf(lg2_ftz(r[e]), 0.69314718f, score[e]);
+        }
+      };
+      float4 r;
+      while (true) {
+        best = Best{NAN, 0x7fffffff};
+        each(kMode == kDrawn && (k > 0 || after), std::true_type(), g,
+             [&](float (&z)[kPer], float (&q)[kPer], float (&score)[kPer], int v, int places) {
+               evaluate(z, q, score, v);
+               float top = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) s[e] = __logf(r[e]) + noise[e];
-          }
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) top = e < places ? fmaxf(top, s[e]) : top;
-          if (top > best.score || (best.v == 0x7fffffff && top >= best.score)) {   // (later words have higher indices)
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-              if (e < places) best = better(best, Best{s[e], tame(y[e]), v + e});
-          }
-        };
-        each(kMode == kDrawn && !untouched,
-             [&](float (&z)[kPer], float (&q)[kPer], int v) {
-               float noise[kPer];
-               if (aligned) {
-#pragma unroll
-                 for (int e = 0; e < kPer; e += 4) {
-                   const float4 x = *reinterpret_cast<const float4*>(g + v + e);
-                   noise[e] = x.x, noise[e + 1] = x.y, noise[e + 2] = x.z, noise[e + 3] = x.w;
-                 }
-               } else {
-#pragma unroll
-                 for (int e = 0; e < kPer; ++e) noise[e] = g[v + e];
-               }
-               scores(z, q, v, noise, kPer);
-             },
-             [&](float (&z)[kPer], float (&q)[kPer], int v) {
-               float noise[kPer];
-#pragma unroll
-               for (int e = 0; e < kPer; ++e) noise[e] = g[v];
-               Best words = best;
-               best = Best{-INFINITY, 0.f, 0x7fffffff};
-               scores(z, q, v, noise, 1);
-               best = better(words, best);
+               for (int e = 0; e < kPer; ++e) top = fmaxf(top, e < places ? score[e] : -INFINITY);
+               if (places == kPer) offer(best, top, v);
+               else best = better(Best{top, v}, best);
              });
-        const float4 r = reduce(ex, turn, a.splits, make_float4(best.score, best.z, __int_as_float(best.v), 0.f),
-                                make_float4(-INFINITY, 0.f, __int_as_float(0x7fffffff), 0.f), [](float4 x) {
-                                  const Best y = warp_best(Best{x.x, x.y, __float_as_int(x.z)});
-                                  return make_float4(y.score, y.z, __int_as_float(y.v), 0.f);
-                                });
-        best = Best{r.x, r.y, __float_as_int(r.z)};
-        if (!after || best.score > -INFINITY) break;
+        if (best.v == 0x7fffffff) best.score = -INFINITY;
+        r = reduce(ex, turn, a.splits, make_float4(best.score, __int_as_float(best.v), 0.f, 0.f),
+                   make_float4(-INFINITY, __int_as_float(0x7fffffff), 0.f, 0.f), [](float4 x) {
+                     const Best y = warp_best(Best{x.x, __float_as_int(x.y)});
+                     return make_float4(y.score, __int_as_float(y.v), 0.f, 0.f);
+                   });
+        if (!after || r.x > -INFINITY) break;
+        after = false;
       }
-      said = best.v, said_z = best.z;
-      if (said == 0x7fffffff) said = 0, said_z = tame(value(target + first));   // (no number among the scores)
+      // The thread whose word it is finds the element and tells it.
+      if (best.v == __float_as_int(r.y)) {
+        const int v = best.v;
+        said = v, said_z = value(target_row + v);
+        if (v >= row.element(w0) && v < row.element(w1)) {
+          float z[kPer], q[kPer], score[kPer];
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) {
+            z[e] = value(target_row + v + e);
+            if (kMode == kDrawn && (k > 0 || after)) q[e] = value(draft_row + v + e);
+            score[e] = g[v + e];
+          }
+          evaluate(z, q, score, v);
+          for (int e = kPer - 1; e >= 0; --e)
+            if (fmaxf(score[e], -INFINITY) == best.score) said = v + e;
+          said_z = value(target_row + said);
+        }
+        a.out_tokens[out + count - 1] = said;
+        a.logprob[out + count - 1] = fmaf(fmaf(tame(said_z), c2, -st.M), 0.69314718f, -logf(st.S));
+      }
     }
-    if (tid == 0) said_sh[count - 1] = said, said_z_sh[count - 1] = said_z, said_st_sh[count - 1] = st;
+    else if (tid == 0) {
+      said_sh[count - 1] = said, said_z_sh[count - 1] = said_z, said_st_sh[count - 1] = st;
+    }
     break;
   }
   grid_dependents_launch();
@@ -567,8 +585,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
   if (tid < n) {
     const bool on = tid < count;
     a.path[out + tid] = !on ? -1 : tid == 0 ? 0 : path_sh[tid];
-    a.out_tokens[out + tid] = on ? said_sh[tid] : -1;
-    a.logprob[out + tid] = on ? fmaf(fmaf(said_z_sh[tid], c2, -said_st_sh[tid].M), 0.69314718f, -logf(said_st_sh[tid].S)) : 0.f;
+    if (kMode == kGreedy || tid != count - 1) {          // (the last token is told already)
+      a.out_tokens[out + tid] = on ? said_sh[tid] : -1;
+      a.logprob[out + tid] = on ? fmaf(fmaf(said_z_sh[tid], c2, -said_st_sh[tid].M), 0.69314718f, -logf(said_st_sh[tid].S)) : 0.f;
+    }
     if (tid == 0) a.count[b] = count;
   }
 }
