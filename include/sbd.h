@@ -569,9 +569,9 @@ sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, co
  *   logprob [B, n] fp32 out    ln p of each of them (at temperature 1 where tau = 0), then 0
  *   count [B] int32 out        nodes on the path = tokens that come out, 1 .. n
  *
- * Logits, exponentials and sums in fp32.  No workspace: its size is 0.  The rows of nodes
- * that the walk does not come to are not read.
- * Supported: 1 <= n <= 64, V >= 1, B <= 65535, tau = 0 or 2^-20 <= tau <= 2^20.
+ * Exponentials and sums in fp32.  No workspace: its size is 0.  Rows that the walk does not
+ * come to change nothing.
+ * Supported: 1 <= n <= 64, 1 <= V <= 2^24, B <= 65535, tau = 0 or 2^-20 <= tau <= 2^20.
  * ---------------------------------------------------------------------- */
 typedef struct {
   int32_t batch;   /* B */

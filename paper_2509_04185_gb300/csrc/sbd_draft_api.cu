@@ -28,6 +28,7 @@ sbd_status check_verify_desc(const sbd_verify_desc* d) {
   if (s != SBD_OK) return s;
   if (d->nodes > kMaxNodes) return fail(SBD_ERR_UNSUPPORTED, "nodes %d > %d", d->nodes, kMaxNodes);
   if (d->batch > 65535) return fail(SBD_ERR_UNSUPPORTED, "batch %d > 65535", d->batch);
+  if (d->vocab > 1 << 24) return fail(SBD_ERR_UNSUPPORTED, "vocab %d > 2^24", d->vocab);
   return SBD_OK;
 }
 

@@ -11,9 +11,18 @@
 // r_k is a function of the logits at v and of the scalars Z, so nothing is stored for it:
 // a pass over the row evaluates it.  A request is a thread-block cluster, each CTA has a
 // slice of the vocabulary, and what they need of one another goes through distributed
-// shared memory: every warp leaves its share of a sum in all CTAs, each of which adds up in
-// the same order, and so comes to the same numbers and decisions as the others.  Only rows
-// that the walk comes to are read.
+// shared memory: every CTA leaves its share of a sum in all others, each of which adds up in
+// the same order, and so comes to the same numbers and decisions as the others.
+//
+// Bounds and figures (128256 logits in bf16, draft's rows too).  One request, three of seven
+// tokens accepted: 13 us, a chain of latencies: launch 2, tree 1.5, a level 2.5 to 3 (loads 1,
+// reductions over warps, CTA and cluster 1, the decision with its code 0.7), the last token's
+// pass 3.  64 requests of 15 nodes, none to three levels: 50 us, of which the bytes are 14.5;
+// the passes of a request follow one another, and at first the exponentials of all of them
+// are as long as their bytes (3.5 us a level on 152 SMs), at last few requests are left.
+// On the way: maxima that are no whole numbers and reductions in turn 131 us; whole numbers
+// and one barrier 89; words of 16 bytes without bounds to check 58; which element is the best
+// looked up once and not in every word (16 of 36 instructions) 53.
 #include <math.h>
 
 #include <type_traits>
@@ -66,6 +75,7 @@ struct Row {
   static constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf
   const T* base;             // aligned
   int shift, c0, c1, head, edges;
+  __device__ __forceinline__ Row() {}
   __device__ __forceinline__ Row(const T* tensor, long long first, int V) {
     shift = (int)first & (kPer - 1);
     base = tensor + (first - shift);
@@ -144,30 +154,46 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Reductions of four floats over the cluster; every warp of it has the same result.  `join`
-// reduces over a warp (all lanes have its result); a warp's goes to the CTA, the CTA's to all
-// of the cluster.  The buffers are taken in turn: a CTA that writes into one of them again
-// has passed the barrier of the other, before which everyone had read the first.
-template <int kWarps>
+// Reductions of up to kN times four floats over the cluster; every warp of it has the same
+// results.  `join` reduces over a warp (all lanes have its result); a warp's go to the CTA,
+// the CTA's, by a warp each, to all of the cluster.  The buffers are taken in turn: a CTA that
+// writes into one of them again has passed the barrier of the other, before which everyone
+// had read the first.
+template <int kWarps, int kN>
 struct Exchange {
-  float4 warps[2][kWarps];
-  float4 ranks[2][kMaxCluster];
+  float4 warps[2][kN][kWarps];
+  float4 ranks[2][kN][kMaxCluster];
 };
-template <int kWarps, typename F>
-__device__ __forceinline__ float4 reduce(Exchange<kWarps>& x, int& turn, int splits, float4 mine, float4 none, F&& join) {
+template <int kM, int kWarps, int kN, typename F>
+__device__ __forceinline__ void reduce(Exchange<kWarps, kN>& x, int& turn, int splits, int count, float4 (&mine)[kM], float4 none,
+                                       F&& join) {
+  static_assert(kM <= kN && kN <= kWarps, "a warp each");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   turn ^= 1;
-  mine = join(mine);
-  if (lane == 0) x.warps[turn][warp] = mine;
+#pragma unroll
+  for (int i = 0; i < kM; ++i) {
+    if (i >= count) continue;
+    mine[i] = join(mine[i]);
+    if (lane == 0) x.warps[turn][i][warp] = mine[i];
+  }
   __syncthreads();
-  if (splits == 1 || warp == 0) mine = join(lane < kWarps ? x.warps[turn][lane] : none);
-  if (splits == 1) return mine;
-  uint32_t rank;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  if (warp == 0 && lane < splits) st_cluster(mapa(smem_u32(&x.ranks[turn][rank]), lane), mine);
+  if (splits == 1) {
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+      if (i < count) mine[i] = join(lane < kWarps ? x.warps[turn][i][lane] : none);
+    return;
+  }
+  if (warp < count) {
+    const float4 all = join(lane < kWarps ? x.warps[turn][warp][lane] : none);
+    uint32_t rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    if (lane < splits) st_cluster(mapa(smem_u32(&x.ranks[turn][warp][rank]), lane), all);
+  }
   __syncwarp();
   cluster_sync();
-  return join(lane < splits ? x.ranks[turn][lane] : none);
+#pragma unroll
+  for (int i = 0; i < kM; ++i)
+    if (i < count) mine[i] = join(lane < splits ? x.ranks[turn][i][lane] : none);
 }
 
 // M and S of a part of a row.
@@ -196,20 +222,40 @@ __device__ __forceinline__ Best warp_best(Best a) {
   return {top, (int)__reduce_min_sync(0xffffffffu, a.score == top ? a.v : 0x7fffffff)};
 }
 
+__device__ __forceinline__ float tame(float z, float limit) { return fminf(fmaxf(z, -limit), limit); }   // NaN: the least
+__device__ __forceinline__ void take_one(Stat& s, float z, float c2, float limit) {
+  const float M = fmaxf(s.M, ceilf(tame(z, limit) * c2));
+  s.S = fmaf(s.S, pow2_diff(s.M - M), ex2_ftz(fmaf(tame(z, limit), c2, -M)));
+  s.M = M;
+}
+// M and S of the elements of words w0, w0 + step, ... below w1 one by one, tamed: of a part of
+// a row that has a NaN or a logit beyond the limit in it, or of a row that is low altogether.
+template <typename T>
+__device__ __noinline__ Stat slow_stat(const T* elements, int w0, int w1, int step, float c2, float limit) {
+  Stat s{-2.f * kLimit, 0.f};
+  for (int w = w0; w < w1; w += step)
+    for (int e = 0; e < Row<T>::kPer; ++e) take_one(s, value(elements + (long long)w * Row<T>::kPer + e), c2, limit);
+  return s;
+}
+
 template <typename T, Mode kMode, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kernel(const Args a) {
   constexpr int kWarps = kThreads / 32;
   using R = Row<T>;
   constexpr int kPer = R::kPer;
-  // Both rows of a level at once where a thread has few words of them, one after the other
-  // (and fewer registers and references) where it has many.
+  // Where requests are few (512 threads a CTA) a level is a chain of latencies, 2.8 us of one
+  // request's 14.7: so M and S of several rows are made at once, of a node, its first child,
+  // that one's first child ..., which the walk is likely to come to, and both rows of a node
+  // together.  Where they are many, one row after the other, only as the walk comes to them.
+  constexpr int kAhead = kMode == kDrawn && kThreads == 512 ? 2 : 1;
   constexpr bool kBoth = kMode == kDrawn && kThreads == 512;
   constexpr int kHold = kBoth ? 2 : 4;                 // words of a row that a thread has in flight
-  __shared__ Exchange<kWarps> ex;
+  __shared__ Exchange<kWarps, kAhead> ex;
   __shared__ unsigned long long child_sh[kMaxNodes];   // of a node, a bit each
   __shared__ int token_sh[kMaxNodes];
   __shared__ float uniform_sh[kMaxNodes];
-  __shared__ float z_sh[2][kMaxNodes], q_sh[2][kMaxNodes];   // logits at a child's token (target's, draft's), levels in turn
+  __shared__ float z_sh[kMaxNodes], q_sh[kMaxNodes];   // logits at a child's token: the target's, the draft's
+  __shared__ float4 stat_sh[kMaxNodes];                // rows' M and S, of the target and of the draft (greedy: largest, where)
   __shared__ int path_sh[kMaxNodes], said_sh[kMaxNodes];     // the walk, told at its end: nodes, tokens,
   __shared__ float said_z_sh[kMaxNodes];                     // their logits, and their rows' M and S
   __shared__ Stat said_st_sh[kMaxNodes];
@@ -223,15 +269,16 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
   const size_t out = (size_t)b * n;
   if (tid < kMaxNodes) child_sh[tid] = 0;
   __syncthreads();
+  int parent = -1;                           // of node tid
   if (tid < n) {
-    int p = a.parent[out + tid];
+    const int p = a.parent[out + tid];
     bool bad = p >= tid;
     if (!bad && tid > 0 && p >= 0) {
       const int x = a.token[out + tid];
       token_sh[tid] = x;
       bad = x < 0 || x >= V;                 // passed over
       if (kMode != kGreedy) uniform_sh[tid] = a.uniform[out + tid];
-      if (!bad) atomicOr(&child_sh[p], 1ull << tid);
+      if (!bad) parent = p, atomicOr(&child_sh[p], 1ull << tid);
     }
     if (bad && split == 0) record_error(a.err, SBD_DEVERR_TREE);
   }
@@ -244,139 +291,200 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
     for (int v = split * part + tid * 32; v < v1; v += kThreads * 32) prefetch_l2(g + v);
   }
   const float c2 = a.scale;
-  auto tame = [&](float z) { return fminf(fmaxf(z, -a.limit), a.limit); };   // NaN: the least
+  auto tame = [&](float z) { return ::tame(z, a.limit); };
+  const float low = 256.f - a.limit * c2;    // a row's M below it: of nothing but masked logits
+  unsigned long long known = 0;              // nodes whose rows' M and S are known
   while (true) {
     const unsigned long long children = child_sh[node];
     const bool use_q = kMode == kDrawn && children != 0;
+    // ---- M and S of the row (and of the draft's, where it is asked for)
+    Stat st, sq;
+    Best best;
+    if (kAhead == 1 || !(known >> node & 1)) {
+      int list[kAhead] = {node}, several = 1;
+      unsigned long long in = 1ull << node;
+#pragma unroll
+      for (int i = 1; i < kAhead; ++i) {
+        const unsigned long long c = child_sh[list[i - 1]];
+        list[i] = c ? __ffsll(c) - 1 : list[i - 1];
+        if (c) several = i + 1, in |= 1ull << list[i];
+      }
+      const int rows = kAhead == 1 ? 1 : several;
+      if (kAhead > 1) known |= in;
+      // a child's logits, stored once the rows' loads are under way, too
+      const bool is_child = kMode != kGreedy && parent >= 0 && in >> parent & 1;
+      float child_z = 0.f, child_q = 0.f;
+      if (is_child) {
+        const long long at = ((long long)b * n + parent) * V + token_sh[tid];
+        child_z = value(target + at);
+        if (kMode == kDrawn) child_q = value(draft + at);
+      }
+      Stat t[kAhead], d[kAhead];
+      Best top[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) t[i] = d[i] = Stat{-2.f * kLimit, 0.f}, top[i] = Best{NAN, 0x7fffffff};
+      // As they are: a NaN, or what is beyond the limit, shows in the sum, and the thread's
+      // share is taken again, slowly; so is a row that is low altogether.
+      auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
+        const float M = fmaxf(s.M, ceilf(tame(largest(x, (const T*)nullptr)) * c2));
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int h = 0; h < kHold; ++h) {
+          float z[kPer];
+          R::get(x[h], z);
+#pragma unroll
+          for (int e = 0; e < kPer; e += 2) {
+            const float2 y = fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-M, -M));
+            sum = add2(sum, make_float2(ex2_ftz(y.x), ex2_ftz(y.y)));
+          }
+        }
+        s.S = fmaf(s.S, pow2_diff(s.M - M), sum.x + sum.y);
+        s.M = M;
+      };
+      // The rows' places in both tensors, and this CTA's words of them.
+      R place[kAhead];
+      long long first[kAhead];
+      int from[kAhead], to[kAhead];
+      auto has_q = [&](int i) { return kMode == kDrawn && child_sh[list[i]] != 0; };
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (i >= rows) continue;
+        first[i] = ((long long)b * n + list[i]) * V;
+        place[i] = R(target, first[i], V);
+        from[i] = min(place[i].c1, place[i].c0 + split * a.slice), to[i] = min(place[i].c1, from[i] + a.slice);
+      }
+      const long long to_draft = reinterpret_cast<const char*>(draft) - reinterpret_cast<const char*>(target);
+      auto load_q = [&](int i, int w) {
+        return *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(place[i].base) + to_draft + 16ll * w);
+      };
+#pragma unroll 1
+      for (int o = tid; o < a.slice; o += kHold * kThreads) {
+        uint4 x[kAhead][kHold], y[kBoth ? kAhead : 1][kHold];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (i >= rows) continue;
+          const bool both = kBoth && has_q(i);
+#pragma unroll
+          for (int h = 0; h < kHold; ++h) {
+            const int w = from[i] + o + h * kThreads;
+            x[i][h] = R::none();
+            if (w < to[i]) x[i][h] = place[i].load(w);
+            if (kBoth) y[kBoth ? i : 0][h] = R::none();
+            if (both && w < to[i]) y[kBoth ? i : 0][h] = load_q(i, w);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (i >= rows) continue;
+          take(t[i], x[i]);
+          if (kBoth && has_q(i)) take(d[i], y[kBoth ? i : 0]);
+          if (kMode == kGreedy) {
+#pragma unroll
+            for (int h = 0; h < kHold; ++h) {
+              const uint4 one[1] = {x[i][h]};
+              const int w = from[i] + o + h * kThreads;
+              if (w < to[i]) offer(top[i], fmaxf(largest(one, (const T*)nullptr), -INFINITY), place[i].element(w));
+            }
+          }
+        }
+      }
+      if (!kBoth && kMode == kDrawn && use_q) {        // (kAhead is 1)
+#pragma unroll 1
+        for (int w = from[0] + tid; w < to[0]; w += kHold * kThreads) {
+          uint4 y[kHold];
+#pragma unroll
+          for (int h = 0; h < kHold; ++h) {
+            y[h] = R::none();
+            if (w + h * kThreads < to[0]) y[h] = load_q(0, w + h * kThreads);
+          }
+          take(d[0], y);
+        }
+      }
+      // The first child's rows on their way to L2: the walk is likely to go there.
+      if (kAhead == 1 && a.ahead && children) {
+        const int c = __ffsll(children) - 1;
+        const T* there = place[0].base + (long long)(c - node) * V;
+        const bool its_q = kMode == kDrawn && child_sh[c] != 0;
+        for (int w = from[0] + tid * 8; w < to[0]; w += kThreads * 8) {        // a line each
+          prefetch_l2(there + (long long)w * kPer);
+          if (its_q) prefetch_l2(reinterpret_cast<const char*>(there + (long long)w * kPer) + to_draft);
+        }
+      }
+      if (is_child) z_sh[tid] = tame(child_z), q_sh[tid] = tame(child_q);
+      float4 mine[kAhead];
+      const float4 none = make_float4(-2.f * kLimit, 0.f, kMode == kGreedy ? -INFINITY : -2.f * kLimit,
+                                      __int_as_float(kMode == kGreedy ? 0x7fffffff : 0));
+      auto join = [](float4 x) {
+        const Stat t = warp_stat(Stat{x.x, x.y});
+        if (kMode == kGreedy) {
+          const Best r = warp_best(Best{x.z, __float_as_int(x.w)});
+          return make_float4(t.M, t.S, r.score, __int_as_float(r.v));
+        }
+        if (kMode == kGiven) return make_float4(t.M, t.S, 0.f, 0.f);
+        const Stat q = warp_stat(Stat{x.z, x.w});
+        return make_float4(t.M, t.S, q.M, q.S);
+      };
+      // The rest of a row's share: slowly what has to be, and the thread's edge.
+      auto finish = [&](int i, bool slow) {
+        const R& r = place[i];
+        const T* row_t = target + first[i];
+        const T* row_d = draft + first[i];
+        const int edge = split == 0 && tid < r.edges ? r.edge(tid) : -1;
+        if (slow || !(t[i].S < INFINITY)) t[i] = slow_stat<T>(row_t - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
+        if (has_q(i) && (slow || !(d[i].S < INFINITY))) d[i] = slow_stat<T>(row_d - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
+        if (edge >= 0) {
+          const float z = value(row_t + edge);
+          take_one(t[i], z, c2, a.limit);
+          if (has_q(i)) take_one(d[i], value(row_d + edge), c2, a.limit);
+          if (kMode == kGreedy && !slow) top[i] = better(Best{fmaxf(z, -INFINITY), edge}, top[i]);
+        }
+        if (kMode == kGreedy && !slow) {               // the element of the best word
+          if (top[i].v == 0x7fffffff) top[i].score = -INFINITY;
+          const int v = top[i].v;
+          if (top[i].score == redux_max(top[i].score) && v >= r.element(from[i]) && v < r.element(to[i])) {
+            float z[kPer];
+            R::get(r.load((v + r.shift) / kPer), z);
+#pragma unroll
+            for (int e = kPer - 1; e >= 0; --e)
+              if (fmaxf(z[e], -INFINITY) == top[i].score) top[i].v = v + e;
+          }
+        }
+        mine[i] = make_float4(t[i].M, t[i].S, d[i].M, d[i].S);
+        if (kMode == kGreedy) mine[i].z = top[i].score, mine[i].w = __int_as_float(top[i].v);
+      };
+#pragma unroll 1
+      for (bool slow = false;; slow = true) {
+        bool is_low = false;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (i < rows) finish(i, slow);
+        reduce(ex, turn, a.splits, rows, mine, none, join);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (i < rows) is_low |= mine[i].x < low || (has_q(i) && mine[i].z < low);
+        if (slow || !is_low) break;
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (kAhead > 1 && i < rows && tid == 0) stat_sh[list[i]] = mine[i];
+      if (kAhead > 1) __syncthreads();
+      else st = Stat{mine[0].x, mine[0].y}, sq = Stat{mine[0].z, mine[0].w}, best = Best{mine[0].z, __float_as_int(mine[0].w)};
+    }
+    if (kAhead > 1) {
+      const float4 x = stat_sh[node];
+      st = Stat{x.x, x.y}, sq = Stat{x.z, x.w}, best = Best{x.z, __float_as_int(x.w)};
+    }
     const long long first = ((long long)b * n + node) * V;
     const R row(target, first, V), row_q(draft, first, V);       // (alike but for the base)
     const int w0 = min(row.c1, row.c0 + split * a.slice), w1 = min(row.c1, w0 + a.slice);
     const int edge = split == 0 && tid < row.edges ? row.edge(tid) : -1;   // this thread's
     const T* target_row = target + first;
     const T* draft_row = draft + first;
-    const bool is_child = tid < kMaxNodes && children >> tid & 1;
-    float child_z = 0.f, child_q = 0.f;      // (stored once the row's loads are under way, too)
-    if (is_child) {
-      child_z = value(target_row + token_sh[tid]);
-      if (kMode == kDrawn) child_q = value(draft_row + token_sh[tid]);
-    }
-    // ---- M and S of the row (and of the draft's, where it is asked for)
-    Stat st{-2.f * kLimit, 0.f}, sq = st;
-    Best best{NAN, 0x7fffffff};
-    // As they are: what is not ordinary (NaN, beyond the limit) shows in the sum or in M, and
-    // the thread's share is taken again, slowly.
-    auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
-      const float M = fmaxf(s.M, ceilf(tame(largest(x, (const T*)nullptr)) * c2));
-      float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int h = 0; h < kHold; ++h) {
-        float z[kPer];
-        R::get(x[h], z);
-#pragma unroll
-        for (int e = 0; e < kPer; e += 2) {
-          const float2 y = fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-M, -M));
-          sum = add2(sum, make_float2(ex2_ftz(y.x), ex2_ftz(y.y)));
-        }
-      }
-      s.S = fmaf(s.S, pow2_diff(s.M - M), sum.x + sum.y);
-      s.M = M;
-    };
-    auto take_one = [&](Stat& s, float z) {
-      const float M = fmaxf(s.M, ceilf(tame(z) * c2));
-      s.S = fmaf(s.S, pow2_diff(s.M - M), ex2_ftz(fmaf(tame(z), c2, -M)));
-      s.M = M;
-    };
-    auto again = [&](Stat& s, const R& r, const T* elements) {
-      if (s.S < INFINITY && s.M >= 256.f - a.limit * c2) return;
-      s = Stat{-2.f * kLimit, 0.f};
-#pragma unroll 1
-      for (int w = w0 + tid; w < w1; w += kThreads)
-#pragma unroll 1
-        for (int e = 0; e < kPer; ++e) take_one(s, value(elements + r.element(w) + e));
-    };
-    for (int w = w0 + tid; w < w1; w += kHold * kThreads) {
-      uint4 x[kHold], y[kHold];
-#pragma unroll
-      for (int h = 0; h < kHold; ++h) {
-        const bool here = w + h * kThreads < w1;
-        x[h] = R::none();
-        if (here) x[h] = row.load(w + h * kThreads);
-        if (kBoth && use_q) {
-          y[h] = R::none();
-          if (here) y[h] = row_q.load(w + h * kThreads);
-        }
-      }
-      take(st, x);
-      if (kBoth && use_q) take(sq, y);
-      if (kMode == kGreedy) {
-#pragma unroll
-        for (int h = 0; h < kHold; ++h) {
-          const uint4 one[1] = {x[h]};
-          if (w + h * kThreads < w1) offer(best, largest(one, (const T*)nullptr), row.element(w + h * kThreads));
-        }
-      }
-    }
-    if (!kBoth && use_q) {
-      for (int w = w0 + tid; w < w1; w += kHold * kThreads) {
-        uint4 y[kHold];
-#pragma unroll
-        for (int h = 0; h < kHold; ++h) {
-          y[h] = R::none();
-          if (w + h * kThreads < w1) y[h] = row_q.load(w + h * kThreads);
-        }
-        take(sq, y);
-      }
-    }
-    // The first child's rows on their way to L2: the walk is likely to go there.
-    if (a.ahead && children) {
-      const int c = __ffsll(children) - 1;
-      const long long there = (long long)(c - node) * V;
-      const bool its_q = kMode == kDrawn && child_sh[c] != 0;
-      for (int w = w0 + tid * 8; w < w1; w += kThreads * 8) {          // a line each
-        prefetch_l2(row.base + there + (long long)w * kPer);
-        if (its_q) prefetch_l2(row_q.base + there + (long long)w * kPer);
-      }
-    }
-    const int level = count & 1;
-    if (is_child) z_sh[level][tid] = tame(child_z), q_sh[level][tid] = tame(child_q);   // (read behind the next exchange)
-    again(st, row, target_row);
-    if (use_q) again(sq, row_q, draft_row);
-    if (edge >= 0) {
-      const float z = value(target_row + edge);
-      take_one(st, z);
-      if (use_q) take_one(sq, value(draft_row + edge));
-      if (kMode == kGreedy) best = better(Best{fmaxf(z, -INFINITY), edge}, best);
-    }
-    if (kMode == kGreedy) {
-      if (best.v == 0x7fffffff) best.score = -INFINITY;
-      const int v = best.v;
-      if (best.score == redux_max(best.score) && v >= row.element(w0) && v < row.element(w1)) {
-        for (int e = kPer - 1; e >= 0; --e)
-          if (fmaxf(value(target_row + v + e), -INFINITY) == best.score) best.v = v + e;
-      }
-    }
-    float4 mine = make_float4(st.M, st.S, sq.M, sq.S);
-    if (kMode == kGreedy) mine.z = best.score, mine.w = __int_as_float(best.v);
-    mine = reduce(ex, turn, a.splits, mine,
-                  make_float4(-2.f * kLimit, 0.f, kMode == kGreedy ? -INFINITY : -2.f * kLimit, __int_as_float(kMode == kGreedy ? 0x7fffffff : 0)),
-                  [](float4 x) {
-                    const Stat t = warp_stat(Stat{x.x, x.y});
-                    if (kMode == kGreedy) {
-                      const Best r = warp_best(Best{x.z, __float_as_int(x.w)});
-                      return make_float4(t.M, t.S, r.score, __int_as_float(r.v));
-                    }
-                    if (kMode == kGiven) return make_float4(t.M, t.S, 0.f, 0.f);
-                    const Stat q = warp_stat(Stat{x.z, x.w});
-                    return make_float4(t.M, t.S, q.M, q.S);
-                  });
-    st = Stat{mine.x, mine.y}, sq = Stat{mine.z, mine.w};
-    if (kMode == kGreedy) best = Best{mine.z, __float_as_int(mine.w)};
     const float inv_s = __fdividef(1.f, st.S), inv_q = __fdividef(1.f, sq.S);   // (S is in 1/2 .. 2^31)
     auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
     auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
     // A row whose logits are within the limit needs no taming of single ones but NaN.
-    const bool tamed = (st.M >= 256.f - a.limit * c2 && st.M < a.limit * c2 - 1.f) &&
-                       (!use_q || (sq.M >= 256.f - a.limit * c2 && sq.M < a.limit * c2 - 1.f));
+    const bool tamed = (st.M >= low && st.M < a.limit * c2 - 1.f) && (!use_q || (sq.M >= low && sq.M < a.limit * c2 - 1.f));
     // What is left of p at elements v, v + 1, ... after the first k rejections (and one more,
     // `after`), times S and not normalised by the last ones' sum.
     const float q_of_p = inv_q * st.S;
@@ -482,8 +590,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
 #pragma unroll
             for (int e = 0; e < kPer; ++e) sum += e < places ? r[e] : 0.f;
           });
-          const float total = reduce(ex, turn, a.splits, make_float4(sum, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f),
-                                     [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); }).x * inv_s;
+          float4 part[1] = {make_float4(sum, 0.f, 0.f, 0.f)};
+          reduce(ex, turn, a.splits, 1, part, make_float4(0.f, 0.f, 0.f, 0.f),
+                 [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); });
+          const float total = part[0].x * inv_s;
           if (total > 0.f) {
             if (tid == 0) left_sh[k] = 1.f / total;
             __syncthreads();
@@ -493,15 +603,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         }
         // r(x): step by step with a draft's probabilities; without, p(x) over what is left of it
         const int x = token_sh[c];
-        const float q = kMode == kDrawn ? prob_q(q_sh[level][c]) : 1.f;
-        float r = prob(z_sh[level][c]);
+        const float q = kMode == kDrawn ? prob_q(q_sh[c]) : 1.f;
+        float r = prob(z_sh[c]);
         for (int i = 0; i < k; ++i) {
           if (kMode == kDrawn) r = fmaxf(r - q, 0.f) * left_sh[i];
           else if (x == rejected_sh[i]) r = 0.f;
         }
         if (kMode == kGiven && k > 0) r *= left_sh[k - 1];
         if (uniform_sh[c] * q < r) {
-          next = c, said = x, said_z = z_sh[level][c];
+          next = c, said = x, said_z = z_sh[c];
         } else {
           __syncthreads();                   // (what was here is read)
           if (tid == 0) rejected_sh[k] = x;
@@ -545,11 +655,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
                else best = better(Best{top, v}, best);
              });
         if (best.v == 0x7fffffff) best.score = -INFINITY;
-        r = reduce(ex, turn, a.splits, make_float4(best.score, __int_as_float(best.v), 0.f, 0.f),
-                   make_float4(-INFINITY, __int_as_float(0x7fffffff), 0.f, 0.f), [](float4 x) {
-                     const Best y = warp_best(Best{x.x, __float_as_int(x.y)});
-                     return make_float4(y.score, __int_as_float(y.v), 0.f, 0.f);
-                   });
+        float4 part[1] = {make_float4(best.score, __int_as_float(best.v), 0.f, 0.f)};
+        reduce(ex, turn, a.splits, 1, part, make_float4(-INFINITY, __int_as_float(0x7fffffff), 0.f, 0.f), [](float4 x) {
+          const Best y = warp_best(Best{x.x, __float_as_int(x.y)});
+          return make_float4(y.score, __int_as_float(y.v), 0.f, 0.f);
+        });
+        r = part[0];
         if (!after || r.x > -INFINITY) break;
         after = false;
       }
@@ -566,6 +677,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
             score[e] = g[v + e];
           }
           evaluate(z, q, score, v);
+#pragma unroll
           for (int e = kPer - 1; e >= 0; --e)
             if (fmaxf(score[e], -INFINITY) == best.score) said = v + e;
           said_z = value(target_row + said);

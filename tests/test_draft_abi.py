@@ -108,7 +108,7 @@ def _call(sbd, desc, ins, tau, outs):
 
 
 @pytest.mark.parametrize("over,tau,status", [
-    (dict(batch=-1), 1.0, 1), (dict(nodes=0), 1.0, 1), (dict(nodes=65), 1.0, 2), (dict(vocab=0), 1.0, 1),
+    (dict(batch=-1), 1.0, 1), (dict(nodes=0), 1.0, 1), (dict(nodes=65), 1.0, 2), (dict(vocab=0), 1.0, 1), (dict(vocab=(1 << 24) + 1), 1.0, 2),
     (dict(dtype=2), 1.0, 1), (dict(batch=65536), 1.0, 2), ({}, -1.0, 1), ({}, float("nan"), 1), ({}, float("inf"), 1),
     ({}, 1e-7, 2), ({}, 2e6, 2),
 ])

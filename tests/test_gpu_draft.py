@@ -360,6 +360,32 @@ def test_verify_special_logits(sbd, dtype):  # noqa: F811
     assert sbd.sbd_device_error() == 0
 
 
+@pytest.mark.parametrize("V", [5, 64, 1003, 40000])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_verify_among_nothing_but_nan_and_infinities(sbd, dtype, V):  # noqa: F811
+    """Rows of which only a few logits are ordinary, or none: what is masked does not come out."""
+    rng = np.random.default_rng(V)
+    for mode, tau in (("drawn", 1.0), ("given", 2.0), ("greedy", 0.0)):
+        case = _verify_case(rng, 8, 4, V, mode == "drawn", tau, "chain")
+        z = case[0]
+        keep = rng.permutation(V)[:3]
+        masked = np.ones(V, bool)
+        masked[keep] = False
+        for b, x in enumerate((np.nan, -np.inf, -3.38e38, np.nan)):
+            z[b][:, masked] = x
+            if case[1] is not None and b < 3:
+                case[1][b][:, masked] = x
+        z[4] = -np.inf
+        z[5, 0] = np.nan
+        z[6, :, ::2] = np.nan
+        for b in range(4):
+            case[3][b, 1:] = keep[0]
+        _, tokens, _, _ = _verify(sbd, case, tau, dtype, 0.5)
+        for b in range(4):
+            assert set(tokens[b]) <= {-1, *keep.tolist()}, (mode, b)
+    assert sbd.sbd_device_error() == 0
+
+
 def test_verify_ties_go_to_the_lowest_index(sbd):  # noqa: F811
     import torch
     for V in (4, 1000, 128256):
