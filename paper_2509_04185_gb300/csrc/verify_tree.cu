@@ -239,7 +239,7 @@ __device__ __noinline__ Stat slow_stat(const T* elements, int w0, int w1, int st
 }
 
 template <typename T, Mode kMode, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDrawn ? 1 : 2) verify_kernel(const Args a) {
   constexpr int kWarps = kThreads / 32;
   using R = Row<T>;
   constexpr int kPer = R::kPer;
@@ -353,6 +353,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         place[i] = R(target, first[i], V);
         from[i] = min(place[i].c1, place[i].c0 + split * a.slice), to[i] = min(place[i].c1, from[i] + a.slice);
       }
+      // This thread's edge of a single row, on its way with the row (two rows leave no registers for it).
+      const int edge0 = kAhead == 1 && split == 0 && tid < place[0].edges ? place[0].edge(tid) : -1;
+      float edge_z = 0.f, edge_q = 0.f;
+      if (edge0 >= 0) {
+        edge_z = value(target + first[0] + edge0);
+        if (has_q(0)) edge_q = value(draft + first[0] + edge0);
+      }
       const long long to_draft = reinterpret_cast<const char*>(draft) - reinterpret_cast<const char*>(target);
       auto load_q = [&](int i, int w) {
         return *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(place[i].base) + to_draft + 16ll * w);
@@ -429,13 +436,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 4) verify_kern
         const R& r = place[i];
         const T* row_t = target + first[i];
         const T* row_d = draft + first[i];
-        const int edge = split == 0 && tid < r.edges ? r.edge(tid) : -1;
+        const int edge = kAhead == 1 ? edge0 : split == 0 && tid < r.edges ? r.edge(tid) : -1;
         if (slow || !(t[i].S < INFINITY)) t[i] = slow_stat<T>(row_t - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
         if (has_q(i) && (slow || !(d[i].S < INFINITY))) d[i] = slow_stat<T>(row_d - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
         if (edge >= 0) {
-          const float z = value(row_t + edge);
+          const float z = kAhead == 1 ? edge_z : value(row_t + edge);
           take_one(t[i], z, c2, a.limit);
-          if (has_q(i)) take_one(d[i], value(row_d + edge), c2, a.limit);
+          if (has_q(i)) take_one(d[i], kAhead == 1 ? edge_q : value(row_d + edge), c2, a.limit);
           if (kMode == kGreedy && !slow) top[i] = better(Best{fmaxf(z, -INFINITY), edge}, top[i]);
         }
         if (kMode == kGreedy && !slow) {               // the element of the best word
