@@ -37,6 +37,7 @@ struct Args {
   int share;                 // heads of a warp
   int shares;                // warps of a token
   float eps;
+  int* err;
 };
 
 template <typename T>
@@ -81,12 +82,15 @@ struct Piece<float> {
   }
 };
 
-// Cosine and sine of position * f.
-__device__ __forceinline__ void rotation(int position, float f, float* c, float* s) {
+// f / 2 pi, what of it is behind the point, times 2^64.
+__device__ __forceinline__ uint64_t turns_of(float f) {
   const double turns = (double)f * 0.15915494309189533577;          // 1 / (2 pi)
   const double part = turns - floor(turns);                         // whole turns a position: none
-  const uint64_t fixed = (uint64_t)(part * 18446744073709551616.0);  // (part = 1 by rounding: 2^64 - 1, a turn)
-  const int32_t angle = (int32_t)((fixed * (uint64_t)(int64_t)position) >> 32);
+  return (uint64_t)(part * 18446744073709551616.0);                  // (part = 1 by rounding: 2^64 - 1, a turn)
+}
+// Cosine and sine of position * f.
+__device__ __forceinline__ void rotation(int position, uint64_t turns, float* c, float* s) {
+  const int32_t angle = (int32_t)((turns * (uint64_t)(int64_t)position) >> 32);
   sincospif((float)angle * 4.656612873077392578125e-10f, s, c);     // 2^-31: half turns
 }
 
@@ -106,39 +110,107 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return d;
 }
 
-// kNeighbours: pairs are (2 j, 2 j + 1), else (j, j + R / 2).
-template <typename T, int D, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads, 5) norm_rope_kernel(const Args a) {
-  constexpr int kLanes = D / 16;             // of a row
-  constexpr int kRows = 32 / kLanes;         // of a warp
-  constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;       // rows that a lane has in flight
-  grid_dependency_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long job = (long long)blockIdx.x * (kThreads / 32) + warp;
-  const int t = (int)(job / a.shares), share = (int)(job - (long long)t * a.shares);
-  if (t >= a.tokens) return;
-  const int l = lane % kLanes, r = lane / kLanes;
-  const uint32_t row_mask = ((1u << kLanes) - 1) << (r * kLanes);
-  const int turned = a.R / 16;               // lanes whose pieces are rotated
-  const bool turn = l < turned;
-  const int d0 = turn ? 8 * l : a.R + 16 * (l - turned);
-  const int d1 = turn ? a.R / 2 + 8 * l : d0 + 8;
-  // Of pair i of this lane: halves (d0 + i, d1 + i), or neighbours d0 + 2 i, of d1 from i = 4.
-  float c[8], s[8];
-  {
-    float cj[2], sj[2];                      // of angles 2 lane, 2 lane + 1
-    const int position = a.R ? a.positions[t] : 0;
+// What a lane does with its 16 dimensions of a row.  kNeighbours: pairs are (2 j, 2 j + 1),
+// else (j, j + R / 2).  kAll: all D dimensions are rotated.
+template <typename T, int D, bool kNeighbours, bool kAll>
+struct Lane {
+  static constexpr int kLanes = D / 16;      // of a row
+  static constexpr int kRows = 32 / kLanes;  // of a warp
+  uint32_t row_mask;
+  int d0, d1;                                // its pieces
+  bool turn;                                 // they are rotated
+  float2 A[8], B[8];                         // of elements 2 e, 2 e + 1: d0 + 2 e, from e = 4 d1 + 2 (e - 4)
+
+  __device__ __forceinline__ Lane(int R) {
+    const int lane = threadIdx.x & 31, l = lane % kLanes, turned = R / 16;
+    row_mask = ((1u << kLanes) - 1) << (lane - l);
+    turn = kAll || l < turned;
+    d0 = turn ? 8 * l : R + 16 * (l - turned);
+    d1 = turn ? R / 2 + 8 * l : d0 + 8;
+  }
+  // The factors, from the token's angles 2 lane, 2 lane + 1 (whole warp).
+  __device__ __forceinline__ void factors(const T* weight, const float (&cj)[2], const float (&sj)[2]) {
+    float w[16], c[8], s[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      cj[i] = 1.f, sj[i] = 0.f;
-      if (2 * lane < a.R / 2) rotation(position, a.inv_freq[2 * lane + i], &cj[i], &sj[i]);
+    for (int e = 0; e < 16; ++e) w[e] = 1.f;
+    if (weight) {
+      Piece<T> w0, w1;
+      w0.load(weight + d0), w1.load(weight + d1);
+      w0.get(w), w1.get(w + 8);
     }
+    // Of pair i: halves (d0 + i, d1 + i), or neighbours d0 + 2 i, of d1 from i = 4.
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int j = turn ? (kNeighbours ? (i < 4 ? d0 : d1) / 2 + i % 4 : d0 + i) : 0;
       c[i] = __shfl_sync(0xffffffffu, cj[i & 1], j >> 1);
       s[i] = __shfl_sync(0xffffffffu, sj[i & 1], j >> 1);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (!kAll && !turn) {
+        A[e] = make_float2(w[2 * e], w[2 * e + 1]), B[e] = make_float2(0.f, 0.f);
+      } else if (kNeighbours) {
+        A[e] = make_float2(w[2 * e] * c[e], w[2 * e + 1] * c[e]);
+        B[e] = make_float2(-w[2 * e + 1] * s[e], w[2 * e] * s[e]);
+      } else {
+        const int i = 2 * (e & 3);
+        const float sign = e < 4 ? -1.f : 1.f;
+        A[e] = make_float2(w[2 * e] * c[i], w[2 * e + 1] * c[i + 1]);
+        B[e] = make_float2(sign * w[(2 * e + 8) % 16] * s[i], sign * w[(2 * e + 9) % 16] * s[i + 1]);
+      }
+    }
+  }
+  // A row's pieces (the lanes of a row together).
+  __device__ __forceinline__ void row(Piece<T>& x0, Piece<T>& x1, bool norm, float eps) const {
+    float x[16];
+    x0.get(x), x1.get(x + 8);
+    float2 X[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) X[e] = make_float2(x[2 * e], x[2 * e + 1]);
+    float inv = 1.f;
+    if (norm) {
+      float2 sum = mul2(X[0], X[0]);
+#pragma unroll
+      for (int e = 1; e < 8; ++e) sum = fma2(X[e], X[e], sum);
+      float all = sum.x + sum.y;
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o /= 2) all += __shfl_xor_sync(row_mask, all, o);
+      inv = rsqrtf(fmaf(all, 1.f / D, eps));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float2 other = kNeighbours ? make_float2(X[e].y, X[e].x) : X[e ^ 4];
+      // (a part that is not turned is not touched by what an infinity times 0 is)
+      if (!kAll && !turn) other = make_float2(0.f, 0.f);
+      float2 y = fma2(X[e], A[e], mul2(other, B[e]));
+      if (norm) y = mul2(y, make_float2(inv, inv));
+      x[2 * e] = y.x, x[2 * e + 1] = y.y;
+    }
+    x0.set(x), x1.set(x + 8);
+  }
+};
+
+// Few tokens, or fp32: a warp has some heads of one, three turns of rows (a turn: a row for
+// each lane group) in flight.  Bound: latency up to some hundred tokens (16 tokens 3.4 us, of
+// which a launch 2), HBM for prompts (fp32, 16000 tokens 125 us, 6.3 TB/s).
+template <typename T, int D, bool kNeighbours>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_kernel(const Args a) {
+  using L = Lane<T, D, kNeighbours, false>;
+  constexpr int kRows = L::kRows;
+  constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;       // rows that a lane has in flight
+  grid_dependency_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long job = (long long)blockIdx.x * (kThreads / 32) + warp;
+  const int t = (int)(job / a.shares), share = (int)(job - (long long)t * a.shares);
+  if (t >= a.tokens) return;
+  const int r = lane / L::kLanes;
+  L my(a.R);
+  float cj[2], sj[2];                        // of angles 2 lane, 2 lane + 1
+  const int position = a.R ? a.positions[t] : 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    cj[i] = 1.f, sj[i] = 0.f;
+    if (2 * lane < a.R / 2) rotation(position, turns_of(a.inv_freq[2 * lane + i]), &cj[i], &sj[i]);
   }
   const int g = t / a.group, in_group = t - g * a.group;
   const int begin = share * a.share, end = min(a.heads, begin + a.share);
@@ -146,73 +218,23 @@ __global__ void __launch_bounds__(kThreads, 5) norm_rope_kernel(const Args a) {
   auto rows = [&](int first, int count, const T* src, T* dst, const T* weight, bool copy) {
     const int lo = max(begin, first) - first, hi = min(end, first + count) - first;
     if (lo >= hi) return;
-    float2 A[8], B[8];                       // of elements 2 e, 2 e + 1: d0 + 2 e, from e = 4 d1 + 2 (e - 4)
-    if (!copy) {
-      float w[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) w[e] = 1.f;
-      if (weight) {
-        Piece<T> w0, w1;
-        w0.load(weight + d0), w1.load(weight + d1);
-        w0.get(w), w1.get(w + 8);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (!turn) {
-          A[e] = make_float2(w[2 * e], w[2 * e + 1]), B[e] = make_float2(0.f, 0.f);
-        } else if (kNeighbours) {
-          A[e] = make_float2(w[2 * e] * c[e], w[2 * e + 1] * c[e]);
-          B[e] = make_float2(-w[2 * e + 1] * s[e], w[2 * e] * s[e]);
-        } else {
-          const int i = 2 * (e & 3);
-          const float sign = e < 4 ? -1.f : 1.f;
-          A[e] = make_float2(w[2 * e] * c[i], w[2 * e + 1] * c[i + 1]);
-          B[e] = make_float2(sign * w[(2 * e + 8) % 16] * s[i], sign * w[(2 * e + 9) % 16] * s[i + 1]);
-        }
-      }
-    }
+    if (!copy) my.factors(weight, cj, sj);
     Piece<T> p0[kAhead], p1[kAhead];
     constexpr int kStep = kRows * D;
     src += (lo + r) * D, dst += (lo + r) * D;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (lo + r + u * kRows < hi) p0[u].load(src + u * kStep + d0), p1[u].load(src + u * kStep + d1);
+      if (lo + r + u * kRows < hi) p0[u].load(src + u * kStep + my.d0), p1[u].load(src + u * kStep + my.d1);
 #pragma unroll 1
     for (int h0 = lo + r; h0 < hi; h0 += kAhead * kRows) {
       src += kAhead * kStep;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-      if (h0 + u * kRows >= hi) break;
-      Piece<T> x0 = p0[u], x1 = p1[u];
-      if (h0 + (u + kAhead) * kRows < hi) p0[u].load(src + u * kStep + d0), p1[u].load(src + u * kStep + d1);
-      if (!copy) {
-        float x[16];
-        x0.get(x), x1.get(x + 8);
-        float2 X[8], Y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) X[e] = make_float2(x[2 * e], x[2 * e + 1]);
-        float inv = 1.f;
-        if (weight) {
-          float2 sum = mul2(X[0], X[0]);
-#pragma unroll
-          for (int e = 1; e < 8; ++e) sum = fma2(X[e], X[e], sum);
-          float all = sum.x + sum.y;
-#pragma unroll
-          for (int o = kLanes / 2; o > 0; o /= 2) all += __shfl_xor_sync(row_mask, all, o);
-          inv = rsqrtf(fmaf(all, 1.f / D, a.eps));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float2 other = kNeighbours ? make_float2(X[e].y, X[e].x) : X[e ^ 4];
-          // (a part that is not turned is not touched by what an infinity times 0 is)
-          if (!turn) other = make_float2(0.f, 0.f);
-          Y[e] = fma2(X[e], A[e], mul2(other, B[e]));
-          if (weight) Y[e] = mul2(Y[e], make_float2(inv, inv));
-          x[2 * e] = Y[e].x, x[2 * e + 1] = Y[e].y;
-        }
-        x0.set(x), x1.set(x + 8);
-      }
-      x0.store(dst + u * kStep + d0), x1.store(dst + u * kStep + d1);
+        if (h0 + u * kRows >= hi) break;
+        Piece<T> x0 = p0[u], x1 = p1[u];
+        if (h0 + (u + kAhead) * kRows < hi) p0[u].load(src + u * kStep + my.d0), p1[u].load(src + u * kStep + my.d1);
+        if (!copy) my.row(x0, x1, weight != nullptr, a.eps);
+        x0.store(dst + u * kStep + my.d0), x1.store(dst + u * kStep + my.d1);
       }
       dst += kAhead * kStep;
     }
@@ -226,9 +248,148 @@ __global__ void __launch_bounds__(kThreads, 5) norm_rope_kernel(const Args a) {
   grid_dependents_launch();
 }
 
-template <typename T, int D>
-const void* kernel_of(bool neighbours) {
-  return neighbours ? (const void*)norm_rope_kernel<T, D, true> : (const void*)norm_rope_kernel<T, D, false>;
+// Many tokens (bf16): every warp streams whole tokens through a ring in shared memory, pieces of up
+// to kPiece bytes (heads of queries, keys or values of a token) that bulk copies bring and
+// take away; rows are worked on in place, values not touched at all.  What is in flight does
+// not depend on registers or on where a token ends.
+// Bound: HBM.  32768 tokens of 32 + 8 + 8 heads of 128 dimensions 128 us, 6.3 TB/s, 0.93 of the
+// copy rate (a plain copy of as many bytes 120; from registers 143).  More in flight than 128
+// KB an SM is slower: rings of 4 pieces with as many warps 147 us, of 3 pieces and 12 warps 146,
+// pieces copied and not worked on 123 with 128 KB and 129 with 192.
+constexpr int kPiece = 4096;
+constexpr int kStages = 2;
+constexpr int kStreamCtas = 4;               // that share an SM
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(dst),
+               "r"(smem_u32(src)), "r"(bytes)
+               : "memory");
+}
+
+template <typename T, int D, bool kNeighbours, bool kAll>
+__global__ void __launch_bounds__(kThreads) norm_rope_stream_kernel(const Args a) {
+  using L = Lane<T, D, kNeighbours, kAll>;
+  constexpr int kHeads = kPiece / (D * (int)sizeof(T));        // of a piece
+  static_assert(kHeads % L::kRows == 0, "whole turns");
+  constexpr int kRow = D * (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t ring_raw[];
+  __shared__ __align__(8) uint64_t full[kThreads / 32][kStages];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* const ring = ring_raw + warp * kStages * kPiece;
+  if (lane == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(&full[warp][s], 1);
+    fence_mbar_init();
+  }
+  __syncwarp();
+  grid_dependency_wait();
+  const int warps = gridDim.x * (kThreads / 32), first = blockIdx.x * (kThreads / 32) + warp;
+  const bool values = a.heads > a.Hq + a.Hkv;
+  auto next_token = [&](int t) { return t > a.tokens - 1 - warps ? a.tokens : t + warps; };
+  // The place that is loaded from: a token's queries, keys, values, so many bytes into them.
+  int load_t = first, load_part = 0, load_at = 0, loaded = 0;
+  const uint8_t* load_src = nullptr;
+  auto load_begin = [&]() {
+    const int g = a.group >= a.tokens ? 0 : load_t / a.group, i = load_t - g * a.group;
+    const long long at = load_part == 0   ? g * a.q_group_stride + i * a.q_token_stride
+                         : load_part == 1 ? g * a.k_group_stride + i * a.k_token_stride
+                                          : g * a.v_group_stride + i * a.v_token_stride;
+    load_src = (const uint8_t*)(load_part == 0 ? a.q : load_part == 1 ? a.k : a.v) + at * (int)sizeof(T);
+  };
+  auto load = [&]() {                        // (one lane)
+    if (load_t >= a.tokens) return;
+    const int all = (load_part == 0 ? a.Hq : a.Hkv) * kRow, n = min(kPiece, all - load_at), s = loaded % kStages;
+    mbar_arrive_expect_tx(&full[warp][s], n);
+    bulk_load(ring + s * kPiece, load_src + load_at, n, &full[warp][s]);
+    ++loaded;
+    load_at += kPiece;
+    if (load_at < all) return;
+    load_at = 0;
+    if (++load_part == (values ? 3 : 2)) load_part = 0, load_t = next_token(load_t);
+    if (load_t < a.tokens) load_begin();
+  };
+  if (lane == 0 && load_t < a.tokens) {
+    load_begin();
+    for (int s = 0; s < kStages; ++s) load();
+  }
+  L my(a.R);
+  const bool has_angle = 2 * lane < a.R / 2;
+  uint64_t turns[2] = {0, 0};
+  float cj[2] = {1.f, 1.f}, sj[2] = {0.f, 0.f};
+  if (has_angle) turns[0] = turns_of(a.inv_freq[2 * lane]), turns[1] = turns_of(a.inv_freq[2 * lane + 1]);
+  int position = has_angle && first < a.tokens ? a.positions[first] : 0;
+  int done = 0;
+  bool ok = true;
+  // A part of a token, piece by piece.
+  auto part = [&](int heads, uint8_t* dst, const T* weight, bool copy) {
+    if (!copy) my.factors(weight, cj, sj);
+#pragma unroll 1
+    for (int h0 = 0; h0 < heads; h0 += kHeads, ++done, dst += kPiece) {
+      const int n = min(kHeads, heads - h0), s = done % kStages;
+      ok = mbar_wait(&full[warp][s], (done / kStages) & 1, a.err);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      uint8_t* const x = ring + s * kPiece;
+      if (!copy) {
+        T* row = (T*)x + lane / L::kLanes * D;
+#pragma unroll 2
+        for (int h = lane / L::kLanes; h < n; h += L::kRows, row += L::kRows * D) {
+          Piece<T> x0, x1;
+          x0.load(row + my.d0), x1.load(row + my.d1);
+          my.row(x0, x1, weight != nullptr, a.eps);
+          x0.store(row + my.d0), x1.store(row + my.d1);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      if (lane == 0) {
+        bulk_store(dst, x, n * kRow);
+        // The piece before this one has left its place by now, or nearly: the next one comes there.
+        if (done > 0) {
+          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          load();
+        }
+      }
+      __syncwarp();
+    }
+  };
+  for (int t = first; t < a.tokens; t = next_token(t)) {
+    if (has_angle) {
+      rotation(position, turns[0], &cj[0], &sj[0]);
+      rotation(position, turns[1], &cj[1], &sj[1]);
+      const int next = next_token(t);
+      if (next < a.tokens) position = a.positions[next];
+    }
+    part(a.Hq, (uint8_t*)a.q_out + (long long)t * a.Hq * kRow, (const T*)a.q_weight, false);
+    if (ok) part(a.Hkv, (uint8_t*)a.k_out + (long long)t * a.Hkv * kRow, (const T*)a.k_weight, false);
+    if (ok && values) part(a.Hkv, (uint8_t*)a.v_out + (long long)t * a.Hkv * kRow, nullptr, true);
+    if (!ok) break;
+  }
+  grid_dependents_launch();
+  // No copy is in flight when the CTA ends, whatever became of the waits.
+  if (lane == 0) {
+    for (int i = done; i < loaded; ++i) mbar_wait(&full[warp][i % kStages], (i / kStages) & 1, a.err);
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+}
+
+template <typename T, int D, bool kNeighbours>
+const void* kernel_of(bool stream, bool all) {
+  if constexpr (sizeof(T) == 2)
+    if (stream)
+      return all ? (const void*)norm_rope_stream_kernel<T, D, kNeighbours, true>
+                 : (const void*)norm_rope_stream_kernel<T, D, kNeighbours, false>;
+  return (const void*)norm_rope_kernel<T, D, kNeighbours>;
+}
+template <typename T>
+const void* kernel_for(const sbd_norm_rope_desc& d, bool stream) {
+  const bool all = d.rotary_dim == d.head_dim;
+  if (d.head_dim == 128) return d.interleaved ? kernel_of<T, 128, true>(stream, all) : kernel_of<T, 128, false>(stream, all);
+  return d.interleaved ? kernel_of<T, 64, true>(stream, all) : kernel_of<T, 64, false>(stream, all);
 }
 
 }  // namespace
@@ -259,6 +420,7 @@ sbd_status norm_rope_launch(const sbd_norm_rope_desc& d, const NormRopeTensors& 
   a.Hkv = d.n_kv_heads;
   a.R = d.rotary_dim;
   a.eps = d.eps;
+  a.err = device_error_word();
   a.heads = d.n_q_heads + d.n_kv_heads * (t.v ? 2 : 1);
   const int rows = 512 / d.head_dim;                       // of a warp's turn
   a.share = (a.heads + rows - 1) / rows * rows;
@@ -266,12 +428,20 @@ sbd_status norm_rope_launch(const sbd_norm_rope_desc& d, const NormRopeTensors& 
   while (a.share > rows && (long long)d.tokens * ((a.heads + a.share - 1) / a.share) < 16ll * num_sms())
     a.share = (a.share / rows + 1) / 2 * rows;
   a.shares = (a.heads + a.share - 1) / a.share;
+  // bf16 tokens are streamed from two for every warp on (of 32 + 8 + 8 heads of 128: 2600 tokens
+  // 18.3 us streamed and 15.9 spread, 5000 27.6 and 27.7, 10000 45.6 and 49.3, 16000 66 and 73);
+  // fp32 ones never (16000 tokens 134 and 125).
+  const bool stream = d.dtype == SBD_DTYPE_BF16 && d.tokens >= 2ll * kStreamCtas * (kThreads / 32) * num_sms();
+  const void* fn = d.dtype == SBD_DTYPE_F32 ? kernel_for<float>(d, stream) : kernel_for<__nv_bfloat16>(d, stream);
+  void* args[] = {(void*)&a};
+  if (stream) {
+    const size_t smem = (size_t)(kThreads / 32) * kStages * kPiece;
+    const sbd_status s = allow_smem(fn, smem, "cudaFuncSetAttribute(norm_rope_stream_kernel)");
+    if (s != SBD_OK) return s;
+    return launch_pdl(fn, dim3(kStreamCtas * num_sms()), dim3(kThreads), smem, st, args, "norm_rope_stream_kernel launch");
+  }
   const long long warps = (long long)d.tokens * a.shares, ctas = (warps + kThreads / 32 - 1) / (kThreads / 32);
   if (ctas > 0x7fffffffll) return fail(SBD_ERR_UNSUPPORTED, "%lld CTAs >= 2^31", ctas);
-  const bool f32 = d.dtype == SBD_DTYPE_F32, pairs = d.interleaved != 0;
-  const void* fn = d.head_dim == 128 ? (f32 ? kernel_of<float, 128>(pairs) : kernel_of<__nv_bfloat16, 128>(pairs))
-                                     : (f32 ? kernel_of<float, 64>(pairs) : kernel_of<__nv_bfloat16, 64>(pairs));
-  void* args[] = {(void*)&a};
   return launch_pdl(fn, dim3((unsigned)ctas), dim3(kThreads), 0, st, args, "norm_rope_kernel launch");
 }
 

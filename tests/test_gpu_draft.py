@@ -82,6 +82,45 @@ def test_norm_rope(sbd, dtype, T, Hq, H, D, R, norm, interleaved, layout):  # no
     _rope(sbd, T, Hq, H, D, R, dtype, norm, interleaved, rng.integers(0, 5000, T), layout, values=T != 33)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,Hq,H,D,R,norm,interleaved,layout", [
+    (9000, 3, 2, 64, 64, True, False, "fused"), (9001, 2, 1, 128, 32, True, True, "plain"), (9999, 1, 1, 64, 48, False, False, "blocks"),
+    (8100, 9, 5, 128, 128, True, False, "fused"), (7500, 19, 1, 64, 0, True, False, "fused"), (24001, 1, 1, 128, 128, False, True, "plain")])
+def test_norm_rope_of_prompts(sbd, dtype, T, Hq, H, D, R, norm, interleaved, layout):  # noqa: F811
+    """Tokens enough for the kernel that streams them through shared memory: the same bits as
+    of a few tokens at a time."""
+    import torch
+    dt = getattr(torch, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, Hq + 2 * H, D, generator=gen, device="cuda").to(dt)
+    if layout == "blocks":                       # the last 3 rows of blocks of 5
+        wide = torch.randn(T // 3, 5, Hq + 2 * H, D, generator=gen, device="cuda").to(dt)
+        wide[:, 2:] = x.view(T // 3, 3, Hq + 2 * H, D)
+        x = wide[:, 2:]
+    parts = [x[..., :Hq, :], x[..., Hq:Hq + H, :], x[..., Hq + H:, :]]
+    if layout == "plain":
+        parts = [p.contiguous() for p in parts]
+    w = (1 + 0.3 * torch.randn(2, D, generator=gen, device="cuda")).to(dt) if norm else (None, None)
+    inv = torch.rand(R // 2, generator=gen, device="cuda") if R else None
+    pos = torch.randint(0, 100000, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    for values in (True, False):
+        outs = [torch.full((T + 2, h, D), 7, dtype=dt, device="cuda") for h in (Hq, H, H)]
+        got = [o[1:-1] for o in outs]
+        shaped = [o.view(p.shape) for o, p in zip(got, parts)]
+        sbd.sbd_qk_norm_rope(*parts[:2], parts[2] if values else None, pos, inv, *w, *shaped[:2], shaped[2] if values else None,
+                             eps=1e-5, interleaved=interleaved)
+        flat = [p.reshape(T, -1, D) for p in parts]
+        for i in range(0, T, 1000):
+            few = sbd.sbd_qk_norm_rope(*(f[i:i + 1000].contiguous() for f in flat), pos[i:i + 1000].clone(), inv, *w, eps=1e-5,
+                                       interleaved=interleaved)
+            for j in range(3 if values else 2):
+                assert torch.equal(got[j][i:i + 1000], few[j]), (i, j)
+        for o in outs:
+            assert (o[0] == 7).all() and (o[-1] == 7).all()
+        assert values or (outs[2] == 7).all()
+    assert sbd.sbd_device_error() == 0
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_norm_rope_far_positions(sbd, interleaved):  # noqa: F811
     far = [0, 1, -1, 2 ** 20, 10 ** 7 + 1, 2 ** 31 - 1, -2 ** 31, 2 ** 24 + 1, 999999937]
