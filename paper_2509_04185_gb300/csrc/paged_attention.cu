@@ -29,9 +29,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 // It serves fp32 activations: one product of the tensor cores' 16-bit types does not meet
 // their tolerance.  (Rows as three bf16 parts each would, in three products; not built.)
 // Bound: latency while the ranges are short (one request of 128 keys, 2 KV heads of 64
-// dimensions, 4 rows: 5.2 us, a launch and the chain lengths -> page -> keys -> merge);
+// dimensions, 4 rows: 4.6 us, a launch and the chain lengths -> page -> keys -> merge);
 // then shared memory, every warp reading the tile for its few rows: 8 requests of 2000
-// keys, 8 KV heads of 128 dimensions, 32 rows: 81 us, 26 of 80 TFLOP/s; 4 rows: 39 us;
+// keys, 8 KV heads of 128 dimensions, 32 rows: 79 us, 27 of 80 TFLOP/s; 4 rows: 38 us;
 // 128 rows, four chunks: 295 us.
 // (Divisions by the page size and stores that met in a bank took a quarter more.)
 constexpr int kKeys = 64;                    // keys per tile

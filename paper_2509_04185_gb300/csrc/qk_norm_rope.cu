@@ -8,9 +8,7 @@
 // are the same in every head, so norm weights, cosines and sines become two factors an
 // element, A and B, once for a token's queries and once for its keys:
 //   y_d = (x_d A_d + x_d' B_d) / sqrt(mean x^2 + eps),   d' the other half of d's pair,
-// and a row costs a sum of squares and two products an element, in pairs an instruction.  A
-// warp takes all of a token's heads (several warps share them where tokens are few), a row
-// ahead of the one that it works on.
+// and a row costs a sum of squares and two products an element, in pairs an instruction.
 //
 // Angles.  inv_freq / 2 pi in turns goes to fixed point, 64 bits behind the point; times
 // the position, whole turns fall off the top of the product by themselves, and what is

@@ -347,7 +347,7 @@ def _verify(sbd, case, tau, dtype="bfloat16", compare=0.8):  # noqa: F811
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 @pytest.mark.parametrize("mode", ["drawn", "given", "greedy"])
 @pytest.mark.parametrize("B,n,V,tau", [(1, 1, 1000, 1.0), (1, 8, 128256, 1.0), (3, 1, 1, 1.0), (5, 4, 2, 1.0), (7, 6, 7, 0.8), (40, 12, 333, 1.0),
-                                       (9, 7, 50257, 0.5), (170, 5, 1001, 1.3), (2, 64, 4099, 1.0), (33, 16, 2048, 2.0)])
+                                       (9, 7, 50257, 0.5), (170, 5, 1001, 1.3), (2, 64, 4099, 1.0), (33, 16, 2048, 2.0), (1, 2, 1 << 24, 1.0), (10, 3, 131072, 1.0)])
 def test_verify(sbd, dtype, mode, B, n, V, tau):  # noqa: F811
     rng = np.random.default_rng(B * n + V)
     tau = 0.0 if mode == "greedy" else tau
