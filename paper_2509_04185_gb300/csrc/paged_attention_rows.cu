@@ -640,9 +640,10 @@ static sbd_dev::TcKernel rows_instance() {
   return {(const void*)paged_rows_kernel<D, kBlk, kTree>, C::kSmem, C::kThreads};
 }
 sbd_dev::TcKernel paged_rows_kernel_for(int D, int k, bool tree) {
+  // (only a tree's call has parents, which its instances read)
+  if (!tree) return D == 128 ? rows_instance<128, 32, false>() : rows_instance<64, 32, false>();
   if (k > 32) return D == 128 ? rows_instance<128, 64, true>() : rows_instance<64, 64, true>();
-  if (tree) return D == 128 ? rows_instance<128, 32, true>() : rows_instance<64, 32, true>();
-  return D == 128 ? rows_instance<128, 32, false>() : rows_instance<64, 32, false>();
+  return D == 128 ? rows_instance<128, 32, true>() : rows_instance<64, 32, true>();
 }
 
 }  // namespace sbd
