@@ -244,3 +244,79 @@ def test_the_binding_refuses_what_does_not_fit(sbd):  # noqa: F811
         with pytest.raises(error):
             sbd.sbd_cache_append_path_q8(k_new, vc, p, s, slots, *t.cache, *t.scale)
     assert sbd.sbd_device_error() == 0
+
+
+def test_a_cache_of_more_than_4_gb(sbd):  # noqa: F811
+    """Offsets past 32 bits: the pages lie at the end of the cache."""
+    import torch
+    D, H, P, n = 128, 8, 128, 40
+    n_pages = (1 << 32) // (D * H * P) + 40
+    rng = np.random.default_rng(3)
+    q, codes, scales, table, lens, kb, vb = tp._attention_case(rng, 1, n, 4, 1, D, P, [700])
+    parent = tp._i32(td._trees(rng, 1, n))
+    cache = [torch.zeros(n_pages, H, P, D, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scale = [torch.zeros(n_pages, H, device="cuda") for _ in range(2)]
+    base = n_pages - codes[0].shape[0]
+    for w in range(2):
+        cache[w][base:, H - 1] = torch.from_numpy(codes[w][:, 0]).cuda()
+        scale[w][base:, H - 1] = torch.from_numpy(scales[w][:, 0]).cuda()
+    f8 = [c.view(torch.float8_e4m3fn) for c in cache]
+    for dt in (torch.bfloat16, torch.float32):
+        dev = [torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(dt).cuda() for x in (q, kb, vb)]
+        wide = [torch.zeros(1, n, H * x.shape[2], D, dtype=dt, device="cuda") for x in dev]
+        for w, x in zip(wide, dev):
+            w[:, :, -x.shape[2]:] = x
+        out = sbd.sbd_tree_attention_q8(wide[0], *f8, *scale, tp._i32(np.where(table >= 0, table + base, -1)), tp._i32(lens), *wide[1:], parent)
+        small = sbd.sbd_tree_attention_q8(dev[0], *(tp._f8(c) for c in codes), *(td._f32(s) for s in scales), tp._i32(table), tp._i32(lens),
+                                          *dev[1:], parent)
+        tol = 2e-2 if dt == torch.bfloat16 else 1e-5
+        assert (out[:, :, -4:].float() - small.float()).abs().max().item() <= tol * small.abs().max().item()
+    x = torch.randn(1, 4, H, D, device="cuda")
+    path, start = tp._i32([[0, 2, 3, -1]]), tp._i32([0, 3])
+    sbd.sbd_cache_append_path_q8(x, x, path, start, tp._i32((n_pages - 1) * P + np.arange(4)), *f8, *scale)
+    got = f8[0][-1, :, :3].float() * scale[0][-1][:, None, None]
+    assert (got.transpose(0, 1) - x[0, [0, 2, 3]]).abs().max().item() <= 2.0 ** -4 * x.abs().max().item()
+    assert sbd.sbd_device_error() == 0
+
+
+def test_many_requests(sbd):  # noqa: F811
+    """More requests than a wave, each with a tree of its own."""
+    import torch
+    rng = np.random.default_rng(8)
+    B, n, V = 5000, 4, 9
+    case = td._verify_case(rng, B, n, V, True, 1.0)
+    td._verify(sbd, case, 1.0, "float32", 0.9)
+    path, start, slots, pages = td._path_case(rng, B, n, 16, 3)
+    codes, scale = [np.full((pages, 1, 16, 64), 0x31, np.uint8)] * 2, [np.full((pages, 1), 2.0 ** -9, np.float32)] * 2
+    td._append(sbd, rng.normal(size=(B, n, 1, 64)), path, start, slots, codes, scale, 16, "bfloat16")
+    x = torch.randn(B, n, 3, 64, device="cuda").bfloat16()
+    pos, inv = torch.zeros(B, n, dtype=torch.int32, device="cuda"), torch.ones(32, device="cuda")
+    q, k, v = sbd.sbd_qk_norm_rope(x[:, :, :1], x[:, :, 1:2], x[:, :, 2:], pos, inv)
+    assert torch.equal(q, x[:, :, :1]) and torch.equal(k, x[:, :, 1:2]) and torch.equal(v, x[:, :, 2:])
+    assert sbd.sbd_device_error() == 0
+
+
+def test_the_first_calls_of_a_process_are_captured():
+    """No call has to be made before a capture."""
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.path[:0] = [%r, %r]
+import torch
+import paper_2509_04185_gb300 as sbd
+import test_gpu_draft_turn as t
+turn = t._Turn(sbd, 1)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    outs = turn()
+graph.replay()
+torch.cuda.synchronize()
+got = turn.state(outs)
+turn.reset()
+assert t._same(got, turn.state(turn())) and sbd.sbd_device_error() == 0
+print("captured")
+""" % (ROOT, os.path.join(ROOT, "tests"))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
