@@ -292,7 +292,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
   }
   const float c2 = a.scale;
   auto tame = [&](float z) { return ::tame(z, a.limit); };
-  const float low = 256.f - a.limit * c2;    // a row's M below it: of nothing but masked logits
+  // A row's M below the one: of nothing but masked logits; from the other on: logits beyond the limit.
+  const float low = 256.f - a.limit * c2, high = a.limit * c2 - 1.f;
+  auto is_out = [&](float M) { return M < low || M >= high; };
   unsigned long long known = 0;              // nodes whose rows' M and S are known
   while (true) {
     const unsigned long long children = child_sh[node];
@@ -323,8 +325,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       Best top[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) t[i] = d[i] = Stat{-2.f * kLimit, 0.f}, top[i] = Best{NAN, 0x7fffffff};
-      // As they are: a NaN, or what is beyond the limit, shows in the sum, and the thread's
-      // share is taken again, slowly; so is a row that is low altogether.
+      // As they are: a NaN shows in the sum, and the thread's share is taken again, slowly.  A
+      // logit beyond the limit shows in M (what is only just beyond leaves the sum finite), and
+      // the row is taken again, as is one that is low altogether.
       auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
         const float M = fmaxf(s.M, ceilf(tame(largest(x, (const T*)nullptr)) * c2));
         float2 sum = make_float2(0.f, 0.f);
@@ -461,15 +464,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       };
 #pragma unroll 1
       for (bool slow = false;; slow = true) {
-        bool is_low = false;
+        bool again = false;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
           if (i < rows) finish(i, slow);
         reduce(ex, turn, a.splits, rows, mine, none, join);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-          if (i < rows) is_low |= mine[i].x < low || (has_q(i) && mine[i].z < low);
-        if (slow || !is_low) break;
+          if (i < rows) again |= is_out(mine[i].x) || (has_q(i) && is_out(mine[i].z));
+        if (slow || !again) break;
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
@@ -491,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
     auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
     auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
     // A row whose logits are within the limit needs no taming of single ones but NaN.
-    const bool tamed = (st.M >= low && st.M < a.limit * c2 - 1.f) && (!use_q || (sq.M >= low && sq.M < a.limit * c2 - 1.f));
+    const bool tamed = !is_out(st.M) && (!use_q || !is_out(sq.M));
     // What is left of p at elements v, v + 1, ... after the first k rejections (and one more,
     // `after`), times S and not normalised by the last ones' sum.
     const float q_of_p = inv_q * st.S;
