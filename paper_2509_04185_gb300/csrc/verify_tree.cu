@@ -462,17 +462,18 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
         mine[i] = make_float4(t[i].M, t[i].S, d[i].M, d[i].S);
         if (kMode == kGreedy) mine[i].z = top[i].score, mine[i].w = __int_as_float(top[i].v);
       };
-#pragma unroll 1
-      for (bool slow = false;; slow = true) {
-        bool again = false;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-          if (i < rows) finish(i, slow);
-        reduce(ex, turn, a.splits, rows, mine, none, join);
+      for (int i = 0; i < kAhead; ++i)
+        if (i < rows) finish(i, false);
+      reduce(ex, turn, a.splits, rows, mine, none, join);
+      // (each for itself: a row's sums do not depend on the row beside it)
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-          if (i < rows) again |= is_out(mine[i].x) || (has_q(i) && is_out(mine[i].z));
-        if (slow || !again) break;
+      for (int i = 0; i < kAhead; ++i) {
+        if (i >= rows || !(is_out(mine[i].x) || (has_q(i) && is_out(mine[i].z)))) continue;
+        finish(i, true);
+        float4 one[1] = {mine[i]};
+        reduce(ex, turn, a.splits, 1, one, none, join);
+        mine[i] = one[0];
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)

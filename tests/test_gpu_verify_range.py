@@ -33,3 +33,27 @@ def test_a_logit_just_past_what_sums_take_at_once(sbd, B, over):  # noqa: F811
             _, tokens, logprob, count = td._verify(sbd, case, tau, "float32", 0.4)
             assert (count >= 2).all() and (tokens[:, 0] == at).all() and (np.abs(logprob[:, 0]) <= 2.0 ** -16).all()
     assert sbd.sbd_device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("x", [-np.inf, np.nan, 3e38])
+def test_rows_that_the_walk_does_not_come_to_change_nothing(sbd, dtype, x):  # noqa: F811
+    """Bit for bit, also where two rows are worked on at once: a first child's row is masked
+    altogether, or full of what the fast sums do not take."""
+    import torch
+    rng = np.random.default_rng(4)
+    for V in (777, 128256) + 30 * (20011,):
+        target, draft = 2 * rng.normal(size=(2, 1, 4, V))
+        p, q = (np.exp(z[0, 0]) / np.exp(z[0, 0]).sum() for z in (target, draft))
+        token = np.array([[0, int(np.argmax(q - p)), 1, 2]], np.int32)             # refused
+        args = [tp._i32([[-1, 0, 1, 1]]), tp._i32(token), td._f32(np.full((1, 4), 0.9999)), td._f32(rng.gumbel(size=(1, V))), 1.0]
+        outs = []
+        for bad in (False, True):
+            z, d = (torch.from_numpy(y.astype(np.float32)).to(getattr(torch, dtype)).cuda() for y in (target, draft))
+            if bad:
+                z[:, 1:], d[:, 1:] = x, x
+            outs.append(sbd.sbd_verify_tree(z, d, *args))
+        assert outs[0][3].tolist() == [1]
+        for a, b in zip(*outs):
+            assert torch.equal(a, b), V
+    assert sbd.sbd_device_error() == 0
