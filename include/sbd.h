@@ -556,9 +556,9 @@ sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, co
  * (sbd_gumbel_philox).  draft_logits NULL: a drafted token was not drawn but given, q is
  * 1 there and 0 elsewhere.  tau = 0: p is 1 at the largest logit (lowest index of equal
  * ones; NaN is below all); draft_logits, uniform and gumbel are not read.  In a
- * softmax a logit counts as -2^23 tau at least and 2^23 tau at most, NaN as the least: what
- * is masked with -inf or a type's lowest value never comes out beside an ordinary logit,
- * and in a row of nothing else all count alike.
+ * softmax only distances from the row's largest logit count, of any size; NaN counts as -inf.
+ * What is masked with -inf or a type's lowest value never comes out beside an ordinary logit;
+ * in a row of nothing but -inf all count alike, and logits of +inf share all.
  *
  *   target_logits, draft_logits [B, n, V]   desc->dtype; draft row i: what i's children
  *                                           were drawn from (read where it has some)

@@ -75,10 +75,11 @@ def _softmax(z, tau):
     """p, ln p (not ln of p: apart from a logit of 3e38 a sum of exponentials would vanish), and the logits."""
     z = np.asarray(z, np.float64)
     z = np.where(np.isnan(z), -np.inf, z)
-    y = np.clip(z, -2.0 ** 23 * tau, 2.0 ** 23 * tau)
-    m = y.max()
-    e = np.exp((y - m) / tau)
-    return e / e.sum(), (y - m) / tau - math.log(e.sum()), z
+    m = z.max()
+    # (infinities: the largest of them are alike and leave nothing to the others)
+    y = (z - m) / tau if np.isfinite(m) else np.where(z == m, 0.0, -np.inf)
+    e = np.exp(y)
+    return e / e.sum(), y - math.log(e.sum()), z
 
 
 def verify(target, draft, parent, token, uniform, gumbel, tau):

@@ -3,8 +3,9 @@
 //
 // Probabilities are powers of two over a sum, p(v) = 2^(z_v c - M) / S with c = log2(e) / tau
 // and the whole number M = ceil(max z c): parts of a row that took different M are brought
-// together by exact factors, and z c - M is rounded once.  What a row is needed for is M, S,
-// the values at a few drafted tokens, and, where the walk ends, one argmax over
+// together by exact factors, and z c - M is rounded once.  (Where the walk comes to a row whose
+// largest logit is so far from 0 that z c has no such M, or that is masked altogether, it begins
+// again in a form for any row: far_walk.)  What a row is needed for is M, S, the values at a few drafted tokens, and, where the walk ends, one argmax over
 //   ln r(v) + gumbel(v),   r = what is left of p after the rejected children:
 //   r_0 = p,  r_(k+1)(v) = max(r_k(v) - q(v), 0) / Z_k   (draft with probabilities)
 //                        = r_k(v) / Z_k, 0 at the rejected token  (without)
@@ -35,7 +36,7 @@ using namespace sbd_dev;
 
 constexpr int kMaxNodes = 64;
 constexpr int kMaxCluster = 16;
-constexpr float kLimit = 8388608.f;          // logits over tau stay within 2^23
+constexpr float kLimit = 8388608.f;          // of a largest logit over tau: so far a row is in range
 
 enum Mode { kGreedy, kGiven, kDrawn };       // tau = 0; drafts without, with probabilities
 
@@ -50,7 +51,7 @@ struct Args {
   int n, V, splits;
   int slice;                 // words of a CTA
   int ahead;                 // rows are fetched ahead
-  float scale, limit;        // log2(e) / tau and 2^23 tau (tau 1 where it is 0)
+  float scale, limit;        // log2(e) / tau and kLimit tau (tau 1 where it is 0)
 };
 
 __device__ __forceinline__ float redux_max(float v) {
@@ -196,10 +197,22 @@ __device__ __forceinline__ void reduce(Exchange<kWarps, kN>& x, int& turn, int s
     if (i < count) mine[i] = join(lane < splits ? x.ranks[turn][i][lane] : none);
 }
 
-// M and S of a part of a row.
+// M and S of a part of a row.  A row whose largest logit is beyond the limit, up or down (a
+// small tau, a row of nothing but masked logits), has no whole number M to which z c is exact:
+// it has the largest logit itself in the place of M, and S, of powers of (z - M) c, negative.
 struct Stat {
   float M, S;
 };
+// z against the largest logit m of a row: the distance, 0 or less.  NaN is the least; of
+// infinities the largest are alike and leave nothing to the others.
+__device__ __forceinline__ float below(float z, float m) {
+  if (fabsf(m) == INFINITY) return fmaxf(z, -INFINITY) == m ? 0.f : -INFINITY;
+  return fmaxf(z - m, -INFINITY);
+}
+__device__ __forceinline__ float ln_prob(float z, Stat x, float c2) {
+  const float y = x.S < 0.f ? below(z, x.M) * c2 : fmaf(z, c2, -x.M);
+  return fmaf(y, 0.69314718f, -logf(fabsf(x.S)));
+}
 __device__ __forceinline__ Stat warp_stat(Stat a) {
   const float M = redux_max(a.M);
   return {M, warp_sum(a.S * pow2_diff(a.M - M))};
@@ -228,8 +241,8 @@ __device__ __forceinline__ void take_one(Stat& s, float z, float c2, float limit
   s.S = fmaf(s.S, pow2_diff(s.M - M), ex2_ftz(fmaf(tame(z, limit), c2, -M)));
   s.M = M;
 }
-// M and S of the elements of words w0, w0 + step, ... below w1 one by one, tamed: of a part of
-// a row that has a NaN or a logit beyond the limit in it, or of a row that is low altogether.
+// M and S of the elements of words w0, w0 + step, ... below w1 one by one: of a part of a row
+// that has a NaN in it.  (What is beyond the limit counts as the limit here: it shows in M.)
 template <typename T>
 __device__ __noinline__ Stat slow_stat(const T* elements, int w0, int w1, int step, float c2, float limit) {
   Stat s{-2.f * kLimit, 0.f};
@@ -238,76 +251,117 @@ __device__ __noinline__ Stat slow_stat(const T* elements, int w0, int w1, int st
   return s;
 }
 
-template <typename T, Mode kMode, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDrawn ? 1 : 2) verify_kernel(const Args a) {
-  constexpr int kWarps = kThreads / 32;
+// The stat of a row beyond the limit, in two passes: its largest logit, then the sum.  Every
+// thread of the cluster comes, with the same result.  (It finds its places itself: what would be
+// kept for it costs the walk registers.)
+template <typename T, int kWarps, int kN>
+__device__ __noinline__ Stat far_stat(Exchange<kWarps, kN>& ex, int turn, const T* tensor, long long first, int V, int slice,
+                                      int splits, float c2) {
+  constexpr int kPer = Row<T>::kPer, step = 32 * kWarps;
+  const int split = blockIdx.x, tid = threadIdx.x;
+  const Row<T> row(tensor, first, V);
+  const int from = min(row.c1, row.c0 + split * slice), w1 = min(row.c1, from + slice), w0 = from + tid;
+  const T* edge = split == 0 && tid < row.edges ? tensor + first + row.edge(tid) : nullptr;
+  float m = edge ? fmaxf(value(edge), -INFINITY) : -INFINITY;
+  // (four words in flight, as in the walk)
+  auto words = [&](auto&& f) {
+#pragma unroll 1
+    for (int w = w0; w < w1; w += 4 * step) {
+      uint4 x[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        x[h] = Row<T>::none();
+        if (w + h * step < w1) x[h] = row.load(w + h * step);
+      }
+      f(x, w);
+    }
+  };
+  words([&](const uint4 (&x)[4], int) { m = fmaxf(m, largest(x, (const T*)nullptr)); });
+  float4 part[1] = {make_float4(m, 0.f, 0.f, 0.f)};
+  reduce(ex, turn, splits, 1, part, make_float4(-INFINITY, 0.f, 0.f, 0.f),
+         [](float4 x) { return make_float4(redux_max(x.x), 0.f, 0.f, 0.f); });
+  m = part[0].x;
+  float sum = edge ? ex2_ftz(below(value(edge), m) * c2) : 0.f;
+  words([&](const uint4 (&x)[4], int w) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      float z[kPer], s = 0.f;                // (a word's sum for itself: not one long chain)
+      Row<T>::get(x[h], z);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) s += ex2_ftz(below(z[e], m) * c2);
+      if (w + h * step < w1) sum += s;       // (no words: -inf, which a row of nothing else counts)
+    }
+  });
+  part[0] = make_float4(sum, 0.f, 0.f, 0.f);
+  reduce(ex, turn, splits, 1, part, make_float4(0.f, 0.f, 0.f, 0.f),
+         [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); });
+  return Stat{m, -part[0].x};
+}
+
+// What a CTA has in shared memory.
+template <int kWarps, int kAhead>
+struct Shared {
+  Exchange<kWarps, kAhead> ex;
+  unsigned long long child[kMaxNodes];       // of a node, a bit each
+  int token[kMaxNodes];
+  float uniform[kMaxNodes];
+  float z[kMaxNodes], q[kMaxNodes];          // logits at a child's token: the target's, the draft's
+  float4 stat[kMaxNodes];                    // rows' M and S, of the target and of the draft (greedy: largest, where)
+  int path[kMaxNodes], said[kMaxNodes];      // the walk, told at its end: nodes, tokens,
+  float said_z[kMaxNodes];                   // their logits, and their rows' M and S
+  Stat said_st[kMaxNodes];
+  int rejected[kMaxNodes];                   // tokens
+  float left[kMaxNodes];                     // 1 / Z
+};
+// Where requests are few (512 threads a CTA) a level is a chain of latencies, 2.8 us of one
+// request's 13: so M and S of several rows are made at once, of a node, its first child,
+// that one's first child ..., which the walk is likely to come to, and both rows of a node
+// together.  Where they are many, one row after the other, only as the walk comes to them.
+template <Mode kMode, int kThreads>
+constexpr int rows_ahead() { return kMode == kDrawn && kThreads == 512 ? 2 : 1; }
+
+// The walk; `parent`: of node threadIdx.x.  Returns how many nodes are on the path, all told but
+// for their outputs, or, unless kFar, 0 where it comes to a row beyond the limit.  (Two walks,
+// since the registers and instructions for any row cost the other 3 to 4 us of 50.)
+template <typename T, Mode kMode, int kThreads, bool kFar>
+__device__ __forceinline__ int walk(const Args& a, Shared<kThreads / 32, rows_ahead<kMode, kThreads>()>& sh, int& turn, int parent) {
   using R = Row<T>;
   constexpr int kPer = R::kPer;
-  // Where requests are few (512 threads a CTA) a level is a chain of latencies, 2.8 us of one
-  // request's 14.7: so M and S of several rows are made at once, of a node, its first child,
-  // that one's first child ..., which the walk is likely to come to, and both rows of a node
-  // together.  Where they are many, one row after the other, only as the walk comes to them.
-  constexpr int kAhead = kMode == kDrawn && kThreads == 512 ? 2 : 1;
-  constexpr bool kBoth = kMode == kDrawn && kThreads == 512;
+  constexpr int kAhead = kFar ? 1 : rows_ahead<kMode, kThreads>();
+  constexpr bool kBoth = kAhead == 2;
   constexpr int kHold = kBoth ? 2 : 4;                 // words of a row that a thread has in flight
-  __shared__ Exchange<kWarps, kAhead> ex;
-  __shared__ unsigned long long child_sh[kMaxNodes];   // of a node, a bit each
-  __shared__ int token_sh[kMaxNodes];
-  __shared__ float uniform_sh[kMaxNodes];
-  __shared__ float z_sh[kMaxNodes], q_sh[kMaxNodes];   // logits at a child's token: the target's, the draft's
-  __shared__ float4 stat_sh[kMaxNodes];                // rows' M and S, of the target and of the draft (greedy: largest, where)
-  __shared__ int path_sh[kMaxNodes], said_sh[kMaxNodes];     // the walk, told at its end: nodes, tokens,
-  __shared__ float said_z_sh[kMaxNodes];                     // their logits, and their rows' M and S
-  __shared__ Stat said_st_sh[kMaxNodes];
-  __shared__ int rejected_sh[kMaxNodes];               // tokens
-  __shared__ float left_sh[kMaxNodes];                 // 1 / Z
-  if (a.splits > 1) cluster_sync();          // every CTA is there before one writes into another
-  grid_dependency_wait();
-  const int split = blockIdx.x, b = blockIdx.y, n = a.n, V = a.V, tid = threadIdx.x, lane = tid & 31;
+  const int split = blockIdx.x, b = blockIdx.y, n = a.n, V = a.V, tid = threadIdx.x;
   const T* target = (const T*)a.target;
   const T* draft = (const T*)a.draft;
   const size_t out = (size_t)b * n;
-  if (tid < kMaxNodes) child_sh[tid] = 0;
-  __syncthreads();
-  int parent = -1;                           // of node tid
-  if (tid < n) {
-    const int p = a.parent[out + tid];
-    bool bad = p >= tid;
-    if (!bad && tid > 0 && p >= 0) {
-      const int x = a.token[out + tid];
-      token_sh[tid] = x;
-      bad = x < 0 || x >= V;                 // passed over
-      if (kMode != kGreedy) uniform_sh[tid] = a.uniform[out + tid];
-      if (!bad) parent = p, atomicOr(&child_sh[p], 1ull << tid);
-    }
-    if (bad && split == 0) record_error(a.err, SBD_DEVERR_TREE);
-  }
-  __syncthreads();
-  int turn = 0, node = 0, count = 1;
-  // The walk's noise on its way to L2 (and below, a row ahead).
-  if (kMode != kGreedy) {
-    const float* g = a.gumbel + (size_t)b * V;
-    const int part = (V + a.splits - 1) / a.splits, v1 = min(V, (split + 1) * part);
-    for (int v = split * part + tid * 32; v < v1; v += kThreads * 32) prefetch_l2(g + v);
-  }
+  int node = 0, count = 1;
   const float c2 = a.scale;
   auto tame = [&](float z) { return ::tame(z, a.limit); };
-  // A row's M below the one: of nothing but masked logits; from the other on: logits beyond the limit.
+  // A row's M below the one: its largest logit is beyond the limit, or it has none; from the
+  // other on: beyond it on the other side.  In range a logit below the limit counts nothing.
   const float low = 256.f - a.limit * c2, high = a.limit * c2 - 1.f;
   auto is_out = [&](float M) { return M < low || M >= high; };
   unsigned long long known = 0;              // nodes whose rows' M and S are known
   while (true) {
-    const unsigned long long children = child_sh[node];
+    const unsigned long long children = sh.child[node];
     const bool use_q = kMode == kDrawn && children != 0;
     // ---- M and S of the row (and of the draft's, where it is asked for)
     Stat st, sq;
     Best best;
-    if (kAhead == 1 || !(known >> node & 1)) {
+    if constexpr (kFar) {
+      if (parent == node) {                  // a child's logits (behind a barrier when they are read)
+        const long long at = ((long long)b * n + node) * V + sh.token[tid];
+        sh.z[tid] = value(target + at);
+        if (kMode == kDrawn) sh.q[tid] = value(draft + at);
+      }
+      st = far_stat<T>(sh.ex, turn, target, ((long long)b * n + node) * V, V, a.slice, a.splits, c2);
+      if (use_q) sq = far_stat<T>(sh.ex, turn, draft, ((long long)b * n + node) * V, V, a.slice, a.splits, c2);
+    } else if (kAhead == 1 || !(known >> node & 1)) {
       int list[kAhead] = {node}, several = 1;
       unsigned long long in = 1ull << node;
 #pragma unroll
       for (int i = 1; i < kAhead; ++i) {
-        const unsigned long long c = child_sh[list[i - 1]];
+        const unsigned long long c = sh.child[list[i - 1]];
         list[i] = c ? __ffsll(c) - 1 : list[i - 1];
         if (c) several = i + 1, in |= 1ull << list[i];
       }
@@ -317,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       const bool is_child = kMode != kGreedy && parent >= 0 && in >> parent & 1;
       float child_z = 0.f, child_q = 0.f;
       if (is_child) {
-        const long long at = ((long long)b * n + parent) * V + token_sh[tid];
+        const long long at = ((long long)b * n + parent) * V + sh.token[tid];
         child_z = value(target + at);
         if (kMode == kDrawn) child_q = value(draft + at);
       }
@@ -326,8 +380,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) t[i] = d[i] = Stat{-2.f * kLimit, 0.f}, top[i] = Best{NAN, 0x7fffffff};
       // As they are: a NaN shows in the sum, and the thread's share is taken again, slowly.  A
-      // logit beyond the limit shows in M (what is only just beyond leaves the sum finite), and
-      // the row is taken again, as is one that is low altogether.
+      // logit beyond the limit shows in M (what is only just beyond leaves the sum finite), as
+      // does a row that is low altogether.
       auto take = [&](Stat& s, const uint4 (&x)[kHold]) {
         const float M = fmaxf(s.M, ceilf(tame(largest(x, (const T*)nullptr)) * c2));
         float2 sum = make_float2(0.f, 0.f);
@@ -348,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       R place[kAhead];
       long long first[kAhead];
       int from[kAhead], to[kAhead];
-      auto has_q = [&](int i) { return kMode == kDrawn && child_sh[list[i]] != 0; };
+      auto has_q = [&](int i) { return kMode == kDrawn && sh.child[list[i]] != 0; };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         if (i >= rows) continue;
@@ -414,13 +468,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       if (kAhead == 1 && a.ahead && children) {
         const int c = __ffsll(children) - 1;
         const T* there = place[0].base + (long long)(c - node) * V;
-        const bool its_q = kMode == kDrawn && child_sh[c] != 0;
+        const bool its_q = kMode == kDrawn && sh.child[c] != 0;
         for (int w = from[0] + tid * 8; w < to[0]; w += kThreads * 8) {        // a line each
           prefetch_l2(there + (long long)w * kPer);
           if (its_q) prefetch_l2(reinterpret_cast<const char*>(there + (long long)w * kPer) + to_draft);
         }
       }
-      if (is_child) z_sh[tid] = tame(child_z), q_sh[tid] = tame(child_q);
+      if (is_child) sh.z[tid] = child_z, sh.q[tid] = child_q;
       float4 mine[kAhead];
       const float4 none = make_float4(-2.f * kLimit, 0.f, kMode == kGreedy ? -INFINITY : -2.f * kLimit,
                                       __int_as_float(kMode == kGreedy ? 0x7fffffff : 0));
@@ -435,20 +489,20 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
         return make_float4(t.M, t.S, q.M, q.S);
       };
       // The rest of a row's share: slowly what has to be, and the thread's edge.
-      auto finish = [&](int i, bool slow) {
+      auto finish = [&](int i) {
         const R& r = place[i];
         const T* row_t = target + first[i];
         const T* row_d = draft + first[i];
         const int edge = kAhead == 1 ? edge0 : split == 0 && tid < r.edges ? r.edge(tid) : -1;
-        if (slow || !(t[i].S < INFINITY)) t[i] = slow_stat<T>(row_t - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
-        if (has_q(i) && (slow || !(d[i].S < INFINITY))) d[i] = slow_stat<T>(row_d - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
+        if (!(t[i].S < INFINITY)) t[i] = slow_stat<T>(row_t - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
+        if (has_q(i) && !(d[i].S < INFINITY)) d[i] = slow_stat<T>(row_d - r.shift, from[i] + tid, to[i], kThreads, c2, a.limit);
         if (edge >= 0) {
           const float z = kAhead == 1 ? edge_z : value(row_t + edge);
           take_one(t[i], z, c2, a.limit);
           if (has_q(i)) take_one(d[i], kAhead == 1 ? edge_q : value(row_d + edge), c2, a.limit);
-          if (kMode == kGreedy && !slow) top[i] = better(Best{fmaxf(z, -INFINITY), edge}, top[i]);
+          if (kMode == kGreedy) top[i] = better(Best{fmaxf(z, -INFINITY), edge}, top[i]);
         }
-        if (kMode == kGreedy && !slow) {               // the element of the best word
+        if (kMode == kGreedy) {                        // the element of the best word
           if (top[i].v == 0x7fffffff) top[i].score = -INFINITY;
           const int v = top[i].v;
           if (top[i].score == redux_max(top[i].score) && v >= r.element(from[i]) && v < r.element(to[i])) {
@@ -464,25 +518,16 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        if (i < rows) finish(i, false);
-      reduce(ex, turn, a.splits, rows, mine, none, join);
-      // (each for itself: a row's sums do not depend on the row beside it)
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        if (i >= rows || !(is_out(mine[i].x) || (has_q(i) && is_out(mine[i].z)))) continue;
-        finish(i, true);
-        float4 one[1] = {mine[i]};
-        reduce(ex, turn, a.splits, 1, one, none, join);
-        mine[i] = one[0];
-      }
+        if (i < rows) finish(i);
+      reduce(sh.ex, turn, a.splits, rows, mine, none, join);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        if (kAhead > 1 && i < rows && tid == 0) stat_sh[list[i]] = mine[i];
+        if (kAhead > 1 && i < rows && tid == 0) sh.stat[list[i]] = mine[i];
       if (kAhead > 1) __syncthreads();
       else st = Stat{mine[0].x, mine[0].y}, sq = Stat{mine[0].z, mine[0].w}, best = Best{mine[0].z, __float_as_int(mine[0].w)};
     }
     if (kAhead > 1) {
-      const float4 x = stat_sh[node];
+      const float4 x = sh.stat[node];
       st = Stat{x.x, x.y}, sq = Stat{x.z, x.w}, best = Best{x.z, __float_as_int(x.w)};
     }
     const long long first = ((long long)b * n + node) * V;
@@ -491,32 +536,36 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
     const int edge = split == 0 && tid < row.edges ? row.edge(tid) : -1;   // this thread's
     const T* target_row = target + first;
     const T* draft_row = draft + first;
-    const float inv_s = __fdividef(1.f, st.S), inv_q = __fdividef(1.f, sq.S);   // (S is in 1/2 .. 2^31)
-    auto prob = [&](float z) { return ex2_ftz(fmaf(z, c2, -st.M)) * inv_s; };
-    auto prob_q = [&](float z) { return ex2_ftz(fmaf(z, c2, -sq.M)) * inv_q; };
-    // A row whose logits are within the limit needs no taming of single ones but NaN.
-    const bool tamed = !is_out(st.M) && (!use_q || !is_out(sq.M));
+    if (!kFar && (is_out(st.M) || (use_q && is_out(sq.M)))) {
+      if (kMode != kGreedy) return 0;
+      // (of a greedy walk the row's law is only told)
+      st = far_stat<T>(sh.ex, turn, target, first, V, a.slice, a.splits, c2);
+    }
+    const float inv_s = __fdividef(1.f, fabsf(st.S)), inv_q = __fdividef(1.f, fabsf(sq.S));   // (S is in 1/2 .. 2^31)
+    // log2 of what a logit counts, S not taken off (NaN: NaN, or -inf)
+    auto log2_p = [&](float z) { return kFar ? below(z, st.M) * c2 : fmaf(z, c2, -st.M); };
+    auto log2_q = [&](float z) { return kFar ? below(z, sq.M) * c2 : fmaf(z, c2, -sq.M); };
+    auto prob = [&](float z) { return fmaxf(ex2_ftz(log2_p(z)), 0.f) * inv_s; };             // (NaN: 0)
+    auto prob_q = [&](float z) { return fmaxf(ex2_ftz(log2_q(z)), 0.f) * inv_q; };
     // What is left of p at elements v, v + 1, ... after the first k rejections (and one more,
     // `after`), times S and not normalised by the last ones' sum.
-    const float q_of_p = inv_q * st.S;
+    const float q_of_p = inv_q * fabsf(st.S);
     auto remainder = [&](float (&z)[kPer], float (&q)[kPer], int v, int k, bool after, float (&r)[kPer]) {
-      if (!tamed) {
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) z[e] = tame(z[e]), q[e] = kMode == kDrawn ? tame(q[e]) : 0.f;
-      }
 #pragma unroll
       for (int e = 0; e < kPer; e += 2) {
-        float2 x = fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-st.M, -st.M));
+        float2 x = kFar ? make_float2(log2_p(z[e]), log2_p(z[e + 1]))
+                        : fma2(make_float2(z[e], z[e + 1]), make_float2(c2, c2), make_float2(-st.M, -st.M));
         r[e] = ex2_ftz(x.x), r[e + 1] = ex2_ftz(x.y);
         if (kMode == kDrawn) {
-          x = fma2(make_float2(q[e], q[e + 1]), make_float2(c2, c2), make_float2(-sq.M, -sq.M));
+          x = kFar ? make_float2(log2_q(q[e]), log2_q(q[e + 1]))
+                   : fma2(make_float2(q[e], q[e + 1]), make_float2(c2, c2), make_float2(-sq.M, -sq.M));
           q[e] = fmaxf(ex2_ftz(x.x), 0.f), q[e + 1] = fmaxf(ex2_ftz(x.y), 0.f);      // (NaN: 0)
         }
       }
       if (kMode == kDrawn) {
 #pragma unroll 1
         for (int i = 0; i < k; ++i) {
-          const float f = left_sh[i];
+          const float f = sh.left[i];
 #pragma unroll
           for (int e = 0; e < kPer; ++e) r[e] = fmaxf(fmaf(-q_of_p, q[e], r[e]), 0.f) * f;
         }
@@ -527,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
         for (int e = 0; e < kPer; ++e) r[e] = fmaxf(r[e], 0.f);
 #pragma unroll 1
         for (int i = 0; i < k + after; ++i) {
-          const uint32_t at = (uint32_t)(rejected_sh[i] - v);
+          const uint32_t at = (uint32_t)(sh.rejected[i] - v);
           if (at < kPer) {
 #pragma unroll
             for (int e = 0; e < kPer; ++e) r[e] = e == (int)at ? 0.f : r[e];
@@ -586,9 +635,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
     int k = 0;                               // rejections whose remainder is known
     bool pending = false;                    // one more, of which nothing is known yet
     if (kMode == kGreedy) {
-      said = best.v == 0x7fffffff ? 0 : best.v, said_z = tame(best.score);   // (nothing but NaN: 0)
+      said = best.v == 0x7fffffff ? 0 : best.v, said_z = best.score;   // (nothing but NaN: 0)
       for (unsigned long long c = children; c && next < 0; c &= c - 1)
-        if (token_sh[__ffsll(c) - 1] == said) next = __ffsll(c) - 1;
+        if (sh.token[__ffsll(c) - 1] == said) next = __ffsll(c) - 1;
     } else {
       for (unsigned long long todo = children; todo && next < 0; todo &= todo - 1) {
         const int c = __ffsll(todo) - 1;
@@ -602,37 +651,37 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
             for (int e = 0; e < kPer; ++e) sum += e < places ? r[e] : 0.f;
           });
           float4 part[1] = {make_float4(sum, 0.f, 0.f, 0.f)};
-          reduce(ex, turn, a.splits, 1, part, make_float4(0.f, 0.f, 0.f, 0.f),
+          reduce(sh.ex, turn, a.splits, 1, part, make_float4(0.f, 0.f, 0.f, 0.f),
                  [](float4 x) { return make_float4(warp_sum(x.x), 0.f, 0.f, 0.f); });
           const float total = part[0].x * inv_s;
           if (total > 0.f) {
-            if (tid == 0) left_sh[k] = 1.f / total;
+            if (tid == 0) sh.left[k] = 1.f / total;
             __syncthreads();
             ++k;
           }
           pending = false;
         }
         // r(x): step by step with a draft's probabilities; without, p(x) over what is left of it
-        const int x = token_sh[c];
-        const float q = kMode == kDrawn ? prob_q(q_sh[c]) : 1.f;
-        float r = prob(z_sh[c]);
+        const int x = sh.token[c];
+        const float q = kMode == kDrawn ? prob_q(sh.q[c]) : 1.f;
+        float r = prob(sh.z[c]);
         for (int i = 0; i < k; ++i) {
-          if (kMode == kDrawn) r = fmaxf(r - q, 0.f) * left_sh[i];
-          else if (x == rejected_sh[i]) r = 0.f;
+          if (kMode == kDrawn) r = fmaxf(r - q, 0.f) * sh.left[i];
+          else if (x == sh.rejected[i]) r = 0.f;
         }
-        if (kMode == kGiven && k > 0) r *= left_sh[k - 1];
-        if (uniform_sh[c] * q < r) {
-          next = c, said = x, said_z = z_sh[c];
+        if (kMode == kGiven && k > 0) r *= sh.left[k - 1];
+        if (sh.uniform[c] * q < r) {
+          next = c, said = x, said_z = sh.z[c];
         } else {
           __syncthreads();                   // (what was here is read)
-          if (tid == 0) rejected_sh[k] = x;
+          if (tid == 0) sh.rejected[k] = x;
           __syncthreads();
           pending = true;
         }
       }
     }
     if (next >= 0) {
-      if (tid == 0) path_sh[count] = next, said_sh[count - 1] = said, said_z_sh[count - 1] = said_z, said_st_sh[count - 1] = st;
+      if (tid == 0) sh.path[count] = next, sh.said[count - 1] = said, sh.said_z[count - 1] = said_z, sh.said_st[count - 1] = st;
       ++count;
       node = next;
       continue;
@@ -645,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
       auto evaluate = [&](float (&z)[kPer], float (&q)[kPer], float (&score)[kPer], int v) {
         if (k == 0 && !after) {
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) score[e] = fmaf(fmaf(tame(z[e]), c2, -st.M), 0.69314718f, score[e]);
+          for (int e = 0; e < kPer; ++e) score[e] = fmaf(log2_p(z[e]), 0.69314718f, score[e]);
         } else {
           float r[kPer];
           remainder(z, q, v, k, after, r);
@@ -667,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
              });
         if (best.v == 0x7fffffff) best.score = -INFINITY;
         float4 part[1] = {make_float4(best.score, __int_as_float(best.v), 0.f, 0.f)};
-        reduce(ex, turn, a.splits, 1, part, make_float4(-INFINITY, __int_as_float(0x7fffffff), 0.f, 0.f), [](float4 x) {
+        reduce(sh.ex, turn, a.splits, 1, part, make_float4(-INFINITY, __int_as_float(0x7fffffff), 0.f, 0.f), [](float4 x) {
           const Best y = warp_best(Best{x.x, __float_as_int(x.y)});
           return make_float4(y.score, __int_as_float(y.v), 0.f, 0.f);
         });
@@ -694,23 +743,67 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDraw
           said_z = value(target_row + said);
         }
         a.out_tokens[out + count - 1] = said;
-        a.logprob[out + count - 1] = fmaf(fmaf(tame(said_z), c2, -st.M), 0.69314718f, -logf(st.S));
+        a.logprob[out + count - 1] = ln_prob(said_z, st, c2);
       }
     }
     else if (tid == 0) {
-      said_sh[count - 1] = said, said_z_sh[count - 1] = said_z, said_st_sh[count - 1] = st;
+      sh.said[count - 1] = said, sh.said_z[count - 1] = said_z, sh.said_st[count - 1] = st;
     }
     break;
   }
+  return count;
+}
+
+// The walk in the form for any row: every row's largest logit first, in a pass of its own.  (64
+// requests at tau = 1e-6, whose rows are all beyond the limit: 84 us, 43 at tau = 1.)
+template <typename T, Mode kMode, int kThreads>
+__device__ __noinline__ int far_walk(const Args& a, Shared<kThreads / 32, rows_ahead<kMode, kThreads>()>& sh, int turn, int parent) {
+  __syncthreads();                           // (what the other walk left is read)
+  return walk<T, kMode, kThreads, true>(a, sh, turn, parent);
+}
+
+template <typename T, Mode kMode, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kMode == kDrawn ? 1 : 2) verify_kernel(const __grid_constant__ Args a) {
+  __shared__ Shared<kThreads / 32, rows_ahead<kMode, kThreads>()> sh;
+  if (a.splits > 1) cluster_sync();          // every CTA is there before one writes into another
+  grid_dependency_wait();
+  const int split = blockIdx.x, b = blockIdx.y, n = a.n, V = a.V, tid = threadIdx.x;
+  const size_t out = (size_t)b * n;
+  if (tid < kMaxNodes) sh.child[tid] = 0;
+  __syncthreads();
+  int parent = -1;                           // of node tid
+  if (tid < n) {
+    const int p = a.parent[out + tid];
+    bool bad = p >= tid;
+    if (!bad && tid > 0 && p >= 0) {
+      const int x = a.token[out + tid];
+      sh.token[tid] = x;
+      bad = x < 0 || x >= V;                 // passed over
+      if (kMode != kGreedy) sh.uniform[tid] = a.uniform[out + tid];
+      if (!bad) parent = p, atomicOr(&sh.child[p], 1ull << tid);
+    }
+    if (bad && split == 0) record_error(a.err, SBD_DEVERR_TREE);
+  }
+  __syncthreads();
+  // The walk's noise on its way to L2 (and below, a row ahead).
+  if (kMode != kGreedy) {
+    const float* g = a.gumbel + (size_t)b * V;
+    const int part = (V + a.splits - 1) / a.splits, v1 = min(V, (split + 1) * part);
+    for (int v = split * part + tid * 32; v < v1; v += kThreads * 32) prefetch_l2(g + v);
+  }
+  int turn = 0;
+  int count = walk<T, kMode, kThreads, false>(a, sh, turn, parent);
+  if constexpr (kMode != kGreedy)
+    if (count == 0) count = far_walk<T, kMode, kThreads>(a, sh, turn, parent);
   grid_dependents_launch();
   if (split != 0) return;
   __syncthreads();
   if (tid < n) {
     const bool on = tid < count;
-    a.path[out + tid] = !on ? -1 : tid == 0 ? 0 : path_sh[tid];
+    a.path[out + tid] = !on ? -1 : tid == 0 ? 0 : sh.path[tid];
     if (kMode == kGreedy || tid != count - 1) {          // (the last token is told already)
-      a.out_tokens[out + tid] = on ? said_sh[tid] : -1;
-      a.logprob[out + tid] = on ? fmaf(fmaf(said_z_sh[tid], c2, -said_st_sh[tid].M), 0.69314718f, -logf(said_st_sh[tid].S)) : 0.f;
+      a.out_tokens[out + tid] = on ? sh.said[tid] : -1;
+      a.logprob[out + tid] = on ? ln_prob(sh.said_z[tid], sh.said_st[tid], a.scale) : 0.f;
     }
     if (tid == 0) a.count[b] = count;
   }
