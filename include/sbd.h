@@ -600,7 +600,9 @@ sbd_status sbd_verify_tree(const sbd_verify_desc* desc, const void* target_logit
  *                                 as sbd_verify_tree and sbd_block_tables give them
  *
  * Segments, scales, codes and errors are those of sbd_cache_append_q8; a slot that is
- * negative or past max_new is not stored.  Requests do not share the pages they append to.
+ * negative or past max_new is not stored.  Where that, or an entry that is not stored, cuts a
+ * run in two, the second segment enters as by a call after the first's.  Requests do not
+ * share the pages they append to.
  * Supported: 1 <= n <= 64, B <= 65535, strides that are multiples of 16 bytes.
  * ---------------------------------------------------------------------- */
 typedef struct {

@@ -509,6 +509,8 @@ __global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8
 // Tokens have their maxima from shuffles and segments theirs from atomics in shared memory,
 // so that however many segments there are it is one chain: the starts and the path -> the
 // rows, the slots -> old scales -> codes, then earlier codes where a page's scale grew.
+// Segments of one page (an entry between them is not stored) take turns: what the first writes
+// is the second's old scale and earlier codes.
 // Bound: latency.  16 requests of up to four accepted nodes 3.7 us, of which a launch 2; 200
 // requests of up to 33 in fp32, 1600 CTAs, 6.0 (a segment after the other 12.2; segments found
 // by walking back token by token 9.9).
@@ -525,39 +527,133 @@ struct PathArgs {
   int nodes, max_new, Hkv, log2P;
 };
 
+// What a CTA knows of its tokens; of segments, at their beginnings.
+struct PathShared {
+  int slot[kMaxNodes], node[kMaxNodes];
+  int begin[kMaxNodes];                      // of a token's segment, -1: not stored
+  uint32_t joins[2], starts[2];              // tokens that go on with a segment; that begin one
+  uint32_t moved[2];                         // segments whose page's scale grew
+  int max[kMaxNodes];                        // a segment's max |x| (its bits)
+  float scale[kMaxNodes][2];                 // its scale before and after
+  int turn[kMaxNodes];                       // how many segments of its page come before it
+  int several;                               // a page has more than one
+};
+// A CTA's plane of the cache and of the new tokens.
 template <typename T, int D>
-__global__ void __launch_bounds__(kPathThreads) append_path_q8_kernel(const PathArgs a) {
-  constexpr int kUnits = D / 8;              // units of a row
+struct Plane {
+  static constexpr int kUnits = D / 8;       // units of a row
+  uint8_t* cache;
+  float* scales;
+  const T* src;                              // this thread's unit of node 0
+  long long stride;
+  int h, log2P, last, Hkv;
+  __device__ __forceinline__ Plane(const PathArgs& a) {
+    const bool is_v = (int)blockIdx.x >= a.Hkv;
+    const int b = blockIdx.y;
+    h = is_v ? blockIdx.x - a.Hkv : blockIdx.x;
+    log2P = a.log2P, last = (1 << a.log2P) - 1, Hkv = a.Hkv;
+    cache = is_v ? a.v_cache : a.k_cache;
+    scales = is_v ? a.v_scale : a.k_scale;
+    src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)h * D + b * (is_v ? a.v_batch_stride : a.k_batch_stride) +
+          threadIdx.x % kUnits * 8;
+    stride = is_v ? a.v_node_stride : a.k_node_stride;
+  }
+  __device__ __forceinline__ float& scale_of(int slot) const { return scales[(long long)(slot >> log2P) * Hkv + h]; }
+  // Of the segments whose turn it is (`mine`: this thread's token begins one) the scales, and
+  // which of them grew.
+  __device__ __forceinline__ void settle(PathShared& sh, bool mine) const {
+    const int tid = threadIdx.x;
+    if (tid < kMaxNodes) {
+      bool moved = false;
+      if (mine) {
+        const float s = fmaxf(sh.scale[tid][0], scale_for(__int_as_float(sh.max[tid])));
+        sh.scale[tid][1] = s;
+        scale_of(sh.slot[tid]) = s;
+        moved = (sh.slot[tid] & last) && s != sh.scale[tid][0];
+      }
+      const uint32_t all = __ballot_sync(0xffffffffu, moved);
+      if (tid % 32 == 0) sh.moved[tid / 32] = all;
+    }
+    __syncthreads();
+  }
+  // This thread's unit of token j, whose segment begins at j0, into its place.
+  __device__ __forceinline__ void store(const PathShared& sh, const Eight<T>& v, int j, int j0) const {
+    const float s = sh.scale[j0][1];
+    // s is a power of two unless a caller's own scale is kept: then the products are exact
+    const bool exact = (__float_as_uint(s) & 0x007fffffu) == 0;
+    const float inv = 1.f / s;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = exact ? v.get(i) * inv : v.get(i) / s;
+    const int slot = sh.slot[j];
+    uint8_t* dst = cache + ((((long long)(slot >> log2P) * Hkv + h) << log2P) + (slot & last)) * D;
+    *reinterpret_cast<uint2*>(dst + threadIdx.x % kUnits * 8) =
+        make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
+  }
+  // Pages' earlier codes move to the new scale.
+  __device__ __forceinline__ void move(const PathShared& sh) const {
+#pragma unroll 1
+    for (uint64_t todo = sh.moved[0] | (uint64_t)sh.moved[1] << 32; todo; todo &= todo - 1) {
+      const int j = __ffsll(todo) - 1, off = sh.slot[j] & last;
+      const float f = sh.scale[j][0] / sh.scale[j][1];
+      uint8_t* dst = cache + (((long long)(sh.slot[j] >> log2P) * Hkv + h) << log2P) * D;
+#pragma unroll 4
+      for (int u = threadIdx.x; u < off * D / 16; u += kPathThreads) {
+        uint4 c = *reinterpret_cast<const uint4*>(dst + 16 * u);
+        c.x = e4m3x4_times(c.x, f), c.y = e4m3x4_times(c.y, f);
+        c.z = e4m3x4_times(c.z, f), c.w = e4m3x4_times(c.w, f);
+        *reinterpret_cast<uint4*>(dst + 16 * u) = c;
+      }
+    }
+  }
+};
+
+// The segments that are not their page's first, in turns, their rows read again (behind a
+// call: what these need kept in every call's registers cost 0.5 us of 6).
+template <typename T, int D>
+__device__ __noinline__ void later_segments(const PathArgs& a, PathShared& sh) {
+  using P = Plane<T, D>;
+  const P plane(a);
+  const int tid = threadIdx.x;
+  const int turn = tid < kMaxNodes && sh.begin[tid] == tid ? sh.turn[tid] : 0;
+#pragma unroll 1
+  for (int t = 1; __syncthreads_or(turn >= t); ++t) {          // (behind it: what the turn before wrote)
+    if (turn == t) sh.scale[tid][0] = (sh.slot[tid] & plane.last) ? plane.scale_of(sh.slot[tid]) : 0.f;
+    plane.settle(sh, turn == t);
+#pragma unroll 1
+    for (int j = tid / P::kUnits; j < kMaxNodes; j += kPathThreads / P::kUnits) {
+      const int j0 = sh.begin[j];
+      if (j0 < 0 || sh.turn[j0] != t) continue;
+      Eight<T> v;
+      v.load(plane.src + sh.node[j] * plane.stride);
+      plane.store(sh, v, j, j0);
+    }
+    plane.move(sh);
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kPathThreads) append_path_q8_kernel(const __grid_constant__ PathArgs a) {
+  using P = Plane<T, D>;
+  constexpr int kUnits = P::kUnits;
   constexpr int kStep = kPathThreads / kUnits;         // tokens of a turn
   constexpr int kHold = kMaxNodes / kStep;             // units a thread has
-  __shared__ int slot_sh[kMaxNodes];
-  __shared__ int node_sh[kMaxNodes];
-  __shared__ int begin_sh[kMaxNodes];        // of a token's segment, -1: not stored
-  __shared__ uint32_t joins_sh[2], moved_sh[2];        // tokens that go on with a segment; segments whose page's scale grew
-  __shared__ int max_sh[kMaxNodes];          // a segment's max |x| (its bits), at its beginning
-  __shared__ float scale_sh[kMaxNodes][2];   // a segment's scale before and after
+  __shared__ PathShared sh;
   grid_dependency_wait();
-  const int tid = threadIdx.x;
-  const bool is_v = (int)blockIdx.x >= a.Hkv;
-  const int h = is_v ? blockIdx.x - a.Hkv : blockIdx.x, b = blockIdx.y;
-  const int last = (1 << a.log2P) - 1;
+  const P plane(a);
+  const int tid = threadIdx.x, b = blockIdx.y;
   const int node = tid < a.nodes ? a.path[(size_t)b * a.nodes + tid] : -1;
   const long long from = a.new_start[b];
   const int m = (int)max(0ll, min((long long)a.nodes, a.new_start[b + 1] - from));
-  uint8_t* cache = is_v ? a.v_cache : a.k_cache;
-  float* scales = is_v ? a.v_scale : a.k_scale;
   const bool in_tree = (uint32_t)node < (uint32_t)a.nodes;
-  if (tid < kMaxNodes) node_sh[tid] = tid < m && in_tree ? node : -1;
+  if (tid < kMaxNodes) sh.node[tid] = tid < m && in_tree ? node : -1;
   __syncthreads();
-  const T* src = (const T*)(is_v ? a.v_new : a.k_new) + (long long)h * D +
-                 b * (is_v ? a.v_batch_stride : a.k_batch_stride) + tid % kUnits * 8;
-  const long long stride = is_v ? a.v_node_stride : a.k_node_stride;
   const int mine = tid / kUnits;             // its tokens: mine, mine + kStep, ...
   Eight<T> hold[kHold];
 #pragma unroll
   for (int e = 0; e < kHold; ++e) {
-    const int at = node_sh[mine + e * kStep];
-    if (at >= 0) hold[e].load(src + at * stride);
+    const int at = sh.node[mine + e * kStep];
+    if (at >= 0) hold[e].load(plane.src + at * plane.stride);
   }
   if (tid < kMaxNodes) {
     const long long at = from + tid;
@@ -570,30 +666,40 @@ __global__ void __launch_bounds__(kPathThreads) append_path_q8_kernel(const Path
       if (blockIdx.x == 0) record_error(a.err, SBD_DEVERR_TREE);
       slot = -1;
     }
-    slot_sh[tid] = max(slot, -1);
-    max_sh[tid] = 0;
+    sh.slot[tid] = max(slot, -1);
+    sh.max[tid] = 0;
+    if (tid == 0) sh.several = 0;
   }
   __syncthreads();
   if (tid < kMaxNodes) {
-    const int slot = slot_sh[tid], before = tid > 0 ? slot_sh[tid - 1] : -1;
-    const uint32_t joins = __ballot_sync(0xffffffffu, slot >= 0 && before >= 0 && before + 1 == slot && (slot & last) != 0);
-    if (tid % 32 == 0) joins_sh[tid / 32] = joins;
+    const int slot = sh.slot[tid], before = tid > 0 ? sh.slot[tid - 1] : -1;
+    const uint32_t joins = __ballot_sync(0xffffffffu, slot >= 0 && before >= 0 && before + 1 == slot && (slot & plane.last) != 0);
+    const uint32_t starts = __ballot_sync(0xffffffffu, slot >= 0) & ~joins;
+    if (tid % 32 == 0) sh.joins[tid / 32] = joins, sh.starts[tid / 32] = starts;
   }
   __syncthreads();
-  int begin = -1;
+  int begin = -1, turn = 0;
+  float old = 0.f;
   if (tid < kMaxNodes) {
-    const uint64_t joins = joins_sh[0] | (uint64_t)joins_sh[1] << 32;
+    const uint64_t joins = sh.joins[0] | (uint64_t)sh.joins[1] << 32;
     begin = 63 - __clzll(~joins & ((2ull << tid) - 1));          // (token 0 never joins)
-    if (slot_sh[tid] < 0) begin = -1;
-    begin_sh[tid] = begin;
-    if (begin == tid)
-      scale_sh[tid][0] = (slot_sh[tid] & last) ? scales[(long long)(slot_sh[tid] >> a.log2P) * a.Hkv + h] : 0.f;
+    if (sh.slot[tid] < 0) begin = -1;
+    sh.begin[tid] = begin;
+    if (begin == tid) {
+      if (sh.slot[tid] & plane.last) old = plane.scale_of(sh.slot[tid]);
+      // (while that is on its way)
+      const uint64_t starts = sh.starts[0] | (uint64_t)sh.starts[1] << 32;
+      for (uint64_t before = starts & ((1ull << tid) - 1); before; before &= before - 1)
+        turn += (sh.slot[__ffsll(before) - 1] ^ sh.slot[tid]) >> plane.log2P == 0;
+      sh.turn[tid] = turn;
+      if (turn > 0) sh.several = 1;
+    }
   }
   float size[kHold];
 #pragma unroll
   for (int e = 0; e < kHold; ++e) {
     size[e] = 0.f;
-    if (node_sh[mine + e * kStep] >= 0) {
+    if (sh.node[mine + e * kStep] >= 0) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) size[e] = fmaxf(size[e], finite_size(hold[e].get(i)));
     }
@@ -604,54 +710,21 @@ __global__ void __launch_bounds__(kPathThreads) append_path_q8_kernel(const Path
   if (tid % kUnits == 0) {
 #pragma unroll
     for (int e = 0; e < kHold; ++e) {
-      const int j0 = begin_sh[mine + e * kStep];
-      if (j0 >= 0) atomicMax(&max_sh[j0], __float_as_int(size[e]));
+      const int j0 = sh.begin[mine + e * kStep];
+      if (j0 >= 0) atomicMax(&sh.max[j0], __float_as_int(size[e]));
     }
   }
+  if (begin == tid) sh.scale[tid][0] = old;
   __syncthreads();
-  if (tid < kMaxNodes) {
-    bool moved = false;
-    if (begin == tid) {
-      const float s = fmaxf(scale_sh[tid][0], scale_for(__int_as_float(max_sh[tid])));
-      scale_sh[tid][1] = s;
-      scales[(long long)(slot_sh[tid] >> a.log2P) * a.Hkv + h] = s;
-      moved = (slot_sh[tid] & last) && s != scale_sh[tid][0];
-    }
-    const uint32_t all = __ballot_sync(0xffffffffu, moved);
-    if (tid % 32 == 0) moved_sh[tid / 32] = all;
-  }
-  __syncthreads();
+  const bool several = sh.several;
+  plane.settle(sh, begin == tid && turn == 0);
 #pragma unroll
   for (int e = 0; e < kHold; ++e) {
-    const int j = mine + e * kStep, j0 = begin_sh[j];
-    if (j0 < 0) continue;
-    const float s = scale_sh[j0][1];
-    // s is a power of two unless a caller's own scale is kept: then the products are exact
-    const bool exact = (__float_as_uint(s) & 0x007fffffu) == 0;
-    const float inv = 1.f / s;
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = exact ? hold[e].get(i) * inv : hold[e].get(i) / s;
-    const int slot = slot_sh[j];
-    uint8_t* dst = cache + ((((long long)(slot >> a.log2P) * a.Hkv + h) << a.log2P) + (slot & last)) * D;
-    *reinterpret_cast<uint2*>(dst + tid % kUnits * 8) =
-        make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
+    const int j = mine + e * kStep, j0 = sh.begin[j];
+    if (j0 >= 0 && !(several && sh.turn[j0] != 0)) plane.store(sh, hold[e], j, j0);
   }
-  // Pages' earlier codes move to the new scale; the segment of a page that began before
-  // is the first one, unless slots were passed over.
-#pragma unroll 1
-  for (uint64_t todo = moved_sh[0] | (uint64_t)moved_sh[1] << 32; todo; todo &= todo - 1) {
-    const int j = __ffsll(todo) - 1, off = slot_sh[j] & last;
-    const float f = scale_sh[j][0] / scale_sh[j][1];
-    uint8_t* dst = cache + (((long long)(slot_sh[j] >> a.log2P) * a.Hkv + h) << a.log2P) * D;
-#pragma unroll 4
-    for (int u = tid; u < off * D / 16; u += kPathThreads) {
-      uint4 c = *reinterpret_cast<const uint4*>(dst + 16 * u);
-      c.x = e4m3x4_times(c.x, f), c.y = e4m3x4_times(c.y, f);
-      c.z = e4m3x4_times(c.z, f), c.w = e4m3x4_times(c.w, f);
-      *reinterpret_cast<uint4*>(dst + 16 * u) = c;
-    }
-  }
+  plane.move(sh);
+  if (several) later_segments<T, D>(a, sh);
   grid_dependents_launch();
 }
 
