@@ -491,8 +491,8 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
  *     (y1 cos a - y2 sin a, y2 cos a + y1 sin a)
  * where pair j is (j, j + R / 2), or (2 j, 2 j + 1) where desc->interleaved; what
  * lies past the first R = rotary_dim dimensions is not turned.  One rounding at the
- * end.  Angles are exact to 2^-31 of a turn for |position * inv_freq| < 2^21 turns
- * (the product is kept in fixed point, whole turns dropped), so any position does.
+ * end.  Angles are within 2^-26 of a turn, and 2^-52 of their whole turns where those are
+ * more than 2^26 (the product is kept in fixed point, whole turns dropped).
  *
  *   q [T, Hq, D], k, v [T, Hkv, D]   desc->dtype; token t lies (t / group) *
  *                                    group_stride + (t % group) * token_stride

@@ -13,7 +13,8 @@
 // Angles.  inv_freq / 2 pi in turns goes to fixed point, 64 bits behind the point; times
 // the position, whole turns fall off the top of the product by themselves, and what is
 // left is exact to |position| 2^-64 and the rounding of inv_freq / 2 pi to 53 bits.  The
-// top 32 bits are the angle in (-1/2, 1/2] turns, for sincospi.  A lane computes two of
+// top 32 bits are the angle in [-1/2, 1/2) turns, which becomes a float (2^-26 of a turn off
+// at most) for sincospi.  A lane computes two of
 // the token's angles and gets the others by shuffles.
 #include "sbd_internal.cuh"
 
@@ -80,11 +81,13 @@ struct Piece<float> {
   }
 };
 
-// f / 2 pi, what of it is behind the point, times 2^64.
+// f / 2 pi, what of it is behind the point, times 2^64, modulo 2^64.  (Of |f|, whose part behind
+// the point has all its bits; that of a small negative f would be rounded next to 1.)
 __device__ __forceinline__ uint64_t turns_of(float f) {
-  const double turns = (double)f * 0.15915494309189533577;          // 1 / (2 pi)
+  const double turns = fabs((double)f) * 0.15915494309189533577;    // 1 / (2 pi)
   const double part = turns - floor(turns);                         // whole turns a position: none
-  return (uint64_t)(part * 18446744073709551616.0);                  // (part = 1 by rounding: 2^64 - 1, a turn)
+  const uint64_t u = (uint64_t)(part * 18446744073709551616.0);
+  return f < 0.f ? 0 - u : u;
 }
 // Cosine and sine of position * f.
 __device__ __forceinline__ void rotation(int position, uint64_t turns, float* c, float* s) {
