@@ -161,8 +161,25 @@ struct Lane {
       }
     }
   }
-  // A row's pieces (the lanes of a row together).
-  __device__ __forceinline__ void row(Piece<T>& x0, Piece<T>& x1, bool norm, float eps) const {
+  // The sum of a row's squares (the lanes of a row together).
+  __device__ __forceinline__ float squares(const float2 (&X)[8]) const {
+    float2 sum = mul2(X[0], X[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) sum = fma2(X[e], X[e], sum);
+    float all = sum.x + sum.y;
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o /= 2) all += __shfl_xor_sync(row_mask, all, o);
+    return all;
+  }
+  // Of 1 / rms: whether squares have left fp32's range (0), or may have lost bits below it (from
+  // 2^60 on), or there is a NaN; as `odd`, of which the largest tells of several rows.
+  static constexpr uint32_t kOdd = 0x5d800000;
+  // A row's pieces (the lanes of a row together).  An odd row comes out right only with kScaled:
+  // it is taken times a power of two, and eps times its square.  (The loops do not ask row by row:
+  // a branch there cost prompts 3 us of 128, and some thousand tokens 8 %.  A warp that had an odd
+  // row takes all of its rows again at its end.)
+  template <bool kScaled>
+  __device__ __forceinline__ void row(Piece<T>& x0, Piece<T>& x1, bool norm, float eps, uint32_t& odd) const {
     float x[16];
     x0.get(x), x1.get(x + 8);
     float2 X[8];
@@ -170,13 +187,17 @@ struct Lane {
     for (int e = 0; e < 8; ++e) X[e] = make_float2(x[2 * e], x[2 * e + 1]);
     float inv = 1.f;
     if (norm) {
-      float2 sum = mul2(X[0], X[0]);
-#pragma unroll
-      for (int e = 1; e < 8; ++e) sum = fma2(X[e], X[e], sum);
-      float all = sum.x + sum.y;
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o /= 2) all += __shfl_xor_sync(row_mask, all, o);
+      float all = squares(X);
       inv = rsqrtf(fmaf(all, 1.f / D, eps));
+      const uint32_t how = __float_as_uint(inv) - 1;
+      odd = max(odd, how);
+      if (kScaled && how >= kOdd) {
+        const float s = all > 1.f ? 0x1p-80f : 0x1p100f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) X[e] = mul2(X[e], make_float2(s, s));
+        all = squares(X);
+        inv = rsqrtf(fmaf(all, 1.f / D, eps * s * s));
+      }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -191,11 +212,44 @@ struct Lane {
   }
 };
 
+// Queries and keys of a token once more, heads begin .. end of both together, odd rows among them
+// (whole warp; behind a call that makes everything itself, so that nothing is kept for it).
+template <typename T, int D, bool kNeighbours>
+__device__ __noinline__ void again(const Args& a, int t, int begin, int end) {
+  using L = Lane<T, D, kNeighbours, false>;
+  const int lane = threadIdx.x & 31, g = t / a.group, i = t - g * a.group;
+  L my(a.R);
+  float cj[2] = {1.f, 1.f}, sj[2] = {0.f, 0.f};
+  if (2 * lane < a.R / 2) {
+    rotation(a.positions[t], turns_of(a.inv_freq[2 * lane]), &cj[0], &sj[0]);
+    rotation(a.positions[t], turns_of(a.inv_freq[2 * lane + 1]), &cj[1], &sj[1]);
+  }
+  uint32_t odd = 0;
+#pragma unroll 1
+  for (int keys = 0; keys < 2; ++keys) {
+    const T* weight = (const T*)(keys ? a.k_weight : a.q_weight);
+    if (!weight) continue;
+    const int first = keys ? a.Hq : 0, count = keys ? a.Hkv : a.Hq;
+    const int lo = max(begin, first) - first, hi = min(end, first + count) - first;
+    const T* src = keys ? (const T*)a.k + g * a.k_group_stride + i * a.k_token_stride
+                        : (const T*)a.q + g * a.q_group_stride + i * a.q_token_stride;
+    T* dst = (T*)(keys ? a.k_out : a.q_out) + (long long)t * count * D;
+    my.factors(weight, cj, sj);
+#pragma unroll 1
+    for (int h = lo + lane / L::kLanes; h < hi; h += L::kRows) {
+      Piece<T> x0, x1;
+      x0.load(src + h * D + my.d0), x1.load(src + h * D + my.d1);
+      my.template row<true>(x0, x1, true, a.eps, odd);
+      x0.store(dst + h * D + my.d0), x1.store(dst + h * D + my.d1);
+    }
+  }
+}
+
 // Few tokens, or fp32: a warp has some heads of one, three turns of rows (a turn: a row for
 // each lane group) in flight.  Bound: latency up to some hundred tokens (16 tokens 3.4 us, of
 // which a launch 2), HBM for prompts (fp32, 16000 tokens 125 us, 6.3 TB/s).
 template <typename T, int D, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_kernel(const __grid_constant__ Args a) {
   using L = Lane<T, D, kNeighbours, false>;
   constexpr int kRows = L::kRows;
   constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;       // rows that a lane has in flight
@@ -215,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_ke
   }
   const int g = t / a.group, in_group = t - g * a.group;
   const int begin = share * a.share, end = min(a.heads, begin + a.share);
+  uint32_t odd = 0;
   // Heads begin .. end of queries (h < Hq), keys and values.
   auto rows = [&](int first, int count, const T* src, T* dst, const T* weight, bool copy) {
     const int lo = max(begin, first) - first, hi = min(end, first + count) - first;
@@ -234,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_ke
         if (h0 + u * kRows >= hi) break;
         Piece<T> x0 = p0[u], x1 = p1[u];
         if (h0 + (u + kAhead) * kRows < hi) p0[u].load(src + u * kStep + my.d0), p1[u].load(src + u * kStep + my.d1);
-        if (!copy) my.row(x0, x1, weight != nullptr, a.eps);
+        if (!copy) my.template row<false>(x0, x1, weight != nullptr, a.eps, odd);
         x0.store(dst + u * kStep + my.d0), x1.store(dst + u * kStep + my.d1);
       }
       dst += kAhead * kStep;
@@ -246,6 +301,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_ke
        (T*)a.k_out + (long long)t * a.Hkv * D, (const T*)a.k_weight, false);
   rows(a.Hq + a.Hkv, a.heads - a.Hq - a.Hkv, (const T*)a.v + g * a.v_group_stride + in_group * a.v_token_stride,
        (T*)a.v_out + (long long)t * a.Hkv * D, nullptr, true);
+  if (__any_sync(0xffffffffu, odd >= L::kOdd)) {
+    const long long at = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int token = (int)(at / a.shares), begin = (int)(at - (long long)token * a.shares) * a.share;
+    again<T, D, kNeighbours>(a, token, begin, min(a.heads, begin + a.share));
+  }
   grid_dependents_launch();
 }
 
@@ -273,7 +333,7 @@ __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t 
 }
 
 template <typename T, int D, bool kNeighbours, bool kAll>
-__global__ void __launch_bounds__(kThreads) norm_rope_stream_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads) norm_rope_stream_kernel(const __grid_constant__ Args a) {
   using L = Lane<T, D, kNeighbours, kAll>;
   constexpr int kHeads = kPiece / (D * (int)sizeof(T));        // of a piece
   static_assert(kHeads % L::kRows == 0, "whole turns");
@@ -326,6 +386,7 @@ __global__ void __launch_bounds__(kThreads) norm_rope_stream_kernel(const Args a
   int done = 0;
   bool ok = true;
   // A part of a token, piece by piece.
+  uint32_t odd = 0;
   auto part = [&](int heads, uint8_t* dst, const T* weight, bool copy) {
     if (!copy) my.factors(weight, cj, sj);
 #pragma unroll 1
@@ -341,7 +402,7 @@ __global__ void __launch_bounds__(kThreads) norm_rope_stream_kernel(const Args a
         for (int h = lane / L::kLanes; h < n; h += L::kRows, row += L::kRows * D) {
           Piece<T> x0, x1;
           x0.load(row + my.d0), x1.load(row + my.d1);
-          my.row(x0, x1, weight != nullptr, a.eps);
+          my.template row<false>(x0, x1, weight != nullptr, a.eps, odd);
           x0.store(row + my.d0), x1.store(row + my.d1);
         }
         fence_proxy_async_smem();
@@ -376,6 +437,10 @@ __global__ void __launch_bounds__(kThreads) norm_rope_stream_kernel(const Args a
     for (int i = done; i < loaded; ++i) mbar_wait(&full[warp][i % kStages], (i / kStages) & 1, a.err);
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
+  // This warp's tokens once more, where one has an odd row; what the copies wrote is there.
+  __syncwarp();
+  if (!__any_sync(0xffffffffu, odd >= L::kOdd) || !ok) return;
+  for (int t = first; t < a.tokens; t = next_token(t)) again<T, D, kNeighbours>(a, t, 0, a.Hq + a.Hkv);
 }
 
 template <typename T, int D, bool kNeighbours>
