@@ -79,10 +79,13 @@ class DraftedDecoder:
         lens = torch.tensor([len(p) - 1 for p in prompts], dtype=torch.int32, device="cuda")
         self.table, self.length, _, slots, self.n_free = sbd.sbd_block_tables(
             self.length, lens, self.table, self.free, self.n_free, self.page, int(lens.sum()))
-        tokens = torch.cat([p[:-1] for p in prompts]).cuda()
-        positions = torch.cat([torch.arange(len(p) - 1, dtype=torch.int32) for p in prompts]).cuda()
-        _, (_, keys, values) = self._project(tokens, positions)
-        sbd.sbd_cache_append_q8(keys, values, slots, *self.cache, *self.scale)
+        if not torch.equal(self.length, lens):
+            raise RuntimeError("the cache is full")
+        if len(slots):
+            tokens = torch.cat([p[:-1] for p in prompts]).cuda()
+            positions = torch.cat([torch.arange(len(p) - 1, dtype=torch.int32) for p in prompts]).cuda()
+            _, (_, keys, values) = self._project(tokens, positions)
+            sbd.sbd_cache_append_q8(keys, values, slots, *self.cache, *self.scale)
         self.last = torch.stack([p[-1] for p in prompts]).cuda()
 
     def turn(self):
