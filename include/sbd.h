@@ -491,7 +491,7 @@ sbd_status sbd_block_attention_q8(const sbd_attn_q8_desc* desc, const void* q,
  *     (y1 cos a - y2 sin a, y2 cos a + y1 sin a)
  * where pair j is (j, j + R / 2), or (2 j, 2 j + 1) where desc->interleaved; what
  * lies past the first R = rotary_dim dimensions is not turned.  One rounding at the
- * end.  Angles are within 2^-26 of a turn, and 2^-52 of their whole turns where those are
+ * end; squares may leave fp32's range.  Angles are within 2^-26 of a turn, and 2^-52 of their whole turns where those are
  * more than 2^26 (the product is kept in fixed point, whole turns dropped).
  *
  *   q [T, Hq, D], k, v [T, Hkv, D]   desc->dtype; token t lies (t / group) *
@@ -569,8 +569,8 @@ sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, co
  *   logprob [B, n] fp32 out    ln p of each of them (at temperature 1 where tau = 0), then 0
  *   count [B] int32 out        nodes on the path = tokens that come out, 1 .. n
  *
- * Exponentials and sums in fp32.  No workspace: its size is 0.  Rows that the walk does not
- * come to change nothing.
+ * Exponentials and sums in fp32: a probability, or a remainder's sum, below 2^-126 is none.
+ * No workspace: its size is 0.  Rows that the walk does not come to change nothing.
  * Supported: 1 <= n <= 64, 1 <= V <= 2^24, B <= 65535, tau = 0 or 2^-20 <= tau <= 2^20.
  * ---------------------------------------------------------------------- */
 typedef struct {

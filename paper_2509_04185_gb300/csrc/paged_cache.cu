@@ -511,8 +511,8 @@ __global__ void __launch_bounds__(kAppThreads, sizeof(T) == 2 ? 4 : 2) append_q8
 // rows, the slots -> old scales -> codes, then earlier codes where a page's scale grew.
 // Segments of one page (an entry between them is not stored) take turns: what the first writes
 // is the second's old scale and earlier codes.
-// Bound: latency.  16 requests of up to four accepted nodes 3.7 us, of which a launch 2; 200
-// requests of up to 33 in fp32, 1600 CTAs, 6.0 (a segment after the other 12.2; segments found
+// Bound: latency.  16 requests of up to four accepted nodes 3.5 us, of which a launch 2, and 4.9
+// where every page's scale grows; 200 requests of up to 33 in fp32, 1600 CTAs, 6.0 and 6.9 (a segment after the other 12.2; segments found
 // by walking back token by token 9.9).
 constexpr int kPathThreads = 128;
 

@@ -14,8 +14,8 @@
 // the position, whole turns fall off the top of the product by themselves, and what is
 // left is exact to |position| 2^-64 and the rounding of inv_freq / 2 pi to 53 bits.  The
 // top 32 bits are the angle in [-1/2, 1/2) turns, which becomes a float (2^-26 of a turn off
-// at most) for sincospi.  A lane computes two of
-// the token's angles and gets the others by shuffles.
+// at most) for sincospi.  A lane computes two of the token's angles and gets the others by
+// shuffles.
 #include "sbd_internal.cuh"
 
 namespace {
@@ -247,7 +247,8 @@ __device__ __noinline__ void again(const Args& a, int t, int begin, int end) {
 
 // Few tokens, or fp32: a warp has some heads of one, three turns of rows (a turn: a row for
 // each lane group) in flight.  Bound: latency up to some hundred tokens (16 tokens 3.4 us, of
-// which a launch 2), HBM for prompts (fp32, 16000 tokens 125 us, 6.3 TB/s).
+// which a launch 2), HBM for prompts (fp32, 16000 tokens 126 us, 6.3 TB/s).  Instances spill 24 to
+// 32 bytes (of 96 registers in bf16, 128 in fp32).
 template <typename T, int D, bool kNeighbours>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 4) norm_rope_kernel(const __grid_constant__ Args a) {
   using L = Lane<T, D, kNeighbours, false>;
@@ -495,7 +496,10 @@ sbd_status norm_rope_launch(const sbd_norm_rope_desc& d, const NormRopeTensors& 
     a.share = (a.share / rows + 1) / 2 * rows;
   a.shares = (a.heads + a.share - 1) / a.share;
   // bf16 tokens are streamed from two for every warp on (of 32 + 8 + 8 heads of 128: 2600 tokens
-  // 18.3 us streamed and 15.9 spread, 5000 27.6 and 27.7, 10000 45.6 and 49.3, 16000 66 and 73);
+  // 18.3 us streamed and 15.9 spread, 5000 27.6 and 27.7, 10000 45.6 and 49.3, 16000 66 and 73; with
+  // few heads instructions are the limit, 2 to 3.5 TB/s, and streamed is ahead, too: 8 + 2 + 2 of 128,
+  // 32768 tokens 57.5 and 64.6, 4 + 1 + 1 of 128 50.3 and 56.9, 8000 tokens 15.7 and 17.5, 2 + 1 + 1 of
+  // 64 47.6 and 51.0, 8000 tokens 14.7 and 16.2);
   // fp32 ones never (16000 tokens 134 and 125).
   const bool stream = d.dtype == SBD_DTYPE_BF16 && d.tokens >= 2ll * kStreamCtas * (kThreads / 32) * num_sms();
   const void* fn = d.dtype == SBD_DTYPE_F32 ? kernel_for<float>(d, stream) : kernel_for<__nv_bfloat16>(d, stream);

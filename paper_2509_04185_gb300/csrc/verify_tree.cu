@@ -16,7 +16,7 @@
 // the same order, and so comes to the same numbers and decisions as the others.
 //
 // Bounds and figures (128256 logits in bf16, draft's rows too).  One request, three of seven
-// tokens accepted: 13 us, a chain of latencies: launch 2, tree 1.5, a level 2.5 to 3 (loads 1,
+// tokens accepted: 12.4 us, a chain of latencies: launch 2, tree 1.5, a level 2.5 to 3 (loads 1,
 // reductions over warps, CTA and cluster 1, the decision with its code 0.7), the last token's
 // pass 3.  64 requests of 15 nodes, none to three levels: 50 us, of which the bytes are 14.5;
 // the passes of a request follow one another, and at first the exponentials of all of them
@@ -24,6 +24,8 @@
 // On the way: maxima that are no whole numbers and reductions in turn 131 us; whole numbers
 // and one barrier 89; words of 16 bytes without bounds to check 58; which element is the best
 // looked up once and not in every word (16 of 36 instructions) 53.
+// Registers: 64 a thread for four CTAs an SM, where the instances with draft's rows spill (bf16
+// 108 bytes stored and 168 loaded, fp32 56 and 32); three CTAs, with 12 bytes, take 56 us.
 #include <math.h>
 
 #include <type_traits>
@@ -314,7 +316,7 @@ struct Shared {
   float left[kMaxNodes];                     // 1 / Z
 };
 // Where requests are few (512 threads a CTA) a level is a chain of latencies, 2.8 us of one
-// request's 13: so M and S of several rows are made at once, of a node, its first child,
+// request's 12.4: so M and S of several rows are made at once, of a node, its first child,
 // that one's first child ..., which the walk is likely to come to, and both rows of a node
 // together.  Where they are many, one row after the other, only as the walk comes to them.
 template <Mode kMode, int kThreads>
@@ -547,6 +549,8 @@ __device__ __forceinline__ int walk(const Args& a, Shared<kThreads / 32, rows_ah
     auto log2_q = [&](float z) { return kFar ? below(z, sq.M) * c2 : fmaf(z, c2, -sq.M); };
     auto prob = [&](float z) { return fmaxf(ex2_ftz(log2_p(z)), 0.f) * inv_s; };             // (NaN: 0)
     auto prob_q = [&](float z) { return fmaxf(ex2_ftz(log2_q(z)), 0.f) * inv_q; };
+    // (All earlier steps are taken again in every pass: c rejected children cost c passes and c^2 / 2
+    // steps an element.  What is left of the vocabulary is not kept between passes.)
     // What is left of p at elements v, v + 1, ... after the first k rejections (and one more,
     // `after`), times S and not normalised by the last ones' sum.
     const float q_of_p = inv_q * fabsf(st.S);
@@ -755,7 +759,8 @@ __device__ __forceinline__ int walk(const Args& a, Shared<kThreads / 32, rows_ah
 }
 
 // The walk in the form for any row: every row's largest logit first, in a pass of its own.  (64
-// requests at tau = 1e-6, whose rows are all beyond the limit: 84 us, 43 at tau = 1.)
+// trees at tau = 1e-6, whose rows are all beyond the limit: 98 us, 51 at tau = 1; without draft's
+// rows 54 and 36.5.)
 template <typename T, Mode kMode, int kThreads>
 __device__ __noinline__ int far_walk(const Args& a, Shared<kThreads / 32, rows_ahead<kMode, kThreads>()>& sh, int turn, int parent) {
   __syncthreads();                           // (what the other walk left is read)
