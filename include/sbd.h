@@ -569,7 +569,7 @@ sbd_status sbd_tree_attention_q8(const sbd_attn_q8_desc* desc, const void* q, co
  *   logprob [B, n] fp32 out    ln p of each of them (at temperature 1 where tau = 0), then 0
  *   count [B] int32 out        nodes on the path = tokens that come out, 1 .. n
  *
- * Exponentials and sums in fp32: a probability, or a remainder's sum, below 2^-126 is none.
+ * Exponentials and sums in fp32: what is below 2^-126 of a row may count nothing.
  * No workspace: its size is 0.  Rows that the walk does not come to change nothing.
  * Supported: 1 <= n <= 64, 1 <= V <= 2^24, B <= 65535, tau = 0 or 2^-20 <= tau <= 2^20.
  * ---------------------------------------------------------------------- */

@@ -5,7 +5,8 @@
 // and the whole number M = ceil(max z c): parts of a row that took different M are brought
 // together by exact factors, and z c - M is rounded once.  (Where the walk comes to a row whose
 // largest logit is so far from 0 that z c has no such M, or that is masked altogether, it begins
-// again in a form for any row: far_walk.)  What a row is needed for is M, S, the values at a few drafted tokens, and, where the walk ends, one argmax over
+// again in a form for any row: far_walk.)  What a row is needed for is M, S, the values at a few
+// drafted tokens, and, where the walk ends, one argmax over
 //   ln r(v) + gumbel(v),   r = what is left of p after the rejected children:
 //   r_0 = p,  r_(k+1)(v) = max(r_k(v) - q(v), 0) / Z_k   (draft with probabilities)
 //                        = r_k(v) / Z_k, 0 at the rejected token  (without)
